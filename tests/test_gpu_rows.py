@@ -1,0 +1,588 @@
+"""Token-row operators on the GPU against their definitions in 64 bits (rows_reference), at
+the sizes, strides, ids and values where they can go wrong."""
+
+import math
+
+import pytest
+import torch
+
+import rows_reference as ref
+from paper_2008_00325_amd import umap_rows as R
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+F32, F16, BF16, I8, F8 = torch.float32, torch.float16, torch.bfloat16, torch.int8, torch.float8_e4m3fn
+FLOATS = [F32, F16, BF16]
+DIMS = [1, 2, 3, 7, 8, 9, 16, 63, 64, 65, 127, 300, 512, 784, 1001, 1024, 2048, 2056, 4100, 8192, 9001]
+
+
+@pytest.fixture(autouse=True)
+def _seed():
+    torch.manual_seed(5)
+    yield
+    torch.cuda.synchronize()
+
+
+def rand(n, dim, dtype, pad=0, shift=0, spread=1.0):
+    """n x dim values as columns shift .. of rows that are dim + pad + shift long."""
+    x = (torch.randn(n, dim + pad + shift, device=DEV) * spread).to(dtype)
+    return x[:, shift:shift + dim]
+
+
+def hole(n, dim, dtype, pad=0, shift=0):
+    """An output with a frame: whatever is written outside of it shows."""
+    x = torch.full((n, dim + pad + shift), 7.0, device=DEV).to(dtype)
+    return x, x[:, shift:shift + dim]
+
+
+def frame_untouched(whole, dim, shift):
+    f = whole.float()
+    return bool((f[:, :shift] == 7).all() and (f[:, shift + dim:] == 7).all())
+
+
+def eight_bit(n, dim, dtype, group):
+    q = torch.randint(-127, 128, (n, dim), device=DEV)
+    q = q.to(I8) if dtype == I8 else (q.float() * 3.4).to(F8)
+    return q, torch.rand(n, -(-dim // group) if group else 1, device=DEV) + 0.01
+
+
+def near(got, want, bound):
+    got = ref.values(got)
+    assert got.shape == want.shape
+    off = (got - want).abs()
+    bad = ~(off <= bound)
+    assert not bool(bad.any()), f"{int(bad.sum())} values off, the worst {float((off / bound).nan_to_num(9e9).max()):.3g} bounds"
+
+
+# ---- lookup ------------------------------------------------------------------------------------
+
+
+def check_lookup(table, ids, scale, out_dtype, scales=None, group=0, pad=0, shift=0):
+    whole, out = hole(ids.numel(), table.shape[1], out_dtype, pad, shift)
+    R.umap_rows_lookup(table, ids, out, scale=scale, table_scales=scales, group=group)
+    want = ref.lookup(ref.values(table, scales, group), ids, float(torch.tensor(scale, dtype=F32)))
+    near(out, want, (ref.U[out_dtype] + 4 * ref.E32) * want.abs() + ref.TINY[out_dtype])
+    assert frame_untouched(whole, table.shape[1], shift)
+
+
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("dtype,out", [(F32, BF16), (BF16, BF16), (F16, F32), (BF16, F16)])
+def test_lookup_dims(dim, dtype, out):
+    ids = torch.randint(0, 50, (37,), device=DEV)
+    check_lookup(rand(50, dim, dtype), ids, math.sqrt(dim), out)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 0), (0, 1), (5, 3)])
+def test_lookup_strides_and_alignment(dtype, pad, shift):
+    for dim in (5, 64, 301):
+        ids = torch.randint(0, 20, (70,), device=DEV, dtype=torch.int32)
+        check_lookup(rand(20, dim, dtype, pad, shift), ids, 1.0, dtype, pad=shift, shift=pad)
+
+
+@pytest.mark.parametrize("dtype", [I8, F8])
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("dim", [1, 31, 32, 33, 130, 256, 784, 2048])
+def test_lookup_from_8_bits(dtype, group, dim):
+    q, scales = eight_bit(40, dim, dtype, group)
+    ids = torch.randint(-2, 43, (90,), device=DEV)
+    for out in (BF16, F32):
+        check_lookup(q, ids, 1.5, out, scales, group)
+
+
+@pytest.mark.parametrize("kind", [torch.int32, torch.int64])
+def test_lookup_ids_outside_the_table_give_zeros(kind):
+    ids = [0, -1, 9, 10, 3, -2**31, 2**31 - 1] + ([2**32, 2**32 + 1, -2**63, 2**63 - 1, -2**32] if kind == torch.int64 else [])
+    table = rand(10, 40, F32)
+    table[:] = torch.where(table == 0, 1.0, table)
+    out = torch.empty(len(ids), 40, device=DEV)
+    R.umap_rows_lookup(table, torch.tensor(ids, device=DEV, dtype=kind), out)
+    for t, v in enumerate(ids):
+        assert torch.equal(out[t], table[v] if 0 <= v < 10 else torch.zeros_like(out[t])), v
+
+
+def test_lookup_in_order_and_empty_calls():
+    table = rand(33, 100, BF16)
+    out = torch.empty(20, 100, device=DEV, dtype=BF16)
+    R.umap_rows_lookup(table, None, out)
+    assert torch.equal(out, table[:20])
+    R.umap_rows_lookup(table, torch.empty(0, device=DEV, dtype=torch.int64), out[:0])
+    none = torch.empty(0, 100, device=DEV, dtype=BF16)
+    R.umap_rows_lookup(none, torch.zeros(20, device=DEV, dtype=torch.int32), out)   # a table without rows
+    assert not bool(out.any())
+
+
+def test_lookup_passes_nan_and_infinity_through():
+    table = rand(4, 30, BF16)
+    table[1, 3], table[2, 29] = float("nan"), float("inf")
+    out = torch.empty(4, 30, device=DEV, dtype=F32)
+    R.umap_rows_lookup(table, torch.arange(4, device=DEV), out)
+    assert torch.equal(out.isnan(), table.isnan()) and torch.equal(out.isinf(), table.isinf())
+    out16 = torch.empty(1, 30, device=DEV, dtype=F16)   # beyond the type's range: infinity
+    R.umap_rows_lookup(torch.full((1, 30), 1e6, device=DEV), torch.zeros(1, device=DEV, dtype=torch.int32), out16)
+    assert bool(out16.isinf().all())
+
+
+def test_lookup_offsets_beyond_32_bits():
+    pitch = 2**31 + 64
+    store = torch.empty(2 * pitch + 50, device=DEV, dtype=I8)
+    table = store.as_strided((3, 50), (pitch, 1))
+    table[:] = torch.randint(-127, 128, (3, 50), device=DEV)
+    scales = torch.rand(3, 1, device=DEV)
+    out = torch.empty(3, 50, device=DEV)
+    R.umap_rows_lookup(table, torch.tensor([2, 0, 1], device=DEV), out, table_scales=scales)
+    assert torch.equal(out, (table.float() * scales)[[2, 0, 1]])
+
+
+# ---- gradient of the lookup -----------------------------------------------------------------
+
+
+def lookup_grad(dout, ids, rows, scale=1.0, dtype=F32, accumulate=None, pad=0, shift=0):
+    n, dim = dout.shape
+    whole, grad = hole(rows, dim, dtype, pad, shift)
+    if accumulate is not None:
+        grad.copy_(accumulate)
+    work = torch.empty(R.umap_rows_lookup_grad_workspace(n, rows, dim), dtype=torch.uint8, device=DEV)
+    work.random_(0, 256)
+    R.umap_rows_lookup_grad(dout, ids, grad, work, scale=scale, accumulate=accumulate is not None)
+    assert frame_untouched(whole, dim, shift)
+    return grad
+
+
+def check_grad(dout, ids, rows, scale=1.0, dtype=F32, accumulate=None, **kw):
+    got = lookup_grad(dout, ids, rows, scale, dtype, accumulate, **kw)
+    s = float(torch.tensor(scale, dtype=F32))
+    start = None if accumulate is None else ref.values(accumulate)
+    want, size = ref.lookup_grad(ref.values(dout), ids, rows, s, start)
+    near(got, want, ref.U[dtype] * want.abs() + (ref.counts(ids, rows) + 4) * ref.E32 * size + ref.TINY[dtype])
+    return got
+
+
+def zipf(n, rows, kind=torch.int64):
+    u = torch.rand(n, device=DEV, dtype=torch.float64)
+    return (torch.exp(u * math.log(rows + 1)) - 1).long().clamp(0, rows - 1).to(kind)
+
+
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, F32), (F16, BF16)])
+def test_grad_dims(dim, dtype, out):
+    check_grad(rand(203, dim, dtype), zipf(203, 90), 90, math.sqrt(dim), out)
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 255, 1000, 4095, 4096, 4097, 8192, 16384, 16385, 20000, 70001])
+def test_grad_id_counts(n):
+    check_grad(rand(n, 24, BF16), zipf(n, 1500, torch.int32), 1500)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 255, 256, 511, 512, 513, 1000, 2**16, 2**18 - 1, 2**18, 2**18 + 1, 10**6])
+def test_grad_table_sizes(rows):
+    check_grad(rand(5000, 9, F32), zipf(5000, rows), rows)
+    last = torch.full((40,), rows - 1, device=DEV)
+    got = check_grad(rand(40, 9, F32), last, rows)
+    assert not bool(got[:-1].any())
+
+
+@pytest.mark.parametrize("n", [1, 64, 700, 5000, 40000])
+@pytest.mark.parametrize("dim", [8, 520])
+def test_grad_all_one_id_none_and_all_different(n, dim):
+    d = rand(n, dim, BF16)
+    check_grad(d, torch.full((n,), 3, device=DEV), 7)
+    got = check_grad(d, torch.full((n,), -1, device=DEV), 7)
+    assert not bool(got.any())
+    check_grad(d, torch.randperm(n, device=DEV), n)
+
+
+def test_grad_long_runs_of_one_id_between_others():
+    ids = torch.cat([torch.randint(0, 40, (3000,), device=DEV), torch.full((2500,), 17, device=DEV),
+                     torch.full((1111,), 39, device=DEV), torch.full((5,), 0, device=DEV)])
+    check_grad(rand(ids.numel(), 700, BF16), ids[torch.randperm(ids.numel(), device=DEV)], 41, 0.5)
+    check_grad(rand(ids.numel(), 700, F32), ids, 41, -2.0)
+
+
+@pytest.mark.parametrize("kind", [torch.int32, torch.int64])
+def test_grad_ids_outside_take_no_part(kind):
+    ids = [0, -1, 9, 10, 3, 9, -2**31, 2**31 - 1] + ([2**32, 2**32 + 3, -2**63, 2**63 - 1] if kind == torch.int64 else [])
+    d = rand(len(ids), 50, F32)
+    at = torch.tensor(ids, device=DEV)
+    d[(at < 0) | (at >= 10)] = float("nan")
+    got = lookup_grad(d, at.to(kind), 10)
+    assert torch.equal(got[9], d[2] + d[5]) and torch.equal(got[0], d[0]) and torch.equal(got[3], d[4])
+    assert not bool(got[[1, 2, 4, 5, 6, 7, 8]].any())
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 0), (0, 1), (5, 3)])
+def test_grad_strides_and_alignment(dtype, pad, shift):
+    for dim in (5, 64, 301, 1030):
+        check_grad(rand(500, dim, dtype, pad, shift), zipf(500, 60), 60, 1.0, dtype, pad=shift, shift=pad)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("n,dim", [(1, 64), (300, 65), (9000, 516)])
+def test_grad_accumulates_into_the_rows_in_use_only(dtype, n, dim):
+    start = rand(200, dim, dtype)
+    start[150:] = float("nan")
+    ids = zipf(n, 150)
+    d = rand(n, dim, BF16)
+    got = lookup_grad(d, ids, 200, -0.25, dtype, start)
+    assert bool(got[150:].isnan().all())
+    used = ref.counts(ids, 200)[:, 0] > 0
+    assert torch.equal(got[:150].cpu()[~used[:150]], start[:150].cpu()[~used[:150]])
+    check_grad(d, ids, 150, -0.25, dtype, start[:150])
+
+
+def test_grad_of_a_broadcast_row():
+    d = rand(1, 100, F32).expand(600, 100)
+    check_grad(d, zipf(600, 30), 30)
+
+
+def test_grad_same_bits_from_call_to_call_and_after_other_calls():
+    d, ids = rand(30000, 257, BF16), zipf(30000, 3000)
+    first = lookup_grad(d, ids, 3000)
+    lookup_grad(rand(999, 257, BF16), zipf(999, 50), 50)
+    assert torch.equal(first, lookup_grad(d, ids, 3000))
+
+
+def test_grad_is_the_transpose_of_the_lookup():
+    table, ids, d = rand(300, 120, F32), zipf(1000, 300), rand(1000, 120, F32)
+    out = torch.empty(1000, 120, device=DEV)
+    R.umap_rows_lookup(table, ids, out, scale=3.0)
+    grad = lookup_grad(d, ids, 300, 3.0)
+    a, b = (ref.values(out) * ref.values(d)).sum(), (ref.values(grad) * ref.values(table)).sum()
+    size = (ref.values(out).abs() * ref.values(d).abs()).sum()
+    assert abs(float(a - b)) <= 1010 * ref.E32 * float(size)
+
+
+def test_grad_offsets_beyond_32_bits():
+    pitch = 2**30 + 64
+    store = torch.empty(4 * pitch + 40, device=DEV, dtype=F32)
+    grad, d = store.as_strided((5, 40), (pitch, 1)), rand(9, 40, F32)
+    ids = torch.tensor([4, 4, 0, 3, 3, 3, 1, -1, 4], device=DEV)
+    work = torch.empty(R.umap_rows_lookup_grad_workspace(9, 5, 40), dtype=torch.uint8, device=DEV)
+    R.umap_rows_lookup_grad(d, ids, grad, work)
+    want, size = ref.lookup_grad(ref.values(d), ids, 5, 1.0)
+    near(grad.clone(), want, 8 * ref.E32 * size)
+    back = torch.empty(5, 40, device=DEV)   # and read again from there
+    R.umap_rows_lookup_grad(grad, torch.arange(5, device=DEV), back,
+                            torch.empty(R.umap_rows_lookup_grad_workspace(5, 5, 40), dtype=torch.uint8, device=DEV))
+    assert torch.equal(back, grad)
+
+
+# ---- norm ------------------------------------------------------------------------------------------
+
+
+def check_norm(x, dtype, weight=None, residual=None, ids=None, scale=1.0, want_h=False, eps=1e-6, group=0, pad=0, shift=0,
+               alias=None):
+    n = x.shape[0] if ids is None else ids.numel()
+    dim = x.shape[1]
+    s = float(torch.tensor(scale, dtype=F32))
+    x64 = ref.values(x) * s if ids is None else ref.lookup(ref.values(x), ids, s)
+    r64 = None if residual is None else ref.values(residual)
+    w64 = None if weight is None else ref.values(weight[None])[0]
+    h64, y64 = ref.norm(x64, r64, w64, eps)
+    whole, y = hole(n, dim, dtype, pad, shift)
+    h = alias if alias is not None else torch.empty(n, dim, device=DEV, dtype=x.dtype) if want_h else None
+    scales = torch.full((n, -(-dim // group) if group else 1), 7.0, device=DEV) if dtype in ref.LARGEST else None
+    R.umap_rows_norm(x, y, weight=weight, residual=residual, h=h, ids=ids, scale=scale, y_scales=scales, group=group,
+                     eps=eps)
+    assert frame_untouched(whole, dim, shift)
+    if h is not None:
+        parts = x64.abs() + (0 if r64 is None else r64.abs())
+        near(h, h64, ref.U[x.dtype] * h64.abs() + 2 * ref.E32 * parts + ref.TINY[x.dtype])
+    if scales is None:
+        near(y, y64, ref.norm_bound(x64, r64, w64, eps, dtype))
+        return
+    # the scale: the largest |y| of the group over the type's largest; the values: to half a step
+    off = ref.norm_bound(x64, r64, w64, eps, F32)
+    G = group or dim
+    most = torch.stack([y64[:, c:c + G].abs().amax(1) for c in range(0, dim, G)], 1)
+    off_most = torch.stack([off[:, c:c + G].amax(1) for c in range(0, dim, G)], 1)
+    top = ref.LARGEST[dtype]
+    got = scales.cpu().double()
+    assert bool(((got - most / top).abs() <= (off_most + 4 * ref.E32 * most) / top + 1e-45).all())
+    back = ref.values(y, scales, group)
+    step = got[:, torch.arange(dim) // G]
+    half = 0.5 * step if dtype == I8 else torch.maximum(2.0**-4 * y64.abs(), 2.0**-10 * step)
+    assert bool(((back - y64).abs() <= half * (1 + 1e-3) + off + 4 * ref.E32 * y64.abs()).all())
+
+
+@pytest.mark.parametrize("dim", DIMS + [16384, 20001, 32768])
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (F16, F32), (BF16, I8), (F16, F8)])
+def test_norm_dims(dim, dtype, out):
+    w = (1 + 0.2 * torch.randn(dim, device=DEV)).to(dtype)
+    check_norm(rand(13, dim, dtype), out, w, residual=rand(13, dim, dtype, spread=2.0), want_h=True)
+
+
+@pytest.mark.parametrize("dim", [1, 40, 784, 4096, 9001])
+@pytest.mark.parametrize("with_h", [False, True])
+@pytest.mark.parametrize("with_r", [False, True])
+@pytest.mark.parametrize("with_w", [False, True])
+def test_norm_with_and_without_its_parts(dim, with_h, with_r, with_w):
+    check_norm(rand(5, dim, BF16), BF16, rand(1, dim, F32)[0] if with_w else None,
+               rand(5, dim, BF16) if with_r else None, want_h=with_h, scale=1.0 if with_r else 0.5)
+
+
+@pytest.mark.parametrize("out", [I8, F8])
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("dim", [1, 31, 32, 33, 96, 130, 256, 784, 1000, 2048, 5000, 9001, 32768])
+def test_norm_into_8_bits(out, group, dim):
+    check_norm(rand(9, dim, BF16), out, rand(1, dim, BF16)[0], group=group)
+    check_norm(rand(3, dim, F32, 3, 1), out, group=group, pad=1, shift=2)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 0), (0, 1), (5, 3)])
+def test_norm_strides_and_alignment(dtype, pad, shift):
+    for dim in (5, 64, 301, 2049):
+        w = rand(1, dim + 1, dtype)[0, 1:]
+        check_norm(rand(21, dim, dtype, pad, shift), dtype, w, rand(21, dim, dtype, shift, pad), want_h=True, pad=shift, shift=pad)
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 3, 4, 5, 255, 4099])
+def test_norm_row_counts(n):
+    check_norm(rand(n, 48, BF16), BF16, residual=rand(n, 48, BF16), want_h=True)
+    check_norm(rand(n, 48, BF16), I8, residual=rand(n, 48, BF16), want_h=True, group=32)
+
+
+@pytest.mark.parametrize("dim", [7, 300, 2048, 9001])
+def test_norm_of_gathered_rows(dim):
+    x = rand(40, dim, BF16)
+    ids = torch.tensor([0, 39, 5, -1, 5, 40, 2**40, 17], device=DEV)
+    check_norm(x, BF16, rand(1, dim, BF16)[0], ids=ids, scale=8.0, want_h=True)
+    check_norm(x, I8, residual=rand(8, dim, BF16), ids=ids, want_h=True, group=32)
+
+
+@pytest.mark.parametrize("dim", [33, 1000, 4096, 20001])
+def test_norm_in_place(dim):
+    x, r = rand(11, dim, BF16), rand(11, dim, BF16, 3, 1)
+    check_norm(x, BF16, residual=r, alias=r)
+    x, r = rand(11, dim, BF16), rand(11, dim, BF16)
+    check_norm(x, I8, residual=r, alias=x)
+
+
+def test_norm_of_a_broadcast_row():
+    check_norm(rand(1, 130, F32).expand(50, 130), F32, residual=rand(50, 130, F32))
+
+
+@pytest.mark.parametrize("out", [F32, BF16, I8, F8])
+@pytest.mark.parametrize("dim", [40, 1000, 9000])
+def test_norm_of_rows_of_zeros(out, dim):
+    x = rand(6, dim, F32)
+    x[[0, 3]] = 0
+    check_norm(x, out)
+
+
+@pytest.mark.parametrize("dim", [5, 64, 1000, 8192, 32768])
+def test_norm_of_rows_whose_squares_leave_the_range(dim):
+    for size in (1e19, 3e37, 3e-19, 1e-25):
+        check_norm(rand(5, dim, BF16, spread=size).clamp(-3e38, 3e38), F32)
+        check_norm(rand(5, dim, F32, spread=size).clamp(-3e38, 3e38), I8)
+    tiny = rand(5, dim, F32, spread=1e-37)   # y below 2^-100: zeros
+    y, scales = torch.empty(5, dim, device=DEV, dtype=I8), torch.empty(5, 1, device=DEV)
+    R.umap_rows_norm(tiny, y, y_scales=scales)
+    assert not bool(y.any()) and not bool(scales.any())
+
+
+@pytest.mark.parametrize("dim", [9, 300, 2048, 9001])
+@pytest.mark.parametrize("group", [0, 32])
+def test_norm_keeps_nan_and_infinity_in_their_rows(dim, group):
+    x = rand(6, dim, BF16)
+    x[1, dim // 2], x[3, 0], x[4, dim - 1] = float("nan"), float("inf"), -float("inf")
+    y = torch.empty(6, dim, device=DEV, dtype=BF16)
+    R.umap_rows_norm(x, y)
+    assert bool(y[[0, 2, 5]].isfinite().all()) and bool(y[1].isnan().all())
+    assert bool(y[3, 0].isnan()) and bool(y[4, dim - 1].isnan())   # infinity over infinity
+    assert not bool(y[3, 1:].any()) and not bool(y[4, :-1].any())
+    q = torch.empty(6, dim, device=DEV, dtype=I8)
+    scales = torch.empty(6, -(-dim // group) if group else 1, device=DEV)
+    R.umap_rows_norm(x, q, y_scales=scales, group=group)
+    back = torch.empty(6, dim, device=DEV)
+    R.umap_rows_lookup(q, None, back, table_scales=scales, group=group)
+    assert bool(back[[0, 2, 5]].isfinite().all()) and bool(back[1].isnan().all())
+    assert bool(back[3, 0].isnan()) and bool(back[4, dim - 1].isnan())
+    assert not bool(q[[1, 3, 4]].any())
+
+
+def test_norm_offsets_beyond_32_bits():
+    pitch = 2**30 + 8
+    x = torch.empty(4 * pitch + 64, device=DEV, dtype=BF16).as_strided((5, 64), (pitch, 1))
+    x[:] = rand(5, 64, BF16)
+    y = torch.empty(4 * pitch + 64, device=DEV, dtype=BF16).as_strided((5, 64), (pitch, 1))
+    R.umap_rows_norm(x, y)
+    near(y.clone(), ref.norm(ref.values(x), None, None, 1e-6)[1], ref.norm_bound(ref.values(x), None, None, 1e-6, BF16))
+    check_norm(x, F32, ids=torch.tensor([4, 0, 3], device=DEV))
+
+
+# ---- gradient of the norm ---------------------------------------------------------------------------
+
+
+def norm_grad(dy, h, weight=None, dh=None, want_dw=True, eps=1e-6, pad=0, shift=0, into=None):
+    n, dim = dy.shape
+    whole, dx = hole(n, dim, dy.dtype, pad, shift)
+    dx = dx if into is None else into
+    dw = torch.full((dim,), 7.0, device=DEV) if want_dw else None
+    work = None
+    if want_dw:
+        work = torch.empty(R.umap_rows_norm_grad_workspace(n, dim), dtype=torch.uint8, device=DEV)
+        work.random_(0, 256)
+    R.umap_rows_norm_grad(dy, h, dx, weight=weight, dh=dh, dweight=dw, workspace=work, eps=eps)
+    assert frame_untouched(whole, dim, shift)
+    return dx, dw
+
+
+def check_norm_grad(dy, h, weight=None, dh=None, want_dw=True, eps=1e-6, **kw):
+    n, dim = dy.shape
+    w64 = None if weight is None else ref.values(weight[None])[0]
+    dx64, size, dw64, dw_size = ref.norm_grad(ref.values(dy), ref.values(h), w64, eps, None if dh is None else ref.values(dh))
+    steps = (-(-dim // 64) + 40) * ref.E32
+    dx, dw = norm_grad(dy, h, weight, dh, want_dw, eps, **kw)
+    near(dx, dx64, ref.U[dy.dtype] * dx64.abs() + steps * size + ref.TINY[dy.dtype])
+    if want_dw:
+        near(dw[None], dw64[None], ((n + 8) * ref.E32 + steps) * dw_size[None] + 1e-45)
+
+
+@pytest.mark.parametrize("dim", DIMS + [16384, 20001, 32768])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_norm_grad_dims(dim, dtype):
+    w = (1 + 0.2 * torch.randn(dim, device=DEV)).to(dtype)
+    check_norm_grad(rand(13, dim, dtype), rand(13, dim, dtype, spread=2.0), w, rand(13, dim, dtype))
+
+
+@pytest.mark.parametrize("dim", [1, 40, 784, 4096, 9001])
+@pytest.mark.parametrize("with_dh", [False, True])
+@pytest.mark.parametrize("with_dw", [False, True])
+@pytest.mark.parametrize("with_w", [False, True])
+def test_norm_grad_with_and_without_its_parts(dim, with_dh, with_dw, with_w):
+    check_norm_grad(rand(5, dim, BF16), rand(5, dim, BF16), rand(1, dim, F32)[0] if with_w else None,
+                    rand(5, dim, BF16) if with_dh else None, with_dw)
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 3, 5, 255, 511, 513, 4099])
+@pytest.mark.parametrize("dim", [48, 1024])
+def test_norm_grad_row_counts(n, dim):
+    check_norm_grad(rand(n, dim, BF16), rand(n, dim, BF16), rand(1, dim, BF16)[0])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 0), (0, 1), (5, 3)])
+def test_norm_grad_strides_and_alignment(dtype, pad, shift):
+    for dim in (5, 64, 301, 2049):
+        w = rand(1, dim + 1, dtype)[0, 1:]
+        check_norm_grad(rand(21, dim, dtype, pad, shift), rand(21, dim, dtype, shift, pad), w, rand(21, dim, dtype),
+                        pad=shift, shift=pad)
+
+
+@pytest.mark.parametrize("dim", [33, 1000, 4096, 20001])
+def test_norm_grad_in_place(dim):
+    w = rand(1, dim, BF16)[0]
+    for which in ("dy", "dh"):
+        dy, h, dh = (rand(700, dim, BF16) for _ in range(3))
+        check_norm_grad(dy.clone(), h, w, dh.clone())
+        plain = norm_grad(dy, h, w, dh)
+        into = dy if which == "dy" else dh
+        got = norm_grad(dy, h, w, dh, into=into)
+        assert torch.equal(got[0], plain[0]) and torch.equal(got[1], plain[1])
+
+
+def test_norm_grad_of_a_broadcast_row():
+    dy = rand(1, 130, F32).expand(600, 130)
+    check_norm_grad(dy, rand(600, 130, F32), rand(1, 130, F32)[0])
+
+
+@pytest.mark.parametrize("dim", [40, 1000, 9000])
+def test_norm_grad_of_rows_of_zeros_and_of_large_rows(dim):
+    h = rand(6, dim, F32)
+    h[[0, 3]] = 0
+    check_norm_grad(rand(6, dim, F32), h, rand(1, dim, F32)[0])
+    for size in (1e19, 3e37):
+        check_norm_grad(rand(6, dim, F32), rand(6, dim, F32, spread=size).clamp(-3e38, 3e38), rand(1, dim, F32)[0])
+
+
+@pytest.mark.parametrize("dim", [9, 300, 2048, 9001])
+def test_norm_grad_keeps_nan_in_its_row(dim):
+    dy, h = rand(6, dim, BF16), rand(6, dim, BF16)
+    h[1, dim // 2], dy[4, 0] = float("nan"), float("nan")
+    dx, _ = norm_grad(dy, h)
+    assert bool(dx[[0, 2, 3, 5]].isfinite().all()) and bool(dx[[1, 4]].isnan().all())
+
+
+def test_norm_grad_same_bits_from_call_to_call():
+    dy, h, w = rand(3000, 300, BF16), rand(3000, 300, BF16), rand(1, 300, BF16)[0]
+    a = norm_grad(dy, h, w)
+    norm_grad(rand(77, 300, BF16), rand(77, 300, BF16), w)
+    b = norm_grad(dy, h, w)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dim", [7, 64, 784])
+def test_gradients_against_differences(dim):
+    """d/de of L = sum y dy at (T + e V, w + e q), y the norm of the looked-up rows, from differences in 64 bits."""
+    n, rows, scale = 90, 40, 2.0
+    table, w, dy = rand(rows, dim, F32), rand(1, dim, F32)[0], rand(n, dim, F32)
+    ids = zipf(n, rows)
+    h = torch.empty(n, dim, device=DEV)
+    R.umap_rows_lookup(table, ids, h, scale=scale)
+    dx, dw = norm_grad(dy, h, w)
+    grad = lookup_grad(dx, ids, rows, scale)
+    V, q = torch.randn(rows, dim, dtype=torch.float64), torch.randn(dim, dtype=torch.float64)
+
+    def L(e):
+        t = ref.values(table) + e * V
+        return float((ref.norm(ref.lookup(t, ids, scale), None, ref.values(w[None])[0] + e * q, 1e-6)[1] * ref.values(dy)).sum())
+
+    e = 1e-4
+    # fourth-order differences: the remainder is about e^4, far below the fp32 bound
+    slope = (8 * (L(e) - L(-e)) - (L(2 * e) - L(-2 * e))) / (12 * e)
+    got = float((ref.values(grad) * V).sum() + (ref.values(dw[None])[0] * q).sum())
+    _, size, _, dw_size = ref.norm_grad(ref.values(dy), ref.values(h), ref.values(w[None])[0], 1e-6)
+    bound = float((ref.lookup_grad(size, ids, rows, scale)[1] * V.abs()).sum() + (dw_size * q.abs()).sum())
+    assert abs(got - slope) <= (n + dim + 64) * ref.E32 * bound + 1e-7 * abs(slope) + 1e-6
+
+
+# ---- streams and graphs -----------------------------------------------------------------------------
+
+
+def _step(table, ids, w, dy, bufs, stream):
+    h, y, q, scales, back, dx, dw, grad, work, work2 = bufs
+    R.umap_rows_lookup(table, ids, h, scale=2.0, stream=stream)
+    R.umap_rows_norm(h, y, weight=w, stream=stream)
+    R.umap_rows_norm(table, q, weight=w, ids=ids, scale=2.0, y_scales=scales, group=64, stream=stream)
+    R.umap_rows_lookup(q, None, back, table_scales=scales, group=64, stream=stream)
+    R.umap_rows_norm_grad(dy, h, dx, weight=w, dweight=dw, workspace=work, stream=stream)
+    R.umap_rows_lookup_grad(dx, ids, grad, work2, scale=2.0, stream=stream)
+    return [h, y, q, scales, back, dx, dw, grad]
+
+
+def _bufs(n, rows, dim):
+    e = lambda *s, t=BF16: torch.zeros(*s, device=DEV, dtype=t)  # noqa: E731
+    return (e(n, dim), e(n, dim), e(n, dim, t=I8), e(n, -(-dim // 64), t=F32), e(n, dim), e(n, dim), e(dim, t=F32),
+            e(rows, dim, t=F32), e(R.umap_rows_norm_grad_workspace(n, dim), t=torch.uint8),
+            e(R.umap_rows_lookup_grad_workspace(n, rows, dim), t=torch.uint8))
+
+
+def test_on_a_stream_of_its_own_and_in_a_graph():
+    n, rows, dim = 20000, 5000, 200
+    table, w, dy, ids = rand(rows, dim, BF16), rand(1, dim, BF16)[0], rand(n, dim, BF16), zipf(n, rows)
+    want = [x.clone() for x in _step(table, ids, w, dy, _bufs(n, rows, dim), None)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    bufs = _bufs(n, rows, dim)
+    torch.cuda.synchronize()
+    got = _step(table, ids, w, dy, bufs, side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _step(table, ids, w, dy, bufs, torch.cuda.current_stream())
+    for k in range(4):
+        table.copy_(rand(rows, dim, BF16))
+        ids.copy_(zipf(n, rows))
+        dy.copy_(rand(n, dim, BF16))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = [x.clone() for x in got]
+        want = _step(table, ids, w, dy, _bufs(n, rows, dim), None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(seen, want)), k
