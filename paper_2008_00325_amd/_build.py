@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libumap_layout.so")
 
 SOURCES = ["api.hip", "kernels_prep.hip", "kernels_layout.hip", "kernels_hogwild.hip", "kernels_graph.hip",
-           "kernels_probe.hip", "kernels_trust.hip", "rows_api.hip", "kernels_rows.hip", "kernels_rows_grad.hip",
+           "kernels_probe.hip", "kernels_trust.hip", "rows_api.hip", "kernels_rows.hip", "kernels_rows_norm.hip",
+           "kernels_rows_grad.hip",
            "device_memory.cpp", "fit_ab.cpp"]
 
 HIPCC_FLAGS = [

@@ -12,6 +12,30 @@ namespace ul {
 
 namespace {
 
+// Element `i` of an array of type `type` as fp32 (8-bit values without their scale).
+__device__ __forceinline__ float load_elem(const void *p, int32_t type, int64_t i)
+{
+    switch (type) {
+    case UMAP_F32: return static_cast<const float *>(p)[i];
+    case UMAP_F16: return (float)static_cast<const _Float16 *>(p)[i];
+    case UMAP_BF16: return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
+    case UMAP_I8: return (float)static_cast<const int8_t *>(p)[i];
+    default: return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t *>(p)[i], 0);
+    }
+}
+
+// Rounds to nearest even; 8-bit values come in range.
+__device__ __forceinline__ void store_elem(void *p, int32_t type, int64_t i, float v)
+{
+    switch (type) {
+    case UMAP_F32: static_cast<float *>(p)[i] = v; break;
+    case UMAP_F16: static_cast<_Float16 *>(p)[i] = (_Float16)v; break;
+    case UMAP_BF16: static_cast<__bf16 *>(p)[i] = (__bf16)v; break;
+    case UMAP_I8: static_cast<int8_t *>(p)[i] = (int8_t)rintf(v); break;
+    default: static_cast<uint8_t *>(p)[i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false); break;
+    }
+}
+
 constexpr int kThreads = 256;
 constexpr int kItems = 16;
 constexpr int kTile = kThreads * kItems;
@@ -28,7 +52,7 @@ struct Keys {
     __device__ __forceinline__ uint32_t operator()(int64_t t) const
     {
         if (keys) return keys[t];
-        const int64_t v = row_of(ids.data, ids.bytes, t, rows);
+        const int64_t v = row_of(ids, t, rows);
         return v < 0 ? (uint32_t)rows : (uint32_t)v;
     }
 };

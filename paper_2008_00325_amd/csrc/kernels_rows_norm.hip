@@ -1,0 +1,785 @@
+// kernels_rows_norm.hip -- root-mean-square norm of rows and its gradient (umap_rows.h).
+//
+// Bound by memory: a row is read once and stays in registers between its sum of squares
+// and its result, so every input is read and every output written once.  A row belongs
+// to a wave (up to 2,048 columns) or to a workgroup; a thread holds kVec vectors of 8
+// columns of it, and reads its share of the next row before it works on this one.
+#include <algorithm>
+
+#include "rows_device.hpp"
+
+namespace ul {
+
+namespace {
+
+// Lane exchanges inside rows of 16 lanes, without LDS.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v)
+{
+    return v + __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
+}
+// Sum over 8, 16, 32 or 64 neighbouring lanes.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v = add_dpp<kXor1>(v);
+    v = add_dpp<kXor2>(v);
+    v = add_dpp<kHalfMirror>(v);
+    if constexpr (LANES >= 16) v = add_dpp<kMirror>(v);
+    if constexpr (LANES >= 32) v += __shfl_xor(v, 16);
+    if constexpr (LANES >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+__device__ __forceinline__ uint32_t max_u(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// Largest of 4, 8 or 16 neighbouring lanes.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes)
+{
+    v = max_u(v, dpp<kXor1>(v));
+    v = max_u(v, dpp<kXor2>(v));
+    if (lanes >= 8) v = max_u(v, dpp<kHalfMirror>(v));
+    if (lanes >= 16) v = max_u(v, dpp<kMirror>(v));
+    return v;
+}
+
+// Sums and maxima over a row's threads: LANES of a wave, or (kBlock) a workgroup.  Two
+// buffers take turns, so that one barrier per value is enough: a buffer is written again
+// only after the next value's barrier.
+constexpr int kBlock = 0;
+struct RowLds {
+    float v[2][2][16];
+};
+template <int LANES>
+struct RowThreads {
+    RowLds *lds;
+    int turn = 0;
+    __device__ __forceinline__ void sum2(float &a, float &b)
+    {
+        a = lanes_sum<LANES ? LANES : 64>(a);
+        b = lanes_sum<LANES ? LANES : 64>(b);
+        if constexpr (LANES == kBlock) {
+            if ((threadIdx.x & 63) == 0) {
+                lds->v[turn][0][threadIdx.x >> 6] = a;
+                lds->v[turn][1][threadIdx.x >> 6] = b;
+            }
+            __syncthreads();
+            a = b = 0.0f;
+            for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+                a += lds->v[turn][0][w];
+                b += lds->v[turn][1][w];
+            }
+            turn ^= 1;
+        }
+    }
+    __device__ __forceinline__ float sum(float a)
+    {
+        a = lanes_sum<LANES ? LANES : 64>(a);
+        if constexpr (LANES == kBlock) {
+            if ((threadIdx.x & 63) == 0) lds->v[turn][0][threadIdx.x >> 6] = a;
+            __syncthreads();
+            a = 0.0f;
+            for (int w = 0; w < (int)(blockDim.x >> 6); ++w) a += lds->v[turn][0][w];
+            turn ^= 1;
+        }
+        return a;
+    }
+    __device__ __forceinline__ uint32_t max(uint32_t a)
+    {
+        constexpr int kLanes = LANES ? LANES : 64;
+        a = lanes_max(a, kLanes);
+        if constexpr (kLanes >= 32) a = max_u(a, (uint32_t)__shfl_xor((int)a, 16));
+        if constexpr (kLanes >= 64) a = max_u(a, (uint32_t)__shfl_xor((int)a, 32));
+        if constexpr (LANES == kBlock) {
+            if ((threadIdx.x & 63) == 0) lds->v[turn][0][threadIdx.x >> 6] = __uint_as_float(a);
+            __syncthreads();
+            for (int w = 0; w < (int)(blockDim.x >> 6); ++w) a = max_u(a, __float_as_uint(lds->v[turn][0][w]));
+            turn ^= 1;
+        }
+        return a;
+    }
+};
+
+// Whether a sum of squares lost its value to fp32's range: too large, or so small that
+// squares vanished and eps does not outweigh them.  Then the row is taken times
+// range_step(sum), a power of two.
+__device__ __forceinline__ bool out_of_range(float sum, float eps)
+{
+    return !(sum < __builtin_inff()) || (sum < 0x1p-60f && eps < 0x1p-60f);
+}
+__device__ __forceinline__ float range_step(float sum) { return sum < 1.0f ? 0x1p80f : 0x1p-80f; }
+
+// Vector i of a thread: columns c = 8 (thread + i TPR) .. c + 7.  Where the row ends inside
+// it, the vector is taken from column cols - 8 on instead, and its first `dup` columns
+// are another vector's too: they count in no sum, and are written with the same values.
+struct Cols {
+    int at;    // first column
+    int dup;   // 8 and more: past the row
+    __device__ __forceinline__ Cols(int c, int cols) : at(min(c, cols - 8)), dup(c - at) {}
+    __device__ __forceinline__ bool live() const { return dup < 8; }
+    __device__ __forceinline__ bool counts(int j) const { return j >= dup; }
+};
+
+template <int T>
+__device__ __forceinline__ const Elem<T> *row_ptr(const umap_rows &m, int64_t t)
+{
+    return static_cast<const Elem<T> *>(m.data) + t * m.stride;
+}
+template <int T>
+__device__ __forceinline__ Elem<T> *row_out(const umap_rows &m, int64_t t)
+{
+    return static_cast<Elem<T> *>(m.data) + t * m.stride;
+}
+
+__device__ __forceinline__ void load_weight(const RowWeight &weight, int c, float w[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+    if (!weight.data) return;
+    switch (weight.type) {
+    case UMAP_F32: floats8<UMAP_F32>(load8<UMAP_F32>(static_cast<const float *>(weight.data) + c), w); break;
+    case UMAP_F16: floats8<UMAP_F16>(load8<UMAP_F16>(static_cast<const _Float16 *>(weight.data) + c), w); break;
+    default: floats8<UMAP_BF16>(load8<UMAP_BF16>(static_cast<const uint16_t *>(weight.data) + c), w); break;
+    }
+}
+
+// LANES lanes of a wave per row, 256 / LANES rows to a workgroup of 256, or a row per
+// workgroup of any number of waves.
+template <int LANES>
+constexpr int kMostThreads = LANES ? 256 : 1024;
+template <int LANES>
+constexpr int kRowsPerBlock = LANES ? 256 / (LANES ? LANES : 1) : 1;
+template <int LANES>
+__device__ __forceinline__ int row_threads() { return LANES ? LANES : (int)blockDim.x; }
+template <int LANES>
+__device__ __forceinline__ int row_in_block()
+{
+    if constexpr (LANES == kBlock) return 0;
+    else if constexpr (LANES == 64) return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    else return threadIdx.x / LANES;
+}
+
+__device__ __forceinline__ float square_sum(const float e[8], const Cols &c)
+{
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fmaf(e[j], e[j], sum);
+    if (c.dup) {
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = c.counts(j) ? fmaf(e[j], e[j], sum) : sum;
+    }
+    return sum;
+}
+__device__ __forceinline__ float product_sum(const float e[8], const float g[8], const float w[8], const Cols &c)
+{
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fmaf(g[j] * w[j], e[j], sum);
+    if (c.dup) {
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = c.counts(j) ? fmaf(g[j] * w[j], e[j], sum) : sum;
+    }
+    return sum;
+}
+
+// The scale of a group whose largest magnitude has these bits, and the factor that
+// its values take to become 8-bit ones.
+template <int TY>
+struct Quant {
+    static constexpr float kMost = TY == UMAP_I8 ? 127.0f : 448.0f;
+    bool fine;
+    float scale, up;
+    __device__ __forceinline__ explicit Quant(uint32_t bits)
+    {
+        const float m = __uint_as_float(bits);
+        fine = bits >= __float_as_uint(0x1p-100f) && bits < 0x7f800000u;
+        scale = fine ? m * (1.0f / kMost) : bits < 0x7f800000u ? 0.0f : __builtin_nanf("");
+        up = kMost / m;
+    }
+    __device__ __forceinline__ float operator()(float v) const
+    {
+        if constexpr (TY == UMAP_I8) return fine ? rintf(v * up) : 0.0f;
+        else return fine ? v * up : 0.0f;
+    }
+};
+
+// VEC vectors of 8 columns per thread; cols >= 8.  MORE: a thread keeps its weights over
+// its rows and reads a row ahead.
+template <int TX, int TY, int LANES, int VEC, bool MORE>
+__global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, RowIds ids, float scale, umap_rows residual,
+                                                             umap_rows h, RowWeight weight, float eps, umap_rows y)
+{
+    constexpr int kRows = kRowsPerBlock<LANES>;
+    constexpr bool kEight = TY == UMAP_I8 || TY == UMAP_F8;
+    __shared__ RowLds lds;
+    RowThreads<LANES> row{&lds};
+    const int TPR = row_threads<LANES>(), me = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, cols = y.cols;
+    const float over_cols = 1.0f / (float)cols;
+    float w[MORE ? VEC : 1][8];
+    if constexpr (MORE) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[i]);
+    }
+
+    Raw8<TX> a[VEC], b[VEC];
+    auto read = [&](int64_t t) {
+        const int64_t v = row_of(ids, t, x.rows);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int at = Cols(8 * (me + i * TPR), cols).at;
+            if (v >= 0) a[i] = load8<TX>(row_ptr<TX>(x, v) + at);
+            else a[i] = Raw8<TX>{};   // a missing row stands for zeros
+            if (residual.data) b[i] = load8<TX>(row_ptr<TX>(residual, t) + at);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t t = (int64_t)blockIdx.x * kRows + row_in_block<LANES>();
+    if (MORE && t < y.rows) read(t);
+    for (; t < y.rows; t += step) {
+        if (!MORE) read(t);
+        float e[VEC][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            floats8<TX>(a[i], e[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[i][j] *= scale;
+            if (residual.data) {
+                float r[8];
+                floats8<TX>(b[i], r);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[i][j] += r[j];
+            }
+            sum += square_sum(e[i], Cols(8 * (me + i * TPR), cols));
+        }
+        if (MORE && t + step < y.rows) read(t + step);
+        sum = row.sum(sum);
+        if (h.data) {   // behind the sum's barrier: h may lie where other waves read
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const Cols c(8 * (me + i * TPR), cols);
+                if (c.live()) store8<TX>(row_out<TX>(h, t) + c.at, raw8<TX>(e[i]));
+            }
+        }
+        float add = eps;
+        if (out_of_range(sum, eps)) {
+            const float k = range_step(sum);
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[i][j] *= k;
+                sum += square_sum(e[i], Cols(8 * (me + i * TPR), cols));
+            }
+            sum = row.sum(sum);
+            add = eps * k * k;
+        }
+        const float rho = __builtin_amdgcn_rsqf(fmaf(sum, over_cols, add));
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            if constexpr (!MORE) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[i][j] = e[i][j] * rho * w[MORE ? i : 0][j];
+        }
+
+        if constexpr (!kEight) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const Cols c(8 * (me + i * TPR), cols);
+                if (c.live()) store8<TY>(row_out<TY>(y, t) + c.at, raw8<TY>(e[i]));
+            }
+        } else {
+            // magnitudes compare as their bits do, infinities and NaN above all others
+            uint32_t most[VEC], all = 0;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const Cols c(8 * (me + i * TPR), cols);
+                most[i] = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most[i] = max_u(most[i], __float_as_uint(e[i][j]) & 0x7fffffffu);
+                if (c.dup) {
+                    most[i] = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        most[i] = max_u(most[i], c.counts(j) ? __float_as_uint(e[i][j]) & 0x7fffffffu : 0);
+                }
+                all = max_u(all, most[i]);
+            }
+            if (y.group == 0) all = row.max(all);
+            const int lanes = LANES ? min(y.group / 8, LANES) : y.group / 8, groups = y.group ? (cols + y.group - 1) / y.group : 1;
+            float *const scales = y.scales + t * groups;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int v = me + i * TPR;
+                const Cols c(8 * v, cols);
+                const Quant<TY> quant(y.group ? lanes_max(most[i], lanes) : all);
+                if (!c.live()) continue;
+                if (y.group ? (v & (lanes - 1)) == 0 : v == 0) scales[y.group ? v / lanes : 0] = quant.scale;
+                float q[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = quant(e[i][j]);
+                Elem<TY> *const to = row_out<TY>(y, t) + c.at;
+                if (!c.dup) {
+                    store8<TY>(to, raw8<TY>(q));
+                } else {   // the columns of another vector may be another group's
+#pragma unroll
+                    for (int j = 1; j < 8; ++j)
+                        if (c.counts(j)) to[j] = float_elem<TY>(q[j]);
+                }
+            }
+        }
+    }
+}
+
+template <int TX, int LANES, int VEC, bool DW, bool MORE>
+__global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_rows dy, umap_rows h, umap_rows dh,
+                                                                  RowWeight weight, float eps, umap_rows dx,
+                                                                  float *partial)
+{
+    constexpr int kRows = kRowsPerBlock<LANES>;
+    __shared__ RowLds lds;
+    RowThreads<LANES> row{&lds};
+    const int TPR = row_threads<LANES>(), me = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, cols = dy.cols;
+    const float over_cols = 1.0f / (float)cols;
+    // dweight's sums of this thread's columns, in LDS where registers are short
+    constexpr bool kInLds = DW && LANES == kBlock && VEC > 1;
+    extern __shared__ float dw_lds[];
+    float w[MORE ? VEC : 1][8], dw[DW && !kInLds ? VEC : 1][8];
+    auto dw_at = [&](int i, int j) -> float & { return dw_lds[(i * 8 + j) * TPR + me]; };
+    if constexpr (MORE) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < (DW ? VEC : 1); ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (kInLds) dw_at(i, j) = 0.0f;
+            else dw[i][j] = 0.0f;
+        }
+    Raw8<TX> a[VEC], b[VEC], u[VEC];
+    auto read = [&](int64_t t) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int at = Cols(8 * (me + i * TPR), cols).at;
+            a[i] = load8<TX>(row_ptr<TX>(h, t) + at);
+            b[i] = load8<TX>(row_ptr<TX>(dy, t) + at);
+            if (dh.data) u[i] = load8<TX>(row_ptr<TX>(dh, t) + at);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t t = (int64_t)blockIdx.x * kRows + row_in_block<LANES>();
+    if (MORE && t < dy.rows) read(t);
+    for (; t < dy.rows; t += step) {
+        if (!MORE) read(t);
+        Raw8<TX> ha[VEC], db[VEC], ua[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            ha[i] = a[i];
+            db[i] = b[i];
+            if (dh.data) ua[i] = u[i];
+        }
+        if (MORE && t + step < dy.rows) read(t + step);
+        auto sums = [&](float k, float &sum, float &dot) {
+            sum = dot = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const Cols c(8 * (me + i * TPR), cols);
+                float e[8], g[8];
+                floats8<TX>(ha[i], e);
+                floats8<TX>(db[i], g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] *= k;
+                if constexpr (!MORE) load_weight(weight, c.at, w[0]);
+                sum += square_sum(e, c);
+                dot += product_sum(e, g, w[MORE ? i : 0], c);
+            }
+            row.sum2(sum, dot);
+        };
+        float sum, dot, add = eps, k = 1.0f;
+        sums(1.0f, sum, dot);
+        if (out_of_range(sum, eps)) {
+            k = range_step(sum);
+            sums(k, sum, dot);
+            add = eps * k * k;
+        }
+        if constexpr (kInLds && VEC == 2) {   // the floats are formed anew below: kept, they would spill
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+#pragma unroll
+                for (int j = 0; j < Raw8<TX>::kWords; ++j) asm volatile("" : "+v"(ha[i].w[j]), "+v"(db[i].w[j]));
+        }
+        // of the row times k: unit = h k rho, dx = k rho (g - unit (dot rho / cols))
+        const float rho = __builtin_amdgcn_rsqf(fmaf(sum, over_cols, add));
+        const float along = dot * rho * over_cols, out = k * rho;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const Cols c(8 * (me + i * TPR), cols);
+            float e[8], g[8], r[8];
+            floats8<TX>(ha[i], e);
+            floats8<TX>(db[i], g);
+            if constexpr (!MORE) load_weight(weight, c.at, w[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float unit = e[j] * k * rho;
+                if constexpr (kInLds) dw_at(i, j) = fmaf(g[j], unit, dw_at(i, j));
+                else if constexpr (DW) dw[i][j] = fmaf(g[j], unit, dw[i][j]);
+                r[j] = out * (g[j] * w[MORE ? i : 0][j] - unit * along);
+            }
+            if (dh.data) {
+                floats8<TX>(ua[i], e);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) r[j] += e[j];
+            }
+            if (c.live()) store8<TX>(row_out<TX>(dx, t) + c.at, raw8<TX>(r));
+        }
+    }
+    if constexpr (DW) {
+        float *const to = partial + (int64_t)blockIdx.x * cols;
+        constexpr int kShared = LANES ? VEC * 8 * 64 : 1;
+        __shared__ float total[kShared];
+        if constexpr (LANES) {   // the wave's rows, then the block's waves, in order
+            const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+            for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dw[i][j] += __shfl_xor(dw[i][j], o);
+            for (int s = 0; s < 4; ++s) {
+                if (wave == s) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float &at = total[(i * 8 + j) * 64 + lane];
+                            if (s) dw[i][j] += at;
+                            at = dw[i][j];
+                        }
+                }
+                __syncthreads();
+            }
+            if (wave != 3 || lane >= LANES) return;
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const Cols c(8 * (me + i * TPR), cols);
+            float sums[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (kInLds) sums[j] = dw_at(i, j);
+                else sums[j] = dw[i][j];
+            }
+            if (!c.dup) {
+                store8<UMAP_F32>(to + c.at, raw8<UMAP_F32>(sums));
+            } else {
+#pragma unroll
+                for (int j = 1; j < 8; ++j)
+                    if (c.counts(j)) to[c.at + j] = sums[j];
+            }
+        }
+    }
+}
+
+// ---- rows of fewer than 8 columns: a thread per row ----
+constexpr int kNarrow = 7;
+
+__device__ __forceinline__ float weight_at(const RowWeight &weight, int c)
+{
+    if (!weight.data) return 1.0f;
+    switch (weight.type) {
+    case UMAP_F32: return static_cast<const float *>(weight.data)[c];
+    case UMAP_F16: return elem_float<UMAP_F16>(static_cast<const _Float16 *>(weight.data)[c]);
+    default: return elem_float<UMAP_BF16>(static_cast<const uint16_t *>(weight.data)[c]);
+    }
+}
+
+template <int TX, int TY>
+__global__ __launch_bounds__(256) void k_rows_norm_narrow(umap_rows x, RowIds ids, float scale, umap_rows residual,
+                                                          umap_rows h, RowWeight weight, float eps, umap_rows y)
+{
+    const int cols = y.cols;
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < y.rows; t += step) {
+        const int64_t v = row_of(ids, t, x.rows);
+        float e[kNarrow], sum = 0.0f, add = eps;
+#pragma unroll
+        for (int c = 0; c < kNarrow; ++c) {
+            e[c] = 0.0f;
+            if (c >= cols) continue;
+            if (v >= 0) e[c] = elem_float<TX>(row_ptr<TX>(x, v)[c]) * scale;
+            if (residual.data) e[c] += elem_float<TX>(row_ptr<TX>(residual, t)[c]);
+            if (h.data) row_out<TX>(h, t)[c] = float_elem<TX>(e[c]);
+            sum = fmaf(e[c], e[c], sum);
+        }
+        if (out_of_range(sum, eps)) {
+            const float k = range_step(sum);
+            sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < kNarrow; ++c) {
+                e[c] *= k;
+                sum = fmaf(e[c], e[c], sum);
+            }
+            add = eps * k * k;
+        }
+        const float rho = __builtin_amdgcn_rsqf(sum / (float)cols + add);
+        uint32_t most = 0;
+#pragma unroll
+        for (int c = 0; c < kNarrow; ++c) {
+            if (c >= cols) continue;
+            e[c] = e[c] * rho * weight_at(weight, c);
+            most = max_u(most, __float_as_uint(e[c]) & 0x7fffffffu);
+        }
+        if constexpr (TY == UMAP_I8 || TY == UMAP_F8) {
+            const Quant<TY> quant(most);
+            y.scales[t] = quant.scale;   // one group
+#pragma unroll
+            for (int c = 0; c < kNarrow; ++c)
+                if (c < cols) row_out<TY>(y, t)[c] = float_elem<TY>(quant(e[c]));
+        } else {
+#pragma unroll
+            for (int c = 0; c < kNarrow; ++c)
+                if (c < cols) row_out<TY>(y, t)[c] = float_elem<TY>(e[c]);
+        }
+    }
+}
+
+template <int TX>
+__global__ __launch_bounds__(256) void k_rows_norm_grad_narrow(umap_rows dy, umap_rows h, umap_rows dh, RowWeight weight,
+                                                               float eps, umap_rows dx, float *partial)
+{
+    __shared__ float part[4][kNarrow];
+    const int cols = dy.cols;
+    const int64_t step = (int64_t)gridDim.x * 256;
+    float dw[kNarrow] = {};
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < dy.rows; t += step) {
+        float e[kNarrow], g[kNarrow], sum = 0.0f, dot = 0.0f, add = eps, k = 1.0f;
+#pragma unroll
+        for (int c = 0; c < kNarrow; ++c) {
+            e[c] = c < cols ? elem_float<TX>(row_ptr<TX>(h, t)[c]) : 0.0f;
+            g[c] = c < cols ? elem_float<TX>(row_ptr<TX>(dy, t)[c]) : 0.0f;
+            sum = fmaf(e[c], e[c], sum);
+        }
+        if (out_of_range(sum, eps)) {
+            k = range_step(sum);
+            sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < kNarrow; ++c) {
+                e[c] *= k;
+                sum = fmaf(e[c], e[c], sum);
+            }
+            add = eps * k * k;
+        }
+        const float rho = __builtin_amdgcn_rsqf(sum / (float)cols + add);
+#pragma unroll
+        for (int c = 0; c < kNarrow; ++c) {
+            if (c >= cols) continue;
+            e[c] *= rho;
+            dw[c] = fmaf(g[c], e[c], dw[c]);
+            g[c] *= weight_at(weight, c);
+            dot = fmaf(g[c], e[c], dot);
+        }
+        const float along = dot / (float)cols;
+#pragma unroll
+        for (int c = 0; c < kNarrow; ++c) {
+            if (c >= cols) continue;
+            float r = k * rho * (g[c] - e[c] * along);
+            if (dh.data) r += elem_float<TX>(row_ptr<TX>(dh, t)[c]);
+            row_out<TX>(dx, t)[c] = float_elem<TX>(r);
+        }
+    }
+    if (!partial) return;
+#pragma unroll
+    for (int c = 0; c < kNarrow; ++c) {
+        const float sum = lanes_sum<64>(dw[c]);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][c] = sum;
+    }
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c < cols) partial[(int64_t)blockIdx.x * cols + c] = part[0][c] + part[1][c] + part[2][c] + part[3][c];
+}
+
+// out[c] = partial[0][c] + .. + partial[count - 1][c]: 64 columns per workgroup, each of its
+// waves adding a stretch of the rows, then the stretches in order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void k_rows_join(const float *partial, int count, int cols, float *out)
+{
+    __shared__ float part[kJoinWaves][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
+    const int per = (count + kJoinWaves - 1) / kJoinWaves, first = wave * per, last = min(first + per, count);
+    float sum = 0.0f;
+    if (c < cols) {
+#pragma unroll 8
+        for (int b = first; b < last; ++b) sum += partial[(int64_t)b * cols + c];
+    }
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+        for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+        out[c] = sum;
+    }
+}
+
+// How rows lie in workgroups: threads and rows of one.
+struct RowShape {
+    int threads;
+    int rows;
+};
+constexpr int kOneThread = -1;
+// Lanes of a wave while two vectors per lane hold the row, else a workgroup of as many
+// waves as VEC vectors per thread take: one up to `one` columns, two up to 16,384, then
+// four; one thread below 8 columns.
+template <template <int, int> class Launch, typename... Args>
+auto by_cols(int cols, int one, Args... args)
+{
+    const int vectors = (cols + 7) / 8;
+    auto waves = [&](int vec) { return RowShape{64 * ((vectors + 64 * vec - 1) / (64 * vec)), 1}; };
+    if (cols < 8) return Launch<kOneThread, 1>::go(RowShape{256, 256}, args...);
+    if (cols <= 64) return Launch<8, 1>::go(RowShape{256, 32}, args...);
+    if (cols <= 128) return Launch<16, 1>::go(RowShape{256, 16}, args...);
+    if (cols <= 256) return Launch<32, 1>::go(RowShape{256, 8}, args...);
+    if (cols <= 512) return Launch<64, 1>::go(RowShape{256, 4}, args...);
+    if (cols <= 1024) return Launch<64, 2>::go(RowShape{256, 4}, args...);
+    if (cols <= one) return Launch<kBlock, 1>::go(waves(1), args...);
+    if (cols <= 16384) return Launch<kBlock, 2>::go(waves(2), args...);
+    return Launch<kBlock, 4>::go(waves(4), args...);
+}
+
+// Rows that one workgroup takes in turn: few, so that workgroups end and start all the
+// time and the card stays evenly loaded, but enough to read ahead.  us per call on 256 MB
+// of bf16 rows, norm with residual into int8, with 1 / 2 / 4 / 8 turns: 64 columns - / - / 186 /
+// 190, 300 276 / 217 / 203 / 203, 1,024 180 / 166 / 174 / 178, 2,048 179 / 161 / - / 194, 4,096 186 / 166
+// / - / 184, 8,192 193 / 165 / 176 / 173, 16,384 215 / 198 / 185 / 176.  Less where that would leave
+// fewer than four workgroups for each CU.
+unsigned grid_for(int64_t work, int cols)
+{
+    int64_t turns = cols <= 512 ? 4 : cols <= 8192 ? 2 : 8;
+    while (turns > 1 && work / turns < 1024) turns /= 2;
+    return (unsigned)((work + turns - 1) / turns);
+}
+
+// Where every workgroup ends with a sum to hand over: as many as the card holds at once
+// (`waves` of them on a CU), all with the same number of rows, give or take one.
+int64_t even_grid(int64_t work, int threads, int waves)
+{
+    const int64_t most = 256 * std::max(1, waves * 64 / threads);
+    const int64_t turns = (work + most - 1) / most;
+    return (work + turns - 1) / turns;
+}
+// us per call on 256 MB of bf16 rows with upstream gradient and dweight at 8 / 12 / 16 / 20 / 24
+// waves on a CU: 64 columns - / - / 209 / - / 229, 300 341 / - / 241 / 232 / 236, 784 208 / 219 / 239 / - / -,
+// 1,024 204 / 207 / 221 / - / -, 2,048 223 / - / 215 / 226 / 247, 4,096 214 / - / 191 / 191 / 225, 8,192 319 /
+// - / 205 / 206 / 206 (one workgroup).
+constexpr int grad_waves(int lanes, int vec) { return lanes == 64 && vec == 2 ? 8 : 16; }
+
+template <int TX, int TY>
+struct Norm {
+    template <int LANES, int VEC>
+    struct With {
+        static hipError_t go(RowShape shape, const umap_rows *x, RowIds ids, float scale, const umap_rows *residual,
+                             const umap_rows *h, RowWeight weight, float eps, const umap_rows *y, hipStream_t s)
+        {
+            const int64_t work = (y->rows + shape.rows - 1) / shape.rows;
+            const dim3 grid(VEC == 4 ? (unsigned)even_grid(work, shape.threads, 16) : grid_for(work, y->cols));
+            const dim3 threads(shape.threads);
+            const umap_rows r = residual ? *residual : umap_rows{}, to = h ? *h : umap_rows{};
+            if constexpr (LANES == kOneThread)
+                hipLaunchKernelGGL((k_rows_norm_narrow<TX, TY>), grid, threads, 0, s, *x, ids, scale, r, to, weight, eps, *y);
+            else
+                hipLaunchKernelGGL((k_rows_norm<TX, TY, LANES, VEC, (VEC < 4)>), grid, threads, 0, s, *x, ids, scale, r, to, weight, eps, *y);
+            return hipGetLastError();
+        }
+    };
+};
+
+template <int LANES, int VEC>
+struct GradBlocks {
+    static int64_t go(RowShape shape, int64_t n)
+    {
+        return even_grid((n + shape.rows - 1) / shape.rows, shape.threads, grad_waves(LANES, VEC));
+    }
+};
+constexpr int kGradOne = 8192, kNormOne = 4096;   // columns up to which one vector per thread measured best
+
+template <int TX>
+struct Grad {
+    template <int LANES, int VEC>
+    struct With {
+        static hipError_t go(RowShape shape, const umap_rows *dy, const umap_rows *h, const umap_rows *dh,
+                             RowWeight weight, float eps, const umap_rows *dx, float *partial, int64_t *count, hipStream_t s)
+        {
+            const int64_t work = (dy->rows + shape.rows - 1) / shape.rows;
+            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows) : grid_for(work, dy->cols);
+            const dim3 grid((unsigned)*count), threads(shape.threads);
+            const size_t sums = LANES == kBlock && VEC > 1 ? (size_t)shape.threads * VEC * 32 : 0;
+            const umap_rows up = dh ? *dh : umap_rows{};
+            if constexpr (LANES == kOneThread)
+                hipLaunchKernelGGL((k_rows_norm_grad_narrow<TX>), grid, threads, 0, s, *dy, *h, up, weight, eps, *dx, partial);
+            else if (partial)
+                hipLaunchKernelGGL((k_rows_norm_grad<TX, LANES, VEC, true, (VEC < 4)>), grid, threads, sums, s, *dy, *h, up, weight, eps, *dx, partial);
+            else
+                hipLaunchKernelGGL((k_rows_norm_grad<TX, LANES, VEC, false, (VEC < 4)>), grid, threads, 0, s, *dy, *h, up, weight, eps, *dx, nullptr);
+            return hipGetLastError();
+        }
+    };
+};
+
+template <int TX, typename... Args>
+hipError_t norm_from(int32_t type, int cols, Args... args)
+{
+    switch (type) {
+    case UMAP_F32: return by_cols<Norm<TX, UMAP_F32>::template With>(cols, kNormOne, args...);
+    case UMAP_F16: return by_cols<Norm<TX, UMAP_F16>::template With>(cols, kNormOne, args...);
+    case UMAP_BF16: return by_cols<Norm<TX, UMAP_BF16>::template With>(cols, kNormOne, args...);
+    case UMAP_I8: return by_cols<Norm<TX, UMAP_I8>::template With>(cols, kNormOne, args...);
+    default: return by_cols<Norm<TX, UMAP_F8>::template With>(cols, kNormOne, args...);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rows_norm(const umap_rows &x, RowIds ids, float scale, const umap_rows *residual, const umap_rows *h,
+                            RowWeight weight, float eps, const umap_rows &y, hipStream_t s)
+{
+    switch (x.type) {
+    case UMAP_F32: return norm_from<UMAP_F32>(y.type, y.cols, &x, ids, scale, residual, h, weight, eps, &y, s);
+    case UMAP_F16: return norm_from<UMAP_F16>(y.type, y.cols, &x, ids, scale, residual, h, weight, eps, &y, s);
+    default: return norm_from<UMAP_BF16>(y.type, y.cols, &x, ids, scale, residual, h, weight, eps, &y, s);
+    }
+}
+
+int64_t rows_norm_grad_bytes(int64_t n, int32_t cols)
+{
+    if (n < 1) return 16;
+    return by_cols<GradBlocks>(cols, kGradOne, n) * cols * 4;   // one sum of dweight per workgroup
+}
+
+hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const umap_rows *dh, RowWeight weight,
+                                 float eps, const umap_rows &dx, float *dweight, void *workspace, hipStream_t s)
+{
+    int64_t count = 0;
+    float *const partial = dweight ? static_cast<float *>(workspace) : nullptr;
+    if (dy.rows > 0) {
+        hipError_t e;
+        switch (dy.type) {
+        case UMAP_F32: e = by_cols<Grad<UMAP_F32>::With>(dy.cols, kGradOne, &dy, &h, dh, weight, eps, &dx, partial, &count, s); break;
+        case UMAP_F16: e = by_cols<Grad<UMAP_F16>::With>(dy.cols, kGradOne, &dy, &h, dh, weight, eps, &dx, partial, &count, s); break;
+        default: e = by_cols<Grad<UMAP_BF16>::With>(dy.cols, kGradOne, &dy, &h, dh, weight, eps, &dx, partial, &count, s); break;
+        }
+        if (e != hipSuccess) return e;
+    }
+    if (dweight) {
+        hipLaunchKernelGGL(k_rows_join, dim3((dy.cols + 63) / 64), dim3(64 * kJoinWaves), 0, s, partial, (int)count,
+                           dy.cols, dweight);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+}  // namespace ul

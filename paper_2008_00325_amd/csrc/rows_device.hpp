@@ -1,42 +1,152 @@
-// rows_device.hpp -- element types and row helpers of the token-row kernels.
+// rows_device.hpp -- element types and vectors of 8 elements of the token-row kernels.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "umap_rows.h"
+#include "rows_internal.hpp"
 
 namespace ul {
 
-// Element `i` of an array of type `type` as fp32 (8-bit values without their scale).
-__device__ __forceinline__ float load_elem(const void *p, int32_t type, int64_t i)
-{
-    switch (type) {
-    case UMAP_F32: return static_cast<const float *>(p)[i];
-    case UMAP_F16: return (float)static_cast<const _Float16 *>(p)[i];
-    case UMAP_BF16: return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
-    case UMAP_I8: return (float)static_cast<const int8_t *>(p)[i];
-    default: return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t *>(p)[i], 0);
-    }
-}
-
-// Rounds to nearest even; 8-bit values come in range.
-__device__ __forceinline__ void store_elem(void *p, int32_t type, int64_t i, float v)
-{
-    switch (type) {
-    case UMAP_F32: static_cast<float *>(p)[i] = v; break;
-    case UMAP_F16: static_cast<_Float16 *>(p)[i] = (_Float16)v; break;
-    case UMAP_BF16: static_cast<__bf16 *>(p)[i] = (__bf16)v; break;
-    case UMAP_I8: static_cast<int8_t *>(p)[i] = (int8_t)rintf(v); break;
-    default: static_cast<uint8_t *>(p)[i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false); break;
-    }
-}
+__device__ __forceinline__ int64_t row_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // Row of id t, or -1 where it lies outside [0, rows).
-__device__ __forceinline__ int64_t row_of(const void *ids, int32_t bytes, int64_t t, int64_t rows)
+__device__ __forceinline__ int64_t row_of(const RowIds &ids, int64_t t, int64_t rows)
 {
-    const int64_t v = bytes == 4 ? (int64_t)static_cast<const int32_t *>(ids)[t] : bytes == 8 ? static_cast<const int64_t *>(ids)[t] : t;
+    const int64_t v = ids.bytes == 4   ? (int64_t)static_cast<const int32_t *>(ids.data)[t]
+                      : ids.bytes == 8 ? static_cast<const int64_t *>(ids.data)[t]
+                                       : t;
     return v >= 0 && v < rows ? v : -1;
+}
+
+template <int T>
+struct ElemOf;
+template <>
+struct ElemOf<UMAP_F32> { using type = float; };
+template <>
+struct ElemOf<UMAP_F16> { using type = _Float16; };
+template <>
+struct ElemOf<UMAP_BF16> { using type = uint16_t; };
+template <>
+struct ElemOf<UMAP_I8> { using type = int8_t; };
+template <>
+struct ElemOf<UMAP_F8> { using type = uint8_t; };
+template <int T>
+using Elem = typename ElemOf<T>::type;
+
+template <int T>
+__device__ __forceinline__ float elem_float(Elem<T> e)
+{
+    if constexpr (T == UMAP_BF16) return __uint_as_float((uint32_t)e << 16);
+    else if constexpr (T == UMAP_F8) return __builtin_amdgcn_cvt_f32_fp8(e, 0);
+    else return (float)e;
+}
+// To nearest even.  8-bit values come in range, UMAP_I8 ones as whole numbers.
+template <int T>
+__device__ __forceinline__ Elem<T> float_elem(float v)
+{
+    if constexpr (T == UMAP_BF16) return __builtin_bit_cast(uint16_t, (__bf16)v);
+    else if constexpr (T == UMAP_F8) return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
+    else return (Elem<T>)v;
+}
+
+// 8 elements as they lie in memory.  Rows may start at any element, so the loads and
+// stores promise no more than its alignment; they are full-width ones all the same
+// (dword accesses need no alignment on this architecture).
+template <int T>
+struct Raw8 {
+    static constexpr int kWords = 2 * (int)sizeof(Elem<T>);
+    uint32_t w[kWords];
+};
+template <int T>
+struct __attribute__((packed)) Packed8 {
+    uint32_t w[Raw8<T>::kWords];
+};
+
+template <int T>
+__device__ __forceinline__ Raw8<T> load8(const Elem<T> *p)
+{
+    const Packed8<T> m = *reinterpret_cast<const Packed8<T> *>(p);
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::kWords; ++i) r.w[i] = m.w[i];
+    return r;
+}
+template <int T>
+__device__ __forceinline__ void store8(Elem<T> *p, const Raw8<T> &r)
+{
+    Packed8<T> m;
+#pragma unroll
+    for (int i = 0; i < Raw8<T>::kWords; ++i) m.w[i] = r.w[i];
+    *reinterpret_cast<Packed8<T> *>(p) = m;
+}
+
+template <int T>
+__device__ __forceinline__ void floats8(const Raw8<T> &r, float v[8])
+{
+    if constexpr (T == UMAP_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+    } else if constexpr (T == UMAP_F16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)r.w[i]);
+            v[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i] >> 16));
+        }
+    } else if constexpr (T == UMAP_BF16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(r.w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+        }
+    } else if constexpr (T == UMAP_I8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(r.w[i >> 2] >> (8 * (i & 3)));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(r.w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(r.w[i], true);
+            v[4 * i] = lo[0];
+            v[4 * i + 1] = lo[1];
+            v[4 * i + 2] = hi[0];
+            v[4 * i + 3] = hi[1];
+        }
+    }
+}
+
+template <int T>
+__device__ __forceinline__ Raw8<T> raw8(const float v[8])
+{
+    Raw8<T> r;
+    if constexpr (T == UMAP_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(v[i]);
+    } else if constexpr (T == UMAP_F16) {
+        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            r.w[i] = __builtin_bit_cast(uint32_t, half2v{(_Float16)v[2 * i], (_Float16)v[2 * i + 1]});
+    } else if constexpr (T == UMAP_BF16) {
+        typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            r.w[i] = __builtin_bit_cast(uint32_t, bf2v{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
+    } else if constexpr (T == UMAP_I8) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int j = 3; j >= 0; --j) w = w << 8 | ((uint32_t)(int)v[4 * i + j] & 0xff);
+            r.w[i] = w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+            r.w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], w, true);
+        }
+    }
+    return r;
 }
 
 }  // namespace ul

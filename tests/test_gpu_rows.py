@@ -36,6 +36,21 @@ def hole(n, dim, dtype, pad=0, shift=0):
     return x, x[:, shift:shift + dim]
 
 
+class Workspace:
+    """A workspace of just the bytes asked for, with noise in it and a frame behind it."""
+
+    def __init__(self, need):
+        self.whole = torch.randint(0, 256, (need + 4096,), dtype=torch.uint8, device=DEV)
+        self.need, self.frame = need, self.whole[need:].clone()
+
+    @property
+    def inside(self):
+        return self.whole[:self.need]
+
+    def framed(self):
+        return torch.equal(self.whole[self.need:], self.frame)
+
+
 def frame_untouched(whole, dim, shift):
     f = whole.float()
     return bool((f[:, :shift] == 7).all() and (f[:, shift + dim:] == 7).all())
@@ -143,9 +158,9 @@ def lookup_grad(dout, ids, rows, scale=1.0, dtype=F32, accumulate=None, pad=0, s
     whole, grad = hole(rows, dim, dtype, pad, shift)
     if accumulate is not None:
         grad.copy_(accumulate)
-    work = torch.empty(R.umap_rows_lookup_grad_workspace(n, rows, dim), dtype=torch.uint8, device=DEV)
-    work.random_(0, 256)
-    R.umap_rows_lookup_grad(dout, ids, grad, work, scale=scale, accumulate=accumulate is not None)
+    work = Workspace(R.umap_rows_lookup_grad_workspace(n, rows, dim))
+    R.umap_rows_lookup_grad(dout, ids, grad, work.inside, scale=scale, accumulate=accumulate is not None)
+    assert work.framed()
     assert frame_untouched(whole, dim, shift)
     return grad
 
@@ -404,6 +419,16 @@ def test_norm_keeps_nan_and_infinity_in_their_rows(dim, group):
     assert not bool(q[[1, 3, 4]].any())
 
 
+@pytest.mark.parametrize("dim", [5, 9, 300, 2048, 9001])
+def test_norm_without_eps_of_small_rows(dim):
+    for size in (1e-3, 1e-18, 1e-30):   # squares down to 1e-60
+        x, dy = rand(5, dim, F32, spread=size), rand(5, dim, F32)
+        check_norm(x, F32, eps=0.0)
+        dx, _ = norm_grad(dy, x, eps=0.0)
+        dx64, mag, _, _ = ref.norm_grad(ref.values(dy), ref.values(x), None, 0.0)
+        near(dx, dx64, (-(-dim // 64) + 40) * ref.E32 * mag)
+
+
 def test_norm_offsets_beyond_32_bits():
     pitch = 2**30 + 8
     x = torch.empty(4 * pitch + 64, device=DEV, dtype=BF16).as_strided((5, 64), (pitch, 1))
@@ -424,9 +449,9 @@ def norm_grad(dy, h, weight=None, dh=None, want_dw=True, eps=1e-6, pad=0, shift=
     dw = torch.full((dim,), 7.0, device=DEV) if want_dw else None
     work = None
     if want_dw:
-        work = torch.empty(R.umap_rows_norm_grad_workspace(n, dim), dtype=torch.uint8, device=DEV)
-        work.random_(0, 256)
-    R.umap_rows_norm_grad(dy, h, dx, weight=weight, dh=dh, dweight=dw, workspace=work, eps=eps)
+        work = Workspace(R.umap_rows_norm_grad_workspace(n, dim))
+    R.umap_rows_norm_grad(dy, h, dx, weight=weight, dh=dh, dweight=dw, workspace=work and work.inside, eps=eps)
+    assert work is None or work.framed()
     assert frame_untouched(whole, dim, shift)
     return dx, dw
 
@@ -461,6 +486,12 @@ def test_norm_grad_with_and_without_its_parts(dim, with_dh, with_dw, with_w):
 @pytest.mark.parametrize("n", [0, 1, 2, 3, 5, 255, 511, 513, 4099])
 @pytest.mark.parametrize("dim", [48, 1024])
 def test_norm_grad_row_counts(n, dim):
+    check_norm_grad(rand(n, dim, BF16), rand(n, dim, BF16), rand(1, dim, BF16)[0])
+
+
+@pytest.mark.parametrize("dim", [5, 64, 128, 256, 512, 520, 1040, 1200, 2049, 3000, 6500, 8200])
+def test_norm_grad_of_more_rows_than_run_at_once(dim):
+    n = 200_000 // dim + 9000 if dim < 600 else 3000
     check_norm_grad(rand(n, dim, BF16), rand(n, dim, BF16), rand(1, dim, BF16)[0])
 
 
