@@ -4,6 +4,8 @@
 // The positions t are sorted by id, stably (least significant digit first), so the
 // rows that belong to one table row lie one after the other, in the order of t, and
 // are added in that order: the same sum in every call, without atomics.
+#include <algorithm>
+
 #include "launch_sizes.hpp"
 #include "rows_device.hpp"
 #include "rows_internal.hpp"
@@ -13,10 +15,17 @@ namespace ul {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItems = 16;
-constexpr int kTile = kThreads * kItems;
 constexpr int kWaves = kThreads / 64;
+
+// ---- the sort ----
+//
+// Least significant digit first, up to 9 bits at a time.  A tile of 1,024 ITEMS keys belongs to
+// a workgroup: a launch counts the tile's digits, another files its keys behind those
+// of the tiles before.  Up to 8,192 keys one workgroup does all of it in one launch.
+// What bounds it is latency, launch by launch.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxDigit = 9;   // bits
+constexpr int kMaxBins = 1 << kMaxDigit;
 
 // The sort's key of position t: its table row, or `rows` where it has none.
 struct Keys {
@@ -31,108 +40,230 @@ struct Keys {
     }
 };
 
-// counts[digit * tiles + tile]: keys of the tile with that digit.
-__global__ __launch_bounds__(kThreads) void k_digit_counts(Keys keys, int64_t n, int shift, int bits, uint32_t *counts)
+// counts[tile][digit]: keys of the tile with that digit.  The first pass also clears the
+// number of joins.
+template <int ITEMS>
+__global__ __launch_bounds__(kSortThreads) void k_digit_counts(Keys keys, int64_t n, int shift, int bits,
+                                                               uint32_t *counts, uint32_t *joins)
 {
-    __shared__ uint32_t bin[1 << kMaxDigit];
+    __shared__ uint32_t bin[kMaxBins];
     const int bins = 1 << bits;
     const uint32_t mask = bins - 1;
-    for (int d = threadIdx.x; d < bins; d += kThreads) bin[d] = 0;
-    __syncthreads();
-    for (int i = 0; i < kItems; ++i) {
-        const int64_t t = (int64_t)blockIdx.x * kTile + i * kThreads + threadIdx.x;
-        if (t < n) atomicAdd(&bin[(keys(t) >> shift) & mask], 1u);
-    }
-    __syncthreads();
-    for (int d = threadIdx.x; d < bins; d += kThreads) counts[(int64_t)d * gridDim.x + blockIdx.x] = bin[d];
-}
-
-// Exclusive prefix sums of counts[0 .. size), in place, by one workgroup.
-constexpr int kScanThreads = 1024;
-__global__ __launch_bounds__(kScanThreads) void k_scan(uint32_t *counts, int64_t size)
-{
-    __shared__ uint32_t part[kScanThreads / 64];
-    uint32_t carry = 0;
-    for (int64_t base = 0; base < size; base += kScanThreads) {
-        const int64_t i = base + threadIdx.x;
-        const uint32_t own = i < size ? counts[i] : 0;
-        uint32_t sum = own;
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t up = __shfl_up(sum, o);
-            if ((threadIdx.x & 63) >= o) sum += up;
-        }
-        if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        uint32_t before = 0, all = 0;
-        for (int w = 0; w < kScanThreads / 64; ++w) {
-            if (w < (int)(threadIdx.x >> 6)) before += part[w];
-            all += part[w];
-        }
-        if (i < size) counts[i] = carry + before + sum - own;
-        carry += all;
-        __syncthreads();
-    }
-}
-
-// Files the tile's keys and positions behind the counts' prefix sums, in their order:
-// wave w has positions w * 64 kItems .. of the tile, 64 at a time, and among
-// equal digits a lane comes after the lower lanes and the wave's earlier steps.
-__global__ __launch_bounds__(kThreads) void k_file(Keys keys, const uint32_t *from, int64_t n, int shift, int bits,
-                                                   const uint32_t *counts, uint32_t *keys_out, uint32_t *pos_out)
-{
-    __shared__ volatile uint32_t seen[kWaves][1 << kMaxDigit];
-    const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint32_t mask = bins - 1;
-    for (int i = threadIdx.x; i < kWaves * bins; i += kThreads) seen[i / bins][i % bins] = 0;
-    __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kTile + wave * 64 * kItems + lane;
-    uint32_t key[kItems], rank[kItems];
+    const int64_t first = (int64_t)blockIdx.x * (kSortThreads * ITEMS) + threadIdx.x;
+    uint32_t key[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int64_t t = first + i * 64;
-        key[i] = t < n ? keys(t) : 0;
+    for (int i = 0; i < ITEMS; ++i)
+        if (first + i * kSortThreads < n) key[i] = keys(first + i * kSortThreads);
+    for (int d = threadIdx.x; d < bins; d += kSortThreads) bin[d] = 0;
+    if (joins && blockIdx.x == 0 && threadIdx.x == 0) *joins = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+        if (first + i * kSortThreads < n) atomicAdd(&bin[(key[i] >> shift) & mask], 1u);
+    __syncthreads();
+    for (int d = threadIdx.x; d < bins; d += kSortThreads) counts[(int64_t)blockIdx.x * bins + d] = bin[d];
+}
+
+// Many tiles: counts[tile][d] becomes the number in the tiles before, counts[tiles][d] that in
+// all of them.  A thread per digit.
+__global__ __launch_bounds__(64) void k_tile_sums(uint32_t *counts, int64_t tiles, int bins)
+{
+    const int d = blockIdx.x * 64 + threadIdx.x;
+    if (d >= bins) return;
+    uint32_t sum = 0;
+    constexpr int kAhead = 16;
+    for (int64_t t0 = 0; t0 < tiles; t0 += kAhead) {
+        uint32_t c[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) c[u] = t0 + u < tiles ? counts[(t0 + u) * bins + d] : 0;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (t0 + u < tiles) counts[(t0 + u) * bins + d] = sum;
+            sum += c[u];
+        }
+    }
+    counts[tiles * bins + d] = sum;
+}
+
+struct SortLds {
+    uint32_t seen[kSortWaves][kMaxBins];
+    uint32_t wave_total[kSortWaves];
+};
+
+// Ranks of a tile's keys: wave w has positions 64 ITEMS w .. of the tile, 64 at a time, and
+// among equal digits a key comes after those of lower lanes, of the wave's earlier steps
+// and of lower waves.  `there`: how many of the thread's keys exist.
+template <int ITEMS>
+__device__ __forceinline__ void rank_in_wave(const uint32_t key[ITEMS], int there, int shift, uint32_t mask, SortLds &lds,
+                                             uint32_t rank[ITEMS])
+{
+    volatile uint32_t *const seen = lds.seen[threadIdx.x >> 6];
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
         const uint32_t d = (key[i] >> shift) & mask;
-        unsigned long long same = __ballot(t < n);
-        for (int b = 0; b < bits; ++b) {
+        uint64_t same = __ballot(i < there);
+#pragma unroll
+        for (int b = 0; b < kMaxDigit; ++b) {
             const bool on = (d >> b) & 1;
-            const unsigned long long with = __ballot(on);
+            const uint64_t with = __ballot(on);
             same &= on ? with : ~with;
         }
-        const uint32_t before = seen[wave][d];
+        const uint32_t before = seen[d];
         const uint32_t lower = __popcll(same & ((1ull << lane) - 1));
         rank[i] = before + lower;
         __builtin_amdgcn_wave_barrier();
-        if (t < n && lower == 0) seen[wave][d] = before + (uint32_t)__popcll(same);
+        if (i < there && lower == 0) seen[d] = before + (uint32_t)__popcll(same);
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+// Exclusive prefix sums over the digits of all[threadIdx.x]; a barrier's work.
+__device__ __forceinline__ uint32_t digit_start(uint32_t all, SortLds &lds)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    uint32_t up = all;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_up(up, o);
+        if (lane >= o) up += v;
+    }
+    if (lane == 63) lds.wave_total[wave] = up;
     __syncthreads();
-    for (int d = threadIdx.x; d < bins; d += kThreads) {
-        uint32_t at = counts[(int64_t)d * gridDim.x + blockIdx.x];
-        for (int w = 0; w < kWaves; ++w) {
-            const uint32_t c = seen[w][d];
-            seen[w][d] = at;
+    up -= all;
+    for (int w = 0; w < wave && w < kMaxBins / 64; ++w) up += lds.wave_total[w];
+    return up;
+}
+
+// Files the tile's keys and positions where their digit's turn is.  SUMMED: k_tile_sums
+// has run; else each workgroup adds up the tiles' counts itself.
+template <int ITEMS, bool SUMMED>
+__global__ __launch_bounds__(kSortThreads) void k_file(Keys keys, const uint32_t *from, int64_t n, int shift, int bits,
+                                                       const uint32_t *counts, int tiles, uint32_t *keys_out,
+                                                       uint32_t *pos_out)
+{
+    __shared__ SortLds lds;
+    const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const uint32_t mask = bins - 1;
+    const int64_t first = (int64_t)blockIdx.x * (kSortThreads * ITEMS) + wave * 64 * ITEMS + lane;
+    uint32_t key[ITEMS], pos[ITEMS], rank[ITEMS];
+    int there = 0;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int64_t t = first + i * 64;
+        key[i] = t < n ? keys(t) : 0;
+        pos[i] = from && t < n ? from[t] : (uint32_t)t;
+        there += t < n;
+    }
+    // this thread's digit: its keys in the tiles before this one, and in all
+    uint32_t mine = 0, all = 0;
+    const int d = threadIdx.x;
+    if (d < bins) {
+        if constexpr (SUMMED) {
+            mine = counts[(int64_t)blockIdx.x * bins + d];
+            all = counts[(int64_t)tiles * bins + d];
+        } else {
+#pragma unroll 16
+            for (int t = 0; t < tiles; ++t) {
+                const uint32_t c = counts[t * bins + d];
+                all += c;
+                mine += t < (int)blockIdx.x ? c : 0;
+            }
+        }
+    }
+    for (int i = lane; i < bins; i += 64) lds.seen[wave][i] = 0;
+    __builtin_amdgcn_wave_barrier();
+    rank_in_wave<ITEMS>(key, there, shift, mask, lds, rank);
+    uint32_t at = digit_start(all, lds) + mine;   // behind its barrier all waves have counted
+    if (d < bins) {
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = lds.seen[w][d];
+            lds.seen[w][d] = at;
             at += c;
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int64_t t = first + i * 64;
-        if (t >= n) continue;
-        const uint32_t at = seen[wave][(key[i] >> shift) & mask] + rank[i];
-        keys_out[at] = key[i];
-        pos_out[at] = from ? from[t] : (uint32_t)t;
+    for (int i = 0; i < ITEMS; ++i) {
+        if (i >= there) continue;
+        const uint32_t to = lds.seen[wave][(key[i] >> shift) & mask] + rank[i];
+        keys_out[to] = key[i];
+        pos_out[to] = pos[i];
+    }
+}
+
+// The whole sort of up to 1,024 ITEMS keys by one workgroup.
+template <int ITEMS>
+__global__ __launch_bounds__(kSortThreads) void k_sort_few(Keys keys, int n, int passes, int bits, uint32_t *keys_out,
+                                                           uint32_t *pos_out, uint32_t *joins)
+{
+    __shared__ SortLds lds;
+    __shared__ uint32_t key_at[kSortThreads * ITEMS];
+    __shared__ uint16_t pos_at[kSortThreads * ITEMS];
+    const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const uint32_t mask = bins - 1;
+    const int first = wave * 64 * ITEMS + lane;
+    uint32_t key[ITEMS], pos[ITEMS], rank[ITEMS];
+    int there = 0;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int t = first + i * 64;
+        key[i] = t < n ? keys(t) : 0;
+        pos[i] = t;
+        there += t < n;
+    }
+    if (threadIdx.x == 0) *joins = 0;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * bits;
+        for (int i = lane; i < bins; i += 64) lds.seen[wave][i] = 0;
+        __builtin_amdgcn_wave_barrier();
+        rank_in_wave<ITEMS>(key, there, shift, mask, lds, rank);
+        __syncthreads();
+        const int d = threadIdx.x;
+        uint32_t all = 0;
+        if (d < bins)
+            for (int w = 0; w < kSortWaves; ++w) all += lds.seen[w][d];
+        uint32_t at = digit_start(all, lds);
+        if (d < bins) {
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = lds.seen[w][d];
+                lds.seen[w][d] = at;
+                at += c;
+            }
+        }
+        __syncthreads();
+        const bool last = pass == passes - 1;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (i >= there) continue;
+            const uint32_t to = lds.seen[wave][(key[i] >> shift) & mask] + rank[i];
+            if (last) {
+                keys_out[to] = key[i];
+                pos_out[to] = pos[i];
+            } else {
+                key_at[to] = key[i];
+                pos_at[to] = (uint16_t)pos[i];
+            }
+        }
+        if (last) break;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (i >= there) continue;
+            key[i] = key_at[first + i * 64];
+            pos[i] = pos_at[first + i * 64];
+        }
     }
 }
 
 // ---- sums of equal keys' rows ----
 //
-// The sorted positions are cut into chunks of equal length, so that a wave's work does
-// not depend on how often an id occurs; a wave adds the rows of one chunk for one slab of
-// 64 VEC columns.  An id whose positions all lie in the chunk is done then; of one that
-// crosses a border the chunk leaves its part, in slot 0 where the id began in an earlier
-// chunk, else in slot 1, and k_join_parts adds the parts in order.
-constexpr int kMostChunk = 64;   // a lane for each position
+// The sorted positions are cut into chunks of equal length, so that the work does not
+// depend on how often an id occurs; a wave (LANES lanes of it for narrow rows) adds the
+// rows of one chunk for one slab of LANES VEC columns.  An id that begins in a chunk and
+// ends in it or in the next one is the chunk's own.  Of a longer one each chunk leaves its
+// part, in slot 1 where the id begins, else in slot 0, and k_join_parts adds the parts in
+// order.
 constexpr uint32_t kNoKey = 0xffffffffu;
 
 // VEC elements of a row as they lie in memory.
@@ -184,12 +315,52 @@ struct Sorted {
     int64_t n;
     int32_t chunk;
 };
+// Chunks in which an id that needs joining begins.
+struct Joins {
+    uint32_t *count, *chunks;
+};
 
-constexpr int kZeroRows = 16;   // rows that a wave looks up and clears
+// LANES lanes that work on one chunk: all values below are the same in each of them.
+template <int LANES>
+struct Group {
+    int base = threadIdx.x & 63 & ~(LANES - 1);
+    __device__ __forceinline__ uint64_t ballot(bool v) const
+    {
+        const uint64_t all = __ballot(v);
+        if constexpr (LANES == 64) return all;
+        else return all >> base & ((1ull << LANES) - 1);
+    }
+    __device__ __forceinline__ uint32_t at(uint32_t v, int i) const
+    {
+        if constexpr (LANES == 64) return (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+        else return (uint32_t)__shfl((int)v, base + i);
+    }
+};
 
-template <int TD, int TG, int VEC>
+// The keys and rows of a chunk, one to a lane.
+template <int LANES>
+struct Chunk {
+    uint32_t key, from;
+    int count;        // positions that have a row (those without come last)
+    uint64_t ends;    // positions that are their key's last
+    __device__ __forceinline__ Chunk(const Sorted &sorted, int64_t p0, int64_t rows, const Group<LANES> &group)
+    {
+        const int lane = threadIdx.x & (LANES - 1);
+        const int64_t p = p0 + lane;
+        const bool mine = lane < sorted.chunk && p < sorted.n;
+        key = mine ? sorted.keys[p] : kNoKey;
+        from = mine ? sorted.pos[p] : 0;
+        const uint32_t next = mine && p + 1 < sorted.n ? sorted.keys[p + 1] : kNoKey;
+        count = __popcll(group.ballot(mine && key < (uint32_t)rows));
+        ends = group.ballot(mine && key != next);
+    }
+};
+
+constexpr int kZeroRows = 4;   // rows that a wave looks up and clears
+
+template <int TD, int TG, int LANES, int VEC>
 __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slabs, umap_rows dout, float scale,
-                                                         umap_rows grad, bool accumulate, float *parts,
+                                                         umap_rows grad, bool accumulate, float *parts, Joins joins,
                                                          int64_t chunk_blocks)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -211,120 +382,205 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
         const float zero[VEC] = {};
         for (; rows; rows &= rows - 1) {
             const int64_t row = first + __builtin_ctzll(rows);
-            for (int s = 0; s < slabs; ++s)
-                store_sums<TG, VEC>(grad, row, VecCols<VEC>((s * 64 + lane) * VEC, grad.cols), zero, 0.0f, false);
+            for (int c = lane * VEC; c < grad.cols; c += 64 * VEC)
+                store_sums<TG, VEC>(grad, row, VecCols<VEC>(c, grad.cols), zero, 0.0f, false);
         }
         return;
     }
-    const int64_t unit = block * kWaves + wave, chunk = unit / slabs;
+    const Group<LANES> group;
+    int64_t unit = block * kWaves + wave;
+    if constexpr (LANES < 64) unit = unit * (64 / LANES) + lane / LANES;
+    const int64_t chunk = unit / slabs;
     const int slab = (int)(unit - chunk * slabs);
     const int64_t p0 = chunk * sorted.chunk;
     if (p0 >= sorted.n) return;
-    const int64_t p = p0 + lane;
-    const bool mine = lane < sorted.chunk && p < sorted.n;
-    const uint32_t key = mine ? sorted.keys[p] : kNoKey;
-    const uint32_t next = mine && p + 1 < sorted.n ? sorted.keys[p + 1] : kNoKey;
-    const uint32_t from = mine ? sorted.pos[p] : 0;
-    const uint32_t before = p0 > 0 ? sorted.keys[p0 - 1] : kNoKey;
-    const int count = __popcll(__ballot(mine && key < (uint32_t)grad.rows));   // positions without a row come last
-    if (count == 0) return;
-    const uint64_t ends = __ballot(key != next);
-    bool open = before == (uint32_t)__builtin_amdgcn_readfirstlane(key);   // the id began in an earlier chunk
-    const VecCols<VEC> cols((slab * 64 + lane) * VEC, grad.cols);
+    const Chunk<LANES> here(sorted, p0, grad.rows, group);
+    if (here.count == 0) return;
+    const Chunk<LANES> next(sorted, p0 + sorted.chunk, grad.rows, group);
+    const uint32_t first_key = group.at(here.key, 0);
+    // the chunk's first id may have begun before it: in the last chunk (then that one has
+    // all of it, if it ends here), or earlier
+    bool open = p0 > 0 && sorted.keys[p0 - 1] == first_key;
+    int begin = 0;
+    if (open && here.ends && (p0 == sorted.chunk || sorted.keys[p0 - sorted.chunk - 1] != first_key)) {
+        begin = __builtin_ctzll(here.ends) + 1;
+        open = false;
+    }
+    const VecCols<VEC> cols((slab * LANES + (threadIdx.x & (LANES - 1))) * VEC, grad.cols);
     const Elem<TD> *const base = static_cast<const Elem<TD> *>(dout.data);
-    float *const part = parts + chunk * 2 * grad.cols;
     float sum[VEC] = {};
     auto leave = [&](int slot) {
-        float *const to = part + (int64_t)slot * grad.cols + cols.at;
+        float *const to = parts + (chunk * 2 + slot) * grad.cols + cols.at;
         if (cols.live()) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j)
                 if (j >= cols.dup) to[j] = sum[j];
         }
     };
-    constexpr int kAhead = 8;
-    for (int i0 = 0; i0 < count; i0 += kAhead) {
-        Vec<TD, VEC> row[kAhead];
+    // rows in flight while those before them are added
+    constexpr int kAhead = VEC * sizeof(Elem<TD>) > 16 ? 4 : 8;
+    auto add = [&](const Chunk<LANES> &of, int i0, int end) {
+        Vec<TD, VEC> row[kAhead], ahead[kAhead];
+        auto read = [&](int from, Vec<TD, VEC> to[kAhead]) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (i0 + u < count && cols.live())
-                row[u] = load_vec<TD, VEC>(base + (int64_t)(uint32_t)__builtin_amdgcn_readlane(from, i0 + u) * dout.stride + cols.at);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int i = i0 + u;
-            if (i >= count) break;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) sum[j] += elem_float<TD>(row[u].e[j]);
-            if (ends >> i & 1) {
-                if (open) leave(0);
-                else store_sums<TG, VEC>(grad, (uint32_t)__builtin_amdgcn_readlane(key, i), cols, sum, scale, accumulate);
-                open = false;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
+            for (int u = 0; u < kAhead; ++u) {
+                if (from + u >= end) break;
+                const int64_t t = group.at(of.from, from + u);   // by all lanes, those without columns too
+                if (cols.live()) to[u] = load_vec<TD, VEC>(base + t * dout.stride + cols.at);
             }
+        };
+        read(i0, row);
+        for (; i0 < end; i0 += kAhead) {
+            read(i0 + kAhead, ahead);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = i0 + u;
+                if (i >= end) break;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) sum[j] += elem_float<TD>(row[u].e[j]);
+                if (of.ends >> i & 1) {
+                    if (open) leave(0);
+                    else store_sums<TG, VEC>(grad, group.at(of.key, i), cols, sum, scale, accumulate);
+                    open = false;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) row[u] = ahead[u];
         }
+    };
+    add(here, begin, here.count);
+    if (begin >= here.count || here.ends >> (here.count - 1) & 1) return;   // the last id ends with the chunk
+    if (open) {
+        leave(0);
+    } else if (next.ends) {   // it ends in the next chunk
+        add(next, 0, __builtin_ctzll(next.ends) + 1);
+    } else {
+        leave(1);
+        if (slab == 0 && (threadIdx.x & (LANES - 1)) == 0) joins.chunks[atomicAdd(joins.count, 1u)] = (uint32_t)chunk;
     }
-    if (!(ends >> (count - 1) & 1)) leave(open ? 0 : 1);
 }
 
-// The ids that cross a chunk's end and begin in it: slot 1 of the chunk and slot 0 of those
-// that follow.  1,024 columns to a workgroup of 1,024 threads, a quarter of the parts to
-// each 256 of them; the quarters are added in order.
-constexpr int kJoinThreads = 1024, kJoinCols = 1024;
+// The ids over several chunks: slot 1 of the chunk in which one begins and slot 0 of those
+// that follow.  256 columns to a workgroup: a wave has four columns per lane and a stretch
+// of the parts, and the waves' sums are added in order.  (The order of the list changes
+// nothing in the sums.)
+constexpr int kJoinWaves = 16, kJoinCols = 256;
 
 template <int TG>
-__global__ __launch_bounds__(kJoinThreads) void k_join_parts(Sorted sorted, float scale, umap_rows grad, bool accumulate,
-                                                             const float *parts)
+__global__ __launch_bounds__(64 * kJoinWaves) void k_join_parts(Sorted sorted, float scale, umap_rows grad, bool accumulate,
+                                                                const float *parts, Joins joins)
 {
-    __shared__ float quarter[3][kJoinCols];
-    const int64_t chunk = row_block(), p0 = chunk * sorted.chunk, p1 = p0 + sorted.chunk;
-    if (p1 >= sorted.n) return;
-    const uint32_t key = sorted.keys[p1 - 1];
-    if (key >= (uint32_t)grad.rows || sorted.keys[p1] != key || (p0 > 0 && sorted.keys[p0 - 1] == key)) return;
-    // the chunks after this one that begin with the key
-    const int lane = threadIdx.x & 63;
-    int64_t more = 0;
-    for (;;) {
-        const int64_t p = (chunk + 1 + more + lane) * sorted.chunk;
-        const uint64_t same = __ballot(p < sorted.n && sorted.keys[p] == key);
-        const int here = ~same ? __builtin_ctzll(~same) : 64;
-        more += here;
-        if (here < 64) break;
-    }
-    const int q = threadIdx.x >> 8, cols = grad.cols;
-    const int64_t each = (more + 3) / 4, first = min(each * q, more), last = min(first + each, more);
-    for (int c0 = blockIdx.z * kJoinCols; c0 < cols; c0 += gridDim.z * kJoinCols) {
-        float sum[4] = {};
-        const float *const at = parts + (chunk + 1) * 2 * cols;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = c0 + j * 256 + (threadIdx.x & 255);
-            if (c >= cols) continue;
-            if (q == 0) sum[j] = parts[(chunk * 2 + 1) * cols + c];
-#pragma unroll 4
-            for (int64_t m = first; m < last; ++m) sum[j] += at[m * 2 * cols + c];
-            if (q > 0) quarter[q - 1][j * 256 + (threadIdx.x & 255)] = sum[j];
+    __shared__ float stretch[kJoinWaves][kJoinCols];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cols = grad.cols;
+    const uint32_t count = *joins.count;
+    for (uint32_t j = blockIdx.x; j < count; j += gridDim.x) {
+        const int64_t chunk = joins.chunks[j];
+        const uint32_t key = sorted.keys[(chunk + 1) * sorted.chunk];
+        // the chunks after this one that begin with the key
+        int64_t more = 0;
+        for (;;) {
+            const int64_t p = (chunk + 1 + more + lane) * sorted.chunk;
+            const uint64_t same = __ballot(p < sorted.n && sorted.keys[p] == key);
+            const int here = ~same ? __builtin_ctzll(~same) : 64;
+            more += here;
+            if (here < 64) break;
         }
-        __syncthreads();
-        if (q == 0) {
+        const int64_t each = (more + kJoinWaves - 1) / kJoinWaves;
+        const int64_t first = min(each * wave, more), last = min(first + each, more);
+        for (int c0 = blockIdx.y * kJoinCols; c0 < cols; c0 += gridDim.y * kJoinCols) {
+            const int c = c0 + lane * 4;
+            const float *const begun = parts + (chunk * 2 + 1) * cols, *const after = parts + (chunk + 1) * 2 * cols;
+            float sum[4] = {};
+            if (c + 4 <= cols) {
+                auto add = [&](const float *p) {
+                    const Vec<UMAP_F32, 4> v = load_vec<UMAP_F32, 4>(p + c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = j * 256 + (int)threadIdx.x, c = c0 + i;
-                if (c >= cols) continue;
-                const float total = scale * (((sum[j] + quarter[0][i]) + quarter[1][i]) + quarter[2][i]);
-                Elem<TG> *const to = static_cast<Elem<TG> *>(grad.data) + (int64_t)key * grad.stride + c;
+                    for (int i = 0; i < 4; ++i) sum[i] += v.e[i];
+                };
+                if (wave == 0) add(begun);
+#pragma unroll 16
+                for (int64_t m = first; m < last; ++m) add(after + m * 2 * cols);
+            } else {
+                for (int i = 0; i < 4 && c + i < cols; ++i) {
+                    if (wave == 0) sum[i] = begun[c + i];
+#pragma unroll 16
+                    for (int64_t m = first; m < last; ++m) sum[i] += after[m * 2 * cols + c + i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) stretch[wave][lane * 4 + i] = sum[i];
+            __syncthreads();
+            for (int i = threadIdx.x; i < kJoinCols && c0 + i < cols; i += 64 * kJoinWaves) {
+                float total = stretch[0][i];
+                for (int w = 1; w < kJoinWaves; ++w) total += stretch[w][i];
+                total *= scale;
+                Elem<TG> *const to = static_cast<Elem<TG> *>(grad.data) + (int64_t)key * grad.stride + c0 + i;
                 *to = float_elem<TG>(accumulate ? elem_float<TG>(*to) + total : total);
             }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
-int64_t align16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
-int64_t tile_count(int64_t n) { return (n + kTile - 1) / kTile; }
+// Keys per tile of the sort: 4,096 while there are few tiles, so that more CUs work, else 16,384;
+// beyond 64 of those the tiles' counts are added up in a launch of their own.
+struct SortPlan {
+    int items;   // per thread
+    int64_t tiles;
+    bool summed;
+    explicit SortPlan(int64_t n)
+    {
+        items = n <= 1024 ? 1 : n <= 32 * 4096 ? 4 : 16;
+        if (few(n)) items = n <= 1024 ? 1 : n <= 4096 ? 4 : 8;
+        tiles = (n + kSortThreads * items - 1) / (kSortThreads * items);
+        summed = tiles > 64;
+    }
+    static bool few(int64_t n) { return n <= 8192; }
+};
 
-// Columns per lane: as many as leave no lane of a wave without any.
-int vec_for(int cols) { return cols <= 64 ? 1 : cols <= 128 ? 2 : cols <= 256 ? 4 : 8; }
+struct SortPass {
+    Keys from;
+    const uint32_t *pos;
+    int64_t n;
+    int shift, bits;
+    uint32_t *counts;
+    int tiles;
+    uint32_t *keys_out, *pos_out, *joins;
+    hipStream_t s;
+
+    template <int ITEMS>
+    hipError_t run(bool summed) const
+    {
+        const dim3 grid((unsigned)tiles), threads(kSortThreads);
+        hipLaunchKernelGGL((k_digit_counts<ITEMS>), grid, threads, 0, s, from, n, shift, bits, counts, joins);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (summed) {
+            hipLaunchKernelGGL(k_tile_sums, dim3(((1u << bits) + 63) / 64), dim3(64), 0, s, counts, (int64_t)tiles, 1 << bits);
+            if (hipError_t e = hipGetLastError()) return e;
+            hipLaunchKernelGGL((k_file<ITEMS, true>), grid, threads, 0, s, from, pos, n, shift, bits, counts, tiles,
+                               keys_out, pos_out);
+        } else {
+            hipLaunchKernelGGL((k_file<ITEMS, false>), grid, threads, 0, s, from, pos, n, shift, bits, counts, tiles,
+                               keys_out, pos_out);
+        }
+        return hipGetLastError();
+    }
+};
+
+int64_t align16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+// Lanes and columns per lane: as many columns as leave no lane of a wave without any, and
+// where a wave's lanes are more than the columns, several chunks to a wave.
+struct RowShape {
+    int lanes, vec;
+    explicit RowShape(int cols)
+    {
+        lanes = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+        vec = cols <= 64 ? 1 : cols <= 128 ? 2 : cols <= 256 ? 4 : 8;
+    }
+};
 
 // Positions per chunk: about 8,192 waves where there are enough of them.
 struct ChunkPlan {
@@ -332,64 +588,78 @@ struct ChunkPlan {
     int64_t chunks;
     ChunkPlan(int64_t n, int32_t cols)
     {
-        const int width = 64 * vec_for(cols);
+        const RowShape shape(cols);
+        const int width = shape.lanes * shape.vec;
         slabs = (cols + width - 1) / width;
-        chunk = kMostChunk;
-        while (chunk > 8 && (n + chunk - 1) / chunk * slabs < 8192) chunk /= 2;
+        chunk = shape.lanes;
+        while (chunk > 8 && (n + chunk - 1) / chunk * slabs * shape.lanes / 64 < 8192) chunk /= 2;
         chunks = (n + chunk - 1) / chunk;
     }
 };
 
 struct Workspace {
-    int64_t sorted, counts, parts, bytes;
+    int64_t sorted, counts, joins, parts, bytes;
     Workspace(int64_t n, int32_t cols)
     {
         const ChunkPlan plan(n, cols);
-        sorted = align16(n * 4);
+        sorted = align16(n * 4);   // keys and positions, twice: a pass goes from one pair to the other
         counts = 4 * sorted;
-        parts = counts + align16(tile_count(n) * (4 << kMaxDigit));
-        bytes = parts + align16(plan.chunks * 2 * cols * 4) + 16;
+        joins = counts + align16((SortPlan(n).tiles + 1) * (4 << kMaxDigit));
+        parts = joins + 16 + align16(plan.chunks * 4);
+        bytes = parts + align16(plan.chunks * 2 * cols * 4);
     }
 };
 
-template <int TD, int TG, int VEC>
-hipError_t sum_chunks(const Sorted &sorted, const ChunkPlan &plan, const umap_rows &dout, float scale,
-                      const umap_rows &grad, bool accumulate, float *parts, hipStream_t s)
+// What the launches of one call share.
+struct Call {
+    Sorted sorted;
+    ChunkPlan plan;
+    umap_rows dout, grad;
+    float scale;
+    bool accumulate;
+    float *parts;
+    Joins joins;
+    hipStream_t s;
+};
+
+template <int TD, int TG, int LANES, int VEC>
+hipError_t sum_chunks(const Call &c)
 {
-    const int64_t chunk_blocks = (plan.chunks * plan.slabs + kWaves - 1) / kWaves;
-    const int64_t zero_blocks = accumulate ? 0 : (grad.rows + kZeroRows * kWaves - 1) / (kZeroRows * kWaves);
+    const int per_block = kThreads / LANES;
+    const int64_t chunk_blocks = (c.plan.chunks * c.plan.slabs + per_block - 1) / per_block;
+    const int64_t zero_blocks = c.accumulate ? 0 : (c.grad.rows + kZeroRows * kWaves - 1) / (kZeroRows * kWaves);
     const Grid2 g = grid2(chunk_blocks + zero_blocks, kThreads);
-    hipLaunchKernelGGL((k_chunk_sums<TD, TG, VEC>), dim3(g.x, g.y), dim3(kThreads), 0, s, sorted, plan.slabs, dout,
-                       scale, grad, accumulate, parts, chunk_blocks);
+    hipLaunchKernelGGL((k_chunk_sums<TD, TG, LANES, VEC>), dim3(g.x, g.y), dim3(kThreads), 0, c.s, c.sorted, c.plan.slabs,
+                       c.dout, c.scale, c.grad, c.accumulate, c.parts, c.joins, chunk_blocks);
     if (hipError_t e = hipGetLastError()) return e;
-    if (plan.chunks < 2) return hipSuccess;
-    const Grid2 j = grid2(plan.chunks, kJoinThreads);
-    const int across = (grad.cols + kJoinCols - 1) / kJoinCols;
-    hipLaunchKernelGGL((k_join_parts<TG>), dim3(j.x, j.y, across < 16 ? across : 16), dim3(kJoinThreads), 0, s, sorted,
-                       scale, grad, accumulate, parts);
+    if (c.plan.chunks < 3) return hipSuccess;   // no id needs joining
+    const int across = (c.grad.cols + kJoinCols - 1) / kJoinCols;
+    hipLaunchKernelGGL((k_join_parts<TG>), dim3((unsigned)std::min<int64_t>(c.plan.chunks, 256), across < 64 ? across : 64),
+                       dim3(64 * kJoinWaves), 0, c.s, c.sorted, c.scale, c.grad, c.accumulate, c.parts, c.joins);
     return hipGetLastError();
 }
 
 template <int TD, int TG>
-hipError_t sum_by_cols(const Sorted &sorted, const ChunkPlan &plan, const umap_rows &dout, float scale,
-                       const umap_rows &grad, bool accumulate, float *parts, hipStream_t s)
+hipError_t sum_by_cols(const Call &c)
 {
-    switch (vec_for(grad.cols)) {
-    case 1: return sum_chunks<TD, TG, 1>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    case 2: return sum_chunks<TD, TG, 2>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    case 4: return sum_chunks<TD, TG, 4>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    default: return sum_chunks<TD, TG, 8>(sorted, plan, dout, scale, grad, accumulate, parts, s);
+    const RowShape shape(c.grad.cols);
+    if (shape.lanes == 16) return sum_chunks<TD, TG, 16, 1>(c);
+    if (shape.lanes == 32) return sum_chunks<TD, TG, 32, 1>(c);
+    switch (shape.vec) {
+    case 1: return sum_chunks<TD, TG, 64, 1>(c);
+    case 2: return sum_chunks<TD, TG, 64, 2>(c);
+    case 4: return sum_chunks<TD, TG, 64, 4>(c);
+    default: return sum_chunks<TD, TG, 64, 8>(c);
     }
 }
 
 template <int TD>
-hipError_t sum_into(const Sorted &sorted, const ChunkPlan &plan, const umap_rows &dout, float scale,
-                    const umap_rows &grad, bool accumulate, float *parts, hipStream_t s)
+hipError_t sum_into(const Call &c)
 {
-    switch (grad.type) {
-    case UMAP_F32: return sum_by_cols<TD, UMAP_F32>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    case UMAP_F16: return sum_by_cols<TD, UMAP_F16>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    default: return sum_by_cols<TD, UMAP_BF16>(sorted, plan, dout, scale, grad, accumulate, parts, s);
+    switch (c.grad.type) {
+    case UMAP_F32: return sum_by_cols<TD, UMAP_F32>(c);
+    case UMAP_F16: return sum_by_cols<TD, UMAP_F16>(c);
+    default: return sum_by_cols<TD, UMAP_BF16>(c);
     }
 }
 
@@ -409,31 +679,41 @@ hipError_t launch_rows_lookup_grad(const umap_rows &dout, RowIds ids, float scal
     char *w = static_cast<char *>(workspace);
     uint32_t *buf[4], *counts = reinterpret_cast<uint32_t *>(w + at.counts);
     for (int i = 0; i < 4; ++i) buf[i] = reinterpret_cast<uint32_t *>(w + i * at.sorted);
-    const uint32_t *keys = nullptr, *pos = nullptr;
-    const unsigned tiles = (unsigned)tile_count(n);
+    uint32_t *const join_count = reinterpret_cast<uint32_t *>(w + at.joins);
     int key_bits = 1;
     while ((grad.rows >> key_bits) != 0) ++key_bits;   // keys 0 .. rows
     const int passes = (key_bits + kMaxDigit - 1) / kMaxDigit, bits = (key_bits + passes - 1) / passes;
-    for (int pass = 0; n > 0 && pass < passes; ++pass) {
-        const Keys from{keys, ids, grad.rows};
-        uint32_t *keys_out = buf[2 * (pass & 1)], *pos_out = buf[2 * (pass & 1) + 1];
-        hipLaunchKernelGGL(k_digit_counts, dim3(tiles), dim3(kThreads), 0, s, from, n, pass * bits, bits, counts);
+    const uint32_t *keys = nullptr, *pos = nullptr;
+    const SortPlan sort(n);
+    if (n > 0 && SortPlan::few(n)) {
+        const Keys from{nullptr, ids, grad.rows};
+        const dim3 one(1), threads(kSortThreads);
+        if (sort.items == 1)
+            hipLaunchKernelGGL((k_sort_few<1>), one, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count);
+        else if (sort.items == 4)
+            hipLaunchKernelGGL((k_sort_few<4>), one, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count);
+        else
+            hipLaunchKernelGGL((k_sort_few<8>), one, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count);
         if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL(k_scan, dim3(1), dim3(kScanThreads), 0, s, counts, (int64_t)tiles << bits);
-        if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL(k_file, dim3(tiles), dim3(kThreads), 0, s, from, pos, n, pass * bits, bits, counts, keys_out,
-                           pos_out);
-        if (hipError_t e = hipGetLastError()) return e;
-        keys = keys_out;
-        pos = pos_out;
+        keys = buf[0];
+        pos = buf[1];
+    } else {
+        for (int pass = 0; n > 0 && pass < passes; ++pass) {
+            const SortPass p{Keys{keys, ids, grad.rows}, pos, n, pass * bits, bits, counts, (int)sort.tiles,
+                             buf[2 * (pass & 1)], buf[2 * (pass & 1) + 1], pass ? nullptr : join_count, s};
+            const hipError_t e = sort.items == 4 ? p.run<4>(sort.summed) : p.run<16>(sort.summed);
+            if (e != hipSuccess) return e;
+            keys = p.keys_out;
+            pos = p.pos_out;
+        }
     }
     const ChunkPlan plan(n, grad.cols);
-    const Sorted sorted{keys, pos, n, plan.chunk};
-    float *const parts = reinterpret_cast<float *>(w + at.parts);
+    const Call call{Sorted{keys, pos, n, plan.chunk}, plan, dout, grad, scale, accumulate,
+                    reinterpret_cast<float *>(w + at.parts), Joins{join_count, join_count + 4}, s};
     switch (dout.type) {
-    case UMAP_F32: return sum_into<UMAP_F32>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    case UMAP_F16: return sum_into<UMAP_F16>(sorted, plan, dout, scale, grad, accumulate, parts, s);
-    default: return sum_into<UMAP_BF16>(sorted, plan, dout, scale, grad, accumulate, parts, s);
+    case UMAP_F32: return sum_into<UMAP_F32>(call);
+    case UMAP_F16: return sum_into<UMAP_F16>(call);
+    default: return sum_into<UMAP_BF16>(call);
     }
 }
 
