@@ -1,8 +1,9 @@
 // kernels_rows.hip -- rows of a table by id, times a scale (umap_rows.h).
 //
 // Bound by memory: each row is read once and written once, and nothing is computed but
-// the product.  A thread takes vectors of 8 columns; rows that end inside a vector have
-// their last vector start at cols - 8, where it writes some columns a second time with
+// the product.  A thread takes vectors of V columns, 8 or (where a side is fp32, so that a
+// lane's 16 bytes lie next to its neighbours') 4; rows that end inside a vector have
+// their last vector start at cols - V, where it writes some columns a second time with
 // the same values.
 #include "launch_sizes.hpp"
 #include "rows_device.hpp"
@@ -22,7 +23,7 @@ struct LookupPlan {
     uint32_t inv_vpr;   // ceil(2^20 / vpr): i / vpr = i * inv_vpr >> 20 for i < 2^10, vpr <= 2^10
 };
 
-template <int TI, int TO, int U>
+template <int TI, int TO, int V, int U>
 __global__ __launch_bounds__(kThreads) void k_rows_lookup(umap_rows table, RowIds ids, float scale, umap_rows out,
                                                           LookupPlan plan)
 {
@@ -42,11 +43,11 @@ __global__ __launch_bounds__(kThreads) void k_rows_lookup(umap_rows table, RowId
     for (int u = 0; u < U; ++u) {
         const int i = u * kThreads + threadIdx.x;
         const int row = plan.segments > 1 ? 0 : (int)((uint32_t)i * plan.inv_vpr >> 20);
-        c[u] = min((v0 + i - row * plan.vpr) * 8, table.cols - 8);
+        c[u] = min((v0 + i - row * plan.vpr) * V, table.cols - V);
         t[u] = first + row;
         v[u] = i < here ? row_of(ids, t[u], table.rows) : -1;
     }
-    Raw8<TI> r[U];
+    Raw<TI, V> r[U];
     float lo[U], hi[U];   // scales of the vector's first and last column
     const Elem<TI> *const T = static_cast<const Elem<TI> *>(table.data);
     constexpr bool kScaled = TI == UMAP_I8 || TI == UMAP_F8;
@@ -56,25 +57,25 @@ __global__ __launch_bounds__(kThreads) void k_rows_lookup(umap_rows table, RowId
     for (int u = 0; u < U; ++u) {
         lo[u] = hi[u] = 0.0f;
         if (v[u] < 0) continue;
-        r[u] = load8<TI>(T + v[u] * table.stride + c[u]);
+        r[u] = load_raw<TI, V>(T + v[u] * table.stride + c[u]);
         if constexpr (kScaled) {
             lo[u] = table.scales[v[u] * groups + (c[u] >> shift)];
-            hi[u] = table.scales[v[u] * groups + ((c[u] + 7) >> shift)];
+            hi[u] = table.scales[v[u] * groups + ((c[u] + V - 1) >> shift)];
         }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (u * kThreads + (int)threadIdx.x >= here) continue;
-        float x[8] = {};
+        float x[V] = {};
         if (v[u] >= 0) {
-            floats8<TI>(r[u], x);
+            floats_of<TI, V>(r[u], x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < V; ++i) {
                 if constexpr (kScaled) x[i] *= (c[u] + i) >> shift == c[u] >> shift ? lo[u] : hi[u];
                 x[i] *= scale;
             }
         }
-        store8<TO>(static_cast<Elem<TO> *>(out.data) + t[u] * out.stride + c[u], raw8<TO>(x));
+        store_raw<TO, V>(static_cast<Elem<TO> *>(out.data) + t[u] * out.stride + c[u], raw_of<TO, V>(x));
     }
 }
 
@@ -101,17 +102,17 @@ dim3 grid_of(int64_t blocks)
     return dim3(g.x, g.y);
 }
 
-template <int TI, int TO, int U>
+template <int TI, int TO, int V, int U>
 hipError_t lookup_u(const umap_rows &table, RowIds ids, float scale, const umap_rows &out, hipStream_t s)
 {
     LookupPlan plan;
-    plan.vpr = (out.cols + 7) / 8;
+    plan.vpr = (out.cols + V - 1) / V;
     plan.segments = (plan.vpr + kThreads * U - 1) / (kThreads * U);
     plan.rows_per_block = plan.segments > 1 ? 1 : kThreads * U / plan.vpr;
     plan.inv_vpr = ((1u << 20) + plan.vpr - 1) / plan.vpr;
     const int64_t blocks = plan.segments > 1 ? out.rows * plan.segments
                                              : (out.rows + plan.rows_per_block - 1) / plan.rows_per_block;
-    hipLaunchKernelGGL((k_rows_lookup<TI, TO, U>), grid_of(blocks), dim3(kThreads), 0, s, table, ids, scale, out, plan);
+    hipLaunchKernelGGL((k_rows_lookup<TI, TO, V, U>), grid_of(blocks), dim3(kThreads), 0, s, table, ids, scale, out, plan);
     return hipGetLastError();
 }
 
@@ -123,8 +124,9 @@ hipError_t lookup(const umap_rows &table, RowIds ids, float scale, const umap_ro
                            dim3(kThreads), 0, s, table, ids, scale, out);
         return hipGetLastError();
     }
-    if (out.rows * ((out.cols + 7) / 8) >= (int64_t)1 << 20) return lookup_u<TI, TO, 4>(table, ids, scale, out, s);
-    return lookup_u<TI, TO, 1>(table, ids, scale, out, s);
+    constexpr int V = TI == UMAP_F32 || TO == UMAP_F32 ? 4 : 8;
+    if (out.rows * ((out.cols + V - 1) / V) >= (int64_t)1 << 20) return lookup_u<TI, TO, V, 4>(table, ids, scale, out, s);
+    return lookup_u<TI, TO, V, 1>(table, ids, scale, out, s);
 }
 
 template <int TI>

@@ -266,17 +266,6 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(Keys keys, int n, int
 // order.
 constexpr uint32_t kNoKey = 0xffffffffu;
 
-// VEC elements of a row as they lie in memory.
-template <int T, int VEC>
-struct __attribute__((packed)) Vec {
-    Elem<T> e[VEC];
-};
-template <int T, int VEC>
-__device__ __forceinline__ Vec<T, VEC> load_vec(const Elem<T> *p)
-{
-    return *reinterpret_cast<const Vec<T, VEC> *>(p);
-}
-
 // Columns of a lane: VEC from `at` on, the first `dup` of which are another lane's (the
 // row ends inside the vector, which then lies at its end); dup >= VEC: none.
 template <int VEC>
@@ -292,21 +281,21 @@ __device__ __forceinline__ void store_sums(const umap_rows &grad, int64_t row, c
 {
     if (!c.live()) return;
     Elem<TG> *const to = static_cast<Elem<TG> *>(grad.data) + row * grad.stride + c.at;
-    Vec<TG, VEC> v;
+    float v[VEC];
     if (accumulate) {
-        v = load_vec<TG, VEC>(to);
+        floats_of<TG, VEC>(load_raw<TG, VEC>(to), v);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) v.e[j] = float_elem<TG>(fmaf(scale, sum[j], elem_float<TG>(v.e[j])));
+        for (int j = 0; j < VEC; ++j) v[j] = fmaf(scale, sum[j], v[j]);
     } else {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) v.e[j] = float_elem<TG>(scale * sum[j]);
+        for (int j = 0; j < VEC; ++j) v[j] = scale * sum[j];
     }
     if (!c.dup) {
-        *reinterpret_cast<Vec<TG, VEC> *>(to) = v;
+        store_raw<TG, VEC>(to, raw_of<TG, VEC>(v));
     } else {
 #pragma unroll
         for (int j = 1; j < VEC; ++j)
-            if (j >= c.dup) to[j] = v.e[j];
+            if (j >= c.dup) to[j] = float_elem<TG>(v[j]);
     }
 }
 
@@ -358,7 +347,7 @@ struct Chunk {
 
 constexpr int kZeroRows = 4;   // rows that a wave looks up and clears
 
-template <int TD, int TG, int LANES, int VEC>
+template <int TD, int TG, int LANES, int VEC, int PARTS>
 __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slabs, umap_rows dout, float scale,
                                                          umap_rows grad, bool accumulate, float *parts, Joins joins,
                                                          int64_t chunk_blocks)
@@ -406,27 +395,40 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
         begin = __builtin_ctzll(here.ends) + 1;
         open = false;
     }
-    const VecCols<VEC> cols((slab * LANES + (threadIdx.x & (LANES - 1))) * VEC, grad.cols);
+    const int me = threadIdx.x & (LANES - 1);
+    auto cols = [&](int h) { return VecCols<VEC>(((slab * PARTS + h) * LANES + me) * VEC, grad.cols); };
     const Elem<TD> *const base = static_cast<const Elem<TD> *>(dout.data);
-    float sum[VEC] = {};
+    float sum[PARTS][VEC] = {};
     auto leave = [&](int slot) {
-        float *const to = parts + (chunk * 2 + slot) * grad.cols + cols.at;
-        if (cols.live()) {
+        float *const to = parts + (chunk * 2 + slot) * grad.cols;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (j >= cols.dup) to[j] = sum[j];
+        for (int h = 0; h < PARTS; ++h) {
+            const VecCols<VEC> c = cols(h);
+            if (!c.live()) continue;
+            if (!c.dup) {
+                store_raw<UMAP_F32, VEC>(to + c.at, raw_of<UMAP_F32, VEC>(sum[h]));
+            } else {
+#pragma unroll
+                for (int j = 1; j < VEC; ++j)
+                    if (j >= c.dup) to[c.at + j] = sum[h][j];
+            }
         }
     };
     // rows in flight while those before them are added
-    constexpr int kAhead = VEC * sizeof(Elem<TD>) > 16 ? 4 : 8;
+    constexpr int kAhead = PARTS * VEC * sizeof(Elem<TD>) > 16 ? 4 : 8;
+    struct Row {
+        Raw<TD, VEC> part[PARTS];
+    };
     auto add = [&](const Chunk<LANES> &of, int i0, int end) {
-        Vec<TD, VEC> row[kAhead], ahead[kAhead];
-        auto read = [&](int from, Vec<TD, VEC> to[kAhead]) {
+        Row row[kAhead], ahead[kAhead];
+        auto read = [&](int from, Row to[kAhead]) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (from + u >= end) break;
-                const int64_t t = group.at(of.from, from + u);   // by all lanes, those without columns too
-                if (cols.live()) to[u] = load_vec<TD, VEC>(base + t * dout.stride + cols.at);
+                const Elem<TD> *const at = base + (int64_t)group.at(of.from, from + u) * dout.stride;   // by all lanes
+#pragma unroll
+                for (int h = 0; h < PARTS; ++h)
+                    if (cols(h).live()) to[u].part[h] = load_raw<TD, VEC>(at + cols(h).at);
             }
         };
         read(i0, row);
@@ -437,13 +439,22 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
                 const int i = i0 + u;
                 if (i >= end) break;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) sum[j] += elem_float<TD>(row[u].e[j]);
-                if (of.ends >> i & 1) {
-                    if (open) leave(0);
-                    else store_sums<TG, VEC>(grad, group.at(of.key, i), cols, sum, scale, accumulate);
-                    open = false;
+                for (int h = 0; h < PARTS; ++h) {
+                    float v[VEC];
+                    floats_of<TD, VEC>(row[u].part[h], v);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
+                    for (int j = 0; j < VEC; ++j) sum[h][j] += v[j];
+                }
+                if (of.ends >> i & 1) {
+                    const uint32_t key = group.at(of.key, i);
+                    if (open) leave(0);
+#pragma unroll
+                    for (int h = 0; h < PARTS; ++h) {
+                        if (!open) store_sums<TG, VEC>(grad, key, cols(h), sum[h], scale, accumulate);
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) sum[h][j] = 0.0f;
+                    }
+                    open = false;
                 }
             }
 #pragma unroll
@@ -458,7 +469,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
         add(next, 0, __builtin_ctzll(next.ends) + 1);
     } else {
         leave(1);
-        if (slab == 0 && (threadIdx.x & (LANES - 1)) == 0) joins.chunks[atomicAdd(joins.count, 1u)] = (uint32_t)chunk;
+        if (slab == 0 && me == 0) joins.chunks[atomicAdd(joins.count, 1u)] = (uint32_t)chunk;
     }
 }
 
@@ -495,9 +506,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join_parts(Sorted sorted, f
             float sum[4] = {};
             if (c + 4 <= cols) {
                 auto add = [&](const float *p) {
-                    const Vec<UMAP_F32, 4> v = load_vec<UMAP_F32, 4>(p + c);
+                    float v[4];
+                    floats_of<UMAP_F32, 4>(load_raw<UMAP_F32, 4>(p + c), v);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[i] += v.e[i];
+                    for (int i = 0; i < 4; ++i) sum[i] += v[i];
                 };
                 if (wave == 0) add(begun);
 #pragma unroll 16
@@ -574,11 +586,11 @@ int64_t align16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 // Lanes and columns per lane: as many columns as leave no lane of a wave without any, and
 // where a wave's lanes are more than the columns, several chunks to a wave.
 struct RowShape {
-    int lanes, vec;
+    int lanes, slab;   // columns of a slab
     explicit RowShape(int cols)
     {
         lanes = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
-        vec = cols <= 64 ? 1 : cols <= 128 ? 2 : cols <= 256 ? 4 : 8;
+        slab = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : cols <= 256 ? 256 : 512;
     }
 };
 
@@ -589,8 +601,7 @@ struct ChunkPlan {
     ChunkPlan(int64_t n, int32_t cols)
     {
         const RowShape shape(cols);
-        const int width = shape.lanes * shape.vec;
-        slabs = (cols + width - 1) / width;
+        slabs = (cols + shape.slab - 1) / shape.slab;
         chunk = shape.lanes;
         while (chunk > 8 && (n + chunk - 1) / chunk * slabs * shape.lanes / 64 < 8192) chunk /= 2;
         chunks = (n + chunk - 1) / chunk;
@@ -622,14 +633,14 @@ struct Call {
     hipStream_t s;
 };
 
-template <int TD, int TG, int LANES, int VEC>
+template <int TD, int TG, int LANES, int VEC, int PARTS = 1>
 hipError_t sum_chunks(const Call &c)
 {
     const int per_block = kThreads / LANES;
     const int64_t chunk_blocks = (c.plan.chunks * c.plan.slabs + per_block - 1) / per_block;
     const int64_t zero_blocks = c.accumulate ? 0 : (c.grad.rows + kZeroRows * kWaves - 1) / (kZeroRows * kWaves);
     const Grid2 g = grid2(chunk_blocks + zero_blocks, kThreads);
-    hipLaunchKernelGGL((k_chunk_sums<TD, TG, LANES, VEC>), dim3(g.x, g.y), dim3(kThreads), 0, c.s, c.sorted, c.plan.slabs,
+    hipLaunchKernelGGL((k_chunk_sums<TD, TG, LANES, VEC, PARTS>), dim3(g.x, g.y), dim3(kThreads), 0, c.s, c.sorted, c.plan.slabs,
                        c.dout, c.scale, c.grad, c.accumulate, c.parts, c.joins, chunk_blocks);
     if (hipError_t e = hipGetLastError()) return e;
     if (c.plan.chunks < 3) return hipSuccess;   // no id needs joining
@@ -643,13 +654,16 @@ template <int TD, int TG>
 hipError_t sum_by_cols(const Call &c)
 {
     const RowShape shape(c.grad.cols);
-    if (shape.lanes == 16) return sum_chunks<TD, TG, 16, 1>(c);
-    if (shape.lanes == 32) return sum_chunks<TD, TG, 32, 1>(c);
-    switch (shape.vec) {
-    case 1: return sum_chunks<TD, TG, 64, 1>(c);
-    case 2: return sum_chunks<TD, TG, 64, 2>(c);
-    case 4: return sum_chunks<TD, TG, 64, 4>(c);
-    default: return sum_chunks<TD, TG, 64, 8>(c);
+    // a lane's 16 bytes lie next to its neighbours': 8 columns of 16 bits, or twice 4 where a
+    // side is fp32
+    constexpr bool wide = TD == UMAP_F32 || TG == UMAP_F32;
+    switch (shape.slab) {
+    case 16: return sum_chunks<TD, TG, 16, 1>(c);
+    case 32: return sum_chunks<TD, TG, 32, 1>(c);
+    case 64: return sum_chunks<TD, TG, 64, 1>(c);
+    case 128: return sum_chunks<TD, TG, 64, 2>(c);
+    case 256: return sum_chunks<TD, TG, 64, 4>(c);
+    default: return sum_chunks<TD, TG, 64, wide ? 4 : 8, wide ? 2 : 1>(c);
     }
 }
 

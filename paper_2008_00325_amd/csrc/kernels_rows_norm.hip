@@ -142,9 +142,9 @@ __device__ __forceinline__ void load_weight(const RowWeight &weight, int c, floa
     for (int i = 0; i < 8; ++i) w[i] = 1.0f;
     if (!weight.data) return;
     switch (weight.type) {
-    case UMAP_F32: floats8<UMAP_F32>(load8<UMAP_F32>(static_cast<const float *>(weight.data) + c), w); break;
-    case UMAP_F16: floats8<UMAP_F16>(load8<UMAP_F16>(static_cast<const _Float16 *>(weight.data) + c), w); break;
-    default: floats8<UMAP_BF16>(load8<UMAP_BF16>(static_cast<const uint16_t *>(weight.data) + c), w); break;
+    case UMAP_F32: floats_of<UMAP_F32, 8>(load_raw<UMAP_F32, 8>(static_cast<const float *>(weight.data) + c), w); break;
+    case UMAP_F16: floats_of<UMAP_F16, 8>(load_raw<UMAP_F16, 8>(static_cast<const _Float16 *>(weight.data) + c), w); break;
+    default: floats_of<UMAP_BF16, 8>(load_raw<UMAP_BF16, 8>(static_cast<const uint16_t *>(weight.data) + c), w); break;
     }
 }
 
@@ -228,15 +228,15 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
         for (int i = 0; i < VEC; ++i) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[i]);
     }
 
-    Raw8<TX> a[VEC], b[VEC];
+    Raw<TX, 8> a[VEC], b[VEC];
     auto read = [&](int64_t t) {
         const int64_t v = row_of(ids, t, x.rows);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const int at = Cols(8 * (me + i * TPR), cols).at;
-            if (v >= 0) a[i] = load8<TX>(row_ptr<TX>(x, v) + at);
-            else a[i] = Raw8<TX>{};   // a missing row stands for zeros
-            if (residual.data) b[i] = load8<TX>(row_ptr<TX>(residual, t) + at);
+            if (v >= 0) a[i] = load_raw<TX, 8>(row_ptr<TX>(x, v) + at);
+            else a[i] = Raw<TX, 8>{};   // a missing row stands for zeros
+            if (residual.data) b[i] = load_raw<TX, 8>(row_ptr<TX>(residual, t) + at);
         }
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
@@ -248,12 +248,12 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            floats8<TX>(a[i], e[i]);
+            floats_of<TX, 8>(a[i], e[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) e[i][j] *= scale;
             if (residual.data) {
                 float r[8];
-                floats8<TX>(b[i], r);
+                floats_of<TX, 8>(b[i], r);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) e[i][j] += r[j];
             }
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const Cols c(8 * (me + i * TPR), cols);
-                if (c.live()) store8<TX>(row_out<TX>(h, t) + c.at, raw8<TX>(e[i]));
+                if (c.live()) store_raw<TX, 8>(row_out<TX>(h, t) + c.at, raw_of<TX, 8>(e[i]));
             }
         }
         float add = eps;
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const Cols c(8 * (me + i * TPR), cols);
-                if (c.live()) store8<TY>(row_out<TY>(y, t) + c.at, raw8<TY>(e[i]));
+                if (c.live()) store_raw<TY, 8>(row_out<TY>(y, t) + c.at, raw_of<TY, 8>(e[i]));
             }
         } else {
             // magnitudes compare as their bits do, infinities and NaN above all others
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
                 for (int j = 0; j < 8; ++j) q[j] = quant(e[i][j]);
                 Elem<TY> *const to = row_out<TY>(y, t) + c.at;
                 if (!c.dup) {
-                    store8<TY>(to, raw8<TY>(q));
+                    store_raw<TY, 8>(to, raw_of<TY, 8>(q));
                 } else {   // the columns of another vector may be another group's
 #pragma unroll
                     for (int j = 1; j < 8; ++j)
@@ -364,14 +364,14 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
             if constexpr (kInLds) dw_at(i, j) = 0.0f;
             else dw[i][j] = 0.0f;
         }
-    Raw8<TX> a[VEC], b[VEC], u[VEC];
+    Raw<TX, 8> a[VEC], b[VEC], u[VEC];
     auto read = [&](int64_t t) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const int at = Cols(8 * (me + i * TPR), cols).at;
-            a[i] = load8<TX>(row_ptr<TX>(h, t) + at);
-            b[i] = load8<TX>(row_ptr<TX>(dy, t) + at);
-            if (dh.data) u[i] = load8<TX>(row_ptr<TX>(dh, t) + at);
+            a[i] = load_raw<TX, 8>(row_ptr<TX>(h, t) + at);
+            b[i] = load_raw<TX, 8>(row_ptr<TX>(dy, t) + at);
+            if (dh.data) u[i] = load_raw<TX, 8>(row_ptr<TX>(dh, t) + at);
         }
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
     if (MORE && t < dy.rows) read(t);
     for (; t < dy.rows; t += step) {
         if (!MORE) read(t);
-        Raw8<TX> ha[VEC], db[VEC], ua[VEC];
+        Raw<TX, 8> ha[VEC], db[VEC], ua[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             ha[i] = a[i];
@@ -393,8 +393,8 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
             for (int i = 0; i < VEC; ++i) {
                 const Cols c(8 * (me + i * TPR), cols);
                 float e[8], g[8];
-                floats8<TX>(ha[i], e);
-                floats8<TX>(db[i], g);
+                floats_of<TX, 8>(ha[i], e);
+                floats_of<TX, 8>(db[i], g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) e[j] *= k;
                 if constexpr (!MORE) load_weight(weight, c.at, w[0]);
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
 #pragma unroll
-                for (int j = 0; j < Raw8<TX>::kWords; ++j) asm volatile("" : "+v"(ha[i].w[j]), "+v"(db[i].w[j]));
+                for (int j = 0; j < Raw<TX, 8>::kUnits; ++j) asm volatile("" : "+v"(ha[i].w[j]), "+v"(db[i].w[j]));
         }
         // of the row times k: unit = h k rho, dx = k rho (g - unit (dot rho / cols))
         const float rho = __builtin_amdgcn_rsqf(fmaf(sum, over_cols, add));
@@ -423,8 +423,8 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
         for (int i = 0; i < VEC; ++i) {
             const Cols c(8 * (me + i * TPR), cols);
             float e[8], g[8], r[8];
-            floats8<TX>(ha[i], e);
-            floats8<TX>(db[i], g);
+            floats_of<TX, 8>(ha[i], e);
+            floats_of<TX, 8>(db[i], g);
             if constexpr (!MORE) load_weight(weight, c.at, w[0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -434,11 +434,11 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
                 r[j] = out * (g[j] * w[MORE ? i : 0][j] - unit * along);
             }
             if (dh.data) {
-                floats8<TX>(ua[i], e);
+                floats_of<TX, 8>(ua[i], e);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) r[j] += e[j];
             }
-            if (c.live()) store8<TX>(row_out<TX>(dx, t) + c.at, raw8<TX>(r));
+            if (c.live()) store_raw<TX, 8>(row_out<TX>(dx, t) + c.at, raw_of<TX, 8>(r));
         }
     }
     if constexpr (DW) {
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
                 else sums[j] = dw[i][j];
             }
             if (!c.dup) {
-                store8<UMAP_F32>(to + c.at, raw8<UMAP_F32>(sums));
+                store_raw<UMAP_F32, 8>(to + c.at, raw_of<UMAP_F32, 8>(sums));
             } else {
 #pragma unroll
                 for (int j = 1; j < 8; ++j)

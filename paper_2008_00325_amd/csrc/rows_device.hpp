@@ -1,8 +1,10 @@
-// rows_device.hpp -- element types and vectors of 8 elements of the token-row kernels.
+// rows_device.hpp -- element types and vectors of elements of the token-row kernels.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "rows_internal.hpp"
 
@@ -50,61 +52,66 @@ __device__ __forceinline__ Elem<T> float_elem(float v)
     else return (Elem<T>)v;
 }
 
-// 8 elements as they lie in memory.  Rows may start at any element, so the loads and
-// stores promise no more than its alignment; they are full-width ones all the same
-// (dword accesses need no alignment on this architecture).
-template <int T>
-struct Raw8 {
-    static constexpr int kWords = 2 * (int)sizeof(Elem<T>);
-    uint32_t w[kWords];
+// V elements as they lie in memory, in 32-bit words where they fill some.  Rows may start
+// at any element, so the loads and stores promise no more than its alignment; they are
+// full-width ones all the same (dword accesses need no alignment on this architecture).
+template <int T, int V>
+struct Raw {
+    static constexpr bool kWhole = V * sizeof(Elem<T>) % 4 == 0;
+    using Unit = std::conditional_t<kWhole, uint32_t, Elem<T>>;
+    static constexpr int kUnits = V * sizeof(Elem<T>) / sizeof(Unit);
+    Unit w[kUnits];
 };
-template <int T>
-struct __attribute__((packed)) Packed8 {
-    uint32_t w[Raw8<T>::kWords];
+template <int T, int V>
+struct __attribute__((packed)) Packed {
+    typename Raw<T, V>::Unit w[Raw<T, V>::kUnits];
 };
 
-template <int T>
-__device__ __forceinline__ Raw8<T> load8(const Elem<T> *p)
+template <int T, int V>
+__device__ __forceinline__ Raw<T, V> load_raw(const Elem<T> *p)
 {
-    const Packed8<T> m = *reinterpret_cast<const Packed8<T> *>(p);
-    Raw8<T> r;
+    const Packed<T, V> m = *reinterpret_cast<const Packed<T, V> *>(p);
+    Raw<T, V> r;
 #pragma unroll
-    for (int i = 0; i < Raw8<T>::kWords; ++i) r.w[i] = m.w[i];
+    for (int i = 0; i < Raw<T, V>::kUnits; ++i) r.w[i] = m.w[i];
     return r;
 }
-template <int T>
-__device__ __forceinline__ void store8(Elem<T> *p, const Raw8<T> &r)
+template <int T, int V>
+__device__ __forceinline__ void store_raw(Elem<T> *p, const Raw<T, V> &r)
 {
-    Packed8<T> m;
+    Packed<T, V> m;
 #pragma unroll
-    for (int i = 0; i < Raw8<T>::kWords; ++i) m.w[i] = r.w[i];
-    *reinterpret_cast<Packed8<T> *>(p) = m;
+    for (int i = 0; i < Raw<T, V>::kUnits; ++i) m.w[i] = r.w[i];
+    *reinterpret_cast<Packed<T, V> *>(p) = m;
 }
 
-template <int T>
-__device__ __forceinline__ void floats8(const Raw8<T> &r, float v[8])
+template <int T, int V>
+__device__ __forceinline__ void floats_of(const Raw<T, V> &r, float v[V])
 {
-    if constexpr (T == UMAP_F32) {
+    if constexpr (!Raw<T, V>::kWhole) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+        for (int i = 0; i < V; ++i) v[i] = elem_float<T>(r.w[i]);
+    } else if constexpr (T == UMAP_F32) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = __uint_as_float(r.w[i]);
     } else if constexpr (T == UMAP_F16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < V / 2; ++i) {
             v[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)r.w[i]);
             v[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i] >> 16));
         }
     } else if constexpr (T == UMAP_BF16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < V / 2; ++i) {
             v[2 * i] = __uint_as_float(r.w[i] << 16);
             v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
         }
     } else if constexpr (T == UMAP_I8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(r.w[i >> 2] >> (8 * (i & 3)));
+        for (int i = 0; i < V; ++i) v[i] = (float)(int8_t)(r.w[i >> 2] >> (8 * (i & 3)));
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < V / 4; ++i) {
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(r.w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(r.w[i], true);
             v[4 * i] = lo[0];
             v[4 * i + 1] = lo[1];
@@ -114,26 +121,29 @@ __device__ __forceinline__ void floats8(const Raw8<T> &r, float v[8])
     }
 }
 
-template <int T>
-__device__ __forceinline__ Raw8<T> raw8(const float v[8])
+template <int T, int V>
+__device__ __forceinline__ Raw<T, V> raw_of(const float v[V])
 {
-    Raw8<T> r;
-    if constexpr (T == UMAP_F32) {
+    Raw<T, V> r;
+    if constexpr (!Raw<T, V>::kWhole) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(v[i]);
+        for (int i = 0; i < V; ++i) r.w[i] = float_elem<T>(v[i]);
+    } else if constexpr (T == UMAP_F32) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r.w[i] = __float_as_uint(v[i]);
     } else if constexpr (T == UMAP_F16) {
         typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < V / 2; ++i)
             r.w[i] = __builtin_bit_cast(uint32_t, half2v{(_Float16)v[2 * i], (_Float16)v[2 * i + 1]});
     } else if constexpr (T == UMAP_BF16) {
         typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < V / 2; ++i)
             r.w[i] = __builtin_bit_cast(uint32_t, bf2v{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
     } else if constexpr (T == UMAP_I8) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < V / 4; ++i) {
             uint32_t w = 0;
 #pragma unroll
             for (int j = 3; j >= 0; --j) w = w << 8 | ((uint32_t)(int)v[4 * i + j] & 0xff);
@@ -141,7 +151,7 @@ __device__ __forceinline__ Raw8<T> raw8(const float v[8])
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < V / 4; ++i) {
             int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
             r.w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], w, true);
         }
