@@ -2,8 +2,8 @@
 //
 // Bound by memory: a row is read once and stays in registers between its sum of squares
 // and its result, so every input is read and every output written once.  A row belongs
-// to a wave (up to 2,048 columns) or to a workgroup; a thread holds kVec vectors of 8
-// columns of it, and reads its share of the next row before it works on this one.
+// to some lanes of a wave (up to 1,024 columns) or to a workgroup; a thread holds a few vectors of its
+// columns, and reads its share of the next row before it works on this one.
 #include <algorithm>
 
 #include "rows_device.hpp"
@@ -38,13 +38,14 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 __device__ __forceinline__ uint32_t max_u(uint32_t a, uint32_t b) { return a > b ? a : b; }
-// Largest of 4, 8 or 16 neighbouring lanes.
+// Largest of 4, 8, 16 or 32 neighbouring lanes.
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes)
 {
     v = max_u(v, dpp<kXor1>(v));
     v = max_u(v, dpp<kXor2>(v));
     if (lanes >= 8) v = max_u(v, dpp<kHalfMirror>(v));
     if (lanes >= 16) v = max_u(v, dpp<kMirror>(v));
+    if (lanes >= 32) v = max_u(v, (uint32_t)__shfl_xor((int)v, 16));
     return v;
 }
 
@@ -93,7 +94,6 @@ struct RowThreads {
     {
         constexpr int kLanes = LANES ? LANES : 64;
         a = lanes_max(a, kLanes);
-        if constexpr (kLanes >= 32) a = max_u(a, (uint32_t)__shfl_xor((int)a, 16));
         if constexpr (kLanes >= 64) a = max_u(a, (uint32_t)__shfl_xor((int)a, 32));
         if constexpr (LANES == kBlock) {
             if ((threadIdx.x & 63) == 0) lds->v[turn][0][threadIdx.x >> 6] = __uint_as_float(a);
@@ -114,16 +114,25 @@ __device__ __forceinline__ bool out_of_range(float sum, float eps)
 }
 __device__ __forceinline__ float range_step(float sum) { return sum < 1.0f ? 0x1p80f : 0x1p-80f; }
 
-// Vector i of a thread: columns c = 8 (thread + i TPR) .. c + 7.  Where the row ends inside
-// it, the vector is taken from column cols - 8 on instead, and its first `dup` columns
+// Vector i of a thread: columns c = V (thread + i TPR) .. c + V - 1.  Where the row ends inside
+// it, the vector is taken from column cols - V on instead, and its first `dup` columns
 // are another vector's too: they count in no sum, and are written with the same values.
+template <int V>
 struct Cols {
     int at;    // first column
-    int dup;   // 8 and more: past the row
-    __device__ __forceinline__ Cols(int c, int cols) : at(min(c, cols - 8)), dup(c - at) {}
-    __device__ __forceinline__ bool live() const { return dup < 8; }
+    int dup;   // V and more: past the row
+    __device__ __forceinline__ Cols(int c, int cols) : at(min(c, cols - V)), dup(c - at) {}
+    __device__ __forceinline__ bool live() const { return dup < V; }
     __device__ __forceinline__ bool counts(int j) const { return j >= dup; }
+    __device__ __forceinline__ bool shared() const { return dup > 0 && dup < V; }
 };
+// Columns of the norm's vectors: 8, or 4 from fp32 to fp32, so that a lane's 16 bytes lie
+// next to its neighbours' (256 MB of fp32 rows, us with 8 / 4: into fp32 300 columns 107 / 94,
+// 784 100 / 93, 2,048 93 / 90, but 32,768, where registers are short, 126 / 152; into bf16 784 71
+// / 72; into int8 784 67 / 75).  The gradient takes 8 (784 columns 202 / 208).
+template <int TX, int TY, int VEC>
+constexpr int kNormVec = TX == UMAP_F32 && TY == UMAP_F32 && VEC < 4 ? 4 : 8;
+constexpr int kGradVec = 8;
 
 template <int T>
 __device__ __forceinline__ const Elem<T> *row_ptr(const umap_rows &m, int64_t t)
@@ -136,15 +145,16 @@ __device__ __forceinline__ Elem<T> *row_out(const umap_rows &m, int64_t t)
     return static_cast<Elem<T> *>(m.data) + t * m.stride;
 }
 
-__device__ __forceinline__ void load_weight(const RowWeight &weight, int c, float w[8])
+template <int V>
+__device__ __forceinline__ void load_weight(const RowWeight &weight, int c, float w[V])
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+    for (int i = 0; i < V; ++i) w[i] = 1.0f;
     if (!weight.data) return;
     switch (weight.type) {
-    case UMAP_F32: floats_of<UMAP_F32, 8>(load_raw<UMAP_F32, 8>(static_cast<const float *>(weight.data) + c), w); break;
-    case UMAP_F16: floats_of<UMAP_F16, 8>(load_raw<UMAP_F16, 8>(static_cast<const _Float16 *>(weight.data) + c), w); break;
-    default: floats_of<UMAP_BF16, 8>(load_raw<UMAP_BF16, 8>(static_cast<const uint16_t *>(weight.data) + c), w); break;
+    case UMAP_F32: floats_of<UMAP_F32, V>(load_raw<UMAP_F32, V>(static_cast<const float *>(weight.data) + c), w); break;
+    case UMAP_F16: floats_of<UMAP_F16, V>(load_raw<UMAP_F16, V>(static_cast<const _Float16 *>(weight.data) + c), w); break;
+    default: floats_of<UMAP_BF16, V>(load_raw<UMAP_BF16, V>(static_cast<const uint16_t *>(weight.data) + c), w); break;
     }
 }
 
@@ -164,29 +174,31 @@ __device__ __forceinline__ int row_in_block()
     else return threadIdx.x / LANES;
 }
 
-__device__ __forceinline__ float square_sum(const float e[8], const Cols &c)
+template <int V>
+__device__ __forceinline__ float square_sum(const float e[V], const Cols<V> &c)
 {
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum = fmaf(e[j], e[j], sum);
-    if (c.dup) {
+    for (int j = 0; j < V; ++j) sum = fmaf(e[j], e[j], sum);
+    if (c.shared()) {
         sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = c.counts(j) ? fmaf(e[j], e[j], sum) : sum;
+        for (int j = 0; j < V; ++j) sum = c.counts(j) ? fmaf(e[j], e[j], sum) : sum;
     }
-    return sum;
+    return c.live() ? sum : 0.0f;
 }
-__device__ __forceinline__ float product_sum(const float e[8], const float g[8], const float w[8], const Cols &c)
+template <int V>
+__device__ __forceinline__ float product_sum(const float e[V], const float g[V], const float w[V], const Cols<V> &c)
 {
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum = fmaf(g[j] * w[j], e[j], sum);
-    if (c.dup) {
+    for (int j = 0; j < V; ++j) sum = fmaf(g[j] * w[j], e[j], sum);
+    if (c.shared()) {
         sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = c.counts(j) ? fmaf(g[j] * w[j], e[j], sum) : sum;
+        for (int j = 0; j < V; ++j) sum = c.counts(j) ? fmaf(g[j] * w[j], e[j], sum) : sum;
     }
-    return sum;
+    return c.live() ? sum : 0.0f;
 }
 
 // The scale of a group whose largest magnitude has these bits, and the factor that
@@ -201,42 +213,81 @@ struct Quant {
         const float m = __uint_as_float(bits);
         fine = bits >= __float_as_uint(0x1p-100f) && bits < 0x7f800000u;
         scale = fine ? m * (1.0f / kMost) : bits < 0x7f800000u ? 0.0f : __builtin_nanf("");
-        up = kMost / m;
+        up = fine ? kMost * __builtin_amdgcn_rcpf(m) : 0.0f;
     }
     __device__ __forceinline__ float operator()(float v) const
     {
-        if constexpr (TY == UMAP_I8) return fine ? rintf(v * up) : 0.0f;
-        else return fine ? v * up : 0.0f;
+        if constexpr (TY == UMAP_I8) return fine ? fminf(fmaxf(rintf(v * up), -kMost), kMost) : 0.0f;
+        else return fine ? fminf(fmaxf(v * up, -kMost), kMost) : 0.0f;
+    }
+    // 8 of them.  UMAP_I8: adding 1.5 2^23 leaves the nearest whole number in the sum's low
+    // bits, with one rounding of the exact product; |v up| exceeds 127 by at most a few units
+    // of its last place, which rounds to 127.  UMAP_F8: likewise 448.
+    __device__ __forceinline__ Raw<TY, 8> pack(const float v[8]) const
+    {
+        Raw<TY, 8> r;
+        if constexpr (TY == UMAP_I8) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(fmaf(v[4 * i + j], up, 0x1.8p23f));
+                const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0c);
+                r.w[i] = lo | hi;
+            }
+        } else {
+            float s[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = v[j] * up;
+            r = raw_of<TY, 8>(s);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) r.w[i] = fine ? r.w[i] : 0;
+        return r;
     }
 };
 
-// VEC vectors of 8 columns per thread; cols >= 8.  MORE: a thread keeps its weights over
+// Bits of the largest magnitude of V values, above all finite ones where one is not finite.
+template <int V>
+__device__ __forceinline__ uint32_t most_bits(const float e[V], const Cols<V> &c)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) most = max_u(most, __float_as_uint(e[j]) & 0x7fffffffu);
+    if (c.shared()) {
+        most = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) most = max_u(most, c.counts(j) ? __float_as_uint(e[j]) & 0x7fffffffu : 0);
+    }
+    return c.live() ? most : 0;
+}
+
+// 8 VEC columns per thread; cols >= 8.  MORE: a thread keeps its weights over
 // its rows and reads a row ahead.
 template <int TX, int TY, int LANES, int VEC, bool MORE>
 __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, RowIds ids, float scale, umap_rows residual,
                                                              umap_rows h, RowWeight weight, float eps, umap_rows y)
 {
-    constexpr int kRows = kRowsPerBlock<LANES>;
+    constexpr int kRows = kRowsPerBlock<LANES>, V = kNormVec<TX, TY, VEC>, N = VEC * 8 / V;
     constexpr bool kEight = TY == UMAP_I8 || TY == UMAP_F8;
     __shared__ RowLds lds;
     RowThreads<LANES> row{&lds};
     const int TPR = row_threads<LANES>(), me = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, cols = y.cols;
     const float over_cols = 1.0f / (float)cols;
-    float w[MORE ? VEC : 1][8];
+    float w[MORE ? N : 1][V];
     if constexpr (MORE) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[i]);
+        for (int i = 0; i < N; ++i) load_weight<V>(weight, Cols<V>(V * (me + i * TPR), cols).at, w[i]);
     }
-
-    Raw<TX, 8> a[VEC], b[VEC];
+    Raw<TX, V> a[N], b[N];
     auto read = [&](int64_t t) {
         const int64_t v = row_of(ids, t, x.rows);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int at = Cols(8 * (me + i * TPR), cols).at;
-            if (v >= 0) a[i] = load_raw<TX, 8>(row_ptr<TX>(x, v) + at);
-            else a[i] = Raw<TX, 8>{};   // a missing row stands for zeros
-            if (residual.data) b[i] = load_raw<TX, 8>(row_ptr<TX>(residual, t) + at);
+        for (int i = 0; i < N; ++i) {
+            const int at = Cols<V>(V * (me + i * TPR), cols).at;
+            if (v >= 0) a[i] = load_raw<TX, V>(row_ptr<TX>(x, v) + at);
+            else a[i] = Raw<TX, V>{};   // a missing row stands for zeros
+            if (residual.data) b[i] = load_raw<TX, V>(row_ptr<TX>(residual, t) + at);
         }
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
@@ -244,28 +295,30 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
     if (MORE && t < y.rows) read(t);
     for (; t < y.rows; t += step) {
         if (!MORE) read(t);
-        float e[VEC][8];
+        float e[N][V];
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            floats_of<TX, 8>(a[i], e[i]);
+        for (int i = 0; i < N; ++i) {
+            floats_of<TX, V>(a[i], e[i]);
+            if (scale != 1.0f) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[i][j] *= scale;
-            if (residual.data) {
-                float r[8];
-                floats_of<TX, 8>(b[i], r);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) e[i][j] += r[j];
+                for (int j = 0; j < V; ++j) e[i][j] *= scale;
             }
-            sum += square_sum(e[i], Cols(8 * (me + i * TPR), cols));
+            if (residual.data) {
+                float r[V];
+                floats_of<TX, V>(b[i], r);
+#pragma unroll
+                for (int j = 0; j < V; ++j) e[i][j] += r[j];
+            }
+            sum += square_sum<V>(e[i], Cols<V>(V * (me + i * TPR), cols));
         }
         if (MORE && t + step < y.rows) read(t + step);
         sum = row.sum(sum);
         if (h.data) {   // behind the sum's barrier: h may lie where other waves read
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const Cols c(8 * (me + i * TPR), cols);
-                if (c.live()) store_raw<TX, 8>(row_out<TX>(h, t) + c.at, raw_of<TX, 8>(e[i]));
+            for (int i = 0; i < N; ++i) {
+                const Cols<V> c(V * (me + i * TPR), cols);
+                if (c.live()) store_raw<TX, V>(row_out<TX>(h, t) + c.at, raw_of<TX, V>(e[i]));
             }
         }
         float add = eps;
@@ -273,65 +326,53 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
             const float k = range_step(sum);
             sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
+            for (int i = 0; i < N; ++i) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[i][j] *= k;
-                sum += square_sum(e[i], Cols(8 * (me + i * TPR), cols));
+                for (int j = 0; j < V; ++j) e[i][j] *= k;
+                sum += square_sum<V>(e[i], Cols<V>(V * (me + i * TPR), cols));
             }
             sum = row.sum(sum);
             add = eps * k * k;
         }
         const float rho = __builtin_amdgcn_rsqf(fmaf(sum, over_cols, add));
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            if constexpr (!MORE) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[0]);
+        for (int i = 0; i < N; ++i) {
+            if constexpr (!MORE) load_weight<V>(weight, Cols<V>(V * (me + i * TPR), cols).at, w[0]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[i][j] = e[i][j] * rho * w[MORE ? i : 0][j];
+            for (int j = 0; j < V; ++j) e[i][j] = e[i][j] * rho * w[MORE ? i : 0][j];
         }
 
         if constexpr (!kEight) {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const Cols c(8 * (me + i * TPR), cols);
-                if (c.live()) store_raw<TY, 8>(row_out<TY>(y, t) + c.at, raw_of<TY, 8>(e[i]));
+            for (int i = 0; i < N; ++i) {
+                const Cols<V> c(V * (me + i * TPR), cols);
+                if (c.live()) store_raw<TY, V>(row_out<TY>(y, t) + c.at, raw_of<TY, V>(e[i]));
             }
         } else {
             // magnitudes compare as their bits do, infinities and NaN above all others
-            uint32_t most[VEC], all = 0;
+            uint32_t most[N], all = 0;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const Cols c(8 * (me + i * TPR), cols);
-                most[i] = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) most[i] = max_u(most[i], __float_as_uint(e[i][j]) & 0x7fffffffu);
-                if (c.dup) {
-                    most[i] = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        most[i] = max_u(most[i], c.counts(j) ? __float_as_uint(e[i][j]) & 0x7fffffffu : 0);
-                }
+            for (int i = 0; i < N; ++i) {
+                most[i] = most_bits<V>(e[i], Cols<V>(V * (me + i * TPR), cols));
                 all = max_u(all, most[i]);
             }
             if (y.group == 0) all = row.max(all);
-            const int lanes = LANES ? min(y.group / 8, LANES) : y.group / 8, groups = y.group ? (cols + y.group - 1) / y.group : 1;
+            const int lanes = y.group / V, groups = y.group ? (cols + y.group - 1) / y.group : 1;
             float *const scales = y.scales + t * groups;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const int v = me + i * TPR;
-                const Cols c(8 * v, cols);
+                const Cols<V> c(V * v, cols);
                 const Quant<TY> quant(y.group ? lanes_max(most[i], lanes) : all);
                 if (!c.live()) continue;
                 if (y.group ? (v & (lanes - 1)) == 0 : v == 0) scales[y.group ? v / lanes : 0] = quant.scale;
-                float q[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = quant(e[i][j]);
                 Elem<TY> *const to = row_out<TY>(y, t) + c.at;
                 if (!c.dup) {
-                    store_raw<TY, 8>(to, raw_of<TY, 8>(q));
-                } else {   // the columns of another vector may be another group's
+                    store_raw<TY, V>(to, quant.pack(e[i]));
+                } else {   // only its own columns: the others may be another group's
 #pragma unroll
-                    for (int j = 1; j < 8; ++j)
-                        if (c.counts(j)) to[j] = float_elem<TY>(q[j]);
+                    for (int j = 1; j < V; ++j)
+                        if (c.counts(j)) to[j] = float_elem<TY>(quant(e[i][j]));
                 }
             }
         }
@@ -343,7 +384,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
                                                                   RowWeight weight, float eps, umap_rows dx,
                                                                   float *partial)
 {
-    constexpr int kRows = kRowsPerBlock<LANES>;
+    constexpr int kRows = kRowsPerBlock<LANES>, V = kGradVec, N = VEC * 8 / V;
     __shared__ RowLds lds;
     RowThreads<LANES> row{&lds};
     const int TPR = row_threads<LANES>(), me = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, cols = dy.cols;
@@ -351,27 +392,27 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
     // dweight's sums of this thread's columns, in LDS where registers are short
     constexpr bool kInLds = DW && LANES == kBlock && VEC > 1;
     extern __shared__ float dw_lds[];
-    float w[MORE ? VEC : 1][8], dw[DW && !kInLds ? VEC : 1][8];
-    auto dw_at = [&](int i, int j) -> float & { return dw_lds[(i * 8 + j) * TPR + me]; };
+    float w[MORE ? N : 1][V], dw[DW && !kInLds ? N : 1][V];
+    auto dw_at = [&](int i, int j) -> float & { return dw_lds[(i * V + j) * TPR + me]; };
     if constexpr (MORE) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) load_weight(weight, Cols(8 * (me + i * TPR), cols).at, w[i]);
+        for (int i = 0; i < N; ++i) load_weight<V>(weight, Cols<V>(V * (me + i * TPR), cols).at, w[i]);
     }
 #pragma unroll
-    for (int i = 0; i < (DW ? VEC : 1); ++i)
+    for (int i = 0; i < (DW ? N : 1); ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < V; ++j) {
             if constexpr (kInLds) dw_at(i, j) = 0.0f;
             else dw[i][j] = 0.0f;
         }
-    Raw<TX, 8> a[VEC], b[VEC], u[VEC];
+    Raw<TX, V> a[N], b[N], u[N];
     auto read = [&](int64_t t) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int at = Cols(8 * (me + i * TPR), cols).at;
-            a[i] = load_raw<TX, 8>(row_ptr<TX>(h, t) + at);
-            b[i] = load_raw<TX, 8>(row_ptr<TX>(dy, t) + at);
-            if (dh.data) u[i] = load_raw<TX, 8>(row_ptr<TX>(dh, t) + at);
+        for (int i = 0; i < N; ++i) {
+            const int at = Cols<V>(V * (me + i * TPR), cols).at;
+            a[i] = load_raw<TX, V>(row_ptr<TX>(h, t) + at);
+            b[i] = load_raw<TX, V>(row_ptr<TX>(dy, t) + at);
+            if (dh.data) u[i] = load_raw<TX, V>(row_ptr<TX>(dh, t) + at);
         }
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
@@ -379,9 +420,9 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
     if (MORE && t < dy.rows) read(t);
     for (; t < dy.rows; t += step) {
         if (!MORE) read(t);
-        Raw<TX, 8> ha[VEC], db[VEC], ua[VEC];
+        Raw<TX, V> ha[N], db[N], ua[N];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
+        for (int i = 0; i < N; ++i) {
             ha[i] = a[i];
             db[i] = b[i];
             if (dh.data) ua[i] = u[i];
@@ -390,16 +431,16 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
         auto sums = [&](float k, float &sum, float &dot) {
             sum = dot = 0.0f;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const Cols c(8 * (me + i * TPR), cols);
-                float e[8], g[8];
-                floats_of<TX, 8>(ha[i], e);
-                floats_of<TX, 8>(db[i], g);
+            for (int i = 0; i < N; ++i) {
+                const Cols<V> c(V * (me + i * TPR), cols);
+                float e[V], g[V];
+                floats_of<TX, V>(ha[i], e);
+                floats_of<TX, V>(db[i], g);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] *= k;
-                if constexpr (!MORE) load_weight(weight, c.at, w[0]);
-                sum += square_sum(e, c);
-                dot += product_sum(e, g, w[MORE ? i : 0], c);
+                for (int j = 0; j < V; ++j) e[j] *= k;
+                if constexpr (!MORE) load_weight<V>(weight, c.at, w[0]);
+                sum += square_sum<V>(e, c);
+                dot += product_sum<V>(e, g, w[MORE ? i : 0], c);
             }
             row.sum2(sum, dot);
         };
@@ -412,33 +453,33 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
         }
         if constexpr (kInLds && VEC == 2) {   // the floats are formed anew below: kept, they would spill
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)
+            for (int i = 0; i < N; ++i)
 #pragma unroll
-                for (int j = 0; j < Raw<TX, 8>::kUnits; ++j) asm volatile("" : "+v"(ha[i].w[j]), "+v"(db[i].w[j]));
+                for (int j = 0; j < Raw<TX, V>::kUnits; ++j) asm volatile("" : "+v"(ha[i].w[j]), "+v"(db[i].w[j]));
         }
         // of the row times k: unit = h k rho, dx = k rho (g - unit (dot rho / cols))
         const float rho = __builtin_amdgcn_rsqf(fmaf(sum, over_cols, add));
         const float along = dot * rho * over_cols, out = k * rho;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const Cols c(8 * (me + i * TPR), cols);
-            float e[8], g[8], r[8];
-            floats_of<TX, 8>(ha[i], e);
-            floats_of<TX, 8>(db[i], g);
-            if constexpr (!MORE) load_weight(weight, c.at, w[0]);
+        for (int i = 0; i < N; ++i) {
+            const Cols<V> c(V * (me + i * TPR), cols);
+            float e[V], g[V], r[V];
+            floats_of<TX, V>(ha[i], e);
+            floats_of<TX, V>(db[i], g);
+            if constexpr (!MORE) load_weight<V>(weight, c.at, w[0]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < V; ++j) {
                 const float unit = e[j] * k * rho;
                 if constexpr (kInLds) dw_at(i, j) = fmaf(g[j], unit, dw_at(i, j));
                 else if constexpr (DW) dw[i][j] = fmaf(g[j], unit, dw[i][j]);
                 r[j] = out * (g[j] * w[MORE ? i : 0][j] - unit * along);
             }
             if (dh.data) {
-                floats_of<TX, 8>(ua[i], e);
+                floats_of<TX, V>(ua[i], e);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) r[j] += e[j];
+                for (int j = 0; j < V; ++j) r[j] += e[j];
             }
-            if (c.live()) store_raw<TX, 8>(row_out<TX>(dx, t) + c.at, raw_of<TX, 8>(r));
+            if (c.live()) store_raw<TX, V>(row_out<TX>(dx, t) + c.at, raw_of<TX, V>(r));
         }
     }
     if constexpr (DW) {
@@ -449,16 +490,16 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
             const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
             for (int o = LANES; o < 64; o <<= 1)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i)
+                for (int i = 0; i < N; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) dw[i][j] += __shfl_xor(dw[i][j], o);
+                    for (int j = 0; j < V; ++j) dw[i][j] += __shfl_xor(dw[i][j], o);
             for (int s = 0; s < 4; ++s) {
                 if (wave == s) {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i)
+                    for (int i = 0; i < N; ++i)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            float &at = total[(i * 8 + j) * 64 + lane];
+                        for (int j = 0; j < V; ++j) {
+                            float &at = total[(i * V + j) * 64 + lane];
                             if (s) dw[i][j] += at;
                             at = dw[i][j];
                         }
@@ -468,19 +509,19 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
             if (wave != 3 || lane >= LANES) return;
         }
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const Cols c(8 * (me + i * TPR), cols);
-            float sums[8];
+        for (int i = 0; i < N; ++i) {
+            const Cols<V> c(V * (me + i * TPR), cols);
+            float sums[V];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < V; ++j) {
                 if constexpr (kInLds) sums[j] = dw_at(i, j);
                 else sums[j] = dw[i][j];
             }
             if (!c.dup) {
-                store_raw<UMAP_F32, 8>(to + c.at, raw_of<UMAP_F32, 8>(sums));
+                store_raw<UMAP_F32, V>(to + c.at, raw_of<UMAP_F32, V>(sums));
             } else {
 #pragma unroll
-                for (int j = 1; j < 8; ++j)
+                for (int j = 1; j < V; ++j)
                     if (c.counts(j)) to[c.at + j] = sums[j];
             }
         }
@@ -745,8 +786,10 @@ hipError_t norm_from(int32_t type, int cols, Args... args)
 }  // namespace
 
 hipError_t launch_rows_norm(const umap_rows &x, RowIds ids, float scale, const umap_rows *residual, const umap_rows *h,
-                            RowWeight weight, float eps, const umap_rows &y, hipStream_t s)
+                            RowWeight weight, float eps, const umap_rows &to, hipStream_t s)
 {
+    umap_rows y = to;
+    if (y.group >= y.cols) y.group = 0;   // one group: the kernels take a group to lie in one vector of its lanes
     switch (x.type) {
     case UMAP_F32: return norm_from<UMAP_F32>(y.type, y.cols, &x, ids, scale, residual, h, weight, eps, &y, s);
     case UMAP_F16: return norm_from<UMAP_F16>(y.type, y.cols, &x, ids, scale, residual, h, weight, eps, &y, s);

@@ -429,6 +429,22 @@ def test_norm_without_eps_of_small_rows(dim):
         near(dx, dx64, (-(-dim // 64) + 40) * ref.E32 * mag)
 
 
+@pytest.mark.parametrize("dim", [5, 9, 300, 2048, 20001])
+@pytest.mark.parametrize("out", [I8, F8])
+def test_norm_with_weights_that_are_not_finite(dim, out):
+    x, w = rand(5, dim, BF16), rand(1, dim, F32)[0]
+    w[dim // 2], w[0] = float("nan"), float("inf")
+    x[2, 0] = 0   # 0 times infinity
+    group = 32
+    q, scales = torch.full((5, dim), 3, device=DEV).to(out), torch.empty(5, -(-dim // group), device=DEV)
+    R.umap_rows_norm(x, q, weight=w, y_scales=scales, group=group)
+    bad = torch.zeros(scales.shape[1], dtype=torch.bool, device=DEV)
+    bad[[0, dim // 2 // group]] = True
+    assert bool((scales.isnan() == bad).all()) and bool(scales[:, ~bad].isfinite().all())
+    wide = bad.repeat_interleave(group)[:dim]
+    assert not bool(q.float()[:, wide].any())
+
+
 def test_norm_offsets_beyond_32_bits():
     pitch = 2**30 + 8
     x = torch.empty(4 * pitch + 64, device=DEV, dtype=BF16).as_strided((5, 64), (pitch, 1))
