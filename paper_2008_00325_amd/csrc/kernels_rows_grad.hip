@@ -98,19 +98,22 @@ __device__ __forceinline__ void rank_in_wave(const uint32_t key[ITEMS], int ther
                                              uint32_t rank[ITEMS])
 {
     volatile uint32_t *const seen = lds.seen[threadIdx.x >> 6];
-    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const uint32_t d = (key[i] >> shift) & mask;
-        uint64_t same = __ballot(i < there);
+        // the lanes with this digit: those that agree in every bit
+        const uint64_t any = __ballot(i < there);
+        uint32_t lo = (uint32_t)any, hi = (uint32_t)(any >> 32);
 #pragma unroll
         for (int b = 0; b < kMaxDigit; ++b) {
-            const bool on = (d >> b) & 1;
-            const uint64_t with = __ballot(on);
-            same &= on ? with : ~with;
+            const int32_t on = (int32_t)(d << (31 - b)) >> 31;   // the bit, 32 times
+            const uint64_t with = __ballot(on < 0);
+            lo &= ~((uint32_t)with ^ (uint32_t)on);
+            hi &= ~((uint32_t)(with >> 32) ^ (uint32_t)on);
         }
+        const uint64_t same = (uint64_t)hi << 32 | lo;
         const uint32_t before = seen[d];
-        const uint32_t lower = __popcll(same & ((1ull << lane) - 1));
+        const uint32_t lower = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));   // of them, below this one
         rank[i] = before + lower;
         __builtin_amdgcn_wave_barrier();
         if (i < there && lower == 0) seen[d] = before + (uint32_t)__popcll(same);
@@ -133,6 +136,25 @@ __device__ __forceinline__ uint32_t digit_start(uint32_t all, SortLds &lds)
     up -= all;
     for (int w = 0; w < wave && w < kMaxBins / 64; ++w) up += lds.wave_total[w];
     return up;
+}
+
+// The waves' counts of a digit, and their sum; then where each wave's keys of it start.
+__device__ __forceinline__ uint32_t counts_of(int d, const SortLds &lds, uint32_t c[kSortWaves])
+{
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) c[w] = lds.seen[w][d];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) all += c[w];
+    return all;
+}
+__device__ __forceinline__ void starts_of(int d, uint32_t at, const uint32_t c[kSortWaves], SortLds &lds)
+{
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        lds.seen[w][d] = at;
+        at += c[w];
+    }
 }
 
 // Files the tile's keys and positions where their digit's turn is.  SUMMED: k_tile_sums
@@ -174,13 +196,11 @@ __global__ __launch_bounds__(kSortThreads) void k_file(Keys keys, const uint32_t
     for (int i = lane; i < bins; i += 64) lds.seen[wave][i] = 0;
     __builtin_amdgcn_wave_barrier();
     rank_in_wave<ITEMS>(key, there, shift, mask, lds, rank);
-    uint32_t at = digit_start(all, lds) + mine;   // behind its barrier all waves have counted
+    const uint32_t at = digit_start(all, lds) + mine;   // behind its barrier all waves have counted
     if (d < bins) {
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = lds.seen[w][d];
-            lds.seen[w][d] = at;
-            at += c;
-        }
+        uint32_t c[kSortWaves];
+        counts_of(d, lds, c);
+        starts_of(d, at, c, lds);
     }
     __syncthreads();
 #pragma unroll
@@ -192,11 +212,49 @@ __global__ __launch_bounds__(kSortThreads) void k_file(Keys keys, const uint32_t
     }
 }
 
-// The whole sort of up to 1,024 ITEMS keys by one workgroup.
+// Zeros for the row, by one wave.
+__device__ __forceinline__ void clear_row(const umap_rows &grad, int bytes_per, int64_t row)
+{
+    const int lane = threadIdx.x & 63, bytes = grad.cols * bytes_per;
+    char *const to = static_cast<char *>(grad.data) + row * grad.stride * bytes_per;
+    if (bytes >= 16) {   // the last 16 bytes may be written twice
+        const Raw<UMAP_F32, 4> zero{};
+        for (int b = lane * 16; b < bytes; b += 64 * 16)
+            store_raw<UMAP_F32, 4>(reinterpret_cast<float *>(to + min(b, bytes - 16)), zero);
+    } else if (2 * lane < bytes) {
+        reinterpret_cast<uint16_t *>(to)[lane] = 0;
+    }
+}
+
+// Rows that no id points at, where the ids are few: a workgroup marks the ids of its stretch
+// of rows in LDS, then clears the others.  The sort beside it takes one CU.
+constexpr int kMostMarked = 32768;
+__device__ __forceinline__ void clear_unmarked(const Keys &keys, int n, const umap_rows &grad, int bytes_per, int64_t first,
+                                               int rows)
+{
+    __shared__ uint32_t marked[kMostMarked / 32];
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) marked[i] = 0;
+    __syncthreads();
+    for (int t = threadIdx.x; t < n; t += kSortThreads) {
+        const int64_t r = (int64_t)keys(t) - first;
+        if (r >= 0 && r < rows) atomicOr(&marked[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+    for (int r = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < rows; r += kSortWaves)
+        if (!(marked[r >> 5] >> (r & 31) & 1) && first + r < grad.rows) clear_row(grad, bytes_per, first + r);
+}
+
+// The whole sort of up to 1,024 ITEMS keys by one workgroup; the others clear stretches of
+// clear_rows rows.
 template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void k_sort_few(Keys keys, int n, int passes, int bits, uint32_t *keys_out,
-                                                           uint32_t *pos_out, uint32_t *joins)
+                                                           uint32_t *pos_out, uint32_t *joins, umap_rows grad,
+                                                           int bytes_per, int clear_rows)
 {
+    if (blockIdx.x > 0) {
+        clear_unmarked(keys, n, grad, bytes_per, (int64_t)(blockIdx.x - 1) * clear_rows, clear_rows);
+        return;
+    }
     __shared__ SortLds lds;
     __shared__ uint32_t key_at[kSortThreads * ITEMS];
     __shared__ uint16_t pos_at[kSortThreads * ITEMS];
@@ -220,17 +278,10 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(Keys keys, int n, int
         rank_in_wave<ITEMS>(key, there, shift, mask, lds, rank);
         __syncthreads();
         const int d = threadIdx.x;
-        uint32_t all = 0;
-        if (d < bins)
-            for (int w = 0; w < kSortWaves; ++w) all += lds.seen[w][d];
-        uint32_t at = digit_start(all, lds);
-        if (d < bins) {
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = lds.seen[w][d];
-                lds.seen[w][d] = at;
-                at += c;
-            }
-        }
+        uint32_t all = 0, c[kSortWaves];
+        if (d < bins) all = counts_of(d, lds, c);
+        const uint32_t at = digit_start(all, lds);
+        if (d < bins) starts_of(d, at, c, lds);
         __syncthreads();
         const bool last = pass == passes - 1;
 #pragma unroll
@@ -368,12 +419,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
             clear = lo == sorted.n || sorted.keys[lo] != (uint32_t)v;
         }
         uint64_t rows = __ballot(clear) & ((1ull << kZeroRows) - 1);
-        const float zero[VEC] = {};
-        for (; rows; rows &= rows - 1) {
-            const int64_t row = first + __builtin_ctzll(rows);
-            for (int c = lane * VEC; c < grad.cols; c += 64 * VEC)
-                store_sums<TG, VEC>(grad, row, VecCols<VEC>(c, grad.cols), zero, 0.0f, false);
-        }
+        for (; rows; rows &= rows - 1) clear_row(grad, sizeof(Elem<TG>), first + __builtin_ctzll(rows));
         return;
     }
     const Group<LANES> group;
@@ -628,6 +674,7 @@ struct Call {
     umap_rows dout, grad;
     float scale;
     bool accumulate;
+    bool cleared;   // rows without ids are zero already
     float *parts;
     Joins joins;
     hipStream_t s;
@@ -638,7 +685,7 @@ hipError_t sum_chunks(const Call &c)
 {
     const int per_block = kThreads / LANES;
     const int64_t chunk_blocks = (c.plan.chunks * c.plan.slabs + per_block - 1) / per_block;
-    const int64_t zero_blocks = c.accumulate ? 0 : (c.grad.rows + kZeroRows * kWaves - 1) / (kZeroRows * kWaves);
+    const int64_t zero_blocks = c.accumulate || c.cleared ? 0 : (c.grad.rows + kZeroRows * kWaves - 1) / (kZeroRows * kWaves);
     const Grid2 g = grid2(chunk_blocks + zero_blocks, kThreads);
     hipLaunchKernelGGL((k_chunk_sums<TD, TG, LANES, VEC, PARTS>), dim3(g.x, g.y), dim3(kThreads), 0, c.s, c.sorted, c.plan.slabs,
                        c.dout, c.scale, c.grad, c.accumulate, c.parts, c.joins, chunk_blocks);
@@ -701,13 +748,16 @@ hipError_t launch_rows_lookup_grad(const umap_rows &dout, RowIds ids, float scal
     const SortPlan sort(n);
     if (n > 0 && SortPlan::few(n)) {
         const Keys from{nullptr, ids, grad.rows};
-        const dim3 one(1), threads(kSortThreads);
+        // about two workgroups to a CU clear rows meanwhile
+        const int clear_rows = (int)std::min<int64_t>(kMostMarked, (grad.rows + 510) / 511);
+        const dim3 grid(accumulate ? 1 : 1 + (unsigned)((grad.rows + clear_rows - 1) / clear_rows)), threads(kSortThreads);
+        const int bytes_per = grad.type == UMAP_F32 ? 4 : 2;
         if (sort.items == 1)
-            hipLaunchKernelGGL((k_sort_few<1>), one, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count);
+            hipLaunchKernelGGL((k_sort_few<1>), grid, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count, grad, bytes_per, clear_rows);
         else if (sort.items == 4)
-            hipLaunchKernelGGL((k_sort_few<4>), one, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count);
+            hipLaunchKernelGGL((k_sort_few<4>), grid, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count, grad, bytes_per, clear_rows);
         else
-            hipLaunchKernelGGL((k_sort_few<8>), one, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count);
+            hipLaunchKernelGGL((k_sort_few<8>), grid, threads, 0, s, from, (int)n, passes, bits, buf[0], buf[1], join_count, grad, bytes_per, clear_rows);
         if (hipError_t e = hipGetLastError()) return e;
         keys = buf[0];
         pos = buf[1];
@@ -722,7 +772,7 @@ hipError_t launch_rows_lookup_grad(const umap_rows &dout, RowIds ids, float scal
         }
     }
     const ChunkPlan plan(n, grad.cols);
-    const Call call{Sorted{keys, pos, n, plan.chunk}, plan, dout, grad, scale, accumulate,
+    const Call call{Sorted{keys, pos, n, plan.chunk}, plan, dout, grad, scale, accumulate, n > 0 && SortPlan::few(n),
                     reinterpret_cast<float *>(w + at.parts), Joins{join_count, join_count + 4}, s};
     switch (dout.type) {
     case UMAP_F32: return sum_into<UMAP_F32>(call);
