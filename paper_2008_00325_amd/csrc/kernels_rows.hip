@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void k_rows_lookup(umap_rows table, RowId
                 x[i] *= scale;
             }
         }
-        store_raw<TO, V>(static_cast<Elem<TO> *>(out.data) + t[u] * out.stride + c[u], raw_of<TO, V>(x));
+        store_once<TO, V>(static_cast<Elem<TO> *>(out.data) + t[u] * out.stride + c[u], raw_of<TO, V>(x));
     }
 }
 

@@ -13,7 +13,6 @@
 namespace ul {
 
 namespace {
-
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
@@ -212,17 +211,20 @@ __global__ __launch_bounds__(kSortThreads) void k_file(Keys keys, const uint32_t
     }
 }
 
-// Zeros for the row, by one wave.
-__device__ __forceinline__ void clear_row(const umap_rows &grad, int bytes_per, int64_t row)
+// Zeros for a row by `lanes` lanes of which this is number `lane`.
+__device__ __forceinline__ void clear_row(const umap_rows &grad, int bytes_per, int64_t row, int lane, int lanes)
 {
-    const int lane = threadIdx.x & 63, bytes = grad.cols * bytes_per;
+    const int bytes = grad.cols * bytes_per;
     char *const to = static_cast<char *>(grad.data) + row * grad.stride * bytes_per;
     if (bytes >= 16) {   // the last 16 bytes may be written twice
         const Raw<UMAP_F32, 4> zero{};
-        for (int b = lane * 16; b < bytes; b += 64 * 16)
-            store_raw<UMAP_F32, 4>(reinterpret_cast<float *>(to + min(b, bytes - 16)), zero);
-    } else if (2 * lane < bytes) {
-        reinterpret_cast<uint16_t *>(to)[lane] = 0;
+        for (int b = lane * 16; b < bytes; b += lanes * 16) {
+            float *const at = reinterpret_cast<float *>(to + min(b, bytes - 16));
+            if (lanes == 64) store_once<UMAP_F32, 4>(at, zero);
+            else store_raw<UMAP_F32, 4>(at, zero);   // neighbours of one lane meet in the cache
+        }
+    } else {
+        for (int b = lane * 2; b < bytes; b += lanes * 2) *reinterpret_cast<uint16_t *>(to + b) = 0;
     }
 }
 
@@ -241,7 +243,7 @@ __device__ __forceinline__ void clear_unmarked(const Keys &keys, int n, const um
     }
     __syncthreads();
     for (int r = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < rows; r += kSortWaves)
-        if (!(marked[r >> 5] >> (r & 31) & 1) && first + r < grad.rows) clear_row(grad, bytes_per, first + r);
+        if (!(marked[r >> 5] >> (r & 31) & 1) && first + r < grad.rows) clear_row(grad, bytes_per, first + r, threadIdx.x & 63, 64);
 }
 
 // The whole sort of up to 1,024 ITEMS keys by one workgroup; the others clear stretches of
@@ -322,7 +324,7 @@ constexpr uint32_t kNoKey = 0xffffffffu;
 template <int VEC>
 struct VecCols {
     int at, dup;
-    __device__ __forceinline__ VecCols(int c, int cols) : at(max(0, min(c, cols - VEC))), dup(c - at) {}
+    __device__ __forceinline__ VecCols(int c, int cols) : at(min(c, cols - VEC)), dup(c - at) {}   // cols >= VEC
     __device__ __forceinline__ bool live() const { return dup < VEC; }
 };
 
@@ -396,7 +398,13 @@ struct Chunk {
     }
 };
 
-constexpr int kZeroRows = 4;   // rows that a wave looks up and clears
+// Rows that a wave looks up and clears: some 64 KB of them, at most one to a lane.
+__host__ __device__ inline int rows_to_clear(int row_bytes)
+{
+    int rows = 64;
+    while (rows > 8 && (int64_t)rows * row_bytes > 65536) rows /= 2;
+    return rows;
+}
 
 template <int TD, int TG, int LANES, int VEC, int PARTS>
 __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slabs, umap_rows dout, float scale,
@@ -406,9 +414,10 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t block = row_block();
     if (block >= chunk_blocks) {   // rows that no id points at
-        const int64_t first = ((block - chunk_blocks) * kWaves + wave) * kZeroRows;
-        const int64_t v = first + (lane & (kZeroRows - 1));
-        bool clear = v < grad.rows;
+        const int per_wave = rows_to_clear(grad.cols * sizeof(Elem<TG>));
+        const int64_t first = ((block - chunk_blocks) * kWaves + wave) * per_wave;
+        const int64_t v = first + lane;
+        bool clear = lane < per_wave && v < grad.rows;
         if (clear) {
             int64_t lo = 0, hi = sorted.n;   // first position with a key >= v
             while (lo < hi) {
@@ -418,8 +427,12 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
             }
             clear = lo == sorted.n || sorted.keys[lo] != (uint32_t)v;
         }
-        uint64_t rows = __ballot(clear) & ((1ull << kZeroRows) - 1);
-        for (; rows; rows &= rows - 1) clear_row(grad, sizeof(Elem<TG>), first + __builtin_ctzll(rows));
+        if (per_wave == 64) {   // narrow rows: a lane clears its own
+            if (clear) clear_row(grad, sizeof(Elem<TG>), v, 0, 1);
+        } else {
+            for (uint64_t rows = __ballot(clear); rows; rows &= rows - 1)
+                clear_row(grad, sizeof(Elem<TG>), first + __builtin_ctzll(rows), lane, 64);
+        }
         return;
     }
     const Group<LANES> group;
@@ -474,7 +487,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
                 const Elem<TD> *const at = base + (int64_t)group.at(of.from, from + u) * dout.stride;   // by all lanes
 #pragma unroll
                 for (int h = 0; h < PARTS; ++h)
-                    if (cols(h).live()) to[u].part[h] = load_raw<TD, VEC>(at + cols(h).at);
+                    if (cols(h).live()) to[u].part[h] = load_once<TD, VEC>(at + cols(h).at);
             }
         };
         read(i0, row);
@@ -520,15 +533,16 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
 }
 
 // The ids over several chunks: slot 1 of the chunk in which one begins and slot 0 of those
-// that follow.  256 columns to a workgroup: a wave has four columns per lane and a stretch
-// of the parts, and the waves' sums are added in order.  (The order of the list changes
-// nothing in the sums.)
-constexpr int kJoinWaves = 16, kJoinCols = 256;
+// that follow.  64 VEC columns to a workgroup and a stretch of the parts to each of its waves,
+// whose sums are added in order.  (The order of the list changes nothing in the sums.)
+constexpr int kJoinWaves = 16;
+constexpr int join_vec(int cols) { return cols >= 4 ? 4 : 1; }   // a vector's columns must exist
 
-template <int TG>
+template <int TG, int VEC>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_join_parts(Sorted sorted, float scale, umap_rows grad, bool accumulate,
                                                                 const float *parts, Joins joins)
 {
+    constexpr int kJoinCols = 64 * VEC;
     __shared__ float stretch[kJoinWaves][kJoinCols];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cols = grad.cols;
     const uint32_t count = *joins.count;
@@ -547,35 +561,29 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join_parts(Sorted sorted, f
         const int64_t each = (more + kJoinWaves - 1) / kJoinWaves;
         const int64_t first = min(each * wave, more), last = min(first + each, more);
         for (int c0 = blockIdx.y * kJoinCols; c0 < cols; c0 += gridDim.y * kJoinCols) {
-            const int c = c0 + lane * 4;
-            const float *const begun = parts + (chunk * 2 + 1) * cols, *const after = parts + (chunk + 1) * 2 * cols;
-            float sum[4] = {};
-            if (c + 4 <= cols) {
-                auto add = [&](const float *p) {
-                    float v[4];
-                    floats_of<UMAP_F32, 4>(load_raw<UMAP_F32, 4>(p + c), v);
+            const VecCols<VEC> c(c0 + lane * VEC, cols);
+            const float *const begun = parts + (chunk * 2 + 1) * cols + c.at, *const after = parts + (chunk + 1) * 2 * cols + c.at;
+            float sum[VEC] = {};
+            auto add = [&](const float *p) {
+                float v[VEC];
+                floats_of<UMAP_F32, VEC>(load_raw<UMAP_F32, VEC>(p), v);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[i] += v[i];
-                };
-                if (wave == 0) add(begun);
+                for (int i = 0; i < VEC; ++i) sum[i] += v[i];
+            };
+            if (wave == 0) add(begun);
 #pragma unroll 16
-                for (int64_t m = first; m < last; ++m) add(after + m * 2 * cols);
-            } else {
-                for (int i = 0; i < 4 && c + i < cols; ++i) {
-                    if (wave == 0) sum[i] = begun[c + i];
-#pragma unroll 16
-                    for (int64_t m = first; m < last; ++m) sum[i] += after[m * 2 * cols + c + i];
-                }
-            }
+            for (int64_t m = first; m < last; ++m) add(after + m * 2 * cols);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) stretch[wave][lane * 4 + i] = sum[i];
+            for (int i = 0; i < VEC; ++i) stretch[wave][lane * VEC + i] = sum[i];
             __syncthreads();
-            for (int i = threadIdx.x; i < kJoinCols && c0 + i < cols; i += 64 * kJoinWaves) {
-                float total = stretch[0][i];
-                for (int w = 1; w < kJoinWaves; ++w) total += stretch[w][i];
-                total *= scale;
-                Elem<TG> *const to = static_cast<Elem<TG> *>(grad.data) + (int64_t)key * grad.stride + c0 + i;
-                *to = float_elem<TG>(accumulate ? elem_float<TG>(*to) + total : total);
+            if (wave == 0 && c.live()) {
+                float total[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    total[i] = stretch[0][lane * VEC + i];
+                    for (int w = 1; w < kJoinWaves; ++w) total[i] += stretch[w][lane * VEC + i];
+                }
+                store_sums<TG, VEC>(grad, key, c, total, scale, accumulate);
             }
             __syncthreads();
         }
@@ -640,7 +648,10 @@ struct RowShape {
     }
 };
 
-// Positions per chunk: about 8,192 waves where there are enough of them.
+// Positions per chunk: 64 where that leaves 2,048 waves, else fewer.  us per call with at least
+// 2,048 / 4,096 / 8,192 / 16,384 waves: 131,072 rows of 300 columns 75 / 85 / 95 / 111, of 2,048
+// columns 354 / 354 / 355 / 364, 32,768 of 4,096 196 / 195 / 204 / 231, 131,072 of 1,024 with one id
+// 112 / 111 / 154 / 255.
 struct ChunkPlan {
     int32_t slabs, chunk;
     int64_t chunks;
@@ -649,7 +660,7 @@ struct ChunkPlan {
         const RowShape shape(cols);
         slabs = (cols + shape.slab - 1) / shape.slab;
         chunk = shape.lanes;
-        while (chunk > 8 && (n + chunk - 1) / chunk * slabs * shape.lanes / 64 < 8192) chunk /= 2;
+        while (chunk > 8 && (n + chunk - 1) / chunk * slabs * shape.lanes / 64 < 2048) chunk /= 2;
         chunks = (n + chunk - 1) / chunk;
     }
 };
@@ -685,15 +696,19 @@ hipError_t sum_chunks(const Call &c)
 {
     const int per_block = kThreads / LANES;
     const int64_t chunk_blocks = (c.plan.chunks * c.plan.slabs + per_block - 1) / per_block;
-    const int64_t zero_blocks = c.accumulate || c.cleared ? 0 : (c.grad.rows + kZeroRows * kWaves - 1) / (kZeroRows * kWaves);
+    const int64_t per_clear = (int64_t)rows_to_clear(c.grad.cols * sizeof(Elem<TG>)) * kWaves;
+    const int64_t zero_blocks = c.accumulate || c.cleared ? 0 : (c.grad.rows + per_clear - 1) / per_clear;
     const Grid2 g = grid2(chunk_blocks + zero_blocks, kThreads);
     hipLaunchKernelGGL((k_chunk_sums<TD, TG, LANES, VEC, PARTS>), dim3(g.x, g.y), dim3(kThreads), 0, c.s, c.sorted, c.plan.slabs,
                        c.dout, c.scale, c.grad, c.accumulate, c.parts, c.joins, chunk_blocks);
     if (hipError_t e = hipGetLastError()) return e;
     if (c.plan.chunks < 3) return hipSuccess;   // no id needs joining
-    const int across = (c.grad.cols + kJoinCols - 1) / kJoinCols;
-    hipLaunchKernelGGL((k_join_parts<TG>), dim3((unsigned)std::min<int64_t>(c.plan.chunks, 256), across < 64 ? across : 64),
-                       dim3(64 * kJoinWaves), 0, c.s, c.sorted, c.scale, c.grad, c.accumulate, c.parts, c.joins);
+    const int join_cols = 64 * join_vec(c.grad.cols), across = (c.grad.cols + join_cols - 1) / join_cols;
+    const dim3 grid((unsigned)std::min<int64_t>(c.plan.chunks, 256), std::min(across, 64)), threads(64 * kJoinWaves);
+    if (join_vec(c.grad.cols) == 1)
+        hipLaunchKernelGGL((k_join_parts<TG, 1>), grid, threads, 0, c.s, c.sorted, c.scale, c.grad, c.accumulate, c.parts, c.joins);
+    else
+        hipLaunchKernelGGL((k_join_parts<TG, 4>), grid, threads, 0, c.s, c.sorted, c.scale, c.grad, c.accumulate, c.parts, c.joins);
     return hipGetLastError();
 }
 

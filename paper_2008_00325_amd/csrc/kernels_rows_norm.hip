@@ -285,9 +285,9 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = Cols<V>(V * (me + i * TPR), cols).at;
-            if (v >= 0) a[i] = load_raw<TX, V>(row_ptr<TX>(x, v) + at);
+            if (v >= 0) a[i] = load_once<TX, V>(row_ptr<TX>(x, v) + at);
             else a[i] = Raw<TX, V>{};   // a missing row stands for zeros
-            if (residual.data) b[i] = load_raw<TX, V>(row_ptr<TX>(residual, t) + at);
+            if (residual.data) b[i] = load_once<TX, V>(row_ptr<TX>(residual, t) + at);
         }
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const Cols<V> c(V * (me + i * TPR), cols);
-                if (c.live()) store_raw<TX, V>(row_out<TX>(h, t) + c.at, raw_of<TX, V>(e[i]));
+                if (c.live()) store_once<TX, V>(row_out<TX>(h, t) + c.at, raw_of<TX, V>(e[i]));
             }
         }
         float add = eps;
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm(umap_rows x, 
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const Cols<V> c(V * (me + i * TPR), cols);
-                if (c.live()) store_raw<TY, V>(row_out<TY>(y, t) + c.at, raw_of<TY, V>(e[i]));
+                if (c.live()) store_once<TY, V>(row_out<TY>(y, t) + c.at, raw_of<TY, V>(e[i]));
             }
         } else {
             // magnitudes compare as their bits do, infinities and NaN above all others
@@ -410,9 +410,9 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = Cols<V>(V * (me + i * TPR), cols).at;
-            a[i] = load_raw<TX, V>(row_ptr<TX>(h, t) + at);
-            b[i] = load_raw<TX, V>(row_ptr<TX>(dy, t) + at);
-            if (dh.data) u[i] = load_raw<TX, V>(row_ptr<TX>(dh, t) + at);
+            a[i] = load_once<TX, V>(row_ptr<TX>(h, t) + at);
+            b[i] = load_once<TX, V>(row_ptr<TX>(dy, t) + at);
+            if (dh.data) u[i] = load_once<TX, V>(row_ptr<TX>(dh, t) + at);
         }
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
 #pragma unroll
                 for (int j = 0; j < V; ++j) r[j] += e[j];
             }
-            if (c.live()) store_raw<TX, V>(row_out<TX>(dx, t) + c.at, raw_of<TX, V>(r));
+            if (c.live()) store_once<TX, V>(row_out<TX>(dx, t) + c.at, raw_of<TX, V>(r));
         }
     }
     if constexpr (DW) {

@@ -85,6 +85,37 @@ __device__ __forceinline__ void store_raw(Elem<T> *p, const Raw<T, V> &r)
     *reinterpret_cast<Packed<T, V> *>(p) = m;
 }
 
+// Likewise, for what is not needed again before much else has gone by: the caches give it up
+// first, which leaves them to the rows that are (a table's frequent ones, what the next kernel
+// reads).  us per call, plain / so: 32,768 x 4096 bf16 looked up 78 / 72, 70,000 x 300 into fp32 30 /
+// 19, norm of 32,768 x 4096 into int8 and back 239 / 210, its gradient 191 / 170, gradient of 131,072 x
+// 2048 355 / 311 (its loads alone; with its stores as well 335).  A lookup, norm and gradient
+// one after the other on the same 34 to 67 MB, which the caches would hold, lose: 78.6 / 80.3;
+// 134 MB gain: 170 / 149.  Only 16-byte accesses gain (8-bit rows written so: 209 / 220).
+template <int T, int V>
+__device__ __forceinline__ void store_once(Elem<T> *p, const Raw<T, V> &r)
+{
+    if constexpr (sizeof(Raw<T, V>) == 16) {
+        typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(1)));
+        __builtin_nontemporal_store(__builtin_bit_cast(Words, r), reinterpret_cast<Words *>(p));
+    } else {
+        store_raw<T, V>(p, r);
+    }
+}
+template <int T, int V>
+__device__ __forceinline__ Raw<T, V> load_once(const Elem<T> *p)
+{
+    if constexpr (sizeof(Raw<T, V>) == 16) {
+        typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(1)));
+        return __builtin_bit_cast(Raw<T, V>, __builtin_nontemporal_load(reinterpret_cast<const Words *>(p)));
+    } else if constexpr (sizeof(Raw<T, V>) == 8) {
+        typedef uint32_t Words __attribute__((ext_vector_type(2), aligned(1)));
+        return __builtin_bit_cast(Raw<T, V>, __builtin_nontemporal_load(reinterpret_cast<const Words *>(p)));
+    } else {
+        return load_raw<T, V>(p);
+    }
+}
+
 template <int T, int V>
 __device__ __forceinline__ void floats_of(const Raw<T, V> &r, float v[V])
 {
