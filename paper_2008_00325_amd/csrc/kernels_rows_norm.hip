@@ -807,7 +807,9 @@ hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const 
                                  float eps, const umap_rows &dx, float *dweight, void *workspace, hipStream_t s)
 {
     int64_t count = 0;
-    float *const partial = dweight ? static_cast<float *>(workspace) : nullptr;
+    // one workgroup's sums are dweight itself
+    const bool one = dweight && dy.rows > 0 && by_cols<GradBlocks>(dy.cols, kGradOne, dy.rows) == 1;
+    float *const partial = one ? dweight : dweight ? static_cast<float *>(workspace) : nullptr;
     if (dy.rows > 0) {
         hipError_t e;
         switch (dy.type) {
@@ -817,7 +819,7 @@ hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const 
         }
         if (e != hipSuccess) return e;
     }
-    if (dweight) {
+    if (dweight && !one) {
         hipLaunchKernelGGL(k_rows_join, dim3((dy.cols + 63) / 64), dim3(64 * kJoinWaves), 0, s, partial, (int)count,
                            dy.cols, dweight);
         return hipGetLastError();

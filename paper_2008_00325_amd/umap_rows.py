@@ -12,6 +12,7 @@ whatever the library refuses :class:`UmapLayoutError`.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -47,6 +48,8 @@ class umap_rows(ctypes.Structure):
 
 
 _lib = None
+_call: dict = {}   # the library's functions, taking packed umap_rows
+_pack = struct.Struct("@PPqqiiii").pack
 
 
 def lib() -> ctypes.CDLL:
@@ -67,11 +70,15 @@ def lib() -> ctypes.CDLL:
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = result
+            # a packed structure is passed in a fraction of the time that a Structure takes
+            packed = [ctypes.c_char_p if a is M else a for a in args]
+            _call[name] = ctypes.CFUNCTYPE(result, *packed)((name, L))
         _lib = L
     return _lib
 
 
-def _rows(x, name: str, types: dict, scales=None, group: int = 0) -> umap_rows:
+def _rows(x, name: str, types: dict, scales=None, group: int = 0) -> tuple:
+    """A matrix as a packed umap_rows, its rows and its columns."""
     kind = types.get(x.dtype)
     if kind is None:
         raise ValueError(f"{name} must not hold {x.dtype}")
@@ -83,11 +90,10 @@ def _rows(x, name: str, types: dict, scales=None, group: int = 0) -> umap_rows:
     stride, step = x.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{name}: the columns must lie next to each other")
-    if scales is None:
-        return umap_rows(x.data_ptr(), None, rows, stride, cols, kind, group, 0)
-    count = rows * (-(-cols // group) if group > 0 else 1)
-    _flat(scales, f"{name}'s scales", torch.float32, count)
-    return umap_rows(x.data_ptr(), scales.data_ptr(), rows, stride, cols, kind, group, 0)
+    at = 0
+    if scales is not None:
+        at = _flat(scales, f"{name}'s scales", torch.float32, rows * (-(-cols // group) if group > 0 else 1))
+    return _pack(x.data_ptr(), at, rows, stride, cols, kind, group, 0), rows, cols
 
 
 def _flat(x, name: str, dtype, count: int) -> int:
@@ -141,10 +147,11 @@ def umap_rows_lookup(table, ids, out, scale: float = 1.0, table_scales=None, gro
 
     An int8 or float8_e4m3fn table comes with `table_scales`, one fp32 per row and `group` columns (32, 64 or 128;
     0: one per row)."""
-    t = _rows(table, "table", _ANY, table_scales, group)
-    o = _rows(out, "out", _FLOAT)
-    at, kind = _id_args(ids, o.rows)
-    _check(lib().umap_rows_lookup(t, at, kind, scale, o, _stream(stream)))
+    t, _, _ = _rows(table, "table", _ANY, table_scales, group)
+    o, n, _ = _rows(out, "out", _FLOAT)
+    at, kind = _id_args(ids, n)
+    lib()
+    _check(_call["umap_rows_lookup"](t, at, kind, scale, o, _stream(stream)))
 
 
 def umap_rows_lookup_grad_workspace(n: int, rows: int, cols: int) -> int:
@@ -155,11 +162,12 @@ def umap_rows_lookup_grad_workspace(n: int, rows: int, cols: int) -> int:
 def umap_rows_lookup_grad(dout, ids, grad, workspace, scale: float = 1.0, accumulate: bool = False,
                           stream=None) -> None:
     """grad[v] = scale * (sum of dout[t] over ids[t] = v); with `accumulate` added to grad's rows."""
-    d = _rows(dout, "dout", _FLOAT)
-    g = _rows(grad, "grad", _FLOAT)
-    at, kind = _id_args(ids, d.rows)
+    d, n, _ = _rows(dout, "dout", _FLOAT)
+    g, _, _ = _rows(grad, "grad", _FLOAT)
+    at, kind = _id_args(ids, n)
     work, size = _work(workspace)
-    _check(lib().umap_rows_lookup_grad(d, at, kind, scale, g, 1 if accumulate else 0, work, size, _stream(stream)))
+    lib()
+    _check(_call["umap_rows_lookup_grad"](d, at, kind, scale, g, 1 if accumulate else 0, work, size, _stream(stream)))
 
 
 def umap_rows_norm(x, y, weight=None, residual=None, h=None, ids=None, scale: float = 1.0, y_scales=None,
@@ -168,13 +176,14 @@ def umap_rows_norm(x, y, weight=None, residual=None, h=None, ids=None, scale: fl
 
     An int8 or float8_e4m3fn y is written with `y_scales` (see umap_rows_lookup).  h may be the residual itself or,
     without ids, x."""
-    X = _rows(x, "x", _FLOAT)
-    Y = _rows(y, "y", _ANY, y_scales, group)
-    R = None if residual is None else _rows(residual, "residual", _FLOAT)
-    H = None if h is None else _rows(h, "h", _FLOAT)
-    at, kind = _id_args(ids, Y.rows)
-    w, w_kind = _weight_args(weight, X.cols)
-    _check(lib().umap_rows_norm(X, at, kind, scale, R, H, w, w_kind, eps, Y, _stream(stream)))
+    X, _, cols = _rows(x, "x", _FLOAT)
+    Y, n, _ = _rows(y, "y", _ANY, y_scales, group)
+    R = None if residual is None else _rows(residual, "residual", _FLOAT)[0]
+    H = None if h is None else _rows(h, "h", _FLOAT)[0]
+    at, kind = _id_args(ids, n)
+    w, w_kind = _weight_args(weight, cols)
+    lib()
+    _check(_call["umap_rows_norm"](X, at, kind, scale, R, H, w, w_kind, eps, Y, _stream(stream)))
 
 
 def umap_rows_norm_grad_workspace(n: int, cols: int) -> int:
@@ -186,14 +195,15 @@ def umap_rows_norm_grad(dy, h, dx, weight=None, dh=None, dweight=None, workspace
                         stream=None) -> None:
     """Gradient of y = h / sqrt(mean h^2 + eps) * weight for h (plus `dh`, what reaches h otherwise), into dx (which
     may be dy or dh itself), and for the weight, into dweight (fp32; needs the workspace)."""
-    Y = _rows(dy, "dy", _FLOAT)
-    H = _rows(h, "h", _FLOAT)
-    X = _rows(dx, "dx", _FLOAT)
-    U = None if dh is None else _rows(dh, "dh", _FLOAT)
-    w, w_kind = _weight_args(weight, Y.cols)
-    dw = None if dweight is None else _flat(dweight, "dweight", torch.float32, Y.cols)
+    Y, _, cols = _rows(dy, "dy", _FLOAT)
+    H, _, _ = _rows(h, "h", _FLOAT)
+    X, _, _ = _rows(dx, "dx", _FLOAT)
+    U = None if dh is None else _rows(dh, "dh", _FLOAT)[0]
+    w, w_kind = _weight_args(weight, cols)
+    dw = None if dweight is None else _flat(dweight, "dweight", torch.float32, cols)
     work, size = _work(workspace)
-    _check(lib().umap_rows_norm_grad(Y, H, U, w, w_kind, eps, X, dw, work, size, _stream(stream)))
+    lib()
+    _check(_call["umap_rows_norm_grad"](Y, H, U, w, w_kind, eps, X, dw, work, size, _stream(stream)))
 
 
 __all__ = [*EXPORTS, "UmapLayoutError", "umap_rows"]
