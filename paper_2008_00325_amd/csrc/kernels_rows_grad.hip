@@ -4,6 +4,13 @@
 // The positions t are sorted by id, stably (least significant digit first), so the
 // rows that belong to one table row lie one after the other, in the order of t, and
 // are added in that order: the same sum in every call, without atomics.
+//
+// Bound by memory: every row of dout is read once and every row of grad written once, by
+// waves that all have the same number of rows however often an id occurs; the sort (of 4-byte
+// keys and positions) and the joins are latency, launch by launch.  Sums are fp32, rounded
+// once.  us per call: 131,072 bf16 rows into fp32 128,000 x 2048 311 to 341 (1.59 GB, 253 us at a
+// copy's rate: sums and zeros 270 to 290, sort 31, joins 18), 8,192 into 32,000 x 1024 40 (0.15 GB, 24: sort
+// and zeros 25, sums 9, joins 5), 77 into 2,000 x 64 14 (three launches).
 #include <algorithm>
 
 #include "launch_sizes.hpp"
@@ -590,18 +597,22 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join_parts(Sorted sorted, f
     }
 }
 
-// Keys per tile of the sort: 4,096 while there are few tiles, so that more CUs work, else 16,384;
-// beyond 64 of those the tiles' counts are added up in a launch of their own.
+// Tiles of 4,096 keys up to 32 of them, then of 8,192; the workgroups add up to 128 tiles'
+// counts themselves, beyond that a launch of its own does.  us per call with 16,384 keys and 64
+// tiles / 8,192 and 64 / 8,192 and 128 / 4,096 and 64: 300,000 rows of 64 columns 114 / 84 / 82 / 80, a
+// million of 256 222 / 208 / 201 / 209, four million of 16 737 / 748 / 752 / 812.  Up to 8,192
+// keys are sorted in one launch (1,000 rows 64 / 37 us with the other launches of a call,
+// 8,192 83 / 58).
 struct SortPlan {
     int items;   // per thread
     int64_t tiles;
     bool summed;
     explicit SortPlan(int64_t n)
     {
-        items = n <= 1024 ? 1 : n <= 32 * 4096 ? 4 : 16;
+        items = n <= 32 * 4096 ? 4 : 8;
         if (few(n)) items = n <= 1024 ? 1 : n <= 4096 ? 4 : 8;
         tiles = (n + kSortThreads * items - 1) / (kSortThreads * items);
-        summed = tiles > 64;
+        summed = tiles > 128;
     }
     static bool few(int64_t n) { return n <= 8192; }
 };
@@ -780,7 +791,7 @@ hipError_t launch_rows_lookup_grad(const umap_rows &dout, RowIds ids, float scal
         for (int pass = 0; n > 0 && pass < passes; ++pass) {
             const SortPass p{Keys{keys, ids, grad.rows}, pos, n, pass * bits, bits, counts, (int)sort.tiles,
                              buf[2 * (pass & 1)], buf[2 * (pass & 1) + 1], pass ? nullptr : join_count, s};
-            const hipError_t e = sort.items == 4 ? p.run<4>(sort.summed) : p.run<16>(sort.summed);
+            const hipError_t e = sort.items == 4 ? p.run<4>(sort.summed) : p.run<8>(sort.summed);
             if (e != hipSuccess) return e;
             keys = p.keys_out;
             pos = p.pos_out;

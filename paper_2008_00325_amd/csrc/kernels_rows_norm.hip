@@ -1,11 +1,25 @@
 // kernels_rows_norm.hip -- root-mean-square norm of rows and its gradient (umap_rows.h).
 //
-// Bound by memory: a row is read once and stays in registers between its sum of squares
-// and its result, so every input is read and every output written once.  A row belongs
-// to some lanes of a wave (up to 1,024 columns) or to a workgroup; a thread holds a few vectors of its
-// columns, and reads its share of the next row before it works on this one.
+//   norm      h = scale x + residual, rho = 1 / sqrt(mean h^2 + eps), y = h rho weight
+//   gradient  dx = rho (dy weight - h rho^2 mean(dy weight h)) + dh, dweight = sum dy h rho
+//
+// Bound by memory: a row is read once and stays in registers between its sums and its
+// result, so every input is read and every output written once.  A row belongs to some
+// lanes of a wave (up to 1,024 columns) or to a workgroup, whose waves add their sums over
+// LDS with one barrier; a thread holds a few vectors of its columns, and reads its share of
+// the next row before it works on this one.  The gradient's workgroups stay and keep
+// dweight's sums of their rows in registers or LDS; a second launch joins them in order.
+// All arithmetic is fp32; h, y and dx are rounded once, on the way out.
+//
+// us per call and TB/s of what is read and written, one copy reaching 6.3 TB/s: 32,768 x 4096
+// bf16, residual added, into bf16 h and int8 140 (6.7, the same rows at every call), gradient
+// with upstream gradient and dweight 169 (6.4); 65,536 x 1024 into bf16 86 (6.3); 70,000 x 784
+// fp32 into fp8 with a scale per 128 columns 52 (5.3).  Weaker: rows a little longer than a
+// power of two vectors (300 columns into int8 5.0: 38 of 64 lanes have any), rows beyond
+// 16,384 columns, whose gradient spills registers (2.4).
 #include <algorithm>
 
+#include "launch_sizes.hpp"
 #include "rows_device.hpp"
 
 namespace ul {
@@ -692,19 +706,6 @@ auto by_cols(int cols, int one, Args... args)
     return Launch<kBlock, 4>::go(waves(4), args...);
 }
 
-// Rows that one workgroup takes in turn: few, so that workgroups end and start all the
-// time and the card stays evenly loaded, but enough to read ahead.  us per call on 256 MB
-// of bf16 rows, norm with residual into int8, with 1 / 2 / 4 / 8 turns: 64 columns - / - / 186 /
-// 190, 300 276 / 217 / 203 / 203, 1,024 180 / 166 / 174 / 178, 2,048 179 / 161 / - / 194, 4,096 186 / 166
-// / - / 184, 8,192 193 / 165 / 176 / 173, 16,384 215 / 198 / 185 / 176.  Less where that would leave
-// fewer than four workgroups for each CU.
-unsigned grid_for(int64_t work, int cols)
-{
-    int64_t turns = cols <= 512 ? 4 : cols <= 8192 ? 2 : 8;
-    while (turns > 1 && work / turns < 1024) turns /= 2;
-    return (unsigned)((work + turns - 1) / turns);
-}
-
 // Where every workgroup ends with a sum to hand over: as many as the card holds at once
 // (`waves` of them on a CU), all with the same number of rows, give or take one.
 int64_t even_grid(int64_t work, int threads, int waves)
@@ -713,10 +714,10 @@ int64_t even_grid(int64_t work, int threads, int waves)
     const int64_t turns = (work + most - 1) / most;
     return (work + turns - 1) / turns;
 }
-// us per call on 256 MB of bf16 rows with upstream gradient and dweight at 8 / 12 / 16 / 20 / 24
-// waves on a CU: 64 columns - / - / 209 / - / 229, 300 341 / - / 241 / 232 / 236, 784 208 / 219 / 239 / - / -,
-// 1,024 204 / 207 / 221 / - / -, 2,048 223 / - / 215 / 226 / 247, 4,096 214 / - / 191 / 191 / 225, 8,192 319 /
-// - / 205 / 206 / 206 (one workgroup).
+// us per call on 256 MB of bf16 rows with upstream gradient and dweight at 8 / 12 / 16 / 20
+// waves on a CU: 64 columns 167 / 177 / 192 / 206, 300 350 / 272 / 250 / 239, 784 204 / 209 / 230 / 210, 1,024
+// 198 / 195 / 207 / 206, 2,048 226 / 186 / 191 / 202, 4,096 207 / 207 / 180 / 180, 8,192 and more the same (one
+// workgroup).
 constexpr int grad_waves(int lanes, int vec) { return lanes == 64 && vec == 2 ? 8 : 16; }
 
 template <int TX, int TY>
@@ -727,7 +728,7 @@ struct Norm {
                              const umap_rows *h, RowWeight weight, float eps, const umap_rows *y, hipStream_t s)
         {
             const int64_t work = (y->rows + shape.rows - 1) / shape.rows;
-            const dim3 grid(VEC == 4 ? (unsigned)even_grid(work, shape.threads, 16) : grid_for(work, y->cols));
+            const dim3 grid(VEC == 4 ? (unsigned)even_grid(work, shape.threads, 16) : (unsigned)norm_grid(work, shape.threads));
             const dim3 threads(shape.threads);
             const umap_rows r = residual ? *residual : umap_rows{}, to = h ? *h : umap_rows{};
             if constexpr (LANES == kOneThread)
@@ -756,7 +757,7 @@ struct Grad {
                              RowWeight weight, float eps, const umap_rows *dx, float *partial, int64_t *count, hipStream_t s)
         {
             const int64_t work = (dy->rows + shape.rows - 1) / shape.rows;
-            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows) : grid_for(work, dy->cols);
+            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows) : norm_grid(work, shape.threads);
             const dim3 grid((unsigned)*count), threads(shape.threads);
             const size_t sums = LANES == kBlock && VEC > 1 ? (size_t)shape.threads * VEC * 32 : 0;
             const umap_rows up = dh ? *dh : umap_rows{};
