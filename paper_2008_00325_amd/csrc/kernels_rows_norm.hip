@@ -12,9 +12,9 @@
 // All arithmetic is fp32; h, y and dx are rounded once, on the way out.
 //
 // us per call and TB/s of what is read and written, one copy reaching 6.3 TB/s: 32,768 x 4096
-// bf16, residual added, into bf16 h and int8 140 (6.7, the same rows at every call), gradient
-// with upstream gradient and dweight 169 (6.4); 65,536 x 1024 into bf16 86 (6.3); 70,000 x 784
-// fp32 into fp8 with a scale per 128 columns 52 (5.3).  Weaker: rows a little longer than a
+// bf16, residual added, into bf16 h and int8 150 (6.3), gradient with upstream gradient and
+// dweight 169 (6.4), the join 5 more; 131,072 x 1024 bf16 without residual 83 (6.5); 70,000 x 784
+// fp32 into fp8 with a scale per 128 columns 56 (5.0).  Weaker: rows a little longer than a
 // power of two vectors (300 columns into int8 5.0: 38 of 64 lanes have any), rows beyond
 // 16,384 columns, whose gradient spills registers (2.4).
 #include <algorithm>
@@ -728,7 +728,7 @@ struct Norm {
                              const umap_rows *h, RowWeight weight, float eps, const umap_rows *y, hipStream_t s)
         {
             const int64_t work = (y->rows + shape.rows - 1) / shape.rows;
-            const dim3 grid(VEC == 4 ? (unsigned)even_grid(work, shape.threads, 16) : (unsigned)norm_grid(work, shape.threads));
+            const dim3 grid(VEC == 4 ? (unsigned)even_grid(work, shape.threads, 16) : (unsigned)norm_grid(work, y->cols, shape.threads));
             const dim3 threads(shape.threads);
             const umap_rows r = residual ? *residual : umap_rows{}, to = h ? *h : umap_rows{};
             if constexpr (LANES == kOneThread)
@@ -757,7 +757,7 @@ struct Grad {
                              RowWeight weight, float eps, const umap_rows *dx, float *partial, int64_t *count, hipStream_t s)
         {
             const int64_t work = (dy->rows + shape.rows - 1) / shape.rows;
-            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows) : norm_grid(work, shape.threads);
+            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows) : norm_grid(work, dy->cols, shape.threads);
             const dim3 grid((unsigned)*count), threads(shape.threads);
             const size_t sums = LANES == kBlock && VEC > 1 ? (size_t)shape.threads * VEC * 32 : 0;
             const umap_rows up = dh ? *dh : umap_rows{};

@@ -75,17 +75,17 @@ constexpr bool halo_pays(int64_t near, int64_t kept, int64_t n, int32_t dim)
 }
 
 // ---- norm of rows, and its gradient without dweight ----
-// Workgroups for `work` of them, which take four (or as many rows as a workgroup holds) in
-// turn: few, so that workgroups end and start all the time and the card stays evenly loaded,
-// but enough to read ahead.  us per call on 256 MB of bf16 rows with 1 / 2 / 4 / 8 turns: norm
-// with residual into int8, 64 columns 151 / 141 / 142 / 146, 300 243 / 198 / 190 / 191, 1,024 140 / 136 /
-// 142 / 145, 2,048 162 / 152 / 148 / 151, 4,096 156 / 145 / 140 / 145, 5,120 181 / 159 / 153 / 156, 16,384 188 /
-// 169 / 158 / 157; gradient 300 170 / 141 / 139 / 153, 4,096 135 / 126 / 128 / 134, 8,192 191 / 156 / 141 / 137.
-// Less where that would leave fewer than four workgroups for each CU, more where the grid
-// would not fit a launch.
-constexpr int64_t norm_grid(int64_t work, int64_t threads)
+// Workgroups for `work` of them, which take two (up to 512 columns four) times as many rows as
+// they hold in turn: few, so that workgroups end and start all the time and the card stays
+// evenly loaded, but enough to read ahead.  us per call with 1 / 2 / 3 / 4 turns, three sets of
+// inputs in turn: 32,768 x 4096 bf16 with residual into bf16 171 / 175 / 182 / 184, into int8 and
+// read back 215 / 209 / 213 / 216, 131,072 x 1024 172 / 175 / 183 / 184, 16,384 x 8192 without residual 91 / 86 /
+// 87 / 88, 70,000 x 784 fp32 into fp8 and back 87 / 81 / 81 / 82, 200,000 x 300 fp32 into int8 and back
+// 125 / 107 / 102 / 100.  Less where that would leave fewer than four workgroups for each CU, more
+// where the grid would not fit a launch.
+constexpr int64_t norm_grid(int64_t work, int32_t cols, int64_t threads)
 {
-    int64_t turns = 4;
+    int64_t turns = cols <= 512 ? 4 : 2;
     while (turns > 1 && work / turns < 1024) turns /= 2;
     while ((work + turns - 1) / turns * threads >= kGridItems) turns *= 2;
     return (work + turns - 1) / turns;

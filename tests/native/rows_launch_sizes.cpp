@@ -7,6 +7,8 @@
 int main()
 {
     int64_t work, threads;
-    while (scanf("%" SCNd64 " %" SCNd64, &work, &threads) == 2) printf("%" PRId64 "\n", ul::norm_grid(work, threads));
+    int32_t cols;
+    while (scanf("%" SCNd64 " %" SCNd32 " %" SCNd64, &work, &cols, &threads) == 3)
+        printf("%" PRId64 "\n", ul::norm_grid(work, cols, threads));
     return 0;
 }

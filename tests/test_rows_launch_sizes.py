@@ -15,10 +15,11 @@ def test_norm_grids(tmp_path):
     exe = str(tmp_path / "sizes")
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2008_00325_amd", "csrc"),
                     os.path.join(ROOT, "tests", "native", "rows_launch_sizes.cpp"), "-o", exe], check=True, timeout=120)
-    asked = [(w, t) for w in (1, 3, 1000, 1023, 1024, 4096, 10**6, 2**24, 2**24 + 1, 2**31 - 1) for t in (64, 256, 320, 512, 1024)]
-    r = subprocess.run([exe], input="\n".join(f"{w} {t}" for w, t in asked), capture_output=True, text=True, timeout=60)
+    asked = [(w, c, t) for w in (1, 3, 1000, 1023, 1024, 4096, 10**6, 2**24, 2**24 + 1, 2**31 - 1) for t in (64, 256, 320, 512, 1024)
+             for c in (8, 512, 4096)]
+    r = subprocess.run([exe], input="\n".join(f"{w} {c} {t}" for w, c, t in asked), capture_output=True, text=True, timeout=60)
     grids = [int(x) for x in r.stdout.split()]
     assert r.returncode == 0 and len(grids) == len(asked)
-    for (w, t), g in zip(asked, grids):
+    for (w, _, t), g in zip(asked, grids):
         assert 1 <= g <= w and g * t < 2**32
         assert g >= min(w, 1024)
