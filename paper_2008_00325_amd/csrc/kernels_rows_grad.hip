@@ -8,9 +8,9 @@
 // Bound by memory: every row of dout is read once and every row of grad written once, by
 // waves that all have the same number of rows however often an id occurs; the sort (of 4-byte
 // keys and positions) and the joins are latency, launch by launch.  Sums are fp32, rounded
-// once.  us per call: 131,072 bf16 rows into fp32 128,000 x 2048 311 to 341 (1.59 GB, 253 us at a
-// copy's rate: sums and zeros 270 to 290, sort 31, joins 18), 8,192 into 32,000 x 1024 40 (0.15 GB, 24: sort
-// and zeros 25, sums 9, joins 5), 77 into 2,000 x 64 14 (three launches).
+// once.  us per call: 131,072 bf16 rows into fp32 128,000 x 2048 338 (1.58 GB, 251 us at a
+// copy's rate: sums and zeros 287, sort 32, joins 19), 8,192 into 32,000 x 1024 40 (0.15 GB, 24: sort
+// and zeros 27, sums 9, joins 6), 77 into 2,000 x 64 14 (three launches).
 #include <algorithm>
 
 #include "launch_sizes.hpp"
@@ -480,8 +480,11 @@ __global__ __launch_bounds__(kThreads) void k_chunk_sums(Sorted sorted, int slab
             }
         }
     };
-    // rows in flight while those before them are added
-    constexpr int kAhead = PARTS * VEC * sizeof(Elem<TD>) > 16 ? 4 : 8;
+    // rows in flight while those before them are added (us per call with 4 / 6 / 8 rows of 16-bit
+    // types: 131,072 x 2048 into 128,000 rows 351 / 346 / 341, 65,536 x 2048 135 / 127 / 123; with 8 / 16: 343 /
+    // 339, 32,768 x 4096 194 / 189, 300 columns 87 / 84; 70,000 x 784 fp32 with 4 / 8 120 / 117; more gives
+    // nothing)
+    constexpr int kAhead = PARTS * VEC * sizeof(Elem<TD>) > 16 ? 8 : 16;
     struct Row {
         Raw<TD, VEC> part[PARTS];
     };

@@ -12,9 +12,9 @@
 // All arithmetic is fp32; h, y and dx are rounded once, on the way out.
 //
 // us per call and TB/s of what is read and written, one copy reaching 6.3 TB/s: 32,768 x 4096
-// bf16, residual added, into bf16 h and int8 150 (6.3), gradient with upstream gradient and
-// dweight 169 (6.4), the join 5 more; 131,072 x 1024 bf16 without residual 83 (6.5); 70,000 x 784
-// fp32 into fp8 with a scale per 128 columns 56 (5.0).  Weaker: rows a little longer than a
+// bf16, residual added, into bf16 h and int8 152 (6.2), gradient with upstream gradient and
+// dweight 166 (6.5), the join 5 more; 131,072 x 1024 bf16 without residual 83 (6.5); 70,000 x 784
+// fp32 into fp8 with a scale per 128 columns 55 (5.0).  Weaker: rows a little longer than a
 // power of two vectors (300 columns into int8 5.0: 38 of 64 lanes have any), rows beyond
 // 16,384 columns, whose gradient spills registers (2.4).
 #include <algorithm>

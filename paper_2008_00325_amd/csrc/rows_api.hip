@@ -19,7 +19,11 @@ __attribute__((format(printf, 2, 3))) int fail(int code, const char *fmt, ...)
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    return ul::set_error(code, buf);
+    try {
+        return ul::set_error(code, buf);
+    } catch (...) {   // no memory for the message: the code alone
+        return code;
+    }
 }
 
 int launched(hipError_t e, const char *what)

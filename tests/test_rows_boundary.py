@@ -4,6 +4,8 @@ exported and bound, and every invalid argument is refused before any HIP call.""
 import ctypes
 import os
 import re
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -32,6 +34,21 @@ def test_struct_has_the_header_s_layout():
     assert ctypes.sizeof(R.umap_rows) == 48
     assert [R.umap_rows.data.offset, R.umap_rows.scales.offset, R.umap_rows.rows.offset, R.umap_rows.stride.offset,
             R.umap_rows.cols.offset, R.umap_rows.type.offset, R.umap_rows.group.offset] == [0, 8, 16, 24, 32, 36, 40]
+
+
+@pytest.mark.skipif(shutil.which("gcc") is None, reason="gcc not available")
+def test_header_is_plain_c(tmp_path):
+    src = tmp_path / "client.c"
+    src.write_text("""#include "umap_rows.h"
+_Static_assert(sizeof(umap_rows) == 48, "size");
+int main(void)
+{
+    umap_rows m = {0, 0, 0, 8, 8, UMAP_BF16, 0, 0};
+    return umap_rows_lookup(&m, 0, UMAP_I64, 1.0f, &m, 0) + (int)umap_rows_norm_grad_workspace(0, 8);
+}
+""")
+    subprocess.run(["gcc", "-std=c11", "-Wall", "-Wextra", "-Werror", "-pedantic", "-fsyntax-only", "-I", os.path.dirname(HEADER),
+                    str(src)], check=True, timeout=60)
 
 
 def rows(at, n=10, cols=16, type=R.UMAP_F32, stride=None, scales=None, group=0, reserved=0):
