@@ -630,21 +630,18 @@ struct SortPass {
     uint32_t *keys_out, *pos_out, *joins;
     hipStream_t s;
 
-    template <int ITEMS>
-    hipError_t run(bool summed) const
+    template <int ITEMS, bool SUMMED>
+    hipError_t run() const
     {
         const dim3 grid((unsigned)tiles), threads(kSortThreads);
         hipLaunchKernelGGL((k_digit_counts<ITEMS>), grid, threads, 0, s, from, n, shift, bits, counts, joins);
         if (hipError_t e = hipGetLastError()) return e;
-        if (summed) {
+        if constexpr (SUMMED) {
             hipLaunchKernelGGL(k_tile_sums, dim3(((1u << bits) + 63) / 64), dim3(64), 0, s, counts, (int64_t)tiles, 1 << bits);
             if (hipError_t e = hipGetLastError()) return e;
-            hipLaunchKernelGGL((k_file<ITEMS, true>), grid, threads, 0, s, from, pos, n, shift, bits, counts, tiles,
-                               keys_out, pos_out);
-        } else {
-            hipLaunchKernelGGL((k_file<ITEMS, false>), grid, threads, 0, s, from, pos, n, shift, bits, counts, tiles,
-                               keys_out, pos_out);
         }
+        hipLaunchKernelGGL((k_file<ITEMS, SUMMED>), grid, threads, 0, s, from, pos, n, shift, bits, counts, tiles,
+                           keys_out, pos_out);
         return hipGetLastError();
     }
 };
@@ -794,7 +791,7 @@ hipError_t launch_rows_lookup_grad(const umap_rows &dout, RowIds ids, float scal
         for (int pass = 0; n > 0 && pass < passes; ++pass) {
             const SortPass p{Keys{keys, ids, grad.rows}, pos, n, pass * bits, bits, counts, (int)sort.tiles,
                              buf[2 * (pass & 1)], buf[2 * (pass & 1) + 1], pass ? nullptr : join_count, s};
-            const hipError_t e = sort.items == 4 ? p.run<4>(sort.summed) : p.run<8>(sort.summed);
+            const hipError_t e = sort.items == 4 ? p.run<4, false>() : sort.summed ? p.run<8, true>() : p.run<8, false>();
             if (e != hipSuccess) return e;
             keys = p.keys_out;
             pos = p.pos_out;

@@ -106,6 +106,18 @@ def test_lookup_from_8_bits(dtype, group, dim):
         check_lookup(q, ids, 1.5, out, scales, group)
 
 
+@pytest.mark.parametrize("n,dim,dtype,out", [(300_000, 40, BF16, BF16), (300_001, 43, F16, F32), (21_000, 300, F32, F32),
+                                             (1000, 9001, BF16, BF16), (1100, 8195, BF16, F32)])
+def test_lookup_of_many_rows(n, dim, dtype, out):
+    check_lookup(rand(500, dim, dtype), torch.randint(-1, 501, (n,), device=DEV), 0.5, out)
+
+
+@pytest.mark.parametrize("n,dim,dtype,group", [(150_000, 72, I8, 32), (14_000, 650, F8, 128)])
+def test_lookup_of_many_rows_from_8_bits(n, dim, dtype, group):
+    q, scales = eight_bit(700, dim, dtype, group)
+    check_lookup(q, torch.randint(-1, 701, (n,), device=DEV), 1.0, BF16, scales, group)
+
+
 @pytest.mark.parametrize("kind", [torch.int32, torch.int64])
 def test_lookup_ids_outside_the_table_give_zeros(kind):
     ids = [0, -1, 9, 10, 3, -2**31, 2**31 - 1] + ([2**32, 2**32 + 1, -2**63, 2**63 - 1, -2**32] if kind == torch.int64 else [])
@@ -188,6 +200,11 @@ def test_grad_dims(dim, dtype, out):
 @pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 255, 1000, 4095, 4096, 4097, 8192, 16384, 16385, 20000, 70001])
 def test_grad_id_counts(n):
     check_grad(rand(n, 24, BF16), zipf(n, 1500, torch.int32), 1500)
+
+
+@pytest.mark.parametrize("n,rows,dim", [(131_073, 300, 40), (300_000, 70_000, 16), (1_048_577, 5000, 3), (1_200_000, 600_000, 2)])
+def test_grad_many_ids(n, rows, dim):
+    check_grad(rand(n, dim, BF16), zipf(n, rows, torch.int32), rows)
 
 
 @pytest.mark.parametrize("rows", [1, 2, 3, 255, 256, 511, 512, 513, 1000, 2**16, 2**18 - 1, 2**18, 2**18 + 1, 10**6])
@@ -358,6 +375,14 @@ def test_norm_strides_and_alignment(dtype, pad, shift):
 def test_norm_row_counts(n):
     check_norm(rand(n, 48, BF16), BF16, residual=rand(n, 48, BF16), want_h=True)
     check_norm(rand(n, 48, BF16), I8, residual=rand(n, 48, BF16), want_h=True, group=32)
+
+
+@pytest.mark.parametrize("n,dim", [(150_000, 20), (60_000, 100), (30_001, 200), (20_003, 300), (9001, 1000), (5000, 1040), (2500, 8200)])
+def test_norm_of_many_rows(n, dim):
+    r = rand(n, dim, BF16)
+    check_norm(rand(n, dim, BF16), BF16, rand(1, dim, BF16)[0], residual=r, want_h=True)
+    check_norm(rand(n, dim, F32), F32)
+    check_norm(rand(n, dim, BF16), I8, residual=r, alias=r, group=64)
 
 
 @pytest.mark.parametrize("dim", [7, 300, 2048, 9001])
