@@ -714,11 +714,15 @@ int64_t even_grid(int64_t work, int threads, int waves)
     const int64_t turns = (work + most - 1) / most;
     return (work + turns - 1) / turns;
 }
-// us per call on 256 MB of bf16 rows with upstream gradient and dweight at 8 / 12 / 16 / 20
-// waves on a CU: 64 columns 167 / 177 / 192 / 206, 300 350 / 272 / 250 / 239, 784 204 / 209 / 230 / 210, 1,024
-// 198 / 195 / 207 / 206, 2,048 226 / 186 / 191 / 202, 4,096 207 / 207 / 180 / 180, 8,192 and more the same (one
-// workgroup).
-constexpr int grad_waves(int lanes, int vec) { return lanes == 64 && vec == 2 ? 8 : 16; }
+// us per call with upstream gradient and dweight at 8 / 12 / 16 / 20 waves on a CU: 256 MB of bf16
+// rows of 300 columns 350 / 272 / 250 / 239, 784 204 / 209 / 230 / 210, 1,024 198 / 195 / 207 / 206, 2,048 226 / 186 / 191 /
+// 202, 4,096 207 / 207 / 180 / 180, 8,192 and more the same (one workgroup); 128 MB, three sets in turn, at
+// 8 / 12 / 16: 16 columns 217 / 176 / 158, 32 123 / 106 / 100, 64 89 / 97 / 97, 128 88 / 97 / 97, 256 89 / 94 / 98, fp32 196 /
+// 210 / 209 at each of the last three.
+constexpr int grad_waves(int lanes, int vec)
+{
+    return (lanes == 64 && vec == 2) || lanes == 16 || lanes == 32 ? 8 : 16;
+}
 
 template <int TX, int TY>
 struct Norm {
