@@ -121,8 +121,9 @@ int64_t umap_rows_lookup_grad_workspace(int64_t n, int64_t rows, int32_t cols);
  *   eps       finite, >= 0 (a row of zeros with eps = 0 gives NaN).
  *   y         UMAP_F32, UMAP_F16 or UMAP_BF16, or UMAP_I8 / UMAP_F8 with scales, which
  *             are written too: of each group of columns the scale is the largest
- *             |y| / 127 (UMAP_I8) or / 448 (UMAP_F8), and the values are y / scale
- *             rounded to nearest even.  A group whose largest |y| is below 2^-100
+ *             |y| / 127 (UMAP_I8) or / 448 (UMAP_F8), and the values are y / scale,
+ *             both quotients formed in fp32 to nearest even, the values then rounded
+ *             likewise.  A group whose largest |y| is below 2^-100
  *             is stored as zeros with scale 0, one that holds a NaN or an
  *             infinity as zeros with scale NaN (it reads back as NaN).
  *

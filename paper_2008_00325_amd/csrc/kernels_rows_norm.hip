@@ -215,28 +215,39 @@ __device__ __forceinline__ float product_sum(const float e[V], const float g[V],
     return c.live() ? sum : 0.0f;
 }
 
-// The scale of a group whose largest magnitude has these bits, and the factor that
-// its values take to become 8-bit ones.
+// The scale of a group whose largest magnitude has these bits, and its values divided by it.
+// All quotients are fp32's, to nearest even, by Markstein's method: from a reciprocal that is
+// itself rounded to nearest, q = v / s with one correction by the exact remainder v - q s.  The
+// scale lies between 2^-109 and 2^121, so that its reciprocal is an ordinary number (a largest
+// magnitude beyond 2^126 has a subnormal one, which the hardware takes for 0).
 template <int TY>
 struct Quant {
     static constexpr float kMost = TY == UMAP_I8 ? 127.0f : 448.0f;
     bool fine;
     float scale, up;
+    static __device__ __forceinline__ float quotient(float v, float s, float over_s)
+    {
+        const float q = v * over_s;
+        return fmaf(fmaf(-q, s, v), over_s, q);
+    }
     __device__ __forceinline__ explicit Quant(uint32_t bits)
     {
         const float m = __uint_as_float(bits);
         fine = bits >= __float_as_uint(0x1p-100f) && bits < 0x7f800000u;
-        scale = fine ? m * (1.0f / kMost) : bits < 0x7f800000u ? 0.0f : __builtin_nanf("");
-        up = fine ? kMost * __builtin_amdgcn_rcpf(m) : 0.0f;
+        scale = fine ? quotient(m, kMost, 1.0f / kMost) : bits < 0x7f800000u ? 0.0f : __builtin_nanf("");
+        const float near = __builtin_amdgcn_rcpf(scale);   // within a unit of its last place
+        up = fmaf(fmaf(-near, scale, 1.0f), near, near);
     }
+    // A value in its 8-bit type's range; what a group that is not fine holds is for the caller to drop.
+    __device__ __forceinline__ float of(float v) const { return quotient(v, scale, up); }
     __device__ __forceinline__ float operator()(float v) const
     {
-        if constexpr (TY == UMAP_I8) return fine ? fminf(fmaxf(rintf(v * up), -kMost), kMost) : 0.0f;
-        else return fine ? fminf(fmaxf(v * up, -kMost), kMost) : 0.0f;
+        if constexpr (TY == UMAP_I8) return fine ? rintf(of(v)) : 0.0f;
+        else return fine ? of(v) : 0.0f;
     }
     // 8 of them.  UMAP_I8: adding 1.5 2^23 leaves the nearest whole number in the sum's low
-    // bits, with one rounding of the exact product; |v up| exceeds 127 by at most a few units
-    // of its last place, which rounds to 127.  UMAP_F8: likewise 448.
+    // bits.  The group's largest value is at most a unit of its last place above 127 or 448 and
+    // rounds to it.
     __device__ __forceinline__ Raw<TY, 8> pack(const float v[8]) const
     {
         Raw<TY, 8> r;
@@ -245,14 +256,14 @@ struct Quant {
             for (int i = 0; i < 2; ++i) {
                 uint32_t b[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(fmaf(v[4 * i + j], up, 0x1.8p23f));
+                for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(of(v[4 * i + j]) + 0x1.8p23f);
                 const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0c);
                 r.w[i] = lo | hi;
             }
         } else {
             float s[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = v[j] * up;
+            for (int j = 0; j < 8; ++j) s[j] = of(v[j]);
             r = raw_of<TY, 8>(s);
         }
 #pragma unroll
