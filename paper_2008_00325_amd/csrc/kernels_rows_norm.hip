@@ -121,12 +121,15 @@ struct RowThreads {
 
 // Whether a sum of squares lost its value to fp32's range: too large, or so small that
 // squares vanished and eps does not outweigh them.  Then the row is taken times
-// range_step(sum), a power of two.
+// range_step(sum), a power of two.  The smallest rows, one subnormal value of 2^-149 in 32,768
+// columns, so get a mean square of 2^-125, still an ordinary number, as the hardware's root needs
+// it; the largest of those below 2^-62, sum or eps, one of 2^126.
+constexpr float kSmallSum = 0x1p-62f;
 __device__ __forceinline__ bool out_of_range(float sum, float eps)
 {
-    return !(sum < __builtin_inff()) || (sum < 0x1p-60f && eps < 0x1p-60f);
+    return !(sum < __builtin_inff()) || (sum < kSmallSum && eps < kSmallSum);
 }
-__device__ __forceinline__ float range_step(float sum) { return sum < 1.0f ? 0x1p80f : 0x1p-80f; }
+__device__ __forceinline__ float range_step(float sum) { return sum < 1.0f ? 0x1p94f : 0x1p-80f; }
 
 // Vector i of a thread: columns c = V (thread + i TPR) .. c + V - 1.  Where the row ends inside
 // it, the vector is taken from column cols - V on instead, and its first `dup` columns
@@ -482,9 +485,10 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
 #pragma unroll
                 for (int j = 0; j < Raw<TX, V>::kUnits; ++j) asm volatile("" : "+v"(ha[i].w[j]), "+v"(db[i].w[j]));
         }
-        // of the row times k: unit = h k rho, dx = k rho (g - unit (dot rho / cols))
+        // of the row times k: unit = h k rho, dx = k (rho (g - unit (dot rho / cols))), in this order:
+        // k rho may be beyond fp32's range where dx is not
         const float rho = __builtin_amdgcn_rsqf(fmaf(sum, over_cols, add));
-        const float along = dot * rho * over_cols, out = k * rho;
+        const float along = dot * rho * over_cols;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const Cols<V> c(V * (me + i * TPR), cols);
@@ -497,7 +501,7 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_norm_grad(umap_row
                 const float unit = e[j] * k * rho;
                 if constexpr (kInLds) dw_at(i, j) = fmaf(g[j], unit, dw_at(i, j));
                 else if constexpr (DW) dw[i][j] = fmaf(g[j], unit, dw[i][j]);
-                r[j] = out * (g[j] * w[MORE ? i : 0][j] - unit * along);
+                r[j] = k * (rho * (g[j] * w[MORE ? i : 0][j] - unit * along));
             }
             if (dh.data) {
                 floats_of<TX, V>(ua[i], e);
@@ -655,7 +659,7 @@ __global__ __launch_bounds__(256) void k_rows_norm_grad_narrow(umap_rows dy, uma
 #pragma unroll
         for (int c = 0; c < kNarrow; ++c) {
             if (c >= cols) continue;
-            float r = k * rho * (g[c] - e[c] * along);
+            float r = k * (rho * (g[c] - e[c] * along));
             if (dh.data) r += elem_float<TX>(row_ptr<TX>(dh, t)[c]);
             row_out<TX>(dx, t)[c] = float_elem<TX>(r);
         }

@@ -6,7 +6,7 @@ import torch
 
 import rows_reference as ref
 from paper_2008_00325_amd import umap_rows as R
-from test_gpu_rows import BF16, DEV, F8, I8, check_norm
+from test_gpu_rows import BF16, DEV, F8, F32, I8, check_norm, near, norm_grad
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,48 @@ def test_8_bit_values_are_the_nearest_to_their_quotients(out, group, dim):
         value = w / want.repeat_interleave(g)[:dim]
         value = value.round() if out == I8 else value.clamp(-top, top).to(F8).float()
         assert torch.equal(q.cpu().float(), value.expand(3, dim))
+
+
+def smallest(n, dim, size):
+    """fp32 rows of up to 7 times `size` (a power of two, from the smallest subnormal on), one of them with a single value."""
+    x = (torch.randint(-7, 8, (n, dim)).float() * size)
+    x[:, 0] = size
+    x[-1, 1:] = 0
+    return x.to(DEV)
+
+
+@pytest.mark.parametrize("dim", [1, 5, 9, 64, 300, 1000, 2048, 9001, 20001, 32768])
+@pytest.mark.parametrize("eps", [0.0, 1e-44])
+def test_norm_of_the_smallest_rows(dim, eps):
+    """Finite rows have finite norms, from the smallest subnormal value on."""
+    torch.manual_seed(dim)
+    eps = float(torch.tensor(eps))   # as the call takes it
+    for power in (-149, -146, -143, -140, -130, -110, -40, -31, -30):
+        x = smallest(4, dim, 2.0**power)
+        check_norm(x, F32, eps=eps)
+        check_norm(x, F32, residual=x, eps=eps)
+        check_norm(x, I8, eps=eps)
+
+
+@pytest.mark.parametrize("dim", [5, 9, 64, 300, 1000, 2048, 9001, 20001, 32768])
+def test_norm_grad_of_the_smallest_rows(dim):
+    """dx is right wherever it is within fp32's range, 1 / norm within it or not."""
+    torch.manual_seed(dim)
+    for power in (-149, -146, -143, -140, -130, -110, -40, -31, -30):
+        h = smallest(4, dim, 2.0**power)
+        dy, w = torch.randn(4, dim, device=DEV) * 2.0**-40, 1 + 0.2 * torch.randn(dim, device=DEV)
+        dx, dw = norm_grad(dy, h, w, eps=0.0)
+        dx64, size, dw64, dw_size = ref.norm_grad(ref.values(dy), ref.values(h), ref.values(w[None])[0], 0.0)
+        steps = (-(-dim // 64) + 40) * ref.E32
+        near(dx, dx64, steps * size)
+        near(dw[None], dw64[None], (12 * ref.E32 + steps) * dw_size[None])
+
+
+@pytest.mark.parametrize("dim", [5, 300, 9001])
+def test_norm_grad_of_the_largest_rows(dim):
+    torch.manual_seed(dim)
+    h = signs(4, dim) * (1 + 0.9 * torch.rand(4, dim, device=DEV)) * 2.0**127
+    dy = torch.randn(4, dim, device=DEV) * 2.0**40
+    dx, _ = norm_grad(dy, h)
+    dx64, size, _, _ = ref.norm_grad(ref.values(dy), ref.values(h), None, 1e-6)
+    near(dx, dx64, (-(-dim // 64) + 40) * ref.E32 * size + 2.0**-149)
