@@ -140,13 +140,17 @@ int umap_rows_norm(const umap_rows *x, const void *ids, int32_t id_type, float s
  * rho = 1 / sqrt(mean_c h^2 + eps) and g = dy * weight:
  *   dx[t]   = rho g - h rho^3 mean_c(g h) + dh[t]
  *   dweight = sum_t dy[t] * h[t] * rho
- * (x's, the residual's and h's gradient are the same), in fp32, rounded once.
+ * in fp32, rounded once.  dx is the gradient of h, which is also the residual's.
+ * That of umap_rows_norm's x is scale * dx: dx itself where scale is 1, else what
+ * umap_rows_lookup(dx, NULL, .., scale) gives or, where x was gathered,
+ * umap_rows_lookup_grad with that scale.
  *
  *   dy, h    UMAP_F32, UMAP_F16 or UMAP_BF16, of one type, cols 1 .. 32768,
  *            rows < 2^31.
  *   dh       NULL, or the gradient that reaches h by other ways (the same type).
  *   weight   as for umap_rows_norm.
- *   dx       the same type; it may be dy or dh itself (the same data and stride).
+ *   dx       the same type; receives the gradient of h.  It may be dy or dh itself
+ *            (the same data and stride).
  *   dweight  NULL, or cols fp32, overwritten; rows are added in a fixed order.
  *   workspace  NULL when dweight is NULL, else workspace_bytes >=
  *            umap_rows_norm_grad_workspace(rows, cols) bytes of device memory,

@@ -194,7 +194,9 @@ def umap_rows_norm_grad_workspace(n: int, cols: int) -> int:
 def umap_rows_norm_grad(dy, h, dx, weight=None, dh=None, dweight=None, workspace=None, eps: float = 1e-6,
                         stream=None) -> None:
     """Gradient of y = h / sqrt(mean h^2 + eps) * weight for h (plus `dh`, what reaches h otherwise), into dx (which
-    may be dy or dh itself), and for the weight, into dweight (fp32; needs the workspace)."""
+    may be dy or dh itself), and for the weight, into dweight (fp32; needs the workspace).
+
+    dx is the residual's gradient too; x's is dx times umap_rows_norm's scale."""
     Y, _, cols = _rows(dy, "dy", _FLOAT)
     H, _, _ = _rows(h, "h", _FLOAT)
     X, _, _ = _rows(dx, "dx", _FLOAT)
