@@ -5,8 +5,8 @@ two-dimensional torch tensors on the GPU whose columns lie next to each other (r
 apart: views of a wider tensor are taken as they are); scales, ids and workspaces are
 contiguous tensors.  Streams are ``torch.cuda.Stream`` objects, raw ``hipStream_t`` integers or
 None (null stream); tensors that were made on another stream are for the caller to order and to
-keep alive.  The calls do not block.  A tensor of another type, shape or device raises ValueError,
-whatever the library refuses :class:`UmapLayoutError`.
+keep alive.  The calls do not block.  A tensor of another type or shape, or on another GPU than the
+current one, raises ValueError, whatever the library refuses :class:`UmapLayoutError`.
 """
 
 from __future__ import annotations
@@ -49,6 +49,7 @@ class umap_rows(ctypes.Structure):
 
 _lib = None
 _call: dict = {}   # the library's functions, taking packed umap_rows
+_only = -2         # the GPU's number where the process sees just one: tensors on it are in place
 _pack = struct.Struct("@PPqqiiii").pack
 
 
@@ -77,13 +78,26 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+def _place(x, name: str) -> None:
+    """A tensor has to lie on the current GPU, which is where the kernels run."""
+    global _only
+    at = x.get_device()
+    if at < 0:
+        raise ValueError(f"{name} must be a GPU tensor, got one on {x.device}")
+    here = torch.cuda.current_device()
+    if at != here:
+        raise ValueError(f"{name} lies on GPU {at}, the current one is {here}")
+    if torch.cuda.device_count() == 1:
+        _only = at
+
+
 def _rows(x, name: str, types: dict, scales=None, group: int = 0) -> tuple:
     """A matrix as a packed umap_rows, its rows and its columns."""
     kind = types.get(x.dtype)
     if kind is None:
         raise ValueError(f"{name} must not hold {x.dtype}")
-    if not x.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor, got one on {x.device}")
+    if x.get_device() != _only:
+        _place(x, name)
     if x.dim() != 2:
         raise ValueError(f"{name} must be two-dimensional")
     rows, cols = x.shape
@@ -100,8 +114,8 @@ def _flat(x, name: str, dtype, count: int) -> int:
     """Address of a contiguous GPU tensor of `count` elements at least (`dtype` None: any type)."""
     if dtype is not None and x.dtype != dtype:
         raise ValueError(f"{name} must hold {dtype}, got {x.dtype}")
-    if not x.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor, got one on {x.device}")
+    if x.get_device() != _only:
+        _place(x, name)
     if not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if x.numel() < count:
