@@ -7,6 +7,9 @@ contiguous tensors.  Streams are ``torch.cuda.Stream`` objects, raw ``hipStream_
 None (null stream); tensors that were made on another stream are for the caller to order and to
 keep alive.  The calls do not block.  A tensor of another type or shape, or on another GPU than the
 current one, raises ValueError, whatever the library refuses :class:`UmapLayoutError`.
+
+Autograd does not record the calls (the gradients are calls of their own).  What they write counts
+as changed in place: a backward pass that needs the values from before raises an error.
 """
 
 from __future__ import annotations
@@ -15,6 +18,7 @@ import ctypes
 import struct
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .umap_layout import UmapLayoutError, _check, _stream, lib as _layout_lib
 
@@ -166,6 +170,7 @@ def umap_rows_lookup(table, ids, out, scale: float = 1.0, table_scales=None, gro
     at, kind = _id_args(ids, n)
     lib()
     _check(_call["umap_rows_lookup"](t, at, kind, scale, o, _stream(stream)))
+    increment_version(out)
 
 
 def umap_rows_lookup_grad_workspace(n: int, rows: int, cols: int) -> int:
@@ -182,6 +187,7 @@ def umap_rows_lookup_grad(dout, ids, grad, workspace, scale: float = 1.0, accumu
     work, size = _work(workspace)
     lib()
     _check(_call["umap_rows_lookup_grad"](d, at, kind, scale, g, 1 if accumulate else 0, work, size, _stream(stream)))
+    increment_version(grad)
 
 
 def umap_rows_norm(x, y, weight=None, residual=None, h=None, ids=None, scale: float = 1.0, y_scales=None,
@@ -198,6 +204,7 @@ def umap_rows_norm(x, y, weight=None, residual=None, h=None, ids=None, scale: fl
     w, w_kind = _weight_args(weight, cols)
     lib()
     _check(_call["umap_rows_norm"](X, at, kind, scale, R, H, w, w_kind, eps, Y, _stream(stream)))
+    increment_version([x for x in (y, y_scales, h) if x is not None])
 
 
 def umap_rows_norm_grad_workspace(n: int, cols: int) -> int:
@@ -220,6 +227,7 @@ def umap_rows_norm_grad(dy, h, dx, weight=None, dh=None, dweight=None, workspace
     work, size = _work(workspace)
     lib()
     _check(_call["umap_rows_norm_grad"](Y, H, U, w, w_kind, eps, X, dw, work, size, _stream(stream)))
+    increment_version(dx if dweight is None else (dx, dweight))
 
 
 __all__ = [*EXPORTS, "UmapLayoutError", "umap_rows"]
