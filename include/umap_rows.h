@@ -83,7 +83,7 @@ int umap_rows_lookup(const umap_rows *table, const void *ids, int32_t id_type, f
  *   dout       UMAP_F32, UMAP_F16 or UMAP_BF16, one row per id, cols 1 .. 2^20,
  *              rows < 2^31.  Rows whose id is outside [0, grad->rows) take no
  *              part (nothing of them is read: they may hold NaN).
- *   grad       UMAP_F32, UMAP_F16 or UMAP_BF16, rows < 2^31.
+ *   grad       UMAP_F32, UMAP_F16 or UMAP_BF16, rows < 2^31 - 1.
  *   accumulate 0: every row of grad is written, zeros where no id points.
  *              1: the sums are added to grad (in fp32, rounded once); rows without
  *              an id are neither read nor written.  With scale = -step this is an
@@ -119,12 +119,12 @@ int64_t umap_rows_lookup_grad_workspace(int64_t n, int64_t rows, int32_t cols);
  *   weight    cols values of type weight_type (UMAP_F32, UMAP_F16 or UMAP_BF16),
  *             or NULL for ones.
  *   eps       finite, >= 0 (a row of zeros with eps = 0 gives NaN).
- *   y         UMAP_F32, UMAP_F16 or UMAP_BF16, or UMAP_I8 / UMAP_F8 with scales, which
- *             are written too: of each group of columns the scale is the largest
- *             |y| / 127 (UMAP_I8) or / 448 (UMAP_F8), and the values are y / scale,
- *             both quotients formed in fp32 to nearest even, the values then rounded
- *             likewise.  A group whose largest |y| is below 2^-100
- *             is stored as zeros with scale 0, one that holds a NaN or an
+ *   y         rows < 2^31 of UMAP_F32, UMAP_F16 or UMAP_BF16, or of UMAP_I8 / UMAP_F8
+ *             with scales, which are written too: of each group of columns the scale
+ *             is the largest |y| / 127 (UMAP_I8) or / 448 (UMAP_F8), and the values
+ *             are y / scale, both quotients formed in fp32 to nearest even, the
+ *             values then rounded likewise.  A group whose largest |y| is below
+ *             2^-100 is stored as zeros with scale 0, one that holds a NaN or an
  *             infinity as zeros with scale NaN (it reads back as NaN).
  *
  * Sums of squares beyond fp32's range are formed again from scaled values, so
