@@ -600,22 +600,22 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join_parts(Sorted sorted, f
     }
 }
 
-// Tiles of 4,096 keys up to 32 of them, then of 8,192; the workgroups add up to 128 tiles'
-// counts themselves, beyond that a launch of its own does.  us per call with 16,384 keys and 64
-// tiles / 8,192 and 64 / 8,192 and 128 / 4,096 and 64: 300,000 rows of 64 columns 114 / 84 / 82 / 80, a
-// million of 256 222 / 208 / 201 / 209, four million of 16 737 / 748 / 752 / 812.  Up to 8,192
-// keys are sorted in one launch (1,000 rows 64 / 37 us with the other launches of a call,
-// 8,192 83 / 58).
+// Up to 8,192 keys are sorted in one launch; us per call so / by tiles in four: 5,000 of 64 columns added
+// to a table 24 / 33, 8,192 28 / 36, but with 16 keys per thread 16,384 45 / 39.  Then tiles of 4,096
+// keys, whose workgroups add up the tiles' counts themselves, up to 256 tiles; beyond that tiles of
+// 8,192, with a launch for the sums.  4,096 / 8,192 keys, 64 columns: 10,000 ids 36 / 47, 65,536 49 / 64,
+// 131,072 61 / 76, 262,144 67 / 80, 524,288 94 / 103, 1,048,576 150 / 153; 700,000 of 16 columns into
+// 300,000 rows 160 / 166; four million of 16 (4,096 with a launch for the sums) 812 / 752.
 struct SortPlan {
     int items;   // per thread
     int64_t tiles;
     bool summed;
     explicit SortPlan(int64_t n)
     {
-        items = n <= 32 * 4096 ? 4 : 8;
+        summed = n > 256 * 4096;
+        items = summed ? 8 : 4;
         if (few(n)) items = n <= 1024 ? 1 : n <= 4096 ? 4 : 8;
         tiles = (n + kSortThreads * items - 1) / (kSortThreads * items);
-        summed = tiles > 128;
     }
     static bool few(int64_t n) { return n <= 8192; }
 };
@@ -791,7 +791,7 @@ hipError_t launch_rows_lookup_grad(const umap_rows &dout, RowIds ids, float scal
         for (int pass = 0; n > 0 && pass < passes; ++pass) {
             const SortPass p{Keys{keys, ids, grad.rows}, pos, n, pass * bits, bits, counts, (int)sort.tiles,
                              buf[2 * (pass & 1)], buf[2 * (pass & 1) + 1], pass ? nullptr : join_count, s};
-            const hipError_t e = sort.items == 4 ? p.run<4, false>() : sort.summed ? p.run<8, true>() : p.run<8, false>();
+            const hipError_t e = sort.summed ? p.run<8, true>() : p.run<4, false>();
             if (e != hipSuccess) return e;
             keys = p.keys_out;
             pos = p.pos_out;
