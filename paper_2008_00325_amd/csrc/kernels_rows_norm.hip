@@ -732,11 +732,13 @@ int64_t even_grid(int64_t work, int threads, int waves)
 // us per call with upstream gradient and dweight at 8 / 12 / 16 / 20 waves on a CU: 256 MB of bf16
 // rows of 300 columns 350 / 272 / 250 / 239, 784 204 / 209 / 230 / 210, 1,024 198 / 195 / 207 / 206, 2,048 226 / 186 / 191 /
 // 202, 4,096 207 / 207 / 180 / 180, 8,192 and more the same (one workgroup); 128 MB, three sets in turn, at
-// 8 / 12 / 16: 16 columns 217 / 176 / 158, 32 123 / 106 / 100, 64 89 / 97 / 97, 128 88 / 97 / 97, 256 89 / 94 / 98, fp32 196 /
-// 210 / 209 at each of the last three.
-constexpr int grad_waves(int lanes, int vec)
+// 8 / 12 / 16: 128 columns 88 / 97 / 97, 256 89 / 94 / 98, fp32 196 / 210 / 209 at both.  Lanes in eights, which short
+// rows leave partly idle, at 8 / 16: bf16 16 columns 216 / 160, 32 125 / 100, 40 110 / 95, 48 99 / 97, 56 92 / 95, 64 88 / 96;
+// fp32, which the same bound costs 7 % from 32 to 48 columns, 16 312 / 233, 24 233 / 213, 32 200 / 215, 48 198 / 214, 64 197 /
+// 210.
+constexpr int grad_waves(int lanes, int vec, int cols)
 {
-    return (lanes == 64 && vec == 2) || lanes == 16 || lanes == 32 ? 8 : 16;
+    return (lanes == 64 && vec == 2) || lanes == 16 || lanes == 32 || (lanes == 8 && cols > 48) ? 8 : 16;
 }
 
 template <int TX, int TY>
@@ -761,9 +763,9 @@ struct Norm {
 
 template <int LANES, int VEC>
 struct GradBlocks {
-    static int64_t go(RowShape shape, int64_t n)
+    static int64_t go(RowShape shape, int64_t n, int cols)
     {
-        return even_grid((n + shape.rows - 1) / shape.rows, shape.threads, grad_waves(LANES, VEC));
+        return even_grid((n + shape.rows - 1) / shape.rows, shape.threads, grad_waves(LANES, VEC, cols));
     }
 };
 constexpr int kGradOne = 8192, kNormOne = 4096;   // columns up to which one vector per thread measured best
@@ -776,7 +778,7 @@ struct Grad {
                              RowWeight weight, float eps, const umap_rows *dx, float *partial, int64_t *count, hipStream_t s)
         {
             const int64_t work = (dy->rows + shape.rows - 1) / shape.rows;
-            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows) : norm_grid(work, dy->cols, shape.threads);
+            *count = partial || VEC == 4 ? GradBlocks<LANES, VEC>::go(shape, dy->rows, dy->cols) : norm_grid(work, dy->cols, shape.threads);
             const dim3 grid((unsigned)*count), threads(shape.threads);
             const size_t sums = LANES == kBlock && VEC > 1 ? (size_t)shape.threads * VEC * 32 : 0;
             const umap_rows up = dh ? *dh : umap_rows{};
@@ -820,7 +822,7 @@ hipError_t launch_rows_norm(const umap_rows &x, RowIds ids, float scale, const u
 int64_t rows_norm_grad_bytes(int64_t n, int32_t cols)
 {
     if (n < 1) return 16;
-    return by_cols<GradBlocks>(cols, kGradOne, n) * cols * 4;   // one sum of dweight per workgroup
+    return by_cols<GradBlocks>(cols, kGradOne, n, cols) * cols * 4;   // one sum of dweight per workgroup
 }
 
 hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const umap_rows *dh, RowWeight weight,
@@ -828,7 +830,7 @@ hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const 
 {
     int64_t count = 0;
     // one workgroup's sums are dweight itself
-    const bool one = dweight && dy.rows > 0 && by_cols<GradBlocks>(dy.cols, kGradOne, dy.rows) == 1;
+    const bool one = dweight && dy.rows > 0 && by_cols<GradBlocks>(dy.cols, kGradOne, dy.rows, dy.cols) == 1;
     float *const partial = one ? dweight : dweight ? static_cast<float *>(workspace) : nullptr;
     if (dy.rows > 0) {
         hipError_t e;
