@@ -12,11 +12,13 @@
 // All arithmetic is fp32; h, y and dx are rounded once, on the way out.
 //
 // us per call and TB/s of what is read and written, one copy reaching 6.3 TB/s: 32,768 x 4096
-// bf16, residual added, into bf16 h and int8 152 (6.2), gradient with upstream gradient and
-// dweight 166 (6.5), the join 5 more; 131,072 x 1024 bf16 without residual 83 (6.5); 70,000 x 784
-// fp32 into fp8 with a scale per 128 columns 55 (5.0).  Weaker: rows a little longer than a
-// power of two vectors (300 columns into int8 5.0: 38 of 64 lanes have any), rows beyond
-// 16,384 columns, whose gradient spills registers (2.4).
+// bf16, residual added, into bf16 h and int8 156 (6.0), gradient with upstream gradient and
+// dweight 167 (6.5), the join 5 more; 131,072 x 1024 bf16 without residual 85 (6.3); 70,000 x 784
+// fp32 into fp8 with a scale per 128 columns 57 (4.9).  Weaker: rows a little longer than a
+// power of two vectors (300 columns into int8 4.7: 38 of 64 lanes have any), and rows that a
+// workgroup's registers, 128 per thread, do not hold, part of which goes through scratch memory: all beyond
+// 16,384 columns (norm 4.0 to 4.9, gradient 3.2 to 3.8, with dweight 2.0 to 2.5) and gradients from 8,193
+// columns on (bf16 with dweight 4.3 to 5.0, fp32 4.5 to 4.7, with dweight 2.1 to 2.7).
 #include <algorithm>
 
 #include "launch_sizes.hpp"

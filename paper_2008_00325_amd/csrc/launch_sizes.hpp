@@ -78,10 +78,10 @@ constexpr bool halo_pays(int64_t near, int64_t kept, int64_t n, int32_t dim)
 // Workgroups for `work` of them, which take two (up to 512 columns four) times as many rows as
 // they hold in turn: few, so that workgroups end and start all the time and the card stays
 // evenly loaded, but enough to read ahead.  us per call with 1 / 2 / 3 / 4 turns, three sets of
-// inputs in turn: 32,768 x 4096 bf16 with residual into bf16 171 / 175 / 182 / 184, into int8 and
-// read back 215 / 209 / 213 / 216, 131,072 x 1024 172 / 175 / 183 / 184, 16,384 x 8192 without residual 91 / 86 /
-// 87 / 88, 70,000 x 784 fp32 into fp8 and back 87 / 81 / 81 / 82, 200,000 x 300 fp32 into int8 and back
-// 125 / 107 / 102 / 100.  Less where that would leave fewer than four workgroups for each CU, more
+// inputs in turn: 32,768 x 4096 bf16 with residual into bf16 173 / 174 / 183 / 183, into int8 and
+// read back 229 / 219 / 218 / 219, 131,072 x 1024 173 / 176 / 185 / 185, 16,384 x 8192 without residual 94 / 87 /
+// 88 / 88, 70,000 x 784 fp32 into fp8 and back 94 / 86 / 85 / 85, 200,000 x 300 fp32 into int8 and back
+// 135 / 119 / 114 / 112.  Less where that would leave fewer than four workgroups for each CU, more
 // where the grid would not fit a launch.
 constexpr int64_t norm_grid(int64_t work, int32_t cols, int64_t threads)
 {

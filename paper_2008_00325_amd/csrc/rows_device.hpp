@@ -87,11 +87,13 @@ __device__ __forceinline__ void store_raw(Elem<T> *p, const Raw<T, V> &r)
 
 // Likewise, for what is not needed again before much else has gone by: the caches give it up
 // first, which leaves them to the rows that are (a table's frequent ones, what the next kernel
-// reads).  us per call, plain / so: 32,768 x 4096 bf16 looked up 78 / 72, 70,000 x 300 into fp32 30 /
-// 19, norm of 32,768 x 4096 into int8 and back 239 / 210, its gradient 191 / 170, gradient of 131,072 x
-// 2048 355 / 311 (its loads alone; with its stores as well 335).  A lookup, norm and gradient
-// one after the other on the same 34 to 67 MB, which the caches would hold, lose: 78.6 / 80.3;
-// 134 MB gain: 170 / 149.  Only 16-byte accesses gain (8-bit rows written so: 209 / 220).
+// reads).  us per call, plain / so: 32,768 x 4096 bf16 looked up 82 / 75, 70,000 x 300 into fp32 30 /
+// 20, norm of 32,768 x 4096 into int8 and back 244 / 219, its gradient 194 / 173, gradient of 131,072 x
+// 2048 359 / 341.  A lookup, norm and gradient one after the other on the same rows: 8 MB of them
+// 14.9 / 13.3, 34 MB 42.8 / 45.2, 67 MB 79.7 / 81.2 (the caches would hold those), 134 MB 168 / 150.  Stores gain by
+// 16 bytes only (8-bit rows, written by 8: 209 / 220), loads by 8 too.  Vectors of 32 bytes, fp32's 8 columns,
+// go plainly: as two of 16 they lose (70,000 x 784 into fp8 55 / 59, gradient of 200,000 x 300 152 /
+// 177, of 65,536 x 1024 149 / 160; of 16,384 x 4096 155 / 153).
 template <int T, int V>
 __device__ __forceinline__ void store_once(Elem<T> *p, const Raw<T, V> &r)
 {
