@@ -66,15 +66,16 @@ Span scale_span(const umap_rows &m)
 }
 Span flat(const void *p, int64_t bytes) { return {(uintptr_t)p, p && bytes > 0 ? 1 : 0, bytes, 0}; }
 
-// Whether two arrays share a byte.  Columns of one wider buffer (the same pitch)
-// do not, though their address ranges interleave.
+// Whether two arrays share a byte.  Columns of one wider buffer (the same pitch, or a
+// single row among the other's) do not, though their address ranges interleave.
 bool overlap(const Span &a, const Span &b)
 {
     if (a.rows < 1 || b.rows < 1 || a.end() <= b.at || b.end() <= a.at) return false;
-    if (a.rows > 1 && b.rows > 1 && a.pitch == b.pitch && a.pitch > 0) {
+    const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if ((a.rows > 1 || b.rows > 1) && (b.rows == 1 || b.pitch == pitch) && pitch > 0) {
         const Span &lo = a.at <= b.at ? a : b, &hi = a.at <= b.at ? b : a;
-        const int64_t off = (int64_t)((hi.at - lo.at) % (uintptr_t)lo.pitch);
-        return !(off >= lo.width && off + hi.width <= lo.pitch);
+        const int64_t off = (int64_t)((hi.at - lo.at) % (uintptr_t)pitch);
+        return !(off >= lo.width && off + hi.width <= pitch);
     }
     return true;
 }
