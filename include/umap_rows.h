@@ -2,7 +2,10 @@
  * umap_rows.h -- C ABI of the token-row operators of libumap_layout.so: rows of
  * a learned table by id (with scaling) and the gradient of that by sorted ids,
  * and the root-mean-square norm of rows, with a residual's addition, into a
- * float type or into 8 bits with scales, and its gradient.
+ * float type or into 8 bits with scales, and its gradient; the mean and variance
+ * norm and its gradient; and the head over a table of tokens, as a loss (softmax
+ * cross entropy, or the divergence from a teacher's largest logits) and its
+ * gradient, without the logits ever being kept.
  *
  * They stand in front of the layout: a table of word or token vectors is
  * trained, its rows are read by id, normalised (Euclidean distances of
@@ -165,6 +168,110 @@ int umap_rows_norm_grad(const umap_rows *dy, const umap_rows *h, const umap_rows
 
 /* Bytes of umap_rows_norm_grad's workspace (> 0), or UMAP_E_INVAL.  Host only. */
 int64_t umap_rows_norm_grad_workspace(int64_t n, int32_t cols);
+
+/*
+ * umap_rows_cross_entropy -- softmax cross entropy of rows against a whole table:
+ *   z[t][v] = scale * sum_c h[t][c] table[v][c]
+ *   lse[t]  = log sum_v exp z[t][v]
+ *   loss[t] = lse[t] - z[t][targets[t]]
+ * in fp32 from the inputs on.  The logits z are formed tile by tile and not kept.
+ * One row is a call like any other: a token's log-likelihood is minus its loss.
+ *
+ *   h        UMAP_F32, UMAP_F16 or UMAP_BF16, cols 1 .. 32768, rows < 2^24.
+ *   table    h's type and cols, 1 <= rows < 2^26.
+ *   targets  h->rows ids of type target_type (UMAP_I32 or UMAP_I64).  A row whose
+ *            target lies outside [0, table->rows) -- padding is -1, say -- takes
+ *            no part: its loss is 0 (its lse is computed all the same).
+ *   scale    finite.
+ *   loss, lse  h->rows fp32 each, overwritten.
+ *   workspace  workspace_bytes >= umap_rows_cross_entropy_workspace(h->rows,
+ *            table->rows, cols, type) bytes of device memory, 16-byte aligned,
+ *            contents of no meaning before or after; it must stay untouched until
+ *            the work on `stream` is done.
+ *
+ * A row of h or table that is not finite, or logits beyond fp32's range, make the
+ * lse of the rows concerned infinite or NaN.  No output may overlap an input or
+ * another output.  Errors: UMAP_E_INVAL, UMAP_E_DEVICE.
+ */
+int umap_rows_cross_entropy(const umap_rows *h, const umap_rows *table, const void *targets, int32_t target_type,
+                            float scale, float *loss, float *lse, void *workspace, int64_t workspace_bytes,
+                            void *stream);
+
+/* Bytes of umap_rows_cross_entropy's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type);
+
+/*
+ * umap_rows_cross_entropy_grad -- the gradient of dscale * sum_t dloss[t] loss[t].  With
+ *   D[t][v] = dscale dloss[t] (exp(z[t][v] - lse[t]) - (1 if v = targets[t], else 0))
+ *   dh[t]     = scale sum_v D[t][v] table[v]
+ *   dtable[v] = scale sum_t D[t][v] h[t]
+ * The logits are formed again, for a piece of the table at a time, and D of the piece
+ * is kept in h's type (16 bits: each entry off by half a unit in its last place, fp32:
+ * not rounded), all sums are fp32 and rounded once; their order is fixed.
+ *
+ *   h, table, targets, scale  as for umap_rows_cross_entropy.
+ *   lse        what that call gave.
+ *   dloss      NULL (ones), or a weight for each row, fp32.  Rows of weight 0 and
+ *              rows whose target lies outside the table take no part: their dh is
+ *              zeros, and nothing of them reaches dtable (they may hold NaN).
+ *   dscale     finite (one over the rows for a mean, times a loss scale for fp16).
+ *   dh         NULL, or receives the gradient of h: its type and shape.
+ *   dtable     NULL, or receives the gradient of table: its type and shape.  Not
+ *              both NULL.
+ *   accumulate 0: dtable is overwritten; 1: the gradient is added to it (in fp32,
+ *              rounded once), as for a table whose rows are looked up as well.
+ *   workspace  as above, umap_rows_cross_entropy_grad_workspace(..) bytes.
+ *
+ * No output may overlap an input, another output or the workspace.  Errors:
+ * UMAP_E_INVAL, UMAP_E_DEVICE.
+ */
+int umap_rows_cross_entropy_grad(const umap_rows *h, const umap_rows *table, const void *targets, int32_t target_type,
+                                 float scale, const float *lse, const float *dloss, float dscale, const umap_rows *dh,
+                                 const umap_rows *dtable, int32_t accumulate, void *workspace,
+                                 int64_t workspace_bytes, void *stream);
+
+/* Bytes of umap_rows_cross_entropy_grad's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+int64_t umap_rows_cross_entropy_grad_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type);
+
+/*
+ * umap_rows_distill -- the divergence of the softmax over a table from a teacher
+ * of which each row's largest logits are known.  With z and lse as for
+ * umap_rows_cross_entropy, k = teacher->cols and e, f < k:
+ *   q[t][e] = exp(teacher_scale teacher[t][e]) / sum_f exp(teacher_scale teacher[t][f])
+ *   loss[t] = sum_e q[t][e] (log q[t][e] - (z[t][ids[t][e]] - lse[t]))
+ * scale and teacher_scale are one over the temperature, times what else scales the
+ * logits; the factor temperature^2 that usually goes with it is dscale's.
+ *
+ *   h, table, scale, loss, lse, workspace  as for umap_rows_cross_entropy.
+ *   ids       h->rows x k ids of type id_type, without gaps: the teacher's tokens.
+ *             Places whose id lies outside [0, table->rows), and places with a
+ *             logit of -infinity, are empty: they take no part in the sums.  A row
+ *             with empty places only takes no part: its loss is 0.  A token may come
+ *             twice in a row; its shares add up.
+ *   teacher   UMAP_F32, UMAP_F16 or UMAP_BF16, h->rows rows of 1 <= k <= 256 logits.
+ *
+ * Errors: UMAP_E_INVAL, UMAP_E_DEVICE.
+ */
+int umap_rows_distill(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type,
+                      const umap_rows *teacher, float scale, float teacher_scale, float *loss, float *lse,
+                      void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of umap_rows_distill's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+int64_t umap_rows_distill_workspace(int64_t n, int64_t rows, int32_t cols, int32_t k, int32_t type);
+
+/*
+ * umap_rows_distill_grad -- its gradient for h and table (the teacher's logits are
+ * constants): umap_rows_cross_entropy_grad with
+ *   D[t][v] = dscale dloss[t] (exp(z[t][v] - lse[t]) - sum of q[t][e] over ids[t][e] = v)
+ * and the arguments of both.
+ */
+int umap_rows_distill_grad(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type,
+                           const umap_rows *teacher, float scale, float teacher_scale, const float *lse,
+                           const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable,
+                           int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of umap_rows_distill_grad's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+int64_t umap_rows_distill_grad_workspace(int64_t n, int64_t rows, int32_t cols, int32_t k, int32_t type);
 
 #ifdef __cplusplus
 }

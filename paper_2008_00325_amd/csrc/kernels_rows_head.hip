@@ -1,0 +1,732 @@
+// kernels_rows_head.hip -- the head over a table of tokens (umap_rows.h): softmax cross entropy
+// and the divergence from a teacher's largest logits, and their gradient.
+//
+//   z_tv = scale h_t . W_v,  lse_t = log sum_v exp z_tv,  shares q_te of the row's tokens id_te
+//   loss_t = sum_e q_te (log q_te + lse_t - z_{t, id_te})          (cross entropy: one token, q = 1)
+//   D_tv = g_t (exp(z_tv - lse_t) - sum_{e: id_te = v} q_te),  dh = D W,  dW = D^T h,  g_t = dscale scale dloss_t
+//
+// The logits are never kept.  Forward: a tile of them (rows of the table times rows of h) leaves
+// a maximum and a sum of exponentials for each row of h, which a second launch joins; that launch
+// also forms the logits of the rows' own tokens, as dot products.  Gradient: for a piece of the table at a
+// time the logits are formed anew and D is written in the inputs' type (16 bits: half a unit
+// in the last place of every entry, which sums of many entries average out), its entries at the rows' own tokens
+// from those tokens' unrounded p and q, which may nearly cancel; then come the two products.
+//
+// g_t is a number in [1/2, 1) times 2^e_t.  D holds the number, times 2^14 in fp16, whose smallest
+// values would swallow the probabilities of rare tokens; dh gets 2^e_t on the way out, exactly.  dW takes
+// h_t times 2^(e_t - E), E the largest, instead: also exact.
+#include <algorithm>
+#include <cmath>
+
+#include "launch_sizes.hpp"
+#include "rows_product.hpp"
+
+namespace ul {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+// exp(x): hardware's 2^x, off by a unit in the last place and |x| 2^-24; 0 below 2^-126
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float minus_inf() { return -__builtin_inff(); }
+
+// Largest value and sum of exp(value - largest).
+struct MaxSum {
+    float m, s;
+    // Values to subtract from: a largest of -inf (no value yet, or all of them) subtracts nothing.
+    static __device__ __forceinline__ float base(float m) { return m == minus_inf() ? 0.0f : m; }
+    __device__ __forceinline__ void join(MaxSum o)
+    {
+        const float most = fmaxf(m, o.m), b = base(most);
+        s = fmaf(s, exp_of(m - b), o.s * exp_of(o.m - b));
+        m = most;
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// Tiles of a grid of `m` x `n` of them, one per workgroup.
+struct Tiles {
+    int m, n;
+};
+
+// ---- the logits' tiles: forward -------------------------------------------------------------
+
+template <int T, class P>
+__global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, ProductSide h, float scale, Tiles tiles, MaxSum *partial)
+{
+    __shared__ __align__(16) Piece lds[P::kLds / 16];
+    constexpr int FM = P::kFM, FN = P::kFN;
+    const int tm = blockIdx.x % tiles.m, tn = blockIdx.x / tiles.m;
+    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N;
+    Acc4 acc[FM][FN];
+    P::run(w, h, m0, n0, 0, w.cols, lds, acc);
+    MaxSum(*const part)[P::N] = reinterpret_cast<MaxSum(*)[P::N]>(lds);   // behind the product's last barrier
+    const int live = (int)min((int64_t)P::M, w.rows - m0);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        float most = minus_inf();
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                acc[i][j][r] = P::m_of(i) + r < live ? acc[i][j][r] * scale : minus_inf();
+                most = fmaxf(most, acc[i][j][r]);
+            }
+        const float b = MaxSum::base(most);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += exp_of(acc[i][j][r] - b);
+        MaxSum all{most, sum};
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1) all.join({__shfl_xor(all.m, o), __shfl_xor(all.s, o)});
+        if ((threadIdx.x & 63) < 16) part[(threadIdx.x >> 6) / P::kWN][P::n_of(j)] = all;
+    }
+    __syncthreads();
+    for (int n = threadIdx.x; n < P::N; n += P::kThreads) {
+        if (n0 + n >= h.rows) continue;
+        MaxSum all = part[0][n];
+#pragma unroll
+        for (int i = 1; i < P::kWM; ++i) all.join(part[i][n]);
+        partial[(n0 + n) * tiles.m + tm] = all;
+    }
+}
+
+// ---- a row's own tokens ----------------------------------------------------------------------
+
+constexpr int kSlots = 4;   // tokens of a lane: a row has up to 256
+
+struct Taught {
+    RowIds ids;
+    int32_t k;
+    const void *teacher;   // null: one token a row
+    int64_t stride;
+    int32_t type;
+    float scale;
+};
+
+__device__ __forceinline__ float teacher_at(const Taught &x, int64_t t, int e)
+{
+    switch (x.type) {
+    case UMAP_F32: return static_cast<const float *>(x.teacher)[t * x.stride + e];
+    case UMAP_F16: return elem_float<UMAP_F16>(static_cast<const _Float16 *>(x.teacher)[t * x.stride + e]);
+    default: return elem_float<UMAP_BF16>(static_cast<const uint16_t *>(x.teacher)[t * x.stride + e]);
+    }
+}
+
+// Lane l holds tokens l, l + 64, ..: id (-1: none) and share.
+struct OwnTokens {
+    int id[kSlots];
+    float share[kSlots], log_share[kSlots];
+    bool any;
+    __device__ __forceinline__ OwnTokens(const Taught &x, int64_t t, int64_t rows, int lane)
+    {
+        float most = minus_inf();
+        bool here = false;
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            const int e = lane + 64 * s;
+            id[s] = -1;
+            log_share[s] = minus_inf();
+            if (e < x.k) id[s] = (int)row_of(x.ids, t * x.k + e, rows);
+            if (id[s] >= 0) {
+                log_share[s] = x.teacher ? teacher_at(x, t, e) * x.scale : 0.0f;
+                if (log_share[s] == minus_inf()) id[s] = -1;
+            }
+            most = fmaxf(most, log_share[s]);
+            here |= id[s] >= 0;
+        }
+        any = __any(here);
+        most = MaxSum::base(wave_max(most));
+        float sum = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) sum += share[s] = id[s] >= 0 ? exp_of(log_share[s] - most) : 0.0f;
+        sum = wave_sum(sum);
+        const float log_sum = logf(sum);
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            share[s] = id[s] >= 0 ? share[s] / sum : 0.0f;
+            log_share[s] = log_share[s] - most - log_sum;
+        }
+    }
+};
+
+template <int T>
+__device__ __forceinline__ void fetch8(const Elem<T> *row, int c, int cols, float v[8])
+{
+    if (c + 8 <= cols) {
+        floats_of<T, 8>(load_raw<T, 8>(row + c), v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? elem_float<T>(row[c + j]) : 0.0f;
+    }
+}
+
+// Dot products of a row of h with the table's rows of its tokens, into the tokens' lanes.
+template <int T>
+__device__ __forceinline__ void own_logits(const Elem<T> *h, const ProductSide &w, const OwnTokens &own, int k, int lane,
+                                           float scale, float z[kSlots])
+{
+    constexpr int kAtOnce = 4;
+    const int cols = (int)w.cols;
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+        z[s] = 0.0f;
+        const int most = min(64, k - 64 * s);
+        for (int e0 = 0; e0 < most; e0 += kAtOnce) {
+            const Elem<T> *row[kAtOnce];
+            float sum[kAtOnce] = {};
+            int id[kAtOnce];
+            bool some = false;
+#pragma unroll
+            for (int e = 0; e < kAtOnce; ++e) {
+                id[e] = __builtin_amdgcn_readlane(own.id[s], min(e0 + e, 63));
+                if (e0 + e >= most) id[e] = -1;
+                some |= id[e] >= 0;
+                row[e] = static_cast<const Elem<T> *>(w.data) + (int64_t)max(id[e], 0) * w.stride;
+            }
+            if (!some) continue;
+            for (int c = lane * 8; c < cols; c += 512) {
+                float a[8];
+                fetch8<T>(h, c, cols, a);
+#pragma unroll
+                for (int e = 0; e < kAtOnce; ++e) {
+                    if (id[e] < 0) continue;
+                    float b[8];
+                    fetch8<T>(row[e], c, cols, b);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[e] = fmaf(a[j], b[j], sum[e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < kAtOnce; ++e) {
+                const float all = wave_sum(sum[e]) * scale;
+                if (lane == e0 + e) z[s] = all;
+            }
+        }
+    }
+}
+
+// A wave per row: joins the row's tiles, and sums its loss.
+template <int T>
+__global__ __launch_bounds__(256) void k_head_loss(ProductSide w, ProductSide h, float scale, Taught taught, int64_t first,
+                                                   int64_t tiles, const MaxSum *partial, float *loss, float *lse)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= h.rows) return;
+    MaxSum all{minus_inf(), 0.0f};
+    for (int64_t i = lane; i < tiles; i += 64) all.join(partial[t * tiles + i]);
+    for (int o = 1; o < 64; o <<= 1) all.join({__shfl_xor(all.m, o), __shfl_xor(all.s, o)});
+    const float sum = all.m + logf(all.s);
+    const OwnTokens own(taught, first + t, w.rows, lane);
+    float z[kSlots], mine = 0.0f;
+    own_logits<T>(static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, lane, scale, z);
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s)
+        if (own.id[s] >= 0 && own.share[s] != 0.0f) mine = fmaf(own.share[s], own.log_share[s] + (sum - z[s]), mine);
+    mine = wave_sum(mine);
+    if (lane == 0) {
+        lse[first + t] = sum;
+        // rounding can take a loss of nearly nothing below it
+        loss[first + t] = !own.any ? 0.0f : mine < 0.0f ? 0.0f : mine;
+    }
+}
+
+// ---- gradient --------------------------------------------------------------------------------
+
+constexpr int kNoRow = INT32_MIN;
+template <int T>
+constexpr int kShift = T == UMAP_F16 ? 14 : 0;
+
+// What the gradient's launches share of a row: its number in [1/2, 1), with kShift, and its exponent.
+struct RowWeights {
+    float *number;
+    int *exponent;   // kNoRow: the row takes no part
+    const int *largest;   // null: largest_known
+    int largest_known;
+};
+__device__ __forceinline__ int largest_of(const RowWeights &x) { return x.largest ? *x.largest : x.largest_known; }
+
+__device__ __forceinline__ void split_weight(float g, float &number, int &exponent)
+{
+    exponent = 0;
+    number = g;
+    if (g != 0.0f && fabsf(g) < __builtin_inff()) {
+        number = __builtin_amdgcn_frexp_mantf(g);
+        exponent = __builtin_amdgcn_frexp_expf(g);
+    }
+}
+
+// The largest exponent of the rows' weights (finite and not zero), or 0; one workgroup.
+__global__ __launch_bounds__(1024) void k_head_largest(const float *dloss, int64_t n, float factor, int *largest)
+{
+    __shared__ int part[16];
+    int most = kNoRow;
+    for (int64_t t = threadIdx.x; t < n; t += 1024) {
+        const float g = dloss[t] * factor;
+        if (g != 0.0f && fabsf(g) < __builtin_inff()) most = max(most, (int)__builtin_amdgcn_frexp_expf(g));
+    }
+    for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) most = max(most, part[i]);
+        *largest = most == kNoRow ? 0 : most;
+    }
+}
+
+// A wave per row: its weight, its tokens with the entries of D, and the copies of h that the
+// products take, without gaps (`pitch` columns, zeros past the last) and zeros in rows without part.
+template <int T>
+__global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
+                                                   const float *dloss, float factor, RowWeights weights, int *token,
+                                                   float *value, Elem<T> *copy, Elem<T> *scaled, int pitch)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= h.rows) return;
+    const Elem<T> *const row = static_cast<const Elem<T> *>(h.data) + t * h.stride;
+    const OwnTokens own(taught, t, w.rows, lane);
+    const float g = dloss ? dloss[t] * factor : factor;
+    float number;
+    int exponent;
+    split_weight(g, number, exponent);
+    number = ldexpf(number, kShift<T>);
+    const bool part = own.any && g != 0.0f;
+    float z[kSlots];
+    own_logits<T>(row, w, own, part ? taught.k : 0, lane, scale, z);
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+        const int e = lane + 64 * s;
+        int id = part ? own.id[s] : -1;
+        float share = own.share[s];
+        if (taught.k > 1) {   // a token that comes twice: the first place has all its shares
+            share = 0.0f;
+            bool again = false;
+            for (int o = 0; o < taught.k; ++o) {
+                int other_id = 0;
+                float other = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kSlots; ++q)
+                    if (o >> 6 == q) {
+                        other_id = __builtin_amdgcn_readlane(own.id[q], o & 63);
+                        other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own.share[q]), o & 63));
+                    }
+                if (other_id != id) continue;
+                share += other;
+                again |= o < e;
+            }
+            if (again) id = -1;
+        }
+        if (e < taught.k) {
+            token[t * taught.k + e] = id;
+            value[t * taught.k + e] = id < 0 ? 0.0f : number * (exp_of(z[s] - lse[t]) - share);
+        }
+    }
+    if (lane == 0) {
+        weights.number[t] = part ? number : 0.0f;
+        weights.exponent[t] = part ? exponent : kNoRow;
+    }
+    const int by = scaled ? exponent - largest_of(weights) : 0;
+    for (int c = lane * 8; c < pitch; c += 512) {
+        float v[8] = {};
+        if (part) fetch8<T>(row, c, (int)h.cols, v);
+        store_raw<T, 8>(copy + t * pitch + c, raw_of<T, 8>(v));
+        if (!scaled) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], by);
+        store_raw<T, 8>(scaled + t * pitch + c, raw_of<T, 8>(v));
+    }
+}
+
+// D of a piece of the table: d[t][v], `pitch` columns, zeros past the piece's rows.
+template <int T, class P>
+__global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSide h, float scale, Tiles tiles, const float *lse,
+                                                        RowWeights weights, Elem<T> *d, int64_t pitch)
+{
+    __shared__ __align__(16) Piece lds[P::kLds / 16];
+    constexpr int FM = P::kFM, FN = P::kFN;
+    const int tm = blockIdx.x % tiles.m, tn = blockIdx.x / tiles.m;
+    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N;
+    Acc4 acc[FM][FN];
+    P::run(w, h, m0, n0, 0, w.cols, lds, acc);
+    const int live = (int)min((int64_t)P::M, w.rows - m0);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t t = n0 + P::n_of(j);
+        if (t >= h.rows) continue;
+        const float number = weights.number[t], sum = lse[t];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int m = P::m_of(i);
+            float v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float p = number * exp_of(acc[i][j][r] * scale - sum);
+                v[r] = number != 0.0f && m + r < live ? p : 0.0f;
+            }
+            store_raw<T, 4>(d + t * pitch + m0 + m, raw_of<T, 4>(v));
+        }
+    }
+}
+
+// The entries of D at the rows' own tokens.
+template <int T>
+__global__ __launch_bounds__(256) void k_head_own(const int *token, const float *value, int64_t count, int k, int64_t first,
+                                                  int64_t rows, Elem<T> *d, int64_t pitch)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        const int64_t v = token[i] - first;
+        if (token[i] >= 0 && v >= 0 && v < rows) d[i / k * pitch + v] = float_elem<T>(value[i]);
+    }
+}
+
+// dh's sums over a part of the piece, [split][t][c], added to those of the pieces before.
+template <int T, class P>
+__global__ __launch_bounds__(P::kThreads) void k_head_dh(ProductSide w, ProductSide d, Tiles tiles, int64_t depth, bool add,
+                                                         float *sums, int64_t pitch)
+{
+    __shared__ __align__(16) Piece lds[P::kLds / 16];
+    constexpr int FM = P::kFM, FN = P::kFN;
+    const int tile = blockIdx.x % (tiles.m * tiles.n), split = blockIdx.x / (tiles.m * tiles.n);
+    const int tm = tile % tiles.m, tn = tile / tiles.m;
+    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N, k0 = split * depth;
+    Acc4 acc[FM][FN];
+    P::run(w, d, m0, n0, k0, min(k0 + depth, w.rows), lds, acc);
+    float *const to = sums + split * d.rows * pitch;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t t = n0 + P::n_of(j);
+        if (t >= d.rows) continue;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int64_t c = m0 + P::m_of(i);
+            if (c >= pitch) continue;
+            Acc4 *const at = reinterpret_cast<Acc4 *>(to + t * pitch + c);
+            *at = add ? *at + acc[i][j] : acc[i][j];
+        }
+    }
+}
+
+template <int T>
+__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int splits, int64_t pitch, const int *exponent, umap_rows dh)
+{
+    const int64_t groups = pitch / 4, total = dh.rows * groups;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / groups, c = i % groups * 4;
+        Acc4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + t) * pitch + c);
+        const int e = exponent[t];
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = e == kNoRow ? 0.0f : ldexpf(sum[j], e - kShift<T>);
+        Elem<T> *const to = static_cast<Elem<T> *>(dh.data) + t * dh.stride + c;
+        if (c + 4 <= dh.cols) {
+            store_raw<T, 4>(to, raw_of<T, 4>(v));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < dh.cols) to[j] = float_elem<T>(v[j]);
+        }
+    }
+}
+
+// The table's gradient for a piece's rows.
+template <int T, class P>
+__global__ __launch_bounds__(P::kThreads) void k_head_dw(ProductSide h, ProductSide d, Tiles tiles, RowWeights weights, bool add,
+                                                         umap_rows dw)
+{
+    __shared__ __align__(16) Piece lds[P::kLds / 16];
+    constexpr int FM = P::kFM, FN = P::kFN;
+    const int tm = blockIdx.x % tiles.m, tn = blockIdx.x / tiles.m;
+    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N;
+    Acc4 acc[FM][FN];
+    P::run(h, d, m0, n0, 0, h.rows, lds, acc);
+    const int e = h.rows > 0 ? largest_of(weights) - kShift<T> : 0;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t v = n0 + P::n_of(j);
+        if (v >= dw.rows) continue;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int64_t c = m0 + P::m_of(i);
+            if (c >= dw.cols) continue;
+            Elem<T> *const to = static_cast<Elem<T> *>(dw.data) + v * dw.stride + c;
+            float g[4], old[4] = {};
+            const bool whole = c + 4 <= dw.cols;
+            if (add) {
+                if (whole) {
+                    floats_of<T, 4>(load_raw<T, 4>(to), old);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (c + r < dw.cols) old[r] = elem_float<T>(to[r]);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                g[r] = ldexpf(acc[i][j][r], e);
+                if (add) g[r] += old[r];
+            }
+            if (whole) {
+                store_raw<T, 4>(to, raw_of<T, 4>(g));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (c + r < dw.cols) to[r] = float_elem<T>(g[r]);
+            }
+        }
+    }
+}
+
+// ---- sizes -----------------------------------------------------------------------------------
+
+constexpr int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+constexpr int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
+
+constexpr int64_t kTile = 256, kSmallTile = 128;
+// Tiles of 256 x 256 where they give every CU one.
+bool large_tiles(int64_t m, int64_t n) { return over(m, kTile) * over(n, kTile) >= 192; }
+int64_t tile_of(int64_t m, int64_t n) { return large_tiles(m, n) ? kTile : kSmallTile; }
+
+// Forward: rows of h at a time, so that the partial sums stay within 64 MB.
+struct LossSizes {
+    int64_t tiles, rows;
+    LossSizes(int64_t n, int64_t vocab)
+    {
+        tiles = over(vocab, kSmallTile);
+        rows = std::max<int64_t>(kTile, ((int64_t)64 << 20) / (tiles * (int64_t)sizeof(MaxSum)) / kTile * kTile);
+        rows = std::min(rows, n);
+    }
+    int64_t bytes() const { return std::max<int64_t>(16, rows * tiles * (int64_t)sizeof(MaxSum)); }
+};
+
+struct GradSizes {
+    int64_t n, vocab, cols, k, elem;
+    int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
+    // offsets into the workspace
+    int64_t largest, number, exponent, token, value, copy, scaled, d, sums, total;
+    GradSizes(int64_t n_, int64_t vocab_, int32_t cols_, int64_t k_, int32_t type)
+        : n(n_), vocab(vocab_), cols(cols_), k(k_), elem(elem_size(type))
+    {
+        const int64_t budget = (int64_t)256 << 20;
+        int64_t most = std::max<int64_t>(kTile, budget / std::max<int64_t>(1, n * elem) / kTile * kTile);
+        const int64_t pieces = over(vocab, most);
+        piece = up(over(vocab, pieces), kTile);
+        d_pitch = piece;
+        h_pitch = up(cols, 64);
+        sum_pitch = up(cols, 4);
+        const int64_t step = 128 / elem, steps = over(piece, step), tile = tile_of(cols, n);
+        const int64_t tiles = over(cols, tile) * over(std::max<int64_t>(n, 1), tile);
+        splits = std::max<int64_t>(1, std::min((tile == kTile ? 256 : 512) / tiles, steps / 8));
+        depth = over(steps, splits) * step;
+        splits = over(piece, depth);
+        int64_t at = 0;
+        auto take = [&](int64_t bytes) {
+            const int64_t was = at;
+            at += up(bytes, 256);
+            return was;
+        };
+        largest = take(16);
+        number = take(n * 4);
+        exponent = take(n * 4);
+        token = take(n * k * 4);
+        value = take(n * k * 4);
+        copy = take(n * h_pitch * elem);
+        scaled = take(n * h_pitch * elem);
+        d = take(n * d_pitch * elem);
+        sums = take(splits * n * sum_pitch * 4);
+        total = at;
+    }
+};
+
+template <int T, bool AA, bool AB>
+using Large = Product<T, AA, AB, 2, 4, 8, 4>;
+template <int T, bool AA, bool AB>
+using Small = Product<T, AA, AB, 2, 2, 4, 4>;
+
+template <class P>
+Tiles tiles_of(int64_t m, int64_t n)
+{
+    return {(int)over(m, P::M), (int)over(n, P::N)};
+}
+
+template <int T>
+ProductSide side_of(const umap_rows &m, int64_t first, int64_t rows)
+{
+    return {static_cast<const Elem<T> *>(m.data) + first * m.stride, m.stride, rows, m.cols};
+}
+
+template <int T, class P>
+hipError_t lse_tiles(const ProductSide &w, const ProductSide &h, float scale, MaxSum *partial, int64_t *tiles, hipStream_t s)
+{
+    const Tiles g = tiles_of<P>(w.rows, h.rows);
+    *tiles = g.m;
+    hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, h, scale, g, partial);
+    return hipGetLastError();
+}
+
+template <int T>
+hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught, float scale, float *out, float *lse,
+                void *workspace, hipStream_t s)
+{
+    const LossSizes z(h.rows, table.rows);
+    auto *const partial = static_cast<MaxSum *>(workspace);
+    const ProductSide w = side_of<T>(table, 0, table.rows);
+    for (int64_t first = 0; first < h.rows; first += z.rows) {
+        const ProductSide rows = side_of<T>(h, first, std::min(z.rows, h.rows - first));
+        int64_t tiles = 0;
+        hipError_t e = large_tiles(w.rows, rows.rows) ? lse_tiles<T, Large<T, false, false>>(w, rows, scale, partial, &tiles, s)
+                                                      : lse_tiles<T, Small<T, false, false>>(w, rows, scale, partial, &tiles, s);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((k_head_loss<T>), dim3((unsigned)over(rows.rows, 4)), dim3(256), 0, s, w, rows, scale, taught, first,
+                           tiles, partial, out, lse);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <int T, template <int, bool, bool> class Shape>
+hipError_t d_tiles(const ProductSide &w, const ProductSide &h, float scale, const float *lse, const RowWeights &weights, Elem<T> *d,
+                   int64_t pitch, hipStream_t s)
+{
+    using P = Shape<T, false, false>;
+    const Tiles g = tiles_of<P>(pitch, h.rows);
+    hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, h, scale, g, lse,
+                       weights, d, pitch);
+    return hipGetLastError();
+}
+template <int T, template <int, bool, bool> class Shape>
+hipError_t dh_tiles(const ProductSide &w, const ProductSide &d, const GradSizes &z, bool add, float *sums, hipStream_t s)
+{
+    using P = Shape<T, true, false>;
+    const Tiles g = tiles_of<P>(z.cols, z.n);
+    hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s, w, d, g,
+                       z.depth, add, sums, z.sum_pitch);
+    return hipGetLastError();
+}
+template <int T, template <int, bool, bool> class Shape>
+hipError_t dw_tiles(const ProductSide &h, const ProductSide &d, const RowWeights &weights, bool add, const umap_rows &dw, hipStream_t s)
+{
+    using P = Shape<T, true, true>;
+    const Tiles g = tiles_of<P>(dw.cols, dw.rows);
+    hipLaunchKernelGGL((k_head_dw<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, h, d, g, weights, add, dw);
+    return hipGetLastError();
+}
+
+#define UL_LAUNCHED(expr)                      \
+    do {                                       \
+        const hipError_t ul_e_ = (expr);       \
+        if (ul_e_ != hipSuccess) return ul_e_; \
+    } while (0)
+
+template <int T>
+hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught, float scale, const float *lse,
+                const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable, bool add, void *workspace,
+                hipStream_t s)
+{
+    const GradSizes z(h.rows, table.rows, table.cols, taught.k, h.type);
+    char *const base = static_cast<char *>(workspace);
+    auto *const token = reinterpret_cast<int *>(base + z.token);
+    auto *const value = reinterpret_cast<float *>(base + z.value), *const sums = reinterpret_cast<float *>(base + z.sums);
+    auto *const copy = reinterpret_cast<Elem<T> *>(base + z.copy), *const d = reinterpret_cast<Elem<T> *>(base + z.d);
+    auto *const scaled = dloss ? reinterpret_cast<Elem<T> *>(base + z.scaled) : nullptr;
+    const float factor = dscale * scale;
+    int known = 0;
+    if (factor != 0.0f && std::isfinite(factor)) std::frexp(factor, &known);
+    int *const largest = dloss ? reinterpret_cast<int *>(base + z.largest) : nullptr;
+    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, known};
+    if (z.n > 0) {
+        if (dloss) {
+            hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, dloss, z.n, factor, largest);
+            UL_LAUNCHED(hipGetLastError());
+        }
+        hipLaunchKernelGGL((k_head_rows<T>), dim3((unsigned)over(z.n, 4)), dim3(256), 0, s, side_of<T>(table, 0, table.rows),
+                           side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights, token, value, copy, scaled,
+                           (int)z.h_pitch);
+        UL_LAUNCHED(hipGetLastError());
+    }
+    const ProductSide rows{copy, z.h_pitch, z.n, z.cols}, weighted{scaled ? scaled : copy, z.h_pitch, z.n, z.cols};
+    for (int64_t first = 0; first < z.vocab; first += z.piece) {
+        const int64_t here = std::min(z.piece, z.vocab - first);
+        const ProductSide w = side_of<T>(table, first, here), d_side{d, z.d_pitch, z.n, here};
+        if (z.n > 0) {
+            UL_LAUNCHED(large_tiles(here, z.n) ? (d_tiles<T, Large>(w, rows, scale, lse, weights, d, z.d_pitch, s))
+                                               : (d_tiles<T, Small>(w, rows, scale, lse, weights, d, z.d_pitch, s)));
+            hipLaunchKernelGGL((k_head_own<T>), dim3((unsigned)std::min<int64_t>(1024, over(z.n * z.k, 256))), dim3(256), 0, s,
+                               token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch);
+            UL_LAUNCHED(hipGetLastError());
+            if (dh)
+                UL_LAUNCHED(large_tiles(z.cols, z.n) ? (dh_tiles<T, Large>(w, d_side, z, first > 0, sums, s))
+                                                     : (dh_tiles<T, Small>(w, d_side, z, first > 0, sums, s)));
+        }
+        if (dtable) {
+            umap_rows part = *dtable;
+            part.data = static_cast<Elem<T> *>(dtable->data) + first * dtable->stride;
+            part.rows = here;
+            UL_LAUNCHED(large_tiles(z.cols, here) ? (dw_tiles<T, Large>(weighted, d_side, weights, add, part, s))
+                                                  : (dw_tiles<T, Small>(weighted, d_side, weights, add, part, s)));
+        }
+    }
+    if (dh && z.n > 0) {
+        const int64_t total = z.n * z.sum_pitch / 4;
+        hipLaunchKernelGGL((k_head_dh_join<T>), dim3((unsigned)std::min<int64_t>(4096, over(total, 256))), dim3(256), 0, s, sums,
+                           (int)z.splits, z.sum_pitch, weights.exponent, *dh);
+        UL_LAUNCHED(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
+Taught taught_of(RowIds ids, const umap_rows *teacher, float teacher_scale)
+{
+    if (!teacher) return {ids, 1, nullptr, 0, 0, 1.0f};
+    return {ids, teacher->cols, teacher->data, teacher->stride, teacher->type, teacher_scale};
+}
+
+}  // namespace
+
+int64_t rows_head_bytes(int64_t n, int64_t vocab) { return LossSizes(n, vocab).bytes(); }
+
+hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,
+                            float teacher_scale, float *loss_out, float *lse, void *workspace, hipStream_t s)
+{
+    const Taught taught = taught_of(ids, teacher, teacher_scale);
+    switch (h.type) {
+    case UMAP_F32: return loss<UMAP_F32>(h, table, taught, scale, loss_out, lse, workspace, s);
+    case UMAP_F16: return loss<UMAP_F16>(h, table, taught, scale, loss_out, lse, workspace, s);
+    default: return loss<UMAP_BF16>(h, table, taught, scale, loss_out, lse, workspace, s);
+    }
+}
+
+int64_t rows_head_grad_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t k, int32_t type)
+{
+    return GradSizes(n, vocab, cols, k, type).total;
+}
+
+hipError_t launch_rows_head_grad(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,
+                                 float teacher_scale, const float *lse, const float *dloss, float dscale, const umap_rows *dh,
+                                 const umap_rows *dtable, bool accumulate, void *workspace, hipStream_t s)
+{
+    const Taught taught = taught_of(ids, teacher, teacher_scale);
+    switch (h.type) {
+    case UMAP_F32: return grad<UMAP_F32>(h, table, taught, scale, lse, dloss, dscale, dh, dtable, accumulate, workspace, s);
+    case UMAP_F16: return grad<UMAP_F16>(h, table, taught, scale, lse, dloss, dscale, dh, dtable, accumulate, workspace, s);
+    default: return grad<UMAP_BF16>(h, table, taught, scale, lse, dloss, dscale, dh, dtable, accumulate, workspace, s);
+    }
+}
+
+}  // namespace ul

@@ -188,6 +188,107 @@ int check_norm_sizes(int64_t n, int32_t cols)
     return UMAP_OK;
 }
 
+constexpr int64_t kMaxHeadRows = (int64_t)1 << 24, kMaxTokens = (int64_t)1 << 26;
+constexpr int32_t kMaxTaught = 256;
+
+int check_head_sizes(int64_t n, int64_t rows, int32_t cols, int32_t k, int32_t type)
+{
+    if (n < 0 || n >= kMaxHeadRows) return fail(UMAP_E_INVAL, "rows of h must be in [0, 2^24), got %lld", (long long)n);
+    if (rows < 1 || rows >= kMaxTokens)
+        return fail(UMAP_E_INVAL, "rows of table must be in [1, 2^26), got %lld", (long long)rows);
+    if (cols < 1 || cols > kMaxNormCols)
+        return fail(UMAP_E_INVAL, "cols must be in [1, %d], got %d", kMaxNormCols, cols);
+    if (k < 1 || k > kMaxTaught) return fail(UMAP_E_INVAL, "k must be in [1, %d], got %d", kMaxTaught, k);
+    return is_float(type) ? UMAP_OK : fail(UMAP_E_INVAL, "element type %d is not one this call takes", type);
+}
+
+// What the head's calls have in common: h, table, the rows' tokens, the teacher (which may be
+// null where `taught` is false) and the scales.
+int check_head(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type, bool taught,
+               const umap_rows *teacher, float scale, float teacher_scale, ul::RowIds *at)
+{
+    UL_TRY(check(h, "h", kMaxNormCols, false, false));
+    UL_TRY(check(table, "table", kMaxNormCols, false, false));
+    UL_TRY(check_shape(*table, "table", -1, h->cols));
+    if (table->type != h->type) return fail(UMAP_E_INVAL, "table must have h's type");
+    if (taught) {
+        UL_TRY(check(teacher, "teacher", kMaxTaught, false, false));
+        UL_TRY(check_shape(*teacher, "teacher", h->rows, teacher->cols));
+    }
+    const int32_t k = taught ? teacher->cols : 1;
+    UL_TRY(check_head_sizes(h->rows, table->rows, h->cols, k, h->type));
+    UL_TRY(check_ids(ids, id_type, h->rows * k, at));
+    if (!ids && h->rows > 0) return fail(UMAP_E_INVAL, "%s must not be NULL", taught ? "ids" : "targets");
+    if (!isfinite(scale)) return fail(UMAP_E_INVAL, "scale must be finite");
+    return isfinite(teacher_scale) ? UMAP_OK : fail(UMAP_E_INVAL, "teacher_scale must be finite");
+}
+
+int check_floats(const float *p, const char *name, int64_t n, bool needed)
+{
+    if (needed && n > 0 && !p) return fail(UMAP_E_INVAL, "%s must not be NULL", name);
+    return (uintptr_t)p % 4 ? fail(UMAP_E_INVAL, "%s is not aligned", name) : UMAP_OK;
+}
+
+int head(const char *name, const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type, bool taught,
+         const umap_rows *teacher, float scale, float teacher_scale, float *loss, float *lse, void *workspace,
+         int64_t workspace_bytes, void *stream)
+{
+    ul::RowIds at;
+    UL_TRY(check_head(h, table, ids, id_type, taught, teacher, scale, teacher_scale, &at));
+    const int64_t n = h->rows, k = taught ? teacher->cols : 1;
+    UL_TRY(check_floats(loss, "loss", n, true));
+    UL_TRY(check_floats(lse, "lse", n, true));
+    const int64_t need = ul::rows_head_bytes(n, table->rows);
+    UL_TRY(check_workspace(workspace, workspace_bytes, need));
+    const Span hs = span(*h), ts = span(*table), is = flat(ids, n * k * at.bytes), as = taught ? span(*teacher) : flat(nullptr, 0),
+               ls = flat(loss, n * 4), es = flat(lse, n * 4), work = flat(workspace, need);
+    UL_TRY(refuse_overlap("loss", ls, {hs, ts, is, as, es, work}));
+    UL_TRY(refuse_overlap("lse", es, {hs, ts, is, as, work}));
+    UL_TRY(refuse_overlap("workspace", work, {hs, ts, is, as}));
+    if (n == 0) return UMAP_OK;
+    return launched(ul::launch_rows_head(*h, *table, at, taught ? teacher : nullptr, scale, teacher_scale, loss, lse,
+                                         workspace, static_cast<hipStream_t>(stream)),
+                    name);
+}
+
+int head_grad(const char *name, const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type, bool taught,
+              const umap_rows *teacher, float scale, float teacher_scale, const float *lse, const float *dloss,
+              float dscale, const umap_rows *dh, const umap_rows *dtable, int32_t accumulate, void *workspace,
+              int64_t workspace_bytes, void *stream)
+{
+    ul::RowIds at;
+    UL_TRY(check_head(h, table, ids, id_type, taught, teacher, scale, teacher_scale, &at));
+    const int64_t n = h->rows, k = taught ? teacher->cols : 1;
+    UL_TRY(check_floats(lse, "lse", n, true));
+    UL_TRY(check_floats(dloss, "dloss", n, false));
+    if (!isfinite(dscale)) return fail(UMAP_E_INVAL, "dscale must be finite");
+    if (!dh && !dtable) return fail(UMAP_E_INVAL, "dh and dtable must not both be NULL");
+    if (dh) {
+        UL_TRY(check(dh, "dh", kMaxNormCols, true, false));
+        UL_TRY(check_shape(*dh, "dh", n, h->cols));
+        if (dh->type != h->type) return fail(UMAP_E_INVAL, "dh must have h's type");
+    }
+    if (dtable) {
+        UL_TRY(check(dtable, "dtable", kMaxNormCols, true, false));
+        UL_TRY(check_shape(*dtable, "dtable", table->rows, h->cols));
+        if (dtable->type != h->type) return fail(UMAP_E_INVAL, "dtable must have table's type");
+    }
+    if (accumulate != 0 && accumulate != 1) return fail(UMAP_E_INVAL, "accumulate must be 0 or 1, got %d", accumulate);
+    const int64_t need = ul::rows_head_grad_bytes(n, table->rows, h->cols, (int32_t)k, h->type);
+    UL_TRY(check_workspace(workspace, workspace_bytes, need));
+    const Span none = flat(nullptr, 0), hs = span(*h), ts = span(*table), is = flat(ids, n * k * at.bytes),
+               as = taught ? span(*teacher) : none, es = flat(lse, n * 4), ws = flat(dloss, n * 4),
+               dhs = dh ? span(*dh) : none, dts = dtable ? span(*dtable) : none, work = flat(workspace, need);
+    UL_TRY(refuse_overlap("dh", dhs, {hs, ts, is, as, es, ws, dts, work}));
+    UL_TRY(refuse_overlap("dtable", dts, {hs, ts, is, as, es, ws, work}));
+    UL_TRY(refuse_overlap("workspace", work, {hs, ts, is, as, es, ws}));
+    if (n == 0 && (!dtable || accumulate)) return UMAP_OK;
+    return launched(ul::launch_rows_head_grad(*h, *table, at, taught ? teacher : nullptr, scale, teacher_scale, lse, dloss,
+                                              dscale, dh, dtable, accumulate != 0, workspace,
+                                              static_cast<hipStream_t>(stream)),
+                    name);
+}
+
 }  // namespace
 
 extern "C" {
@@ -317,6 +418,63 @@ int umap_rows_norm_grad(const umap_rows *dy, const umap_rows *h, const umap_rows
     return launched(ul::launch_rows_norm_grad(*dy, *h, dh, w, eps, *dx, dweight, workspace,
                                               static_cast<hipStream_t>(stream)),
                     "umap_rows_norm_grad");
+}
+
+int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type)
+{
+    UL_TRY(check_head_sizes(n, rows, cols, 1, type));
+    return ul::rows_head_bytes(n, rows);
+}
+
+int umap_rows_cross_entropy(const umap_rows *h, const umap_rows *table, const void *targets, int32_t target_type,
+                            float scale, float *loss, float *lse, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return head("umap_rows_cross_entropy", h, table, targets, target_type, false, nullptr, scale, 1.0f, loss, lse,
+                workspace, workspace_bytes, stream);
+}
+
+int64_t umap_rows_cross_entropy_grad_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type)
+{
+    UL_TRY(check_head_sizes(n, rows, cols, 1, type));
+    return ul::rows_head_grad_bytes(n, rows, cols, 1, type);
+}
+
+int umap_rows_cross_entropy_grad(const umap_rows *h, const umap_rows *table, const void *targets, int32_t target_type,
+                                 float scale, const float *lse, const float *dloss, float dscale, const umap_rows *dh,
+                                 const umap_rows *dtable, int32_t accumulate, void *workspace, int64_t workspace_bytes,
+                                 void *stream)
+{
+    return head_grad("umap_rows_cross_entropy_grad", h, table, targets, target_type, false, nullptr, scale, 1.0f, lse,
+                     dloss, dscale, dh, dtable, accumulate, workspace, workspace_bytes, stream);
+}
+
+int64_t umap_rows_distill_workspace(int64_t n, int64_t rows, int32_t cols, int32_t k, int32_t type)
+{
+    UL_TRY(check_head_sizes(n, rows, cols, k, type));
+    return ul::rows_head_bytes(n, rows);
+}
+
+int umap_rows_distill(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type,
+                      const umap_rows *teacher, float scale, float teacher_scale, float *loss, float *lse,
+                      void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return head("umap_rows_distill", h, table, ids, id_type, true, teacher, scale, teacher_scale, loss, lse, workspace,
+                workspace_bytes, stream);
+}
+
+int64_t umap_rows_distill_grad_workspace(int64_t n, int64_t rows, int32_t cols, int32_t k, int32_t type)
+{
+    UL_TRY(check_head_sizes(n, rows, cols, k, type));
+    return ul::rows_head_grad_bytes(n, rows, cols, k, type);
+}
+
+int umap_rows_distill_grad(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type,
+                           const umap_rows *teacher, float scale, float teacher_scale, const float *lse,
+                           const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable,
+                           int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return head_grad("umap_rows_distill_grad", h, table, ids, id_type, true, teacher, scale, teacher_scale, lse, dloss,
+                     dscale, dh, dtable, accumulate, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

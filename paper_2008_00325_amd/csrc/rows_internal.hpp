@@ -35,4 +35,15 @@ int64_t rows_norm_grad_bytes(int64_t n, int32_t cols);
 hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const umap_rows *dh, RowWeight weight,
                                  float eps, const umap_rows &dx, float *dweight, void *workspace, hipStream_t s);
 
+// ---- head: loss of rows against a table, with its gradient ----
+// teacher may be null: one token a row, with share 1.
+int64_t rows_head_bytes(int64_t n, int64_t vocab);
+hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,
+                            float teacher_scale, float *loss, float *lse, void *workspace, hipStream_t s);
+int64_t rows_head_grad_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t k, int32_t type);
+// dloss, dh and dtable may be null.
+hipError_t launch_rows_head_grad(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,
+                                 float teacher_scale, const float *lse, const float *dloss, float dscale, const umap_rows *dh,
+                                 const umap_rows *dtable, bool accumulate, void *workspace, hipStream_t s);
+
 }  // namespace ul

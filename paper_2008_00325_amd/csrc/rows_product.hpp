@@ -1,0 +1,194 @@
+// rows_product.hpp -- matrix products on the matrix cores, in tiles, for the kernels of the
+// token rows' head: acc(m, n) = sum_k A(m, k) B(n, k), fp32 sums of 16-bit or fp32 elements.
+//
+// A side lies in memory either along k (element (i, k) at [i][k]: rows of the table against
+// rows of h) or across it (at [k][i]).  A step takes 128 bytes of k of every row of the tile:
+// 64 16-bit elements, or 32 fp32.  Both sides' steps lie in LDS in 16-byte pieces, the place
+// of a piece in its row turned by the row's number so that the lanes that read together meet
+// different banks; a side across k is turned on the way out (ds_read_b64_tr_b16).
+//
+// A fragment is a lane's 16 bytes: row lane % 16 of 16, and of the step's elements of k those
+// from (lane / 16) * 16 bytes on.  How the matrix instruction numbers k does not matter as long as
+// both sides agree.
+#pragma once
+
+#include "rows_device.hpp"
+
+namespace ul {
+
+typedef float Acc4 __attribute__((ext_vector_type(4)));
+
+struct ProductSide {
+    const void *data;
+    int64_t stride;   // elements
+    int64_t rows;     // of the memory; what lies outside counts as zeros
+    int64_t cols;
+};
+
+struct __attribute__((aligned(16))) Piece {
+    uint32_t w[4];
+};
+
+template <int T>
+__device__ __forceinline__ Acc4 multiply(const Piece &a, const Piece &b, Acc4 c)
+{
+    typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+    if constexpr (T == UMAP_BF16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), __builtin_bit_cast(B8, b), c, 0, 0, 0);
+    } else if constexpr (T == UMAP_F16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(H8, a), __builtin_bit_cast(H8, b), c, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w[j]), __uint_as_float(b.w[j]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+// 16 bytes of a row from column c on; columns past the row and rows past the last are zeros.
+template <int T>
+__device__ __forceinline__ Piece fetch_piece(const ProductSide &side, int64_t r, int64_t c)
+{
+    constexpr int kPer = 16 / sizeof(Elem<T>);
+    Piece p = {};
+    if (r >= side.rows || c >= side.cols) return p;
+    const Elem<T> *at = static_cast<const Elem<T> *>(side.data) + r * side.stride + c;
+    if (c + kPer <= side.cols) return __builtin_bit_cast(Piece, load_raw<T, kPer>(at));
+    Elem<T> e[kPer] = {};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (c + j < side.cols) e[j] = at[j];
+    __builtin_memcpy(&p, e, 16);
+    return p;
+}
+
+// One side's step of a tile of I rows.
+template <int T, bool kAcross, int I>
+struct Step {
+    static constexpr int kElem = sizeof(Elem<T>), kPer = 16 / kElem, kDepth = 128 / kElem;
+    static constexpr int kRow = kAcross ? I / kPer : 8;   // pieces of a row in LDS
+    static constexpr int kPieces = I * 8;
+    // How the pieces of row r are turned: along k, the 8 lanes that read 16 bytes at once are of 8
+    // rows; across, 32 lanes read 32 bytes of 8 rows (fp32: 64 lanes 64 bytes of 4 rows).
+    __device__ static __forceinline__ int turn(int r)
+    {
+        if constexpr (!kAcross) return r & 7;
+        else if constexpr (kElem == 2) return ((r & 3) | (r >> 1 & 4)) << 1;
+        else return (r & 12);
+    }
+    // Row and column of LDS piece p, in memory, from the tile's origin.
+    __device__ static __forceinline__ void place(int p, int &r, int &c)
+    {
+        r = p / kRow;
+        c = ((p % kRow) ^ turn(r)) * kPer;
+    }
+    // Fragment of rows i .. i + 15, from the step's first or second half.
+    __device__ static __forceinline__ Piece fragment(const Piece *lds, int i, int half, int lane)
+    {
+        const int j = lane & 15, g = lane >> 4;
+        if constexpr (!kAcross) {
+            const int r = i + j;
+            return lds[r * 8 + ((half * 4 + g) ^ turn(r))];
+        } else if constexpr (kElem == 2) {
+            // 16 lanes fetch 4 rows of k, 16 elements each, and get a column each
+            typedef short S4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) S4 *Lds;
+            Piece p;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int r = half * 32 + g * 8 + q * 4 + (j >> 2), c = i / kPer + (j >> 1 & 1);
+                const auto *at = reinterpret_cast<const uint64_t *>(lds + r * kRow + (c ^ turn(r))) + (j & 1);
+                const S4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at));
+                __builtin_memcpy(&p.w[2 * q], &v, 8);
+            }
+            return p;
+        } else {
+            Piece p;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = half * 16 + g * 4 + q, c = i + j;
+                p.w[q] = lds[r * kRow + ((c >> 2) ^ turn(r))].w[c & 3];
+            }
+            return p;
+        }
+    }
+};
+
+// A tile of WM x WN waves of FM x FN fragments each.
+template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN>
+struct Product {
+    static constexpr int kWM = WM, kWN = WN, kFM = FM, kFN = FN;
+    static constexpr int kThreads = 64 * WM * WN, M = 16 * WM * FM, N = 16 * WN * FN;
+    using A = Step<T, kAcrossA, M>;
+    using B = Step<T, kAcrossB, N>;
+    static constexpr int kDepth = A::kDepth;
+    static constexpr int kLds = (A::kPieces + B::kPieces) * 16;
+    static constexpr int kA = A::kPieces / kThreads, kB = B::kPieces / kThreads;
+
+    template <class S, bool kAcross, int COUNT>
+    static __device__ __forceinline__ void fetch(const ProductSide &side, int64_t i0, int64_t k, Piece out[COUNT])
+    {
+#pragma unroll
+        for (int q = 0; q < COUNT; ++q) {
+            int r, c;
+            S::place(threadIdx.x + q * kThreads, r, c);
+            out[q] = kAcross ? fetch_piece<T>(side, k + r, i0 + c) : fetch_piece<T>(side, i0 + r, k + c);
+        }
+    }
+
+    // acc of rows m0 .. of A and n0 .. of B, over k0 <= k < k1 (k0 a multiple of kDepth).
+    static __device__ __forceinline__ void run(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
+                                               int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+        Piece *const la = lds, *const lb = lds + A::kPieces;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
+        Piece pa[kA], pb[kB];
+        if (k0 < k1) {
+            fetch<A, kAcrossA, kA>(a, m0, k0, pa);
+            fetch<B, kAcrossB, kB>(b, n0, k0, pb);
+        }
+        for (int64_t k = k0; k < k1; k += kDepth) {
+#pragma unroll
+            for (int q = 0; q < kA; ++q) la[threadIdx.x + q * kThreads] = pa[q];
+#pragma unroll
+            for (int q = 0; q < kB; ++q) lb[threadIdx.x + q * kThreads] = pb[q];
+            __syncthreads();
+            if (k + kDepth < k1) {
+                fetch<A, kAcrossA, kA>(a, m0, k + kDepth, pa);
+                fetch<B, kAcrossB, kB>(b, n0, k + kDepth, pb);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                Piece fb[FN];
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[j] = B::fragment(lb, (wn * FN + j) * 16, half, lane);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    const Piece fa = A::fragment(la, (wm * FM + i) * 16, half, lane);
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa, fb[j], acc[i][j]);
+                }
+            }
+            __syncthreads();
+        }
+    }
+
+    // Where a lane's values lie: acc[i][j][r] is row m_of(i) + r of A and row n_of(j) of B.
+    static __device__ __forceinline__ int m_of(int i)
+    {
+        const int wave = threadIdx.x >> 6;
+        return ((wave / WN) * FM + i) * 16 + (threadIdx.x >> 4 & 3) * 4;
+    }
+    static __device__ __forceinline__ int n_of(int j)
+    {
+        const int wave = threadIdx.x >> 6;
+        return ((wave % WN) * FN + j) * 16 + (threadIdx.x & 15);
+    }
+};
+
+}  // namespace ul

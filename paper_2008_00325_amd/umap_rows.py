@@ -31,7 +31,9 @@ UMAP_I32 = 8
 UMAP_I64 = 9
 
 EXPORTS = ("umap_rows_lookup", "umap_rows_lookup_grad", "umap_rows_lookup_grad_workspace", "umap_rows_norm",
-           "umap_rows_norm_grad", "umap_rows_norm_grad_workspace")
+           "umap_rows_norm_grad", "umap_rows_norm_grad_workspace", "umap_rows_cross_entropy",
+           "umap_rows_cross_entropy_workspace", "umap_rows_cross_entropy_grad", "umap_rows_cross_entropy_grad_workspace",
+           "umap_rows_distill", "umap_rows_distill_workspace", "umap_rows_distill_grad", "umap_rows_distill_grad_workspace")
 
 _FLOAT = {torch.float32: UMAP_F32, torch.float16: UMAP_F16, torch.bfloat16: UMAP_BF16}
 _ANY = {**_FLOAT, torch.int8: UMAP_I8, torch.float8_e4m3fn: UMAP_F8}
@@ -70,6 +72,14 @@ def lib() -> ctypes.CDLL:
             "umap_rows_norm": ([M, P, i32, f32, M, M, P, i32, f32, M, P], ctypes.c_int),
             "umap_rows_norm_grad": ([M, M, M, P, i32, f32, M, P, P, i64, P], ctypes.c_int),
             "umap_rows_norm_grad_workspace": ([i64, i32], i64),
+            "umap_rows_cross_entropy": ([M, M, P, i32, f32, P, P, P, i64, P], ctypes.c_int),
+            "umap_rows_cross_entropy_workspace": ([i64, i64, i32, i32], i64),
+            "umap_rows_cross_entropy_grad": ([M, M, P, i32, f32, P, P, f32, M, M, i32, P, i64, P], ctypes.c_int),
+            "umap_rows_cross_entropy_grad_workspace": ([i64, i64, i32, i32], i64),
+            "umap_rows_distill": ([M, M, P, i32, M, f32, f32, P, P, P, i64, P], ctypes.c_int),
+            "umap_rows_distill_workspace": ([i64, i64, i32, i32, i32], i64),
+            "umap_rows_distill_grad": ([M, M, P, i32, M, f32, f32, P, P, f32, M, M, i32, P, i64, P], ctypes.c_int),
+            "umap_rows_distill_grad_workspace": ([i64, i64, i32, i32, i32], i64),
         }
         for name, (args, result) in sig.items():
             fn = getattr(L, name)
@@ -228,6 +238,115 @@ def umap_rows_norm_grad(dy, h, dx, weight=None, dh=None, dweight=None, workspace
     lib()
     _check(_call["umap_rows_norm_grad"](Y, H, U, w, w_kind, eps, X, dw, work, size, _stream(stream)))
     increment_version(dx if dweight is None else (dx, dweight))
+
+
+def _type(dtype) -> int:
+    kind = _FLOAT.get(dtype)
+    if kind is None:
+        raise ValueError(f"rows must not hold {dtype}")
+    return kind
+
+
+def _head_ids(ids, n: int, name: str) -> tuple:
+    if ids is None:
+        raise ValueError(f"{name} must be given")
+    kind = _IDS.get(ids.dtype)
+    if kind is None:
+        raise ValueError(f"{name} must hold int32 or int64, got {ids.dtype}")
+    if ids.numel() != n:
+        raise ValueError(f"{name} holds {ids.numel()} ids, the call needs {n}")
+    return _flat(ids, name, None, n), kind
+
+
+def _head_grads(dh, dtable) -> tuple:
+    return (None if dh is None else _rows(dh, "dh", _FLOAT)[0], None if dtable is None else _rows(dtable, "dtable", _FLOAT)[0])
+
+
+def umap_rows_cross_entropy_workspace(n: int, rows: int, cols: int, dtype) -> int:
+    """Bytes of umap_rows_cross_entropy's workspace, for n rows and a table of rows x cols of `dtype`."""
+    return _count(lib().umap_rows_cross_entropy_workspace(n, rows, cols, _type(dtype)))
+
+
+def umap_rows_cross_entropy(h, table, targets, loss, lse, workspace, scale: float = 1.0, stream=None) -> None:
+    """loss[t] = lse[t] - z[t, targets[t]], lse = logsumexp(z), z = scale * h @ table.T (which is not kept).
+
+    Rows whose target lies outside the table have loss 0."""
+    H, n, _ = _rows(h, "h", _FLOAT)
+    W, _, _ = _rows(table, "table", _FLOAT)
+    at, kind = _head_ids(targets, n, "targets")
+    f32 = torch.float32
+    out, sums = _flat(loss, "loss", f32, n), _flat(lse, "lse", f32, n)
+    work, size = _work(workspace)
+    lib()
+    _check(_call["umap_rows_cross_entropy"](H, W, at, kind, scale, out, sums, work, size, _stream(stream)))
+    increment_version((loss, lse))
+
+
+def umap_rows_cross_entropy_grad_workspace(n: int, rows: int, cols: int, dtype) -> int:
+    """Bytes of umap_rows_cross_entropy_grad's workspace."""
+    return _count(lib().umap_rows_cross_entropy_grad_workspace(n, rows, cols, _type(dtype)))
+
+
+def umap_rows_cross_entropy_grad(h, table, targets, lse, workspace, dh=None, dtable=None, dloss=None, dscale: float = 1.0,
+                                 scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """Gradient of dscale * sum(dloss * loss) for h, into dh, and for the table, into dtable (with `accumulate` added to
+    it); dloss None: ones.  Either may be left out.  Rows without a target and rows of weight 0 take no part."""
+    H, n, _ = _rows(h, "h", _FLOAT)
+    W, _, _ = _rows(table, "table", _FLOAT)
+    at, kind = _head_ids(targets, n, "targets")
+    sums = _flat(lse, "lse", torch.float32, n)
+    weights = None if dloss is None else _flat(dloss, "dloss", torch.float32, n)
+    dH, dW = _head_grads(dh, dtable)
+    work, size = _work(workspace)
+    lib()
+    _check(_call["umap_rows_cross_entropy_grad"](H, W, at, kind, scale, sums, weights, dscale, dH, dW,
+                                                 1 if accumulate else 0, work, size, _stream(stream)))
+    increment_version([x for x in (dh, dtable) if x is not None])
+
+
+def umap_rows_distill_workspace(n: int, rows: int, cols: int, k: int, dtype) -> int:
+    """Bytes of umap_rows_distill's workspace, for n rows with k tokens each and a table of rows x cols of `dtype`."""
+    return _count(lib().umap_rows_distill_workspace(n, rows, cols, k, _type(dtype)))
+
+
+def umap_rows_distill(h, table, ids, teacher, loss, lse, workspace, scale: float = 1.0, teacher_scale: float = 1.0,
+                      stream=None) -> None:
+    """loss[t] = sum over e of q[t, e] * (log q[t, e] - log p[t, ids[t, e]]), q = softmax(teacher_scale * teacher) over the
+    row's tokens, p = softmax(scale * h @ table.T) over the table; lse as for umap_rows_cross_entropy.
+
+    Places whose id lies outside the table are empty; a row with empty places only has loss 0."""
+    H, n, _ = _rows(h, "h", _FLOAT)
+    W, _, _ = _rows(table, "table", _FLOAT)
+    A, _, k = _rows(teacher, "teacher", _FLOAT)
+    at, kind = _head_ids(ids, n * k, "ids")
+    f32 = torch.float32
+    out, sums = _flat(loss, "loss", f32, n), _flat(lse, "lse", f32, n)
+    work, size = _work(workspace)
+    lib()
+    _check(_call["umap_rows_distill"](H, W, at, kind, A, scale, teacher_scale, out, sums, work, size, _stream(stream)))
+    increment_version((loss, lse))
+
+
+def umap_rows_distill_grad_workspace(n: int, rows: int, cols: int, k: int, dtype) -> int:
+    """Bytes of umap_rows_distill_grad's workspace."""
+    return _count(lib().umap_rows_distill_grad_workspace(n, rows, cols, k, _type(dtype)))
+
+
+def umap_rows_distill_grad(h, table, ids, teacher, lse, workspace, dh=None, dtable=None, dloss=None, dscale: float = 1.0,
+                           scale: float = 1.0, teacher_scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """Gradient of dscale * sum(dloss * loss) of umap_rows_distill for h and the table; the teacher is constant."""
+    H, n, _ = _rows(h, "h", _FLOAT)
+    W, _, _ = _rows(table, "table", _FLOAT)
+    A, _, k = _rows(teacher, "teacher", _FLOAT)
+    at, kind = _head_ids(ids, n * k, "ids")
+    sums = _flat(lse, "lse", torch.float32, n)
+    weights = None if dloss is None else _flat(dloss, "dloss", torch.float32, n)
+    dH, dW = _head_grads(dh, dtable)
+    work, size = _work(workspace)
+    lib()
+    _check(_call["umap_rows_distill_grad"](H, W, at, kind, A, scale, teacher_scale, sums, weights, dscale, dH, dW,
+                                           1 if accumulate else 0, work, size, _stream(stream)))
+    increment_version([x for x in (dh, dtable) if x is not None])
 
 
 __all__ = [*EXPORTS, "UmapLayoutError", "umap_rows"]
