@@ -170,6 +170,60 @@ int umap_rows_norm_grad(const umap_rows *dy, const umap_rows *h, const umap_rows
 int64_t umap_rows_norm_grad_workspace(int64_t n, int32_t cols);
 
 /*
+ * umap_rows_layer_norm -- mean and variance norm of rows:
+ *   h[t] = x[t] + residual[t]
+ *   y[t] = (h[t] - mean_c h[t][c]) / sqrt(mean_c (h[t][c] - mean h[t])^2 + eps) * weight + bias
+ * all in fp32 from the inputs on; h and y are rounded once each (y is computed
+ * from the unrounded h).
+ *
+ *   x         UMAP_F32, UMAP_F16 or UMAP_BF16, cols 1 .. 32768, rows < 2^31.
+ *   residual  NULL, or rows of x's type.
+ *   h         NULL, or receives h in x's type.  It may be x or the residual itself
+ *             (the same data and stride).
+ *   weight, bias  cols values each of type weight_type and bias_type (UMAP_F32,
+ *             UMAP_F16 or UMAP_BF16), or NULL for ones and for zeros.
+ *   eps       finite, >= 0 (with eps = 0 a row of equal values gives NaN).
+ *   y         UMAP_F32, UMAP_F16 or UMAP_BF16, x's rows and cols.
+ *
+ * Sums of squares beyond fp32's range are formed again from scaled values, so
+ * finite rows have finite norms.  Apart from h's aliases no output may overlap
+ * an input or another output.  Errors: UMAP_E_INVAL, UMAP_E_DEVICE.
+ */
+int umap_rows_layer_norm(const umap_rows *x, const umap_rows *residual, const umap_rows *h, const void *weight,
+                         int32_t weight_type, const void *bias, int32_t bias_type, float eps, const umap_rows *y,
+                         void *stream);
+
+/*
+ * umap_rows_layer_norm_grad -- its gradient.  With u = (h - mean h) rho,
+ * rho = 1 / sqrt(mean (h - mean h)^2 + eps) and g = dy * weight:
+ *   dx[t]   = rho (g - mean_c g - u mean_c(g u)) + dh[t]
+ *   dweight = sum_t dy[t] * u[t],  dbias = sum_t dy[t]
+ * in fp32, rounded once.  dx is the gradient of h, which is also x's and the
+ * residual's.
+ *
+ *   dy, h    UMAP_F32, UMAP_F16 or UMAP_BF16, of one type, cols 1 .. 32768,
+ *            rows < 2^31.
+ *   dh       NULL, or the gradient that reaches h by other ways (the same type).
+ *   weight   as for umap_rows_layer_norm.
+ *   dx       the same type; receives the gradient of h.  It may be dy or dh itself
+ *            (the same data and stride).
+ *   dweight, dbias  NULL, or cols fp32 each, overwritten; rows are added in a fixed
+ *            order.
+ *   workspace  NULL when both are NULL, else workspace_bytes >=
+ *            umap_rows_layer_norm_grad_workspace(rows, cols) bytes of device
+ *            memory, 16-byte aligned, as for umap_rows_lookup_grad.
+ *
+ * Apart from dx's aliases no output may overlap an input or another output.
+ * Errors: UMAP_E_INVAL, UMAP_E_DEVICE.
+ */
+int umap_rows_layer_norm_grad(const umap_rows *dy, const umap_rows *h, const umap_rows *dh, const void *weight,
+                              int32_t weight_type, float eps, const umap_rows *dx, float *dweight, float *dbias,
+                              void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of umap_rows_layer_norm_grad's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+int64_t umap_rows_layer_norm_grad_workspace(int64_t n, int32_t cols);
+
+/*
  * umap_rows_cross_entropy -- softmax cross entropy of rows against a whole table:
  *   z[t][v] = scale * sum_c h[t][c] table[v][c]
  *   lse[t]  = log sum_v exp z[t][v]

@@ -156,13 +156,13 @@ int check_workspace(const void *workspace, int64_t have, int64_t need)
     return UMAP_OK;
 }
 
-int check_weight(const void *weight, int32_t type, ul::RowWeight *out)
+int check_weight(const void *weight, int32_t type, ul::RowWeight *out, const char *name = "weight")
 {
     *out = {weight, UMAP_F32};
     if (!weight) return UMAP_OK;
-    if (!is_float(type)) return fail(UMAP_E_INVAL, "weight_type %d is not a float type", type);
+    if (!is_float(type)) return fail(UMAP_E_INVAL, "%s_type %d is not a float type", name, type);
     out->type = type;
-    if ((uintptr_t)weight % elem_bytes(type)) return fail(UMAP_E_INVAL, "weight is not aligned");
+    if ((uintptr_t)weight % elem_bytes(type)) return fail(UMAP_E_INVAL, "%s is not aligned", name);
     return UMAP_OK;
 }
 
@@ -418,6 +418,85 @@ int umap_rows_norm_grad(const umap_rows *dy, const umap_rows *h, const umap_rows
     return launched(ul::launch_rows_norm_grad(*dy, *h, dh, w, eps, *dx, dweight, workspace,
                                               static_cast<hipStream_t>(stream)),
                     "umap_rows_norm_grad");
+}
+
+int umap_rows_layer_norm(const umap_rows *x, const umap_rows *residual, const umap_rows *h, const void *weight,
+                         int32_t weight_type, const void *bias, int32_t bias_type, float eps, const umap_rows *y,
+                         void *stream)
+{
+    UL_TRY(check(x, "x", kMaxNormCols, false, false));
+    UL_TRY(check(y, "y", kMaxNormCols, true, false));
+    const int64_t n = x->rows;
+    UL_TRY(check_norm_sizes(n, x->cols));
+    UL_TRY(check_shape(*y, "y", n, x->cols));
+    if (residual) {
+        UL_TRY(check(residual, "residual", kMaxNormCols, false, false));
+        UL_TRY(check_shape(*residual, "residual", n, x->cols));
+        if (residual->type != x->type) return fail(UMAP_E_INVAL, "residual must have x's type");
+    }
+    if (h) {
+        UL_TRY(check(h, "h", kMaxNormCols, true, false));
+        UL_TRY(check_shape(*h, "h", n, x->cols));
+        if (h->type != x->type) return fail(UMAP_E_INVAL, "h must have x's type");
+    }
+    ul::RowWeight w, b;
+    UL_TRY(check_weight(weight, weight_type, &w));
+    UL_TRY(check_weight(bias, bias_type, &b, "bias"));
+    UL_TRY(check_eps(eps));
+    const Span none = flat(nullptr, 0), xs = span(*x), rs = residual ? span(*residual) : none, hs = h ? span(*h) : none,
+               ws = flat(weight, (int64_t)x->cols * elem_bytes(w.type)), bs = flat(bias, (int64_t)x->cols * elem_bytes(b.type));
+    const bool h_is_x = h && same_place(*h, *x), h_is_r = h && residual && same_place(*h, *residual);
+    UL_TRY(refuse_overlap("y", span(*y), {xs, rs, hs, ws, bs}));
+    UL_TRY(refuse_overlap("h", hs, {h_is_x ? none : xs, h_is_r ? none : rs, ws, bs}));
+    if (n == 0) return UMAP_OK;
+    return launched(ul::launch_rows_layer_norm(*x, residual, h, w, b, eps, *y, static_cast<hipStream_t>(stream)),
+                    "umap_rows_layer_norm");
+}
+
+int64_t umap_rows_layer_norm_grad_workspace(int64_t n, int32_t cols)
+{
+    UL_TRY(check_norm_sizes(n, cols));
+    return ul::rows_layer_norm_grad_bytes(n, cols);
+}
+
+int umap_rows_layer_norm_grad(const umap_rows *dy, const umap_rows *h, const umap_rows *dh, const void *weight,
+                              int32_t weight_type, float eps, const umap_rows *dx, float *dweight, float *dbias,
+                              void *workspace, int64_t workspace_bytes, void *stream)
+{
+    UL_TRY(check(dy, "dy", kMaxNormCols, false, false));
+    UL_TRY(check(h, "h", kMaxNormCols, false, false));
+    UL_TRY(check(dx, "dx", kMaxNormCols, true, false));
+    const int64_t n = dy->rows;
+    const int32_t cols = dy->cols;
+    UL_TRY(check_norm_sizes(n, cols));
+    UL_TRY(check_shape(*h, "h", n, cols));
+    UL_TRY(check_shape(*dx, "dx", n, cols));
+    if (dh) {
+        UL_TRY(check(dh, "dh", kMaxNormCols, false, false));
+        UL_TRY(check_shape(*dh, "dh", n, cols));
+    }
+    if (h->type != dy->type || dx->type != dy->type || (dh && dh->type != dy->type))
+        return fail(UMAP_E_INVAL, "dy, h, dh and dx must have one type");
+    ul::RowWeight w;
+    UL_TRY(check_weight(weight, weight_type, &w));
+    UL_TRY(check_eps(eps));
+    UL_TRY(check_floats(dweight, "dweight", cols, false));
+    UL_TRY(check_floats(dbias, "dbias", cols, false));
+    const bool sums = dweight || dbias;
+    const int64_t need = sums ? ul::rows_layer_norm_grad_bytes(n, cols) : 0;
+    if (sums) UL_TRY(check_workspace(workspace, workspace_bytes, need));
+    const Span none = flat(nullptr, 0), ys = span(*dy), hs = span(*h), us = dh ? span(*dh) : none,
+               ws = flat(weight, (int64_t)cols * elem_bytes(w.type)), os = span(*dx), gs = flat(dweight, (int64_t)cols * 4),
+               bs = flat(dbias, (int64_t)cols * 4), work = flat(sums ? workspace : nullptr, need);
+    const bool is_dy = same_place(*dx, *dy), is_dh = dh && same_place(*dx, *dh);
+    UL_TRY(refuse_overlap("dx", os, {is_dy ? none : ys, hs, is_dh ? none : us, ws, gs, bs, work}));
+    UL_TRY(refuse_overlap("dweight", gs, {ys, hs, us, ws, bs, work}));
+    UL_TRY(refuse_overlap("dbias", bs, {ys, hs, us, ws, work}));
+    UL_TRY(refuse_overlap("workspace", work, {ys, hs, us, ws}));
+    if (n == 0 && !sums) return UMAP_OK;
+    return launched(ul::launch_rows_layer_norm_grad(*dy, *h, dh, w, eps, *dx, dweight, dbias, workspace,
+                                                    static_cast<hipStream_t>(stream)),
+                    "umap_rows_layer_norm_grad");
 }
 
 int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type)

@@ -35,6 +35,14 @@ int64_t rows_norm_grad_bytes(int64_t n, int32_t cols);
 hipError_t launch_rows_norm_grad(const umap_rows &dy, const umap_rows &h, const umap_rows *dh, RowWeight weight,
                                  float eps, const umap_rows &dx, float *dweight, void *workspace, hipStream_t s);
 
+// residual and h may be null.
+hipError_t launch_rows_layer_norm(const umap_rows &x, const umap_rows *residual, const umap_rows *h, RowWeight weight,
+                                  RowWeight bias, float eps, const umap_rows &y, hipStream_t s);
+int64_t rows_layer_norm_grad_bytes(int64_t n, int32_t cols);
+// dh, dweight and dbias may be null.
+hipError_t launch_rows_layer_norm_grad(const umap_rows &dy, const umap_rows &h, const umap_rows *dh, RowWeight weight, float eps,
+                                       const umap_rows &dx, float *dweight, float *dbias, void *workspace, hipStream_t s);
+
 // ---- head: loss of rows against a table, with its gradient ----
 // teacher may be null: one token a row, with share 1.
 int64_t rows_head_bytes(int64_t n, int64_t vocab);

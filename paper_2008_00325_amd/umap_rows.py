@@ -31,8 +31,10 @@ UMAP_I32 = 8
 UMAP_I64 = 9
 
 EXPORTS = ("umap_rows_lookup", "umap_rows_lookup_grad", "umap_rows_lookup_grad_workspace", "umap_rows_norm",
-           "umap_rows_norm_grad", "umap_rows_norm_grad_workspace", "umap_rows_cross_entropy",
-           "umap_rows_cross_entropy_workspace", "umap_rows_cross_entropy_grad", "umap_rows_cross_entropy_grad_workspace",
+           "umap_rows_norm_grad", "umap_rows_norm_grad_workspace", "umap_rows_layer_norm",
+           "umap_rows_layer_norm_grad", "umap_rows_layer_norm_grad_workspace",
+           "umap_rows_cross_entropy", "umap_rows_cross_entropy_workspace",
+           "umap_rows_cross_entropy_grad", "umap_rows_cross_entropy_grad_workspace",
            "umap_rows_distill", "umap_rows_distill_workspace", "umap_rows_distill_grad", "umap_rows_distill_grad_workspace")
 
 _FLOAT = {torch.float32: UMAP_F32, torch.float16: UMAP_F16, torch.bfloat16: UMAP_BF16}
@@ -72,6 +74,9 @@ def lib() -> ctypes.CDLL:
             "umap_rows_norm": ([M, P, i32, f32, M, M, P, i32, f32, M, P], ctypes.c_int),
             "umap_rows_norm_grad": ([M, M, M, P, i32, f32, M, P, P, i64, P], ctypes.c_int),
             "umap_rows_norm_grad_workspace": ([i64, i32], i64),
+            "umap_rows_layer_norm": ([M, M, M, P, i32, P, i32, f32, M, P], ctypes.c_int),
+            "umap_rows_layer_norm_grad": ([M, M, M, P, i32, f32, M, P, P, P, i64, P], ctypes.c_int),
+            "umap_rows_layer_norm_grad_workspace": ([i64, i32], i64),
             "umap_rows_cross_entropy": ([M, M, P, i32, f32, P, P, P, i64, P], ctypes.c_int),
             "umap_rows_cross_entropy_workspace": ([i64, i64, i32, i32], i64),
             "umap_rows_cross_entropy_grad": ([M, M, P, i32, f32, P, P, f32, M, M, i32, P, i64, P], ctypes.c_int),
@@ -148,15 +153,15 @@ def _id_args(ids, n: int) -> tuple:
     return _flat(ids, "ids", None, n), kind
 
 
-def _weight_args(weight, cols: int) -> tuple:
+def _weight_args(weight, cols: int, name: str = "weight") -> tuple:
     if weight is None:
         return None, 0
     kind = _FLOAT.get(weight.dtype)
     if kind is None:
-        raise ValueError(f"weight must hold a float type, got {weight.dtype}")
+        raise ValueError(f"{name} must hold a float type, got {weight.dtype}")
     if weight.numel() != cols:
-        raise ValueError(f"{weight.numel()} weights for {cols} columns")
-    return _flat(weight, "weight", None, cols), kind
+        raise ValueError(f"{weight.numel()} {name}{'' if name.endswith('s') else 's'} for {cols} columns")
+    return _flat(weight, name, None, cols), kind
 
 
 def _work(workspace) -> tuple:
@@ -238,6 +243,43 @@ def umap_rows_norm_grad(dy, h, dx, weight=None, dh=None, dweight=None, workspace
     lib()
     _check(_call["umap_rows_norm_grad"](Y, H, U, w, w_kind, eps, X, dw, work, size, _stream(stream)))
     increment_version(dx if dweight is None else (dx, dweight))
+
+
+def umap_rows_layer_norm(x, y, weight=None, bias=None, residual=None, h=None, eps: float = 1e-5, stream=None) -> None:
+    """h = x + residual; y = (h - mean h) / sqrt(mean (h - mean h)^2 + eps) * weight + bias, row by row.
+
+    h may be x or the residual itself."""
+    X, _, cols = _rows(x, "x", _FLOAT)
+    Y, _, _ = _rows(y, "y", _FLOAT)
+    S = None if residual is None else _rows(residual, "residual", _FLOAT)[0]
+    H = None if h is None else _rows(h, "h", _FLOAT)[0]
+    w, w_kind = _weight_args(weight, cols)
+    b, b_kind = _weight_args(bias, cols, "bias")
+    lib()
+    _check(_call["umap_rows_layer_norm"](X, S, H, w, w_kind, b, b_kind, eps, Y, _stream(stream)))
+    increment_version(y if h is None else (y, h))
+
+
+def umap_rows_layer_norm_grad_workspace(n: int, cols: int) -> int:
+    """Bytes of umap_rows_layer_norm_grad's workspace."""
+    return _count(lib().umap_rows_layer_norm_grad_workspace(n, cols))
+
+
+def umap_rows_layer_norm_grad(dy, h, dx, weight=None, dh=None, dweight=None, dbias=None, workspace=None, eps: float = 1e-5,
+                              stream=None) -> None:
+    """Gradient of umap_rows_layer_norm for h (plus `dh`, what reaches h otherwise), into dx (which may be dy or dh
+    itself), for the weight, into dweight, and for the bias, into dbias (both fp32; they need the workspace)."""
+    Y, _, cols = _rows(dy, "dy", _FLOAT)
+    H, _, _ = _rows(h, "h", _FLOAT)
+    X, _, _ = _rows(dx, "dx", _FLOAT)
+    U = None if dh is None else _rows(dh, "dh", _FLOAT)[0]
+    w, w_kind = _weight_args(weight, cols)
+    dw = None if dweight is None else _flat(dweight, "dweight", torch.float32, cols)
+    db = None if dbias is None else _flat(dbias, "dbias", torch.float32, cols)
+    work, size = _work(workspace)
+    lib()
+    _check(_call["umap_rows_layer_norm_grad"](Y, H, U, w, w_kind, eps, X, dw, db, work, size, _stream(stream)))
+    increment_version([x for x in (dx, dweight, dbias) if x is not None])
 
 
 def _type(dtype) -> int:
