@@ -54,11 +54,6 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// Tiles of a grid of `m` x `n` of them, one per workgroup.
-struct Tiles {
-    int m, n;
-};
-
 // ---- the logits' tiles: forward -------------------------------------------------------------
 
 template <int T, class P>
@@ -66,8 +61,8 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
-    const int tm = blockIdx.x % tiles.m, tn = blockIdx.x / tiles.m;
-    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N;
+    const TileAt at = tile_at(tiles, blockIdx.x);
+    const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
     P::run(w, h, m0, n0, 0, w.cols, lds, acc);
     MaxSum(*const part)[P::N] = reinterpret_cast<MaxSum(*)[P::N]>(lds);   // behind the product's last barrier
@@ -99,7 +94,7 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
         MaxSum all = part[0][n];
 #pragma unroll
         for (int i = 1; i < P::kWM; ++i) all.join(part[i][n]);
-        partial[(n0 + n) * tiles.m + tm] = all;
+        partial[(n0 + n) * tiles.m + at.m] = all;
     }
 }
 
@@ -358,8 +353,8 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
-    const int tm = blockIdx.x % tiles.m, tn = blockIdx.x / tiles.m;
-    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N;
+    const TileAt at = tile_at(tiles, blockIdx.x);
+    const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
     P::run(w, h, m0, n0, 0, w.cols, lds, acc);
     const int live = (int)min((int64_t)P::M, w.rows - m0);
@@ -400,9 +395,9 @@ __global__ __launch_bounds__(P::kThreads) void k_head_dh(ProductSide w, ProductS
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
-    const int tile = blockIdx.x % (tiles.m * tiles.n), split = blockIdx.x / (tiles.m * tiles.n);
-    const int tm = tile % tiles.m, tn = tile / tiles.m;
-    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N, k0 = split * depth;
+    const int split = blockIdx.x / (tiles.m * tiles.n);
+    const TileAt tile = tile_at(tiles, blockIdx.x % (tiles.m * tiles.n));
+    const int64_t m0 = (int64_t)tile.m * P::M, n0 = (int64_t)tile.n * P::N, k0 = split * depth;
     Acc4 acc[FM][FN];
     P::run(w, d, m0, n0, k0, min(k0 + depth, w.rows), lds, acc);
     float *const to = sums + split * d.rows * pitch;
@@ -450,8 +445,8 @@ __global__ __launch_bounds__(P::kThreads) void k_head_dw(ProductSide h, ProductS
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
-    const int tm = blockIdx.x % tiles.m, tn = blockIdx.x / tiles.m;
-    const int64_t m0 = (int64_t)tm * P::M, n0 = (int64_t)tn * P::N;
+    const TileAt at = tile_at(tiles, blockIdx.x);
+    const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
     P::run(h, d, m0, n0, 0, h.rows, lds, acc);
     const int e = h.rows > 0 ? largest_of(weights) - kShift<T> : 0;
@@ -554,10 +549,19 @@ struct GradSizes {
     }
 };
 
-template <int T, bool AA, bool AB>
-using Large = Product<T, AA, AB, 2, 4, 8, 4>;
-template <int T, bool AA, bool AB>
-using Small = Product<T, AA, AB, 2, 2, 4, 4>;
+template <int T, bool AA, bool AB, bool kDirect>
+using Large = Product<T, AA, AB, 2, 4, 8, 4, kDirect ? 2 : 0>;
+template <int T, bool AA, bool AB, bool kDirect>
+using Small = Product<T, AA, AB, 2, 2, 4, 4, kDirect ? 4 : 0>;
+
+// Calls f with the shape of a product's tiles: its size, and whether its sides go straight to LDS.
+template <int T, bool AA, bool AB, typename F>
+hipError_t by_shape(bool large, const ProductSide &a, const ProductSide &b, F f)
+{
+    const bool direct = direct_side<T>(a) && direct_side<T>(b);
+    if (large) return direct ? f(Large<T, AA, AB, true>{}) : f(Large<T, AA, AB, false>{});
+    return direct ? f(Small<T, AA, AB, true>{}) : f(Small<T, AA, AB, false>{});
+}
 
 template <class P>
 Tiles tiles_of(int64_t m, int64_t n)
@@ -571,15 +575,6 @@ ProductSide side_of(const umap_rows &m, int64_t first, int64_t rows)
     return {static_cast<const Elem<T> *>(m.data) + first * m.stride, m.stride, rows, m.cols};
 }
 
-template <int T, class P>
-hipError_t lse_tiles(const ProductSide &w, const ProductSide &h, float scale, MaxSum *partial, int64_t *tiles, hipStream_t s)
-{
-    const Tiles g = tiles_of<P>(w.rows, h.rows);
-    *tiles = g.m;
-    hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, h, scale, g, partial);
-    return hipGetLastError();
-}
-
 template <int T>
 hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught, float scale, float *out, float *lse,
                 void *workspace, hipStream_t s)
@@ -590,42 +585,20 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
     for (int64_t first = 0; first < h.rows; first += z.rows) {
         const ProductSide rows = side_of<T>(h, first, std::min(z.rows, h.rows - first));
         int64_t tiles = 0;
-        hipError_t e = large_tiles(w.rows, rows.rows) ? lse_tiles<T, Large<T, false, false>>(w, rows, scale, partial, &tiles, s)
-                                                      : lse_tiles<T, Small<T, false, false>>(w, rows, scale, partial, &tiles, s);
+        hipError_t e = by_shape<T, false, false>(large_tiles(w.rows, rows.rows), w, rows, [&](auto shape) {
+            using P = decltype(shape);
+            const Tiles g = tiles_of<P>(w.rows, rows.rows);
+            tiles = g.m;
+            hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
+                               partial);
+            return hipGetLastError();
+        });
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL((k_head_loss<T>), dim3((unsigned)over(rows.rows, 4)), dim3(256), 0, s, w, rows, scale, taught, first,
                            tiles, partial, out, lse);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     return hipSuccess;
-}
-
-template <int T, template <int, bool, bool> class Shape>
-hipError_t d_tiles(const ProductSide &w, const ProductSide &h, float scale, const float *lse, const RowWeights &weights, Elem<T> *d,
-                   int64_t pitch, hipStream_t s)
-{
-    using P = Shape<T, false, false>;
-    const Tiles g = tiles_of<P>(pitch, h.rows);
-    hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, h, scale, g, lse,
-                       weights, d, pitch);
-    return hipGetLastError();
-}
-template <int T, template <int, bool, bool> class Shape>
-hipError_t dh_tiles(const ProductSide &w, const ProductSide &d, const GradSizes &z, bool add, float *sums, hipStream_t s)
-{
-    using P = Shape<T, true, false>;
-    const Tiles g = tiles_of<P>(z.cols, z.n);
-    hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s, w, d, g,
-                       z.depth, add, sums, z.sum_pitch);
-    return hipGetLastError();
-}
-template <int T, template <int, bool, bool> class Shape>
-hipError_t dw_tiles(const ProductSide &h, const ProductSide &d, const RowWeights &weights, bool add, const umap_rows &dw, hipStream_t s)
-{
-    using P = Shape<T, true, true>;
-    const Tiles g = tiles_of<P>(dw.cols, dw.rows);
-    hipLaunchKernelGGL((k_head_dw<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, h, d, g, weights, add, dw);
-    return hipGetLastError();
 }
 
 #define UL_LAUNCHED(expr)                      \
@@ -660,26 +633,43 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                            (int)z.h_pitch);
         UL_LAUNCHED(hipGetLastError());
     }
-    const ProductSide rows{copy, z.h_pitch, z.n, z.cols}, weighted{scaled ? scaled : copy, z.h_pitch, z.n, z.cols};
+    // the copies' and D's columns past the last are zeros, and so are pieces of them
+    const ProductSide rows{copy, z.h_pitch, z.n, z.h_pitch}, weighted{scaled ? scaled : copy, z.h_pitch, z.n, z.h_pitch};
     for (int64_t first = 0; first < z.vocab; first += z.piece) {
         const int64_t here = std::min(z.piece, z.vocab - first);
-        const ProductSide w = side_of<T>(table, first, here), d_side{d, z.d_pitch, z.n, here};
+        const ProductSide w = side_of<T>(table, first, here), d_side{d, z.d_pitch, z.n, z.d_pitch};
         if (z.n > 0) {
-            UL_LAUNCHED(large_tiles(here, z.n) ? (d_tiles<T, Large>(w, rows, scale, lse, weights, d, z.d_pitch, s))
-                                               : (d_tiles<T, Small>(w, rows, scale, lse, weights, d, z.d_pitch, s)));
+            UL_LAUNCHED((by_shape<T, false, false>(large_tiles(here, z.n), w, rows, [&](auto shape) {
+                using P = decltype(shape);
+                const Tiles g = tiles_of<P>(z.d_pitch, z.n);
+                hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
+                                   lse, weights, d, z.d_pitch);
+                return hipGetLastError();
+            })));
             hipLaunchKernelGGL((k_head_own<T>), dim3((unsigned)std::min<int64_t>(1024, over(z.n * z.k, 256))), dim3(256), 0, s,
                                token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch);
             UL_LAUNCHED(hipGetLastError());
             if (dh)
-                UL_LAUNCHED(large_tiles(z.cols, z.n) ? (dh_tiles<T, Large>(w, d_side, z, first > 0, sums, s))
-                                                     : (dh_tiles<T, Small>(w, d_side, z, first > 0, sums, s)));
+                UL_LAUNCHED((by_shape<T, true, false>(large_tiles(z.cols, z.n), w, d_side, [&](auto shape) {
+                    using P = decltype(shape);
+                    const Tiles g = tiles_of<P>(z.cols, z.n);
+                    hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s, w,
+                                       d_side, g, z.depth, first > 0, sums, z.sum_pitch);
+                    return hipGetLastError();
+                })));
         }
         if (dtable) {
             umap_rows part = *dtable;
             part.data = static_cast<Elem<T> *>(dtable->data) + first * dtable->stride;
             part.rows = here;
-            UL_LAUNCHED(large_tiles(z.cols, here) ? (dw_tiles<T, Large>(weighted, d_side, weights, add, part, s))
-                                                  : (dw_tiles<T, Small>(weighted, d_side, weights, add, part, s)));
+            auto table_rows = [&](auto shape) {
+                using P = decltype(shape);
+                const Tiles g = tiles_of<P>(z.cols, here);
+                hipLaunchKernelGGL((k_head_dw<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, weighted, d_side, g,
+                                   weights, add, part);
+                return hipGetLastError();
+            };
+            UL_LAUNCHED(large_tiles(z.cols, here) ? table_rows(Large<T, true, true, true>{}) : table_rows(Small<T, true, true, true>{}));
         }
     }
     if (dh && z.n > 0) {

@@ -69,13 +69,14 @@ struct Step {
     static constexpr int kElem = sizeof(Elem<T>), kPer = 16 / kElem, kDepth = 128 / kElem;
     static constexpr int kRow = kAcross ? I / kPer : 8;   // pieces of a row in LDS
     static constexpr int kPieces = I * 8;
+    static constexpr int kReads = !kAcross ? 1 : kElem == 2 ? 2 : 4;   // LDS reads of a fragment
     // How the pieces of row r are turned: along k, the 8 lanes that read 16 bytes at once are of 8
-    // rows; across, 32 lanes read 32 bytes of 8 rows (fp32: 64 lanes 64 bytes of 4 rows).
+    // rows; across, 32 lanes read 32 bytes of 8 rows (fp32: 64 bytes of 2 rows).
     __device__ static __forceinline__ int turn(int r)
     {
         if constexpr (!kAcross) return r & 7;
         else if constexpr (kElem == 2) return ((r & 3) | (r >> 1 & 4)) << 1;
-        else return (r & 12);
+        else return r & 4;
     }
     // Row and column of LDS piece p, in memory, from the tile's origin.
     __device__ static __forceinline__ void place(int p, int &r, int &c)
@@ -115,15 +116,84 @@ struct Step {
     }
 };
 
-// A tile of WM x WN waves of FM x FN fragments each.
-template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN>
+// Whether a side is made of whole pieces at 16-byte places, close enough together for 32-bit offsets.
+template <int T>
+bool direct_side(const ProductSide &s)
+{
+    constexpr int kElem = sizeof(Elem<T>), kPer = 16 / kElem;
+    return (uintptr_t)s.data % 16 == 0 && s.stride % kPer == 0 && s.cols % kPer == 0 && s.stride < ((int64_t)1 << 30) / 256 / kElem;
+}
+
+// All of this wave's loads into LDS but the newest `left` have landed, then all waves'.
+template <int LEFT>
+__device__ __forceinline__ void landed()
+{
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // LDS reads alone; the compiler, which counts them, is to know
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// One side's loads straight into LDS: 64 lanes, 64 pieces next to each other.  Lanes whose piece lies outside the
+// matrix are given an offset beyond the buffer, which loads zeros.
+template <int T, bool kAcross, int I, int THREADS>
+struct DirectSide {
+    using S = Step<T, kAcross, I>;
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    static constexpr int kElem = S::kElem, kCount = S::kPieces / THREADS, kRows = THREADS / S::kRow;
+    int row, col;
+    uint32_t offset;
+    static_assert(kRows % (kAcross && kElem == 2 ? 16 : 8) == 0, "a piece's row is turned alike kRows rows on");
+    __device__ __forceinline__ DirectSide(const ProductSide &side, int64_t i0)
+    {
+        S::place(threadIdx.x, row, col);
+        offset = (uint32_t)((row * side.stride + col) * kElem);
+        if (kAcross && i0 + col >= side.cols) offset = 0x80000000u;
+    }
+    __device__ __forceinline__ void load(const ProductSide &side, int64_t i0, int64_t k, bool there, Piece *to, int wave) const
+    {
+        const int64_t r0 = kAcross ? k : i0, c0 = kAcross ? i0 : k;
+        const char *const base = static_cast<const char *>(side.data) + (r0 * side.stride + c0) * kElem;
+        const int64_t rows = min((int64_t)(kAcross ? S::kDepth : I), side.rows - r0);
+        const Words buffer = {(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu,
+                              there && rows > 0 ? (uint32_t)(rows * side.stride * kElem) : 0u, 0x00027000u};
+        const uint32_t at = !kAcross && k + col >= side.cols ? 0x80000000u : offset;
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) Piece *)to + wave * 1024, step = (uint32_t)(kRows * side.stride * kElem);
+#pragma unroll
+        for (int q = 0; q < kCount; ++q)
+            // the whole offset in the lane's register: it is what the hardware compares with the buffer's length
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + q * THREADS * 16),
+                         "v"(at + q * step), "s"(buffer)
+                         : "memory");
+    }
+};
+
+// Tiles of a grid of m x n of them, one per workgroup.  Workgroups go round the 8 XCDs in turn; each XCD takes a
+// stretch of the tiles, which goes over 8 rows of tiles at a time, so that the 32 tiles it works on at once
+// share their sides' panels in its L2.
+struct Tiles {
+    int m, n;
+};
+struct TileAt {
+    int m, n;
+};
+__device__ __forceinline__ TileAt tile_at(const Tiles &tiles, int block)
+{
+    constexpr int kXcds = 8, kRows = 8;
+    const int total = tiles.m * tiles.n, each = total / kXcds, more = total % kXcds, xcd = block % kXcds;
+    const int id = xcd * each + min(xcd, more) + block / kXcds;
+    const int band = id / (kRows * tiles.n), first = band * kRows, rows = min(kRows, tiles.m - first), in = id - first * tiles.n;
+    return {first + in % rows, in / rows};
+}
+
+// A tile of WM x WN waves of FM x FN fragments each.  DEPTH 0: any sides; else steps in LDS at once, for sides in
+// whole pieces (direct_side).
+template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN, int DEPTH>
 struct Product {
     static constexpr int kWM = WM, kWN = WN, kFM = FM, kFN = FN;
     static constexpr int kThreads = 64 * WM * WN, M = 16 * WM * FM, N = 16 * WN * FN;
     using A = Step<T, kAcrossA, M>;
     using B = Step<T, kAcrossB, N>;
     static constexpr int kDepth = A::kDepth;
-    static constexpr int kLds = (A::kPieces + B::kPieces) * 16;
+    static constexpr int kLds = (A::kPieces + B::kPieces) * 16 * (DEPTH ? DEPTH : 1);
     static constexpr int kA = A::kPieces / kThreads, kB = B::kPieces / kThreads;
 
     template <class S, bool kAcross, int COUNT>
@@ -140,6 +210,13 @@ struct Product {
     // acc of rows m0 .. of A and n0 .. of B, over k0 <= k < k1 (k0 a multiple of kDepth).
     static __device__ __forceinline__ void run(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
                                                int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
+    {
+        if constexpr (DEPTH == 0) run_any(a, b, m0, n0, k0, k1, lds, acc);
+        else run_direct(a, b, m0, n0, k0, k1, lds, acc);
+    }
+
+    static __device__ __forceinline__ void run_any(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
+                                                   int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
         Piece *const la = lds, *const lb = lds + A::kPieces;
@@ -176,6 +253,69 @@ struct Product {
             }
             __syncthreads();
         }
+    }
+
+    // Likewise with both sides in whole pieces (direct_side): loads go to LDS by themselves, DEPTH - 1 steps
+    // ahead, and the fragments of a half step are fetched while the half before is multiplied.
+    static __device__ __forceinline__ void run_direct(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
+                                                      int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (k0 >= k1) return;
+        const DirectSide<T, kAcrossA, M, kThreads> da(a, m0);
+        const DirectSide<T, kAcrossB, N, kThreads> db(b, n0);
+        const int steps = (int)((k1 - k0 + kDepth - 1) / kDepth);
+        constexpr int kStage = A::kPieces + B::kPieces;
+        auto load = [&](int s) {
+            Piece *const to = lds + s % DEPTH * kStage;
+            da.load(a, m0, k0 + (int64_t)s * kDepth, s < steps, to, wave);
+            db.load(b, n0, k0 + (int64_t)s * kDepth, s < steps, to + A::kPieces, wave);
+        };
+        Piece fa[2][FM], fb[2][FN];
+        auto fetch_half = [&](int s, int half, int set) {
+            const Piece *const from = lds + s % DEPTH * kStage;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[set][j] = B::fragment(from + A::kPieces, (wn * FN + j) * 16, half, lane);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fa[set][i] = A::fragment(from, (wm * FM + i) * 16, half, lane);
+        };
+        // Fetches and products of a half step in turn, so that LDS serves all waves evenly.
+        auto mix = [] {
+            constexpr int kProducts = FM * FN * (sizeof(Elem<T>) == 4 ? 4 : 1);
+            constexpr int kReads = FM * A::kReads + FN * B::kReads, kEach = kProducts / kReads;
+#pragma unroll
+            for (int q = 0; q < kReads; ++q) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kProducts - kReads * kEach, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto multiply_half = [&](int set) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa[set][i], fb[set][j], acc[i][j]);
+        };
+#pragma unroll
+        for (int s = 0; s < DEPTH; ++s) load(s);
+        landed<(DEPTH - 1) * (kA + kB)>();
+        fetch_half(0, 0, 0);
+        for (int s = 0; s < steps; ++s) {
+            fetch_half(s, 1, 1);
+            multiply_half(0);
+            mix();
+            landed<(DEPTH - 2) * (kA + kB)>();   // step s + 1 is there, and everybody has fetched all of step s
+            load(s + DEPTH);
+            fetch_half(s + 1, 0, 0);   // behind the last step: zeros, which nobody takes
+            multiply_half(1);
+            mix();
+        }
+        landed<0>();
     }
 
     // Where a lane's values lie: acc[i][j][r] is row m_of(i) + r of A and row n_of(j) of B.
