@@ -48,11 +48,6 @@ __device__ __forceinline__ float wave_sum(float v)
     for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
     return v;
 }
-__device__ __forceinline__ float wave_max(float v)
-{
-    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
 
 // ---- the logits' tiles: forward -------------------------------------------------------------
 
@@ -100,7 +95,7 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
 
 // ---- a row's own tokens ----------------------------------------------------------------------
 
-constexpr int kSlots = 4;   // tokens of a lane: a row has up to 256
+constexpr int kMostTokens = 256;   // of a row
 
 struct Taught {
     RowIds ids;
@@ -120,39 +115,69 @@ __device__ __forceinline__ float teacher_at(const Taught &x, int64_t t, int e)
     }
 }
 
-// Lane l holds tokens l, l + 64, ..: id (-1: none) and share.
-struct OwnTokens {
-    int id[kSlots];
-    float share[kSlots], log_share[kSlots];
-    bool any;
-    __device__ __forceinline__ OwnTokens(const Taught &x, int64_t t, int64_t rows, int lane)
+// A row has a wave (up to 64 tokens) or a workgroup of four; each thread one of its tokens.
+template <int WAVES>
+struct RowTeam {
+    static constexpr int kThreads = 64 * WAVES, kRows = 4 / WAVES;   // rows of a workgroup
+    struct Lds {
+        float part[4];
+        int id[kMostTokens];
+        float share[kMostTokens], z[kMostTokens];
+    };
+    Lds *lds;
+    int me, wave;   // in the row
+    __device__ __forceinline__ explicit RowTeam(Lds *l)
+        : lds(l), me(threadIdx.x % kThreads), wave(WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6))
     {
-        float most = minus_inf();
-        bool here = false;
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s) {
-            const int e = lane + 64 * s;
-            id[s] = -1;
-            log_share[s] = minus_inf();
-            if (e < x.k) id[s] = (int)row_of(x.ids, t * x.k + e, rows);
-            if (id[s] >= 0) {
-                log_share[s] = x.teacher ? teacher_at(x, t, e) * x.scale : 0.0f;
-                if (log_share[s] == minus_inf()) id[s] = -1;
-            }
-            most = fmaxf(most, log_share[s]);
-            here |= id[s] >= 0;
+    }
+    template <typename Op>
+    __device__ __forceinline__ float all(float v, Op op) const
+    {
+        for (int o = 1; o < 64; o <<= 1) v = op(v, __shfl_xor(v, o));
+        if constexpr (WAVES > 1) {
+            __syncthreads();
+            if ((me & 63) == 0) lds->part[wave] = v;
+            __syncthreads();
+            v = op(op(lds->part[0], lds->part[1]), op(lds->part[2], lds->part[3]));
         }
-        any = __any(here);
-        most = MaxSum::base(wave_max(most));
-        float sum = 0.0f;
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s) sum += share[s] = id[s] >= 0 ? exp_of(log_share[s] - most) : 0.0f;
-        sum = wave_sum(sum);
-        const float log_sum = logf(sum);
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s) {
-            share[s] = id[s] >= 0 ? share[s] / sum : 0.0f;
-            log_share[s] = log_share[s] - most - log_sum;
+        return v;
+    }
+    __device__ __forceinline__ float sum(float v) const { return all(v, [](float a, float b) { return a + b; }); }
+    __device__ __forceinline__ float max(float v) const { return all(v, [](float a, float b) { return fmaxf(a, b); }); }
+    // Token e's value, for all threads.
+    __device__ __forceinline__ int of(int v, const int *shared, int e) const
+    {
+        return WAVES == 1 ? __builtin_amdgcn_readlane(v, e) : __builtin_amdgcn_readfirstlane(shared[e]);
+    }
+    __device__ __forceinline__ float of(float v, const float *shared, int e) const
+    {
+        return WAVES == 1 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), e)) : shared[e];
+    }
+};
+
+// This thread's token: id (-1: none) and share.
+template <int WAVES>
+struct OwnToken {
+    int id = -1;
+    float share, log_share = minus_inf();
+    bool any;
+    __device__ __forceinline__ OwnToken(const RowTeam<WAVES> &team, const Taught &x, int64_t t, int64_t rows)
+    {
+        if (team.me < x.k) id = (int)row_of(x.ids, t * x.k + team.me, rows);
+        if (id >= 0) {
+            log_share = x.teacher ? teacher_at(x, t, team.me) * x.scale : 0.0f;
+            if (log_share == minus_inf()) id = -1;
+        }
+        if constexpr (WAVES > 1) team.lds->id[team.me] = id;   // read behind the reductions' barriers
+        const float most = MaxSum::base(team.max(log_share));
+        share = id >= 0 ? exp_of(log_share - most) : 0.0f;
+        any = team.max(id >= 0 ? 1.0f : 0.0f) > 0.0f;
+        const float sum = team.sum(share);
+        share = id >= 0 ? share / sum : 0.0f;
+        log_share = log_share - most - logf(sum);
+        if constexpr (WAVES > 1) {
+            team.lds->share[team.me] = share;
+            __syncthreads();
         }
     }
 };
@@ -168,30 +193,26 @@ __device__ __forceinline__ void fetch8(const Elem<T> *row, int c, int cols, floa
     }
 }
 
-// Dot products of a row of h with the table's rows of its tokens, into the tokens' lanes.
-template <int T>
-__device__ __forceinline__ void own_logits(const Elem<T> *h, const ProductSide &w, const OwnTokens &own, int k, int lane,
-                                           float scale, float z[kSlots])
+// Dot products of a row of h with the table's rows of its k tokens: each thread's token's.
+template <int T, int WAVES>
+__device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Elem<T> *h, const ProductSide &w,
+                                           const OwnToken<WAVES> &own, int k, float scale)
 {
     constexpr int kAtOnce = 4;
-    const int cols = (int)w.cols;
+    const int cols = (int)w.cols, lane = team.me & 63;
+    float z = 0.0f;
+    for (int e0 = kAtOnce * team.wave; e0 < k; e0 += kAtOnce * WAVES) {
+        const Elem<T> *row[kAtOnce];
+        float sum[kAtOnce] = {};
+        int id[kAtOnce];
+        bool some = false;
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-        z[s] = 0.0f;
-        const int most = min(64, k - 64 * s);
-        for (int e0 = 0; e0 < most; e0 += kAtOnce) {
-            const Elem<T> *row[kAtOnce];
-            float sum[kAtOnce] = {};
-            int id[kAtOnce];
-            bool some = false;
-#pragma unroll
-            for (int e = 0; e < kAtOnce; ++e) {
-                id[e] = __builtin_amdgcn_readlane(own.id[s], min(e0 + e, 63));
-                if (e0 + e >= most) id[e] = -1;
-                some |= id[e] >= 0;
-                row[e] = static_cast<const Elem<T> *>(w.data) + (int64_t)max(id[e], 0) * w.stride;
-            }
-            if (!some) continue;
+        for (int e = 0; e < kAtOnce; ++e) {
+            id[e] = e0 + e < k ? team.of(own.id, team.lds->id, e0 + e) : -1;
+            some |= id[e] >= 0;
+            row[e] = static_cast<const Elem<T> *>(w.data) + (int64_t)max(id[e], 0) * w.stride;
+        }
+        if (some) {
             for (int c = lane * 8; c < cols; c += 512) {
                 float a[8];
                 fetch8<T>(h, c, cols, a);
@@ -204,38 +225,41 @@ __device__ __forceinline__ void own_logits(const Elem<T> *h, const ProductSide &
                     for (int j = 0; j < 8; ++j) sum[e] = fmaf(a[j], b[j], sum[e]);
                 }
             }
+        }
 #pragma unroll
-            for (int e = 0; e < kAtOnce; ++e) {
-                const float all = wave_sum(sum[e]) * scale;
-                if (lane == e0 + e) z[s] = all;
-            }
+        for (int e = 0; e < kAtOnce; ++e) {
+            const float all = wave_sum(sum[e]) * scale;
+            if constexpr (WAVES == 1) z = lane == e0 + e ? all : z;
+            else if (lane == 0) team.lds->z[e0 + e] = all;
         }
     }
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        z = team.me < k ? team.lds->z[team.me] : 0.0f;
+    }
+    return z;
 }
 
-// A wave per row: joins the row's tiles, and sums its loss.
-template <int T>
+// Joins a row's tiles, and sums its loss.
+template <int T, int WAVES>
 __global__ __launch_bounds__(256) void k_head_loss(ProductSide w, ProductSide h, float scale, Taught taught, int64_t first,
                                                    int64_t tiles, const MaxSum *partial, float *loss, float *lse)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    __shared__ typename RowTeam<WAVES>::Lds lds;
+    const RowTeam<WAVES> team(&lds);
+    const int64_t t = (int64_t)blockIdx.x * RowTeam<WAVES>::kRows + threadIdx.x / RowTeam<WAVES>::kThreads;
     if (t >= h.rows) return;
-    MaxSum all{minus_inf(), 0.0f};
-    for (int64_t i = lane; i < tiles; i += 64) all.join(partial[t * tiles + i]);
-    for (int o = 1; o < 64; o <<= 1) all.join({__shfl_xor(all.m, o), __shfl_xor(all.s, o)});
-    const float sum = all.m + logf(all.s);
-    const OwnTokens own(taught, first + t, w.rows, lane);
-    float z[kSlots], mine = 0.0f;
-    own_logits<T>(static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, lane, scale, z);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s)
-        if (own.id[s] >= 0 && own.share[s] != 0.0f) mine = fmaf(own.share[s], own.log_share[s] + (sum - z[s]), mine);
-    mine = wave_sum(mine);
-    if (lane == 0) {
+    MaxSum mine{minus_inf(), 0.0f};
+    for (int64_t i = team.me; i < tiles; i += RowTeam<WAVES>::kThreads) mine.join(partial[t * tiles + i]);
+    const OwnToken<WAVES> own(team, taught, first + t, w.rows);
+    const float z = own_logit<T, WAVES>(team, static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, scale);
+    const float most = team.max(mine.m);
+    const float sum = most + logf(team.sum(mine.s * exp_of(mine.m - MaxSum::base(most))));
+    const float all = team.sum(own.id >= 0 && own.share != 0.0f ? own.share * (own.log_share + (sum - z)) : 0.0f);
+    if (team.me == 0) {
         lse[first + t] = sum;
         // rounding can take a loss of nearly nothing below it
-        loss[first + t] = !own.any ? 0.0f : mine < 0.0f ? 0.0f : mine;
+        loss[first + t] = !own.any ? 0.0f : all < 0.0f ? 0.0f : all;
     }
 }
 
@@ -282,60 +306,48 @@ __global__ __launch_bounds__(1024) void k_head_largest(const float *dloss, int64
     }
 }
 
-// A wave per row: its weight, its tokens with the entries of D, and the copies of h that the
-// products take, without gaps (`pitch` columns, zeros past the last) and zeros in rows without part.
-template <int T>
+// A row's weight, its tokens with the entries of D, and the copies of h that the products take, without gaps
+// (`pitch` columns, zeros past the last) and zeros in rows without part.
+template <int T, int WAVES>
 __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
                                                    const float *dloss, float factor, RowWeights weights, int *token,
                                                    float *value, Elem<T> *copy, Elem<T> *scaled, int pitch)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    __shared__ typename RowTeam<WAVES>::Lds lds;
+    const RowTeam<WAVES> team(&lds);
+    const int64_t t = (int64_t)blockIdx.x * RowTeam<WAVES>::kRows + threadIdx.x / RowTeam<WAVES>::kThreads;
     if (t >= h.rows) return;
     const Elem<T> *const row = static_cast<const Elem<T> *>(h.data) + t * h.stride;
-    const OwnTokens own(taught, t, w.rows, lane);
+    const OwnToken<WAVES> own(team, taught, t, w.rows);
     const float g = dloss ? dloss[t] * factor : factor;
     float number;
     int exponent;
     split_weight(g, number, exponent);
     number = ldexpf(number, kShift<T>);
     const bool part = own.any && g != 0.0f;
-    float z[kSlots];
-    own_logits<T>(row, w, own, part ? taught.k : 0, lane, scale, z);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-        const int e = lane + 64 * s;
-        int id = part ? own.id[s] : -1;
-        float share = own.share[s];
-        if (taught.k > 1) {   // a token that comes twice: the first place has all its shares
-            share = 0.0f;
-            bool again = false;
-            for (int o = 0; o < taught.k; ++o) {
-                int other_id = 0;
-                float other = 0.0f;
-#pragma unroll
-                for (int q = 0; q < kSlots; ++q)
-                    if (o >> 6 == q) {
-                        other_id = __builtin_amdgcn_readlane(own.id[q], o & 63);
-                        other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own.share[q]), o & 63));
-                    }
-                if (other_id != id) continue;
-                share += other;
-                again |= o < e;
-            }
-            if (again) id = -1;
-        }
-        if (e < taught.k) {
-            token[t * taught.k + e] = id;
-            value[t * taught.k + e] = id < 0 ? 0.0f : number * (exp_of(z[s] - lse[t]) - share);
-        }
+    const float z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
+    int id = part ? own.id : -1;
+    // a token that comes twice: the first place has all its shares
+    float share = 0.0f;
+    bool again = false;
+    for (int o = 0; o < taught.k; ++o) {
+        const int other = team.of(own.id, lds.id, o);
+        const float more = team.of(own.share, lds.share, o);
+        if (other != own.id) continue;
+        share += more;
+        again |= o < team.me;
     }
-    if (lane == 0) {
+    if (again) id = -1;
+    if (team.me < taught.k) {
+        token[t * taught.k + team.me] = id;
+        value[t * taught.k + team.me] = id < 0 ? 0.0f : number * (exp_of(z - lse[t]) - share);
+    }
+    if (team.me == 0) {
         weights.number[t] = part ? number : 0.0f;
         weights.exponent[t] = part ? exponent : kNoRow;
     }
     const int by = scaled ? exponent - largest_of(weights) : 0;
-    for (int c = lane * 8; c < pitch; c += 512) {
+    for (int c = team.me * 8; c < pitch; c += RowTeam<WAVES>::kThreads * 8) {
         float v[8] = {};
         if (part) fetch8<T>(row, c, (int)h.cols, v);
         store_raw<T, 8>(copy + t * pitch + c, raw_of<T, 8>(v));
@@ -496,14 +508,23 @@ int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
 constexpr int64_t kTile = 256, kSmallTile = 128;
 // Tiles of 256 x 256 where they give every CU one.
 bool large_tiles(int64_t m, int64_t n) { return over(m, kTile) * over(n, kTile) >= 192; }
-int64_t tile_of(int64_t m, int64_t n) { return large_tiles(m, n) ? kTile : kSmallTile; }
+
+template <int T, bool AA, bool AB, bool kDirect>
+using Large = Product<T, AA, AB, 2, 4, 8, 4, kDirect ? 2 : 0>;
+template <int T, bool AA, bool AB, bool kDirect>
+using Small = Product<T, AA, AB, 2, 2, 4, 4, kDirect ? 4 : 0>;
+
+// Few rows of h against a table: tiles of 64 x 32.
+template <int T, bool kDirect>
+using Few = Product<T, false, false, 4, 1, 1, 2, kDirect ? 4 : 0>;
+constexpr int64_t kFewRows = 32;
 
 // Forward: rows of h at a time, so that the partial sums stay within 64 MB.
 struct LossSizes {
     int64_t tiles, rows;
     LossSizes(int64_t n, int64_t vocab)
     {
-        tiles = over(vocab, kSmallTile);
+        tiles = over(vocab, n <= kFewRows ? 64 : kSmallTile);
         rows = std::max<int64_t>(kTile, ((int64_t)64 << 20) / (tiles * (int64_t)sizeof(MaxSum)) / kTile * kTile);
         rows = std::min(rows, n);
     }
@@ -512,6 +533,7 @@ struct LossSizes {
 
 struct GradSizes {
     int64_t n, vocab, cols, k, elem;
+    bool dh_large;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
     int64_t largest, number, exponent, token, value, copy, scaled, d, sums, total;
@@ -525,9 +547,13 @@ struct GradSizes {
         d_pitch = piece;
         h_pitch = up(cols, 64);
         sum_pitch = up(cols, 4);
-        const int64_t step = 128 / elem, steps = over(piece, step), tile = tile_of(cols, n);
+        // the product for dh: parts of the piece at a time where its tiles alone do not fill the card
+        const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / 8);
+        const int64_t large = over(cols, kTile) * over(std::max<int64_t>(n, 1), kTile);
+        dh_large = large * most_splits >= 192;
+        const int64_t tile = dh_large ? kTile : kSmallTile;
         const int64_t tiles = over(cols, tile) * over(std::max<int64_t>(n, 1), tile);
-        splits = std::max<int64_t>(1, std::min((tile == kTile ? 256 : 512) / tiles, steps / 8));
+        splits = std::max<int64_t>(1, std::min(256 / tiles, most_splits));
         depth = over(steps, splits) * step;
         splits = over(piece, depth);
         int64_t at = 0;
@@ -549,18 +575,23 @@ struct GradSizes {
     }
 };
 
-template <int T, bool AA, bool AB, bool kDirect>
-using Large = Product<T, AA, AB, 2, 4, 8, 4, kDirect ? 2 : 0>;
-template <int T, bool AA, bool AB, bool kDirect>
-using Small = Product<T, AA, AB, 2, 2, 4, 4, kDirect ? 4 : 0>;
-
 // Calls f with the shape of a product's tiles: its size, and whether its sides go straight to LDS.
 template <int T, bool AA, bool AB, typename F>
 hipError_t by_shape(bool large, const ProductSide &a, const ProductSide &b, F f)
 {
     const bool direct = direct_side<T>(a) && direct_side<T>(b);
+    if constexpr (!AA && !AB)
+        if (b.rows <= kFewRows) return direct ? f(Few<T, true>{}) : f(Few<T, false>{});
     if (large) return direct ? f(Large<T, AA, AB, true>{}) : f(Large<T, AA, AB, false>{});
     return direct ? f(Small<T, AA, AB, true>{}) : f(Small<T, AA, AB, false>{});
+}
+
+// Calls f with the waves of a row: one, or four where rows are few or have many tokens.
+template <typename F>
+hipError_t by_team(int64_t rows, int64_t k, F f)
+{
+    if (rows < 2048 || k >= 8) return f(std::integral_constant<int, 4>{});
+    return f(std::integral_constant<int, 1>{});
 }
 
 template <class P>
@@ -594,9 +625,12 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((k_head_loss<T>), dim3((unsigned)over(rows.rows, 4)), dim3(256), 0, s, w, rows, scale, taught, first,
-                           tiles, partial, out, lse);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = by_team(rows.rows, taught.k, [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            hipLaunchKernelGGL((k_head_loss<T, W>), dim3((unsigned)over(rows.rows, RowTeam<W>::kRows)), dim3(256), 0, s, w, rows, scale,
+                               taught, first, tiles, partial, out, lse);
+            return hipGetLastError();
+        });
     }
     return hipSuccess;
 }
@@ -628,10 +662,13 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
             hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, dloss, z.n, factor, largest);
             UL_LAUNCHED(hipGetLastError());
         }
-        hipLaunchKernelGGL((k_head_rows<T>), dim3((unsigned)over(z.n, 4)), dim3(256), 0, s, side_of<T>(table, 0, table.rows),
-                           side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights, token, value, copy, scaled,
-                           (int)z.h_pitch);
-        UL_LAUNCHED(hipGetLastError());
+        UL_LAUNCHED(by_team(z.n, z.k, [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(256), 0, s,
+                               side_of<T>(table, 0, table.rows), side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
+                               token, value, copy, scaled, (int)z.h_pitch);
+            return hipGetLastError();
+        }));
     }
     // the copies' and D's columns past the last are zeros, and so are pieces of them
     const ProductSide rows{copy, z.h_pitch, z.n, z.h_pitch}, weighted{scaled ? scaled : copy, z.h_pitch, z.n, z.h_pitch};
@@ -650,7 +687,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                                token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch);
             UL_LAUNCHED(hipGetLastError());
             if (dh)
-                UL_LAUNCHED((by_shape<T, true, false>(large_tiles(z.cols, z.n), w, d_side, [&](auto shape) {
+                UL_LAUNCHED((by_shape<T, true, false>(z.dh_large, w, d_side, [&](auto shape) {
                     using P = decltype(shape);
                     const Tiles g = tiles_of<P>(z.cols, z.n);
                     hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s, w,
