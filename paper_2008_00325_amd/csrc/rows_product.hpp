@@ -148,21 +148,27 @@ struct DirectSide {
         offset = (uint32_t)((row * side.stride + col) * kElem);
         if (kAcross && i0 + col >= side.cols) offset = 0x80000000u;
     }
-    __device__ __forceinline__ void load(const ProductSide &side, int64_t i0, int64_t k, bool there, Piece *to, int wave) const
-    {
-        const int64_t r0 = kAcross ? k : i0, c0 = kAcross ? i0 : k;
-        const char *const base = static_cast<const char *>(side.data) + (r0 * side.stride + c0) * kElem;
-        const int64_t rows = min((int64_t)(kAcross ? S::kDepth : I), side.rows - r0);
-        const Words buffer = {(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu,
-                              there && rows > 0 ? (uint32_t)(rows * side.stride * kElem) : 0u, 0x00027000u};
-        const uint32_t at = !kAcross && k + col >= side.cols ? 0x80000000u : offset;
-        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) Piece *)to + wave * 1024, step = (uint32_t)(kRows * side.stride * kElem);
-#pragma unroll
-        for (int q = 0; q < kCount; ++q)
+    // A step's loads: where they read from and go to, and the q-th of them.
+    struct Loads {
+        Words buffer;
+        uint32_t at, lds, step;
+        __device__ __forceinline__ void one(int q) const
+        {
             // the whole offset in the lane's register: it is what the hardware compares with the buffer's length
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + q * THREADS * 16),
                          "v"(at + q * step), "s"(buffer)
                          : "memory");
+        }
+    };
+    __device__ __forceinline__ Loads loads(const ProductSide &side, int64_t i0, int64_t k, bool there, Piece *to, int wave) const
+    {
+        const int64_t r0 = kAcross ? k : i0, c0 = kAcross ? i0 : k;
+        const char *const base = static_cast<const char *>(side.data) + (r0 * side.stride + c0) * kElem;
+        const int64_t rows = min((int64_t)(kAcross ? S::kDepth : I), side.rows - r0);
+        return {Words{(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu,
+                      there && rows > 0 ? (uint32_t)(rows * side.stride * kElem) : 0u, 0x00027000u},
+                !kAcross && k + col >= side.cols ? 0x80000000u : offset,
+                (uint32_t)(uintptr_t)(__attribute__((address_space(3))) Piece *)to + wave * 1024, (uint32_t)(kRows * side.stride * kElem)};
     }
 };
 
@@ -270,50 +276,54 @@ struct Product {
         const DirectSide<T, kAcrossB, N, kThreads> db(b, n0);
         const int steps = (int)((k1 - k0 + kDepth - 1) / kDepth);
         constexpr int kStage = A::kPieces + B::kPieces;
-        auto load = [&](int s) {
-            Piece *const to = lds + s % DEPTH * kStage;
-            da.load(a, m0, k0 + (int64_t)s * kDepth, s < steps, to, wave);
-            db.load(b, n0, k0 + (int64_t)s * kDepth, s < steps, to + A::kPieces, wave);
-        };
+        constexpr int kLoads = kA + kB, kReads = FM + FN;
         Piece fa[2][FM], fb[2][FN];
-        auto fetch_half = [&](int s, int half, int set) {
+        // A half step's products with the fragments of `set`, and between their rows, evenly, the fetches of the next
+        // half's fragments (step s, half `half`, into the other set) and the loads of step l (if kLoading).
+        auto half_step = [&](auto products, int set, int s, int half, auto loading, int l) {
+            constexpr bool kProducts = decltype(products)::value, kLoading = decltype(loading)::value;
             const Piece *const from = lds + s % DEPTH * kStage;
+            Piece *const to = lds + l % DEPTH * kStage;
+            const auto la = da.loads(a, m0, k0 + (int64_t)l * kDepth, l < steps, to, wave);
+            const auto lb = db.loads(b, n0, k0 + (int64_t)l * kDepth, l < steps, to + A::kPieces, wave);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) fb[set][j] = B::fragment(from + A::kPieces, (wn * FN + j) * 16, half, lane);
+            for (int i = 0; i < FM; ++i) {
+                if constexpr (kLoading) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i) fa[set][i] = A::fragment(from, (wm * FM + i) * 16, half, lane);
-        };
-        // Fetches and products of a half step in turn, so that LDS serves all waves evenly.
-        auto mix = [] {
-            constexpr int kProducts = FM * FN * (sizeof(Elem<T>) == 4 ? 4 : 1);
-            constexpr int kReads = FM * A::kReads + FN * B::kReads, kEach = kProducts / kReads;
+                    for (int q = i * kLoads / FM; q < (i + 1) * kLoads / FM; ++q) {
+                        if (q < kA) la.one(q);
+                        else lb.one(q - kA);
+                    }
+                }
 #pragma unroll
-            for (int q = 0; q < kReads; ++q) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+                for (int q = i * kReads / FM; q < (i + 1) * kReads / FM; ++q) {
+                    if (q < FN) fb[set ^ 1][q] = B::fragment(from + A::kPieces, (wn * FN + q) * 16, half, lane);
+                    else fa[set ^ 1][q - FN] = A::fragment(from, (wm * FM + q - FN) * 16, half, lane);
+                }
+                if constexpr (kProducts) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa[set][i], fb[set][j], acc[i][j]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, kProducts - kReads * kEach, 0);
-            __builtin_amdgcn_sched_barrier(0);
         };
-        auto multiply_half = [&](int set) {
+        constexpr auto yes = std::true_type{};
+        constexpr auto no = std::false_type{};
+        for (int s = 0; s < DEPTH; ++s) {
+            Piece *const to = lds + s * kStage;
+            const auto la = da.loads(a, m0, k0 + (int64_t)s * kDepth, s < steps, to, wave);
+            const auto lb = db.loads(b, n0, k0 + (int64_t)s * kDepth, s < steps, to + A::kPieces, wave);
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+            for (int q = 0; q < kA; ++q) la.one(q);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa[set][i], fb[set][j], acc[i][j]);
-        };
-#pragma unroll
-        for (int s = 0; s < DEPTH; ++s) load(s);
-        landed<(DEPTH - 1) * (kA + kB)>();
-        fetch_half(0, 0, 0);
+            for (int q = 0; q < kB; ++q) lb.one(q);
+        }
+        landed<(DEPTH - 1) * kLoads>();
+        half_step(no, 1, 0, 0, no, 0);
         for (int s = 0; s < steps; ++s) {
-            fetch_half(s, 1, 1);
-            multiply_half(0);
-            mix();
-            landed<(DEPTH - 2) * (kA + kB)>();   // step s + 1 is there, and everybody has fetched all of step s
-            load(s + DEPTH);
-            fetch_half(s + 1, 0, 0);   // behind the last step: zeros, which nobody takes
-            multiply_half(1);
-            mix();
+            half_step(yes, 0, s, 1, no, 0);
+            landed<(DEPTH - 2) * kLoads>();   // step s + 1 is there, and everybody has fetched all of step s
+            half_step(yes, 1, s + 1, 0, yes, s + DEPTH);   // behind the last step: zeros, which nobody takes
         }
         landed<0>();
     }
