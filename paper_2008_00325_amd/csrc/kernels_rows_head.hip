@@ -25,20 +25,39 @@ namespace ul {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // exp(x): hardware's 2^x, off by a unit in the last place and |x| 2^-24; 0 below 2^-126
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ __forceinline__ float minus_inf() { return -__builtin_inff(); }
 
-// Largest value and sum of exp(value - largest).
+// What the tiles' exponentials are of, and to what base: 16-bit types' logits are in units of log 2, so that a product
+// and a sum with one rounding lead to the hardware's 2^x; fp32's are in natural units and go through expf, since their
+// results are not rounded any further.
+template <int T>
+struct Logit {
+    float unit;   // times a dot product: a logit
+    __device__ __forceinline__ explicit Logit(float scale) : unit(T == UMAP_F32 ? scale : scale * kLog2e) {}
+    static __device__ __forceinline__ float exp(float x) { return T == UMAP_F32 ? expf(x) : __builtin_amdgcn_exp2f(x); }
+    static __device__ __forceinline__ float log(float x) { return T == UMAP_F32 ? logf(x) : __builtin_amdgcn_logf(x); }
+    static __device__ __forceinline__ float natural(float x) { return T == UMAP_F32 ? x : x * kLn2; }
+    static __device__ __forceinline__ float of_natural(float x) { return T == UMAP_F32 ? x : x * kLog2e; }
+    // exp(dot's logit - less)
+    __device__ __forceinline__ float exp_less(float dot, float less) const
+    {
+        return T == UMAP_F32 ? expf(dot * unit - less) : __builtin_amdgcn_exp2f(fmaf(dot, unit, -less));
+    }
+};
+
+// Largest logit and sum of exp(logit - largest).
 struct MaxSum {
     float m, s;
     // Values to subtract from: a largest of -inf (no value yet, or all of them) subtracts nothing.
     static __device__ __forceinline__ float base(float m) { return m == minus_inf() ? 0.0f : m; }
+    template <int T>
     __device__ __forceinline__ void join(MaxSum o)
     {
         const float most = fmaxf(m, o.m), b = base(most);
-        s = fmaf(s, exp_of(m - b), o.s * exp_of(o.m - b));
+        s = fmaf(s, Logit<T>::exp(m - b), o.s * Logit<T>::exp(o.m - b));
         m = most;
     }
 };
@@ -52,7 +71,8 @@ __device__ __forceinline__ float wave_sum(float v)
 // ---- the logits' tiles: forward -------------------------------------------------------------
 
 template <int T, class P>
-__global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, ProductSide h, float scale, Tiles tiles, MaxSum *partial)
+__global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, ProductSide h, float scale, Tiles tiles, int64_t first_tile,
+                                                          int64_t all_tiles, MaxSum *partial)
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
@@ -62,25 +82,33 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
     P::run(w, h, m0, n0, 0, w.cols, lds, acc);
     MaxSum(*const part)[P::N] = reinterpret_cast<MaxSum(*)[P::N]>(lds);   // behind the product's last barrier
     const int live = (int)min((int64_t)P::M, w.rows - m0);
+    Logit<T> logit(scale);
+    if (live < P::M || logit.unit < 0.0f) {   // the largest is the largest product's but here
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = P::m_of(i) + r < live ? acc[i][j][r] * logit.unit : minus_inf();
+        logit.unit = 1.0f;
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         float most = minus_inf();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                acc[i][j][r] = P::m_of(i) + r < live ? acc[i][j][r] * scale : minus_inf();
-                most = fmaxf(most, acc[i][j][r]);
-            }
+            for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[i][j][r]);
+        if (most != minus_inf()) most *= logit.unit;
         const float b = MaxSum::base(most);
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += exp_of(acc[i][j][r] - b);
+            for (int r = 0; r < 4; ++r) sum += logit.exp_less(acc[i][j][r], b);
         MaxSum all{most, sum};
 #pragma unroll
-        for (int o = 16; o < 64; o <<= 1) all.join({__shfl_xor(all.m, o), __shfl_xor(all.s, o)});
+        for (int o = 16; o < 64; o <<= 1) all.template join<T>({__shfl_xor(all.m, o), __shfl_xor(all.s, o)});
         if ((threadIdx.x & 63) < 16) part[(threadIdx.x >> 6) / P::kWN][P::n_of(j)] = all;
     }
     __syncthreads();
@@ -88,8 +116,8 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
         if (n0 + n >= h.rows) continue;
         MaxSum all = part[0][n];
 #pragma unroll
-        for (int i = 1; i < P::kWM; ++i) all.join(part[i][n]);
-        partial[(n0 + n) * tiles.m + at.m] = all;
+        for (int i = 1; i < P::kWM; ++i) all.template join<T>(part[i][n]);
+        partial[(n0 + n) * all_tiles + first_tile + at.m] = all;
     }
 }
 
@@ -240,6 +268,20 @@ __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Ele
     return z;
 }
 
+// A copy of rows for the products, in whole pieces of 16 bytes: `pitch` columns, zeros past the last.
+template <int T>
+__global__ __launch_bounds__(256) void k_head_pack(ProductSide from, Elem<T> *to, int pitch)
+{
+    const int64_t total = from.rows * (pitch / 8);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / (pitch / 8);
+        const int c = (int)(i % (pitch / 8)) * 8;
+        float v[8] = {};
+        if (c < from.cols) fetch8<T>(static_cast<const Elem<T> *>(from.data) + r * from.stride, c, (int)from.cols, v);
+        store_raw<T, 8>(to + r * pitch + c, raw_of<T, 8>(v));
+    }
+}
+
 // Joins a row's tiles, and sums its loss.
 template <int T, int WAVES>
 __global__ __launch_bounds__(256) void k_head_loss(ProductSide w, ProductSide h, float scale, Taught taught, int64_t first,
@@ -250,11 +292,11 @@ __global__ __launch_bounds__(256) void k_head_loss(ProductSide w, ProductSide h,
     const int64_t t = (int64_t)blockIdx.x * RowTeam<WAVES>::kRows + threadIdx.x / RowTeam<WAVES>::kThreads;
     if (t >= h.rows) return;
     MaxSum mine{minus_inf(), 0.0f};
-    for (int64_t i = team.me; i < tiles; i += RowTeam<WAVES>::kThreads) mine.join(partial[t * tiles + i]);
+    for (int64_t i = team.me; i < tiles; i += RowTeam<WAVES>::kThreads) mine.template join<T>(partial[t * tiles + i]);
     const OwnToken<WAVES> own(team, taught, first + t, w.rows);
     const float z = own_logit<T, WAVES>(team, static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, scale);
     const float most = team.max(mine.m);
-    const float sum = most + logf(team.sum(mine.s * exp_of(mine.m - MaxSum::base(most))));
+    const float sum = Logit<T>::natural(most + Logit<T>::log(team.sum(mine.s * Logit<T>::exp(mine.m - MaxSum::base(most)))));
     const float all = team.sum(own.id >= 0 && own.share != 0.0f ? own.share * (own.log_share + (sum - z)) : 0.0f);
     if (team.me == 0) {
         lse[first + t] = sum;
@@ -311,7 +353,7 @@ __global__ __launch_bounds__(1024) void k_head_largest(const float *dloss, int64
 template <int T, int WAVES>
 __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
                                                    const float *dloss, float factor, RowWeights weights, int *token,
-                                                   float *value, Elem<T> *copy, Elem<T> *scaled, int pitch)
+                                                   float *value, Elem<T> *copy, Elem<T> *scaled, int pitch, int parts)
 {
     __shared__ typename RowTeam<WAVES>::Lds lds;
     const RowTeam<WAVES> team(&lds);
@@ -340,7 +382,7 @@ __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h,
     if (again) id = -1;
     if (team.me < taught.k) {
         token[t * taught.k + team.me] = id;
-        value[t * taught.k + team.me] = id < 0 ? 0.0f : number * (exp_of(z - lse[t]) - share);
+        value[t * taught.k + team.me] = id < 0 ? 0.0f : number * ((T == UMAP_F32 ? expf(z - lse[t]) : exp_of(z - lse[t])) - share);
     }
     if (team.me == 0) {
         weights.number[t] = part ? number : 0.0f;
@@ -350,18 +392,34 @@ __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h,
     for (int c = team.me * 8; c < pitch; c += RowTeam<WAVES>::kThreads * 8) {
         float v[8] = {};
         if (part) fetch8<T>(row, c, (int)h.cols, v);
-        store_raw<T, 8>(copy + t * pitch + c, raw_of<T, 8>(v));
+        for (int p = 0; p < parts; ++p) store_raw<T, 8>(copy + (p * h.rows + t) * pitch + c, raw_of<T, 8>(v));
         if (!scaled) continue;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], by);
-        store_raw<T, 8>(scaled + t * pitch + c, raw_of<T, 8>(v));
+        for (int p = 0; p < parts; ++p) store_raw<T, 8>(scaled + (p * h.rows + t) * pitch + c, raw_of<T, 8>(v));
     }
 }
 
-// D of a piece of the table: d[t][v], `pitch` columns, zeros past the piece's rows.
+// An entry of D as it is stored: rounded, and with two parts what the rounding left below it, `below` elements on.
+template <int T>
+__device__ __forceinline__ void store_entries(Elem<T> *at, int64_t below, float (&v)[4])
+{
+    const Raw<T, 4> r = raw_of<T, 4>(v);
+    store_raw<T, 4>(at, r);
+    if (!below) return;
+    float back[4];
+    floats_of<T, 4>(r, back);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] -= back[i];
+    store_raw<T, 4>(at + below, raw_of<T, 4>(v));
+}
+
+// D of a piece of the table: d[t][v], `pitch` columns, zeros past the piece's rows.  token and value: null, or each
+// row's one token (less the piece's first) and its entry.
 template <int T, class P>
 __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSide h, float scale, Tiles tiles, const float *lse,
-                                                        RowWeights weights, Elem<T> *d, int64_t pitch)
+                                                        RowWeights weights, const int *token, const float *value, int64_t first,
+                                                        Elem<T> *d, int64_t pitch, int64_t below)
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
@@ -370,21 +428,30 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
     Acc4 acc[FM][FN];
     P::run(w, h, m0, n0, 0, w.cols, lds, acc);
     const int live = (int)min((int64_t)P::M, w.rows - m0);
+    const Logit<T> logit(scale);
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int64_t t = n0 + P::n_of(j);
         if (t >= h.rows) continue;
-        const float number = weights.number[t], sum = lse[t];
+        const float number = weights.number[t], less = Logit<T>::of_natural(lse[t]);
+        const int64_t own = token ? token[t] - first - m0 : -1;
+        const int own_m = token && token[t] >= 0 && own >= 0 && own < live ? (int)own : -1;
+        const float own_value = own_m >= 0 ? value[t] : 0.0f;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int m = P::m_of(i);
             float v[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float p = number * exp_of(acc[i][j][r] * scale - sum);
-                v[r] = number != 0.0f && m + r < live ? p : 0.0f;
+                const float p = number * logit.exp_less(acc[i][j][r], less);
+                v[r] = number != 0.0f ? p : 0.0f;
+                v[r] = m + r == own_m ? own_value : v[r];
             }
-            store_raw<T, 4>(d + t * pitch + m0 + m, raw_of<T, 4>(v));
+            if (live < P::M) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = m + r < live ? v[r] : 0.0f;
+            }
+            store_entries<T>(d + t * pitch + m0 + m, below, v);
         }
     }
 }
@@ -392,11 +459,14 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
 // The entries of D at the rows' own tokens.
 template <int T>
 __global__ __launch_bounds__(256) void k_head_own(const int *token, const float *value, int64_t count, int k, int64_t first,
-                                                  int64_t rows, Elem<T> *d, int64_t pitch)
+                                                  int64_t rows, Elem<T> *d, int64_t pitch, int64_t below)
 {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
         const int64_t v = token[i] - first;
-        if (token[i] >= 0 && v >= 0 && v < rows) d[i / k * pitch + v] = float_elem<T>(value[i]);
+        if (token[i] < 0 || v < 0 || v >= rows) continue;
+        Elem<T> *const at = d + i / k * pitch + v;
+        *at = float_elem<T>(value[i]);
+        if (below) at[below] = float_elem<T>(value[i] - elem_float<T>(*at));
     }
 }
 
@@ -428,13 +498,13 @@ __global__ __launch_bounds__(P::kThreads) void k_head_dh(ProductSide w, ProductS
 }
 
 template <int T>
-__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int splits, int64_t pitch, const int *exponent, umap_rows dh)
+__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int parts, int64_t pitch, const int *exponent, umap_rows dh)
 {
     const int64_t groups = pitch / 4, total = dh.rows * groups;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t t = i / groups, c = i % groups * 4;
         Acc4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + t) * pitch + c);
+        for (int s = 0; s < parts; ++s) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + t) * pitch + c);
         const int e = exponent[t];
         float v[4];
 #pragma unroll
@@ -505,55 +575,79 @@ constexpr int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
 
-constexpr int64_t kTile = 256, kSmallTile = 128;
-// Tiles of 256 x 256 where they give every CU one.
-bool large_tiles(int64_t m, int64_t n) { return over(m, kTile) * over(n, kTile) >= 192; }
-
-template <int T, bool AA, bool AB, bool kDirect>
-using Large = Product<T, AA, AB, 2, 4, 8, 4, kDirect ? 2 : 0>;
-template <int T, bool AA, bool AB, bool kDirect>
-using Small = Product<T, AA, AB, 2, 2, 4, 4, kDirect ? 4 : 0>;
-
-// Few rows of h against a table: tiles of 64 x 32.
-template <int T, bool kDirect>
-using Few = Product<T, false, false, 4, 1, 1, 2, kDirect ? 4 : 0>;
+// Tiles of 256 x 256, 128 x 128 and 64 x 64, and of 64 x 32 for few rows of h.
+template <int T, bool AA, bool AB, bool DA, bool DB>
+using Large = Product<T, AA, AB, 2, 4, 8, 4, DA, DB, 2>;
+template <int T, bool AA, bool AB, bool DA, bool DB>
+using Small = Product<T, AA, AB, 2, 2, 4, 4, DA, DB, DA && DB ? 4 : 2>;
+template <int T, bool AA, bool AB, bool DA, bool DB>
+using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DA, DB, DA && DB ? 4 : 2>;
+template <int T, bool DA, bool DB>
+using Few = Product<T, false, false, 4, 1, 1, 2, DA, DB, DA && DB ? 4 : 2>;
 constexpr int64_t kFewRows = 32;
 
-// Forward: rows of h at a time, so that the partial sums stay within 64 MB.
+// The largest tiles that give enough workgroups: `splits` of the products' depth at most, n rows of h's side.
+int64_t tile_for(int64_t m, int64_t n, int64_t splits)
+{
+    n = std::max<int64_t>(n, 1);
+    if (over(m, 256) * over(n, 256) * splits >= 192) return 256;
+    return over(m, 128) * over(n, 128) * splits >= 128 ? 128 : 64;
+}
+
+// Rows of h from which on a table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at
+// most at a time: unaligned loads go at half the rate, and the products read a piece once for every 256 rows of h.
+constexpr int64_t kPackLossRows = 768, kPackGradRows = 384;
+constexpr int64_t kPackBytes = (int64_t)128 << 20;
+int64_t pack_rows(int64_t pitch, int64_t elem) { return std::max<int64_t>(256, kPackBytes / (pitch * elem) / 256 * 256); }
+
+// Forward: rows of h at a time, so that the partial sums stay within 128 MB (a quarter of that with the large tiles).
 struct LossSizes {
-    int64_t tiles, rows;
-    LossSizes(int64_t n, int64_t vocab)
+    int64_t tiles, rows, pitch, piece;
+    int64_t partial, copy, table, total;   // offsets into the workspace
+    LossSizes(int64_t n, int64_t vocab, int32_t cols, int32_t type)
     {
-        tiles = over(vocab, n <= kFewRows ? 64 : kSmallTile);
-        rows = std::max<int64_t>(kTile, ((int64_t)64 << 20) / (tiles * (int64_t)sizeof(MaxSum)) / kTile * kTile);
+        const int64_t elem = elem_size(type);
+        tiles = over(vocab, 64);   // as many as the smallest have
+        rows = std::max<int64_t>(256, ((int64_t)128 << 20) / (tiles * (int64_t)sizeof(MaxSum)) / 256 * 256);
         rows = std::min(rows, n);
+        pitch = up(cols, 64);
+        piece = std::min(pack_rows(pitch, elem), up(vocab, 256));
+        partial = 0;
+        copy = up(rows * tiles * (int64_t)sizeof(MaxSum), 256);
+        table = copy + up(n > kFewRows ? rows * pitch * elem : 0, 256);
+        total = std::max<int64_t>(16, table + (n >= kPackLossRows ? piece * pitch * elem : 0));
     }
-    int64_t bytes() const { return std::max<int64_t>(16, rows * tiles * (int64_t)sizeof(MaxSum)); }
 };
+
+// Rows up to which a 16-bit D has two parts, a value and what its rounding left: few rows do not average the rounding out (a
+// row's token often has most of its gradient, in one entry), and what the products of so few take is the time of the
+// table's bytes.
+constexpr int64_t kTwoPartRows = 128;
 
 struct GradSizes {
     int64_t n, vocab, cols, k, elem;
-    bool dh_large;
+    int64_t parts;     // of D
+    int64_t dh_tile;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
-    int64_t largest, number, exponent, token, value, copy, scaled, d, sums, total;
-    GradSizes(int64_t n_, int64_t vocab_, int32_t cols_, int64_t k_, int32_t type)
+    int64_t largest, number, exponent, token, value, copy, scaled, d, sums, packed, total;
+    GradSizes(int64_t n_, int64_t vocab_, int32_t cols_, int64_t k_, int32_t type, bool pack)
         : n(n_), vocab(vocab_), cols(cols_), k(k_), elem(elem_size(type))
     {
+        parts = elem == 2 && n <= kTwoPartRows ? 2 : 1;
         const int64_t budget = (int64_t)256 << 20;
-        int64_t most = std::max<int64_t>(kTile, budget / std::max<int64_t>(1, n * elem) / kTile * kTile);
-        const int64_t pieces = over(vocab, most);
-        piece = up(over(vocab, pieces), kTile);
-        d_pitch = piece;
+        int64_t most = std::max<int64_t>(256, budget / std::max<int64_t>(1, n * parts * elem) / 256 * 256);
         h_pitch = up(cols, 64);
+        if (pack) most = std::min(most, pack_rows(h_pitch, elem));
+        const int64_t pieces = over(vocab, most);
+        piece = up(over(vocab, pieces), 256);
+        d_pitch = piece;
         sum_pitch = up(cols, 4);
         // the product for dh: parts of the piece at a time where its tiles alone do not fill the card
-        const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / 8);
-        const int64_t large = over(cols, kTile) * over(std::max<int64_t>(n, 1), kTile);
-        dh_large = large * most_splits >= 192;
-        const int64_t tile = dh_large ? kTile : kSmallTile;
-        const int64_t tiles = over(cols, tile) * over(std::max<int64_t>(n, 1), tile);
-        splits = std::max<int64_t>(1, std::min(256 / tiles, most_splits));
+        const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / (elem == 4 ? 2 : 4));
+        dh_tile = tile_for(cols, n * parts, most_splits);
+        const int64_t tiles = over(cols, dh_tile) * over(std::max<int64_t>(n * parts, 1), dh_tile);
+        splits = std::max<int64_t>(1, std::min((dh_tile == 64 ? 512 : 256) / tiles, most_splits));
         depth = over(steps, splits) * step;
         splits = over(piece, depth);
         int64_t at = 0;
@@ -567,23 +661,31 @@ struct GradSizes {
         exponent = take(n * 4);
         token = take(n * k * 4);
         value = take(n * k * 4);
-        copy = take(n * h_pitch * elem);
-        scaled = take(n * h_pitch * elem);
-        d = take(n * d_pitch * elem);
-        sums = take(splits * n * sum_pitch * 4);
+        copy = take(n * parts * h_pitch * elem);
+        scaled = take(n * parts * h_pitch * elem);
+        d = take(n * parts * d_pitch * elem);
+        sums = take(splits * n * parts * sum_pitch * 4);
+        packed = take(pack ? piece * h_pitch * elem : 0);
         total = at;
     }
 };
 
-// Calls f with the shape of a product's tiles: its size, and whether its sides go straight to LDS.
-template <int T, bool AA, bool AB, typename F>
-hipError_t by_shape(bool large, const ProductSide &a, const ProductSide &b, F f)
+// Calls f with the shape of a product's tiles.  A table that does not go straight to LDS is only met with few rows of
+// h (more of them, and it is copied), for which the large tiles are none.
+template <int T, bool AA, bool AB, bool DA, typename F>
+hipError_t by_tile(int64_t tile, F f)
 {
-    const bool direct = direct_side<T>(a) && direct_side<T>(b);
-    if constexpr (!AA && !AB)
-        if (b.rows <= kFewRows) return direct ? f(Few<T, true>{}) : f(Few<T, false>{});
-    if (large) return direct ? f(Large<T, AA, AB, true>{}) : f(Large<T, AA, AB, false>{});
-    return direct ? f(Small<T, AA, AB, true>{}) : f(Small<T, AA, AB, false>{});
+    if constexpr (DA)
+        if (tile == 256) return f(Large<T, AA, AB, DA, true>{});
+    return tile >= 128 ? f(Small<T, AA, AB, DA, true>{}) : f(Tiny<T, AA, AB, DA, true>{});
+}
+// `rows` of a table, which goes straight or not, against rows of h.
+template <int T, typename F>
+hipError_t by_logits(int64_t rows, bool direct, const ProductSide &h, F f)
+{
+    if (h.rows <= kFewRows) return direct && direct_side<T>(h) ? f(Few<T, true, true>{}) : f(Few<T, false, false>{});
+    const int64_t tile = tile_for(rows, h.rows, 1);
+    return direct ? by_tile<T, false, false, true>(tile, f) : by_tile<T, false, false, false>(tile, f);
 }
 
 // Calls f with the waves of a row: one, or four where rows are few or have many tokens.
@@ -606,35 +708,6 @@ ProductSide side_of(const umap_rows &m, int64_t first, int64_t rows)
     return {static_cast<const Elem<T> *>(m.data) + first * m.stride, m.stride, rows, m.cols};
 }
 
-template <int T>
-hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught, float scale, float *out, float *lse,
-                void *workspace, hipStream_t s)
-{
-    const LossSizes z(h.rows, table.rows);
-    auto *const partial = static_cast<MaxSum *>(workspace);
-    const ProductSide w = side_of<T>(table, 0, table.rows);
-    for (int64_t first = 0; first < h.rows; first += z.rows) {
-        const ProductSide rows = side_of<T>(h, first, std::min(z.rows, h.rows - first));
-        int64_t tiles = 0;
-        hipError_t e = by_shape<T, false, false>(large_tiles(w.rows, rows.rows), w, rows, [&](auto shape) {
-            using P = decltype(shape);
-            const Tiles g = tiles_of<P>(w.rows, rows.rows);
-            tiles = g.m;
-            hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
-                               partial);
-            return hipGetLastError();
-        });
-        if (e != hipSuccess) return e;
-        e = by_team(rows.rows, taught.k, [&](auto waves) {
-            constexpr int W = decltype(waves)::value;
-            hipLaunchKernelGGL((k_head_loss<T, W>), dim3((unsigned)over(rows.rows, RowTeam<W>::kRows)), dim3(256), 0, s, w, rows, scale,
-                               taught, first, tiles, partial, out, lse);
-            return hipGetLastError();
-        });
-    }
-    return hipSuccess;
-}
-
 #define UL_LAUNCHED(expr)                      \
     do {                                       \
         const hipError_t ul_e_ = (expr);       \
@@ -642,11 +715,66 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
     } while (0)
 
 template <int T>
+hipError_t pack(const ProductSide &from, Elem<T> *to, int64_t pitch, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_head_pack<T>), dim3((unsigned)std::min<int64_t>(8192, over(from.rows * pitch / 8, 256))), dim3(256), 0, s, from,
+                       to, (int)pitch);
+    return hipGetLastError();
+}
+
+template <int T>
+hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught, float scale, float *out, float *lse,
+                void *workspace, hipStream_t s)
+{
+    const LossSizes z(h.rows, table.rows, h.cols, h.type);
+    char *const base = static_cast<char *>(workspace);
+    auto *const partial = reinterpret_cast<MaxSum *>(base + z.partial);
+    const ProductSide all = side_of<T>(table, 0, table.rows);
+    const bool whole = direct_side<T>(all), packing = !whole && h.rows >= kPackLossRows;
+    const int64_t piece = packing ? z.piece : table.rows;
+    for (int64_t first = 0; first < h.rows; first += z.rows) {
+        const ProductSide given = side_of<T>(h, first, std::min(z.rows, h.rows - first));
+        ProductSide rows = given;
+        if (h.rows > kFewRows && !direct_side<T>(given)) {
+            UL_LAUNCHED(pack<T>(given, reinterpret_cast<Elem<T> *>(base + z.copy), z.pitch, s));
+            rows = {base + z.copy, z.pitch, given.rows, z.pitch};
+        }
+        int64_t tiles = 0;   // of all pieces, whose tiles are of one size: that of the whole table
+        (void)by_logits<T>(table.rows, whole || packing, rows, [&](auto shape) {
+            tiles = over(table.rows, decltype(shape)::M);
+            return hipSuccess;
+        });
+        for (int64_t v = 0; v < table.rows; v += piece) {
+            ProductSide w = side_of<T>(table, v, std::min(piece, table.rows - v));
+            if (packing) {
+                UL_LAUNCHED(pack<T>(w, reinterpret_cast<Elem<T> *>(base + z.table), z.pitch, s));
+                w = {base + z.table, z.pitch, w.rows, z.pitch};
+            }
+            UL_LAUNCHED(by_logits<T>(table.rows, whole || packing, rows, [&](auto shape) {
+                using P = decltype(shape);
+                const Tiles g = tiles_of<P>(w.rows, rows.rows);
+                hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
+                                   v / P::M, tiles, partial);
+                return hipGetLastError();
+            }));
+        }
+        UL_LAUNCHED(by_team(rows.rows, taught.k, [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            hipLaunchKernelGGL((k_head_loss<T, W>), dim3((unsigned)over(rows.rows, RowTeam<W>::kRows)), dim3(256), 0, s, all, given, scale,
+                               taught, first, tiles, partial, out, lse);
+            return hipGetLastError();
+        }));
+    }
+    return hipSuccess;
+}
+
+template <int T>
 hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught, float scale, const float *lse,
                 const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable, bool add, void *workspace,
                 hipStream_t s)
 {
-    const GradSizes z(h.rows, table.rows, table.cols, taught.k, h.type);
+    const bool whole = direct_side<T>(side_of<T>(table, 0, table.rows)), packing = !whole && h.rows >= kPackGradRows;
+    const GradSizes z(h.rows, table.rows, table.cols, taught.k, h.type, packing);
     char *const base = static_cast<char *>(workspace);
     auto *const token = reinterpret_cast<int *>(base + z.token);
     auto *const value = reinterpret_cast<float *>(base + z.value), *const sums = reinterpret_cast<float *>(base + z.sums);
@@ -666,34 +794,46 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
             constexpr int W = decltype(waves)::value;
             hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(256), 0, s,
                                side_of<T>(table, 0, table.rows), side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
-                               token, value, copy, scaled, (int)z.h_pitch);
+                               token, value, copy, scaled, (int)z.h_pitch, (int)z.parts);
             return hipGetLastError();
         }));
     }
     // the copies' and D's columns past the last are zeros, and so are pieces of them
-    const ProductSide rows{copy, z.h_pitch, z.n, z.h_pitch}, weighted{scaled ? scaled : copy, z.h_pitch, z.n, z.h_pitch};
+    const int64_t d_rows = z.n * z.parts, below = z.parts > 1 ? z.n * z.d_pitch : 0;
+    const ProductSide rows{copy, z.h_pitch, z.n, z.h_pitch}, weighted{scaled ? scaled : copy, z.h_pitch, d_rows, z.h_pitch};
     for (int64_t first = 0; first < z.vocab; first += z.piece) {
         const int64_t here = std::min(z.piece, z.vocab - first);
-        const ProductSide w = side_of<T>(table, first, here), d_side{d, z.d_pitch, z.n, z.d_pitch};
+        ProductSide w = side_of<T>(table, first, here);
+        if (packing) {
+            UL_LAUNCHED(pack<T>(w, reinterpret_cast<Elem<T> *>(base + z.packed), z.h_pitch, s));
+            w = {base + z.packed, z.h_pitch, here, z.h_pitch};
+        }
+        const ProductSide d_side{d, z.d_pitch, d_rows, z.d_pitch};
         if (z.n > 0) {
-            UL_LAUNCHED((by_shape<T, false, false>(large_tiles(here, z.n), w, rows, [&](auto shape) {
+            const bool one = z.k == 1;
+            UL_LAUNCHED((by_logits<T>(here, whole || packing, rows, [&](auto shape) {
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(z.d_pitch, z.n);
                 hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
-                                   lse, weights, d, z.d_pitch);
+                                   lse, weights, one ? token : nullptr, one ? value : nullptr, first, d, z.d_pitch, below);
                 return hipGetLastError();
             })));
-            hipLaunchKernelGGL((k_head_own<T>), dim3((unsigned)std::min<int64_t>(1024, over(z.n * z.k, 256))), dim3(256), 0, s,
-                               token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch);
-            UL_LAUNCHED(hipGetLastError());
-            if (dh)
-                UL_LAUNCHED((by_shape<T, true, false>(z.dh_large, w, d_side, [&](auto shape) {
+            if (!one) {
+                hipLaunchKernelGGL((k_head_own<T>), dim3((unsigned)std::min<int64_t>(1024, over(z.n * z.k, 256))), dim3(256), 0, s,
+                                   token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch, below);
+                UL_LAUNCHED(hipGetLastError());
+            }
+            if (dh) {
+                auto rows_sums = [&](auto shape) {
                     using P = decltype(shape);
-                    const Tiles g = tiles_of<P>(z.cols, z.n);
+                    const Tiles g = tiles_of<P>(z.cols, d_rows);
                     hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s, w,
                                        d_side, g, z.depth, first > 0, sums, z.sum_pitch);
                     return hipGetLastError();
-                })));
+                };
+                UL_LAUNCHED(whole || packing ? (by_tile<T, true, false, true>(z.dh_tile, rows_sums))
+                                             : (by_tile<T, true, false, false>(z.dh_tile, rows_sums)));
+            }
         }
         if (dtable) {
             umap_rows part = *dtable;
@@ -706,13 +846,13 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                                    weights, add, part);
                 return hipGetLastError();
             };
-            UL_LAUNCHED(large_tiles(z.cols, here) ? table_rows(Large<T, true, true, true>{}) : table_rows(Small<T, true, true, true>{}));
+            UL_LAUNCHED((by_tile<T, true, true, true>(tile_for(z.cols, here, 1), table_rows)));
         }
     }
     if (dh && z.n > 0) {
         const int64_t total = z.n * z.sum_pitch / 4;
         hipLaunchKernelGGL((k_head_dh_join<T>), dim3((unsigned)std::min<int64_t>(4096, over(total, 256))), dim3(256), 0, s, sums,
-                           (int)z.splits, z.sum_pitch, weights.exponent, *dh);
+                           (int)(z.splits * z.parts), z.sum_pitch, weights.exponent, *dh);
         UL_LAUNCHED(hipGetLastError());
     }
     return hipSuccess;
@@ -726,7 +866,7 @@ Taught taught_of(RowIds ids, const umap_rows *teacher, float teacher_scale)
 
 }  // namespace
 
-int64_t rows_head_bytes(int64_t n, int64_t vocab) { return LossSizes(n, vocab).bytes(); }
+int64_t rows_head_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t type) { return LossSizes(n, vocab, cols, type).total; }
 
 hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,
                             float teacher_scale, float *loss_out, float *lse, void *workspace, hipStream_t s)
@@ -741,7 +881,8 @@ hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds i
 
 int64_t rows_head_grad_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t k, int32_t type)
 {
-    return GradSizes(n, vocab, cols, k, type).total;
+    const int64_t plain = GradSizes(n, vocab, cols, k, type, false).total;   // how the table lies is not known here
+    return n < kPackGradRows ? plain : std::max(plain, GradSizes(n, vocab, cols, k, type, true).total);
 }
 
 hipError_t launch_rows_head_grad(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,

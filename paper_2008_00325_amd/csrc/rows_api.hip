@@ -238,7 +238,7 @@ int head(const char *name, const umap_rows *h, const umap_rows *table, const voi
     const int64_t n = h->rows, k = taught ? teacher->cols : 1;
     UL_TRY(check_floats(loss, "loss", n, true));
     UL_TRY(check_floats(lse, "lse", n, true));
-    const int64_t need = ul::rows_head_bytes(n, table->rows);
+    const int64_t need = ul::rows_head_bytes(n, table->rows, h->cols, h->type);
     UL_TRY(check_workspace(workspace, workspace_bytes, need));
     const Span hs = span(*h), ts = span(*table), is = flat(ids, n * k * at.bytes), as = taught ? span(*teacher) : flat(nullptr, 0),
                ls = flat(loss, n * 4), es = flat(lse, n * 4), work = flat(workspace, need);
@@ -502,7 +502,7 @@ int umap_rows_layer_norm_grad(const umap_rows *dy, const umap_rows *h, const uma
 int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type)
 {
     UL_TRY(check_head_sizes(n, rows, cols, 1, type));
-    return ul::rows_head_bytes(n, rows);
+    return ul::rows_head_bytes(n, rows, cols, type);
 }
 
 int umap_rows_cross_entropy(const umap_rows *h, const umap_rows *table, const void *targets, int32_t target_type,
@@ -530,7 +530,7 @@ int umap_rows_cross_entropy_grad(const umap_rows *h, const umap_rows *table, con
 int64_t umap_rows_distill_workspace(int64_t n, int64_t rows, int32_t cols, int32_t k, int32_t type)
 {
     UL_TRY(check_head_sizes(n, rows, cols, k, type));
-    return ul::rows_head_bytes(n, rows);
+    return ul::rows_head_bytes(n, rows, cols, type);
 }
 
 int umap_rows_distill(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type,

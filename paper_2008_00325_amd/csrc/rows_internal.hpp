@@ -45,7 +45,7 @@ hipError_t launch_rows_layer_norm_grad(const umap_rows &dy, const umap_rows &h, 
 
 // ---- head: loss of rows against a table, with its gradient ----
 // teacher may be null: one token a row, with share 1.
-int64_t rows_head_bytes(int64_t n, int64_t vocab);
+int64_t rows_head_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t type);
 hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,
                             float teacher_scale, float *loss, float *lse, void *workspace, hipStream_t s);
 int64_t rows_head_grad_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t k, int32_t type);

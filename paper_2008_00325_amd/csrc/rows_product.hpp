@@ -75,7 +75,7 @@ struct Step {
     __device__ static __forceinline__ int turn(int r)
     {
         if constexpr (!kAcross) return r & 7;
-        else if constexpr (kElem == 2) return ((r & 3) | (r >> 1 & 4)) << 1;
+        else if constexpr (kElem == 2) return (((r & 3) | (r >> 1 & 4)) << 1) & (kRow - 1);
         else return r & 4;
     }
     // Row and column of LDS piece p, in memory, from the tile's origin.
@@ -132,43 +132,104 @@ __device__ __forceinline__ void landed()
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// One side's loads straight into LDS: 64 lanes, 64 pieces next to each other.  Lanes whose piece lies outside the
-// matrix are given an offset beyond the buffer, which loads zeros.
+// How a side's steps get into LDS, where piece p of a tile's step is thread p % THREADS's.
+
+// Straight: 64 lanes, 64 pieces next to each other.  Lanes whose piece lies outside the matrix are given an offset
+// beyond the buffer, which loads zeros.
 template <int T, bool kAcross, int I, int THREADS>
 struct DirectSide {
     using S = Step<T, kAcross, I>;
     typedef uint32_t Words __attribute__((ext_vector_type(4)));
     static constexpr int kElem = S::kElem, kCount = S::kPieces / THREADS, kRows = THREADS / S::kRow;
+    static constexpr int kInFlight = kCount;   // of a step, behind whose loads a wave waits
+    const ProductSide &side;
+    const int64_t i0;
     int row, col;
     uint32_t offset;
     static_assert(kRows % (kAcross && kElem == 2 ? 16 : 8) == 0, "a piece's row is turned alike kRows rows on");
-    __device__ __forceinline__ DirectSide(const ProductSide &side, int64_t i0)
+    __device__ __forceinline__ DirectSide(const ProductSide &of, int64_t first) : side(of), i0(first)
     {
         S::place(threadIdx.x, row, col);
         offset = (uint32_t)((row * side.stride + col) * kElem);
         if (kAcross && i0 + col >= side.cols) offset = 0x80000000u;
     }
-    // A step's loads: where they read from and go to, and the q-th of them.
-    struct Loads {
+    struct Loads {   // of one step
         Words buffer;
         uint32_t at, lds, step;
-        __device__ __forceinline__ void one(int q) const
-        {
-            // the whole offset in the lane's register: it is what the hardware compares with the buffer's length
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + q * THREADS * 16),
-                         "v"(at + q * step), "s"(buffer)
-                         : "memory");
-        }
     };
-    __device__ __forceinline__ Loads loads(const ProductSide &side, int64_t i0, int64_t k, bool there, Piece *to, int wave) const
+    __device__ __forceinline__ Loads loads(int64_t k, bool there, Piece *to) const
     {
         const int64_t r0 = kAcross ? k : i0, c0 = kAcross ? i0 : k;
         const char *const base = static_cast<const char *>(side.data) + (r0 * side.stride + c0) * kElem;
         const int64_t rows = min((int64_t)(kAcross ? S::kDepth : I), side.rows - r0);
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         return {Words{(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu,
                       there && rows > 0 ? (uint32_t)(rows * side.stride * kElem) : 0u, 0x00027000u},
                 !kAcross && k + col >= side.cols ? 0x80000000u : offset,
                 (uint32_t)(uintptr_t)(__attribute__((address_space(3))) Piece *)to + wave * 1024, (uint32_t)(kRows * side.stride * kElem)};
+    }
+    // The q-th of the step's loads.
+    __device__ __forceinline__ void one(const Loads &x, int q) const
+    {
+        // the whole offset in the lane's register: it is what the hardware compares with the buffer's length
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(x.lds + q * THREADS * 16),
+                     "v"(x.at + q * x.step), "s"(x.buffer)
+                     : "memory");
+    }
+    __device__ __forceinline__ void start(int64_t) {}
+};
+
+// By way of registers, which hold a step until its place in LDS is free: any alignment and any length of rows.
+template <int T, bool kAcross, int I, int THREADS>
+struct AnySide {
+    using S = Step<T, kAcross, I>;
+    static constexpr int kElem = S::kElem, kCount = S::kPieces / THREADS, kRows = THREADS / S::kRow;
+    static constexpr int kInFlight = 0;
+    const ProductSide &side;
+    const int64_t i0;
+    int64_t offset;
+    Piece held[kCount];
+    static_assert(kRows % (kAcross && kElem == 2 ? 16 : 8) == 0, "a piece's row is turned alike kRows rows on");
+    __device__ __forceinline__ AnySide(const ProductSide &of, int64_t first) : side(of), i0(first)
+    {
+        int row, col;
+        S::place(threadIdx.x, row, col);
+        offset = row * side.stride + col;
+    }
+    __device__ __forceinline__ void take(int64_t k, bool there, int q)
+    {
+        const int64_t r0 = kAcross ? k : i0, c0 = kAcross ? i0 : k;
+        constexpr int R = kAcross ? S::kDepth : I, C = kAcross ? I : S::kDepth;
+        if (r0 + R <= side.rows && c0 + C <= side.cols) {   // the same for all
+            const Elem<T> *const base = static_cast<const Elem<T> *>(side.data) + (r0 + q * kRows) * side.stride + c0;
+            held[q] = __builtin_bit_cast(Piece, load_raw<T, S::kPer>(base + offset));
+        } else if (there) {
+            int row, col;
+            S::place(threadIdx.x + q * THREADS, row, col);
+            held[q] = fetch_piece<T>(side, r0 + row, c0 + col);
+        }
+    }
+    struct Loads {   // puts the step that is held, takes the one behind it
+        int64_t next;
+        bool there;
+        Piece *lds;
+    };
+    __device__ __forceinline__ Loads loads(int64_t k, bool there, Piece *to) const
+    {
+        return {k + S::kDepth, there, to + threadIdx.x};
+    }
+    __device__ __forceinline__ void one(const Loads &x, int q)
+    {
+        x.lds[q * THREADS] = held[q];
+        take(x.next, x.there, q);
+    }
+    __device__ __forceinline__ void start(int64_t k)
+    {
+#pragma unroll
+        for (int q = 0; q < kCount; ++q) {
+            held[q] = Piece{};
+            take(k, true, q);
+        }
     }
 };
 
@@ -190,81 +251,27 @@ __device__ __forceinline__ TileAt tile_at(const Tiles &tiles, int block)
     return {first + in % rows, in / rows};
 }
 
-// A tile of WM x WN waves of FM x FN fragments each.  DEPTH 0: any sides; else steps in LDS at once, for sides in
-// whole pieces (direct_side).
-template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN, int DEPTH>
+// A tile of WM x WN waves of FM x FN fragments each; sides that go straight to LDS (direct_side) or any; DEPTH steps
+// in LDS, all but one of them on their way.
+//
+// A step is two halves.  The fragments of a half are fetched while the half before is multiplied, and a step's loads
+// are issued, when its place has become free, between the products too: evenly, since eight waves that issue
+// theirs at once wait for each other.
+template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN, bool kDirectA, bool kDirectB, int DEPTH>
 struct Product {
     static constexpr int kWM = WM, kWN = WN, kFM = FM, kFN = FN;
     static constexpr int kThreads = 64 * WM * WN, M = 16 * WM * FM, N = 16 * WN * FN;
     using A = Step<T, kAcrossA, M>;
     using B = Step<T, kAcrossB, N>;
-    static constexpr int kDepth = A::kDepth;
-    static constexpr int kLds = (A::kPieces + B::kPieces) * 16 * (DEPTH ? DEPTH : 1);
-    static constexpr int kA = A::kPieces / kThreads, kB = B::kPieces / kThreads;
-
-    template <class S, bool kAcross, int COUNT>
-    static __device__ __forceinline__ void fetch(const ProductSide &side, int64_t i0, int64_t k, Piece out[COUNT])
-    {
-#pragma unroll
-        for (int q = 0; q < COUNT; ++q) {
-            int r, c;
-            S::place(threadIdx.x + q * kThreads, r, c);
-            out[q] = kAcross ? fetch_piece<T>(side, k + r, i0 + c) : fetch_piece<T>(side, i0 + r, k + c);
-        }
-    }
+    using SideA = std::conditional_t<kDirectA, DirectSide<T, kAcrossA, M, kThreads>, AnySide<T, kAcrossA, M, kThreads>>;
+    using SideB = std::conditional_t<kDirectB, DirectSide<T, kAcrossB, N, kThreads>, AnySide<T, kAcrossB, N, kThreads>>;
+    static constexpr int kDepth = A::kDepth, kStage = A::kPieces + B::kPieces;
+    static constexpr int kLds = kStage * 16 * DEPTH;
+    static_assert(DEPTH == 2 || (kDirectA && kDirectB), "what goes by way of registers is a step ahead there already");
 
     // acc of rows m0 .. of A and n0 .. of B, over k0 <= k < k1 (k0 a multiple of kDepth).
     static __device__ __forceinline__ void run(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
                                                int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
-    {
-        if constexpr (DEPTH == 0) run_any(a, b, m0, n0, k0, k1, lds, acc);
-        else run_direct(a, b, m0, n0, k0, k1, lds, acc);
-    }
-
-    static __device__ __forceinline__ void run_any(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
-                                                   int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
-    {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-        Piece *const la = lds, *const lb = lds + A::kPieces;
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
-        Piece pa[kA], pb[kB];
-        if (k0 < k1) {
-            fetch<A, kAcrossA, kA>(a, m0, k0, pa);
-            fetch<B, kAcrossB, kB>(b, n0, k0, pb);
-        }
-        for (int64_t k = k0; k < k1; k += kDepth) {
-#pragma unroll
-            for (int q = 0; q < kA; ++q) la[threadIdx.x + q * kThreads] = pa[q];
-#pragma unroll
-            for (int q = 0; q < kB; ++q) lb[threadIdx.x + q * kThreads] = pb[q];
-            __syncthreads();
-            if (k + kDepth < k1) {
-                fetch<A, kAcrossA, kA>(a, m0, k + kDepth, pa);
-                fetch<B, kAcrossB, kB>(b, n0, k + kDepth, pb);
-            }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                Piece fb[FN];
-#pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = B::fragment(lb, (wn * FN + j) * 16, half, lane);
-#pragma unroll
-                for (int i = 0; i < FM; ++i) {
-                    const Piece fa = A::fragment(la, (wm * FM + i) * 16, half, lane);
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa, fb[j], acc[i][j]);
-                }
-            }
-            __syncthreads();
-        }
-    }
-
-    // Likewise with both sides in whole pieces (direct_side): loads go to LDS by themselves, DEPTH - 1 steps
-    // ahead, and the fragments of a half step are fetched while the half before is multiplied.
-    static __device__ __forceinline__ void run_direct(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
-                                                      int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 #pragma unroll
@@ -272,58 +279,59 @@ struct Product {
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
         if (k0 >= k1) return;
-        const DirectSide<T, kAcrossA, M, kThreads> da(a, m0);
-        const DirectSide<T, kAcrossB, N, kThreads> db(b, n0);
+        SideA da(a, m0);
+        SideB db(b, n0);
         const int steps = (int)((k1 - k0 + kDepth - 1) / kDepth);
-        constexpr int kStage = A::kPieces + B::kPieces;
-        constexpr int kLoads = kA + kB, kReads = FM + FN;
-        Piece fa[2][FM], fb[2][FN];
-        // A half step's products with the fragments of `set`, and between their rows, evenly, the fetches of the next
-        // half's fragments (step s, half `half`, into the other set) and the loads of step l (if kLoading).
+        constexpr int kA = SideA::kCount, kLoads = kA + SideB::kCount;
+        constexpr int kInFlight = kDirectA && kDirectB ? SideA::kInFlight + SideB::kInFlight : 0;
+        Piece fa[FM], fb[2][FN];
+        // A half step's products with fb[set], row by row, and between the rows the fetches of the next half's fragments
+        // (step s, half `half`; a row's of A once its own are multiplied) and, if `loading`, the loads of step l.
         auto half_step = [&](auto products, int set, int s, int half, auto loading, int l) {
             constexpr bool kProducts = decltype(products)::value, kLoading = decltype(loading)::value;
             const Piece *const from = lds + s % DEPTH * kStage;
             Piece *const to = lds + l % DEPTH * kStage;
-            const auto la = da.loads(a, m0, k0 + (int64_t)l * kDepth, l < steps, to, wave);
-            const auto lb = db.loads(b, n0, k0 + (int64_t)l * kDepth, l < steps, to + A::kPieces, wave);
+            const auto la = da.loads(k0 + (int64_t)l * kDepth, l < steps, to);
+            const auto lb = db.loads(k0 + (int64_t)l * kDepth, l < steps, to + A::kPieces);
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 if constexpr (kLoading) {
 #pragma unroll
                     for (int q = i * kLoads / FM; q < (i + 1) * kLoads / FM; ++q) {
-                        if (q < kA) la.one(q);
-                        else lb.one(q - kA);
+                        if (q < kA) da.one(la, q);
+                        else db.one(lb, q - kA);
                     }
                 }
 #pragma unroll
-                for (int q = i * kReads / FM; q < (i + 1) * kReads / FM; ++q) {
-                    if (q < FN) fb[set ^ 1][q] = B::fragment(from + A::kPieces, (wn * FN + q) * 16, half, lane);
-                    else fa[set ^ 1][q - FN] = A::fragment(from, (wm * FM + q - FN) * 16, half, lane);
-                }
+                for (int j = i * FN / FM; j < (i + 1) * FN / FM; ++j)
+                    fb[set ^ 1][j] = B::fragment(from + A::kPieces, (wn * FN + j) * 16, half, lane);
                 if constexpr (kProducts) {
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa[set][i], fb[set][j], acc[i][j]);
+                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply<T>(fa[i], fb[set][j], acc[i][j]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                fa[i] = A::fragment(from, (wm * FM + i) * 16, half, lane);
             }
         };
         constexpr auto yes = std::true_type{};
         constexpr auto no = std::false_type{};
+        da.start(k0);
+        db.start(k0);
         for (int s = 0; s < DEPTH; ++s) {
             Piece *const to = lds + s * kStage;
-            const auto la = da.loads(a, m0, k0 + (int64_t)s * kDepth, s < steps, to, wave);
-            const auto lb = db.loads(b, n0, k0 + (int64_t)s * kDepth, s < steps, to + A::kPieces, wave);
+            const auto la = da.loads(k0 + (int64_t)s * kDepth, s < steps, to);
+            const auto lb = db.loads(k0 + (int64_t)s * kDepth, s < steps, to + A::kPieces);
 #pragma unroll
-            for (int q = 0; q < kA; ++q) la.one(q);
+            for (int q = 0; q < kA; ++q) da.one(la, q);
 #pragma unroll
-            for (int q = 0; q < kB; ++q) lb.one(q);
+            for (int q = 0; q < SideB::kCount; ++q) db.one(lb, q);
         }
-        landed<(DEPTH - 1) * kLoads>();
+        landed<(DEPTH - 1) * kInFlight>();
         half_step(no, 1, 0, 0, no, 0);
         for (int s = 0; s < steps; ++s) {
             half_step(yes, 0, s, 1, no, 0);
-            landed<(DEPTH - 2) * kLoads>();   // step s + 1 is there, and everybody has fetched all of step s
-            half_step(yes, 1, s + 1, 0, yes, s + DEPTH);   // behind the last step: zeros, which nobody takes
+            landed<(DEPTH - 2) * kInFlight>();   // step s + 1 is there, and everybody has fetched all of step s
+            half_step(yes, 1, s + 1, 0, yes, s + DEPTH);   // behind the last step: nobody takes them
         }
         landed<0>();
     }
