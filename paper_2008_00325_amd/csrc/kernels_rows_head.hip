@@ -471,14 +471,21 @@ __global__ __launch_bounds__(256) void k_head_own(const int *token, const float 
 }
 
 // dh's sums over a part of the piece, [split][t][c], added to those of the pieces before.
+struct RowSums {
+    ProductSide w, d;
+    Tiles tiles;
+    int64_t depth;
+    bool add;
+    float *sums;
+    int64_t pitch;
+};
 template <int T, class P>
-__global__ __launch_bounds__(P::kThreads) void k_head_dh(ProductSide w, ProductSide d, Tiles tiles, int64_t depth, bool add,
-                                                         float *sums, int64_t pitch)
+__device__ __forceinline__ void rows_tile(const RowSums &x, int block, Piece *lds)
 {
-    __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
-    const int split = blockIdx.x / (tiles.m * tiles.n);
-    const TileAt tile = tile_at(tiles, blockIdx.x % (tiles.m * tiles.n));
+    const auto &[w, d, tiles, depth, add, sums, pitch] = x;
+    const int split = block / (tiles.m * tiles.n);
+    const TileAt tile = tile_at(tiles, block % (tiles.m * tiles.n));
     const int64_t m0 = (int64_t)tile.m * P::M, n0 = (int64_t)tile.n * P::N, k0 = split * depth;
     Acc4 acc[FM][FN];
     P::run(w, d, m0, n0, k0, min(k0 + depth, w.rows), lds, acc);
@@ -497,14 +504,31 @@ __global__ __launch_bounds__(P::kThreads) void k_head_dh(ProductSide w, ProductS
     }
 }
 
-template <int T>
+// dh from the sums' parts: four columns per thread, or per 16 threads where there are many parts, each of which adds
+// every 16th.
+template <int T, int SLICES>
 __global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int parts, int64_t pitch, const int *exponent, umap_rows dh)
 {
+    constexpr int kGroups = 256 / SLICES;
+    __shared__ Acc4 part[SLICES > 1 ? SLICES : 1][kGroups];
     const int64_t groups = pitch / 4, total = dh.rows * groups;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / groups, c = i % groups * 4;
+    const int slice = threadIdx.x / kGroups, in = threadIdx.x % kGroups;
+    for (int64_t i0 = (int64_t)blockIdx.x * kGroups; i0 < total; i0 += (int64_t)gridDim.x * kGroups) {
+        const int64_t i = i0 + in, t = i / groups, c = i % groups * 4;
         Acc4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < parts; ++s) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + t) * pitch + c);
+        if (i < total) {
+#pragma unroll 4
+            for (int s = slice; s < parts; s += SLICES) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + t) * pitch + c);
+        }
+        if constexpr (SLICES > 1) {
+            __syncthreads();
+            part[slice][in] = sum;
+            __syncthreads();
+            if (slice) continue;
+#pragma unroll
+            for (int s = 1; s < SLICES; ++s) sum += part[s][in];
+        }
+        if (i >= total) continue;
         const int e = exponent[t];
         float v[4];
 #pragma unroll
@@ -521,13 +545,19 @@ __global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int par
 }
 
 // The table's gradient for a piece's rows.
+struct TableRows {
+    ProductSide h, d;
+    Tiles tiles;
+    RowWeights weights;
+    bool add;
+    umap_rows dw;
+};
 template <int T, class P>
-__global__ __launch_bounds__(P::kThreads) void k_head_dw(ProductSide h, ProductSide d, Tiles tiles, RowWeights weights, bool add,
-                                                         umap_rows dw)
+__device__ __forceinline__ void table_tile(const TableRows &x, int block, Piece *lds)
 {
-    __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
-    const TileAt at = tile_at(tiles, blockIdx.x);
+    const auto &[h, d, tiles, weights, add, dw] = x;
+    const TileAt at = tile_at(tiles, block);
     const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
     P::run(h, d, m0, n0, 0, h.rows, lds, acc);
@@ -568,6 +598,28 @@ __global__ __launch_bounds__(P::kThreads) void k_head_dw(ProductSide h, ProductS
     }
 }
 
+template <int T, class P>
+__global__ __launch_bounds__(P::kThreads) void k_head_dh(RowSums x)
+{
+    __shared__ __align__(16) Piece lds[P::kLds / 16];
+    rows_tile<T, P>(x, blockIdx.x, lds);
+}
+template <int T, class P>
+__global__ __launch_bounds__(P::kThreads) void k_head_dw(TableRows x)
+{
+    __shared__ __align__(16) Piece lds[P::kLds / 16];
+    table_tile<T, P>(x, blockIdx.x, lds);
+}
+// Both in one launch, for products too small to fill the card: `rows` workgroups of the first.
+template <int T, class P, class Q>
+__global__ __launch_bounds__(P::kThreads) void k_head_dh_dw(RowSums x, int rows, TableRows y)
+{
+    static_assert(P::kThreads == Q::kThreads, "");
+    __shared__ __align__(16) Piece lds[std::max(P::kLds, Q::kLds) / 16];
+    if ((int)blockIdx.x < rows) rows_tile<T, P>(x, blockIdx.x, lds);
+    else table_tile<T, Q>(y, blockIdx.x - rows, lds);
+}
+
 // ---- sizes -----------------------------------------------------------------------------------
 
 constexpr int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -575,23 +627,40 @@ constexpr int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
 
-// Tiles of 256 x 256, 128 x 128 and 64 x 64, and of 64 x 32 for few rows of h.
+// Tiles of 256 x 256; of 128 x 128, two workgroups to a CU or, where there is but one, with more steps on their way;
+// of 64 x 64; and of 64 x 32 for few rows of h.
 template <int T, bool AA, bool AB, bool DA, bool DB>
 using Large = Product<T, AA, AB, 2, 4, 8, 4, DA, DB, 2>;
-template <int T, bool AA, bool AB, bool DA, bool DB>
-using Small = Product<T, AA, AB, 2, 2, 4, 4, DA, DB, DA && DB ? 4 : 2>;
+template <int T, bool AA, bool AB, bool DA, bool DB, int DEPTH>
+using Small = Product<T, AA, AB, 2, 2, 4, 4, DA, DB, DEPTH>;
 template <int T, bool AA, bool AB, bool DA, bool DB>
 using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DA, DB, DA && DB ? 4 : 2>;
 template <int T, bool DA, bool DB>
 using Few = Product<T, false, false, 4, 1, 1, 2, DA, DB, DA && DB ? 4 : 2>;
 constexpr int64_t kFewRows = 32;
 
-// The largest tiles that give enough workgroups: `splits` of the products' depth at most, n rows of h's side.
-int64_t tile_for(int64_t m, int64_t n, int64_t splits)
+enum class Shape { large, pairs, deep, tiny };
+constexpr int64_t side_of(Shape s) { return s == Shape::large ? 256 : s == Shape::tiny ? 64 : 128; }
+
+// Parts of a product's depth, `most` of them at the utmost, so that `tiles` tiles fill `places`.
+constexpr int64_t parts_for(int64_t tiles, int64_t places, int64_t most) { return std::max<int64_t>(1, std::min(places / tiles, most)); }
+// Rounds that tiles take, in parts of their depth, over the parts.
+double rounds_of(int64_t tiles, int64_t places, int64_t most)
+{
+    const int64_t parts = parts_for(tiles, places, most);
+    return (double)over(tiles * parts, places) / (double)parts;
+}
+
+// The shape for a product of m x n (n of h's side) whose depth may be split into `most` parts.  A round of 256 large
+// tiles takes as long as two of 512 small ones would, if these were not 1.2 times as slow (fp32's are not: there the
+// matrix cores are).
+Shape shape_for(int64_t m, int64_t n, int64_t most, int64_t elem)
 {
     n = std::max<int64_t>(n, 1);
-    if (over(m, 256) * over(n, 256) * splits >= 192) return 256;
-    return over(m, 128) * over(n, 128) * splits >= 128 ? 128 : 64;
+    const int64_t large = over(m, 256) * over(n, 256), small = over(m, 128) * over(n, 128);
+    if (small * most < 128) return Shape::tiny;
+    if (large * most >= 192 && 4.0 * rounds_of(large, 256, most) <= (elem == 2 ? 2.4 : 2.0) * rounds_of(small, 512, most)) return Shape::large;
+    return small > 256 || most > 1 ? Shape::pairs : Shape::deep;
 }
 
 // Rows of h from which on a table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at
@@ -627,7 +696,7 @@ constexpr int64_t kTwoPartRows = 128;
 struct GradSizes {
     int64_t n, vocab, cols, k, elem;
     int64_t parts;     // of D
-    int64_t dh_tile;
+    Shape dh_shape;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
     int64_t largest, number, exponent, token, value, copy, scaled, d, sums, packed, total;
@@ -645,9 +714,9 @@ struct GradSizes {
         sum_pitch = up(cols, 4);
         // the product for dh: parts of the piece at a time where its tiles alone do not fill the card
         const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / (elem == 4 ? 2 : 4));
-        dh_tile = tile_for(cols, n * parts, most_splits);
-        const int64_t tiles = over(cols, dh_tile) * over(std::max<int64_t>(n * parts, 1), dh_tile);
-        splits = std::max<int64_t>(1, std::min((dh_tile == 64 ? 512 : 256) / tiles, most_splits));
+        dh_shape = shape_for(cols, n * parts, most_splits, elem);
+        const int64_t side = side_of(dh_shape), tiles = over(cols, side) * over(std::max<int64_t>(n * parts, 1), side);
+        splits = parts_for(tiles, dh_shape == Shape::large ? 256 : 512, most_splits);
         depth = over(steps, splits) * step;
         splits = over(piece, depth);
         int64_t at = 0;
@@ -670,22 +739,24 @@ struct GradSizes {
     }
 };
 
-// Calls f with the shape of a product's tiles.  A table that does not go straight to LDS is only met with few rows of
-// h (more of them, and it is copied), for which the large tiles are none.
+// Calls f with a product's tiles.  A table that does not go straight to LDS is only met with few rows of h (with more of
+// them it is copied), for which the large tiles are none.
 template <int T, bool AA, bool AB, bool DA, typename F>
-hipError_t by_tile(int64_t tile, F f)
+hipError_t by_shape(Shape shape, F f)
 {
-    if constexpr (DA)
-        if (tile == 256) return f(Large<T, AA, AB, DA, true>{});
-    return tile >= 128 ? f(Small<T, AA, AB, DA, true>{}) : f(Tiny<T, AA, AB, DA, true>{});
+    if constexpr (DA) {
+        if (shape == Shape::large) return f(Large<T, AA, AB, DA, true>{});
+        if (shape == Shape::deep) return f(Small<T, AA, AB, DA, true, 4>{});
+    }
+    return shape != Shape::tiny ? f(Small<T, AA, AB, DA, true, 2>{}) : f(Tiny<T, AA, AB, DA, true>{});
 }
 // `rows` of a table, which goes straight or not, against rows of h.
 template <int T, typename F>
 hipError_t by_logits(int64_t rows, bool direct, const ProductSide &h, F f)
 {
     if (h.rows <= kFewRows) return direct && direct_side<T>(h) ? f(Few<T, true, true>{}) : f(Few<T, false, false>{});
-    const int64_t tile = tile_for(rows, h.rows, 1);
-    return direct ? by_tile<T, false, false, true>(tile, f) : by_tile<T, false, false, false>(tile, f);
+    const Shape shape = shape_for(rows, h.rows, 1, sizeof(Elem<T>));
+    return direct ? by_shape<T, false, false, true>(shape, f) : by_shape<T, false, false, false>(shape, f);
 }
 
 // Calls f with the waves of a row: one, or four where rows are few or have many tokens.
@@ -823,36 +894,57 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                                    token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch, below);
                 UL_LAUNCHED(hipGetLastError());
             }
-            if (dh) {
-                auto rows_sums = [&](auto shape) {
-                    using P = decltype(shape);
-                    const Tiles g = tiles_of<P>(z.cols, d_rows);
-                    hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s, w,
-                                       d_side, g, z.depth, first > 0, sums, z.sum_pitch);
-                    return hipGetLastError();
-                };
-                UL_LAUNCHED(whole || packing ? (by_tile<T, true, false, true>(z.dh_tile, rows_sums))
-                                             : (by_tile<T, true, false, false>(z.dh_tile, rows_sums)));
-            }
         }
+        umap_rows part = {};
+        Shape dw_shape = Shape::tiny;
         if (dtable) {
-            umap_rows part = *dtable;
+            part = *dtable;
             part.data = static_cast<Elem<T> *>(dtable->data) + first * dtable->stride;
             part.rows = here;
-            auto table_rows = [&](auto shape) {
+            dw_shape = shape_for(z.cols, here, 1, z.elem);
+        }
+        const bool sums_due = dh && z.n > 0;
+        auto row_sums = [&](Tiles g) { return RowSums{w, d_side, g, z.depth, first > 0, sums, z.sum_pitch}; };
+        auto table_rows = [&](Tiles g) { return TableRows{weighted, d_side, g, weights, add, part}; };
+        if (sums_due && dtable && (whole || packing) && z.dh_shape == Shape::tiny && dw_shape == Shape::tiny) {
+            using P = Tiny<T, true, false, true, true>;
+            using Q = Tiny<T, true, true, true, true>;
+            const Tiles g = tiles_of<P>(z.cols, d_rows), o = tiles_of<Q>(z.cols, here);
+            const int64_t rows_count = (int64_t)g.m * g.n * z.splits;
+            hipLaunchKernelGGL((k_head_dh_dw<T, P, Q>), dim3((unsigned)(rows_count + (int64_t)o.m * o.n)), dim3(P::kThreads), 0, s,
+                               row_sums(g), (int)rows_count, table_rows(o));
+            UL_LAUNCHED(hipGetLastError());
+            continue;
+        }
+        if (sums_due) {
+            auto launch = [&](auto shape) {
                 using P = decltype(shape);
-                const Tiles g = tiles_of<P>(z.cols, here);
-                hipLaunchKernelGGL((k_head_dw<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, weighted, d_side, g,
-                                   weights, add, part);
+                const Tiles g = tiles_of<P>(z.cols, d_rows);
+                hipLaunchKernelGGL((k_head_dh<T, P>), dim3((unsigned)((int64_t)g.m * g.n * z.splits)), dim3(P::kThreads), 0, s,
+                                   row_sums(g));
                 return hipGetLastError();
             };
-            UL_LAUNCHED((by_tile<T, true, true, true>(tile_for(z.cols, here, 1), table_rows)));
+            UL_LAUNCHED(whole || packing ? (by_shape<T, true, false, true>(z.dh_shape, launch))
+                                         : (by_shape<T, true, false, false>(z.dh_shape, launch)));
+        }
+        if (dtable) {
+            UL_LAUNCHED((by_shape<T, true, true, true>(dw_shape, [&](auto shape) {
+                using P = decltype(shape);
+                const Tiles g = tiles_of<P>(z.cols, here);
+                hipLaunchKernelGGL((k_head_dw<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, table_rows(g));
+                return hipGetLastError();
+            })));
         }
     }
     if (dh && z.n > 0) {
         const int64_t total = z.n * z.sum_pitch / 4;
-        hipLaunchKernelGGL((k_head_dh_join<T>), dim3((unsigned)std::min<int64_t>(4096, over(total, 256))), dim3(256), 0, s, sums,
-                           (int)(z.splits * z.parts), z.sum_pitch, weights.exponent, *dh);
+        const int parts = (int)(z.splits * z.parts);
+        if (parts >= 8)
+            hipLaunchKernelGGL((k_head_dh_join<T, 16>), dim3((unsigned)std::min<int64_t>(4096, over(total, 16))), dim3(256), 0, s, sums,
+                               parts, z.sum_pitch, weights.exponent, *dh);
+        else
+            hipLaunchKernelGGL((k_head_dh_join<T, 1>), dim3((unsigned)std::min<int64_t>(4096, over(total, 256))), dim3(256), 0, s, sums,
+                               parts, z.sum_pitch, weights.exponent, *dh);
         UL_LAUNCHED(hipGetLastError());
     }
     return hipSuccess;
