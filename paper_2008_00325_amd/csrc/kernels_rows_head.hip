@@ -189,11 +189,20 @@ struct OwnToken {
     int id = -1;
     float share, log_share = minus_inf();
     bool any;
+    bool alone = false;   // all threads have the row's one token
     __device__ __forceinline__ OwnToken(const RowTeam<WAVES> &team, const Taught &x, int64_t t, int64_t rows)
     {
+        if (!x.teacher) {   // one token, which all threads know
+            id = (int)row_of(x.ids, t, rows);
+            share = 1.0f;
+            log_share = 0.0f;
+            any = id >= 0;
+            alone = true;
+            return;
+        }
         if (team.me < x.k) id = (int)row_of(x.ids, t * x.k + team.me, rows);
         if (id >= 0) {
-            log_share = x.teacher ? teacher_at(x, t, team.me) * x.scale : 0.0f;
+            log_share = teacher_at(x, t, team.me) * x.scale;
             if (log_share == minus_inf()) id = -1;
         }
         if constexpr (WAVES > 1) team.lds->id[team.me] = id;   // read behind the reductions' barriers
@@ -221,7 +230,7 @@ __device__ __forceinline__ void fetch8(const Elem<T> *row, int c, int cols, floa
     }
 }
 
-// Dot products of a row of h with the table's rows of its k tokens: each thread's token's.
+// Dot products of a row of h with the table's rows of its k tokens: each thread's token's (the one token's, for all).
 template <int T, int WAVES>
 __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Elem<T> *h, const ProductSide &w,
                                            const OwnToken<WAVES> &own, int k, float scale)
@@ -229,6 +238,17 @@ __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Ele
     constexpr int kAtOnce = 4;
     const int cols = (int)w.cols, lane = team.me & 63;
     float z = 0.0f;
+    if (k == 1 && own.alone) {
+        const Elem<T> *const row = static_cast<const Elem<T> *>(w.data) + (int64_t)max(own.id, 0) * w.stride;
+        for (int c = team.me * 8; own.id >= 0 && c < cols; c += 8 * RowTeam<WAVES>::kThreads) {
+            float a[8], b[8];
+            fetch8<T>(h, c, cols, a);
+            fetch8<T>(row, c, cols, b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z = fmaf(a[j], b[j], z);
+        }
+        return team.sum(z) * scale;
+    }
     for (int e0 = kAtOnce * team.wave; e0 < k; e0 += kAtOnce * WAVES) {
         const Elem<T> *row[kAtOnce];
         float sum[kAtOnce] = {};
@@ -297,7 +317,8 @@ __global__ __launch_bounds__(256) void k_head_loss(ProductSide w, ProductSide h,
     const float z = own_logit<T, WAVES>(team, static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, scale);
     const float most = team.max(mine.m);
     const float sum = Logit<T>::natural(most + Logit<T>::log(team.sum(mine.s * Logit<T>::exp(mine.m - MaxSum::base(most)))));
-    const float all = team.sum(own.id >= 0 && own.share != 0.0f ? own.share * (own.log_share + (sum - z)) : 0.0f);
+    float all = own.id >= 0 && own.share != 0.0f ? own.share * (own.log_share + (sum - z)) : 0.0f;
+    if (!own.alone) all = team.sum(all);
     if (team.me == 0) {
         lse[first + t] = sum;
         // rounding can take a loss of nearly nothing below it
@@ -372,7 +393,8 @@ __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h,
     // a token that comes twice: the first place has all its shares
     float share = 0.0f;
     bool again = false;
-    for (int o = 0; o < taught.k; ++o) {
+    if (own.alone) share = 1.0f;
+    for (int o = 0; o < (own.alone ? 0 : taught.k); ++o) {
         const int other = team.of(own.id, lds.id, o);
         const float more = team.of(own.share, lds.share, o);
         if (other != own.id) continue;
