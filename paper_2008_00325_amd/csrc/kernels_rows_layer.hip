@@ -4,9 +4,11 @@
 //   gradient  u = off rho, g = dy weight, dx = rho (g - mean g - u mean(g u)) + dh, dweight = sum dy u, dbias = sum dy
 //
 // Bound by memory: as in the root-mean-square norm a row is read once and stays in
-// registers, in the same lanes, waves and workgroups.  The sums take two turns: the mean first, then the
-// sums of h - mean and of its square, the first of which corrects the mean's own rounding (a row of 1000 +- 1
-// keeps its digits).  The gradient keeps the sums of dweight and dbias of a workgroup's rows in registers or
+// registers, in the same lanes, waves and workgroups.  All its sums are taken at once, of differences from the row's
+// first value h0: e = h - h0, mean h = h0 + mean e, mean off^2 = mean e^2 - (mean e)^2, and mean(g off) likewise.  That
+// loses at most the factor 1 + (mean e)^2 / mean off^2 in precision, however far the mean is from zero; rows for which it
+// is over 17 (h0 four deviations off), or whose squares leave fp32's range, are read again and taken in two turns, the
+// mean first.  The gradient keeps the sums of dweight and dbias of a workgroup's rows in registers or
 // LDS; a second launch joins the workgroups in order.  Beyond 16,384 columns neither holds them: there each row's
 // mean and rho are written down, and a launch of its own forms the two sums, reading dy and h a second time.
 #include "rows_norm_device.hpp"
@@ -15,75 +17,108 @@ namespace ul {
 
 namespace {
 
+// v plus its value 16 or 32 lanes away, in both: the hardware swaps the halves of two registers, here of one and the same.
+__device__ __forceinline__ float add_16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Sums over a row's threads, K values at once; the two buffers take turns, so that one barrier is
 // enough: a buffer is written again only after the next sum's barrier.
 struct LayerLds {
-    float v[2][2][16];
+    float v[2][16][4];
 };
 template <int LANES>
 struct LayerSums {
     LayerLds *lds;
     int turn = 0;
-    __device__ __forceinline__ void operator()(float (&v)[2])
+    template <int K>
+    __device__ __forceinline__ void operator()(float (&v)[K])
     {
-        v[0] = lanes_sum<LANES ? LANES : 64>(v[0]);
-        v[1] = lanes_sum<LANES ? LANES : 64>(v[1]);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = add_dpp<kXor1>(v[k]);
+            v[k] = add_dpp<kXor2>(v[k]);
+            v[k] = add_dpp<kHalfMirror>(v[k]);
+            if constexpr (LANES != 8) v[k] = add_dpp<kMirror>(v[k]);
+            if constexpr (LANES == 32 || LANES == 64 || LANES == kBlock) v[k] = add_16(v[k]);
+            if constexpr (LANES == 64 || LANES == kBlock) v[k] = add_32(v[k]);
+        }
         if constexpr (LANES == kBlock) {
+            typedef float F4 __attribute__((ext_vector_type(4)));
+            F4(&at)[16] = reinterpret_cast<F4(&)[16]>(lds->v[turn]);
             if ((threadIdx.x & 63) == 0) {
-                lds->v[turn][0][threadIdx.x >> 6] = v[0];
-                lds->v[turn][1][threadIdx.x >> 6] = v[1];
+                F4 mine = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < K; ++k) mine[k] = v[k];
+                at[threadIdx.x >> 6] = mine;
             }
             __syncthreads();
-            v[0] = v[1] = 0.0f;
-            for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
-                v[0] += lds->v[turn][0][w];
-                v[1] += lds->v[turn][1][w];
-            }
+            F4 all = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int w = 0; w < (int)(blockDim.x >> 6); ++w) all += at[w];
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = all[k];
             turn ^= 1;
         }
     }
 };
 
-// Sums of a[i][j] and of a[i][j] b[i][j] over a row.
-template <int LANES, int V, int N>
-__device__ __forceinline__ void row_sums(LayerSums<LANES> &row, const float (&a)[N][V], const float (&b)[N][V], int me, int TPR,
-                                         int cols, float (&sums)[2])
+// Sums over a row of what `terms` adds for column j of the thread's vector i.
+template <int LANES, int V, int N, int K, typename Terms>
+__device__ __forceinline__ void row_sums(LayerSums<LANES> &row, int me, int TPR, int cols, float (&sums)[K], Terms terms)
 {
-    sums[0] = sums[1] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) sums[k] = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const Cols<V> c(V * (me + i * TPR), cols);
-        float s = 0.0f, q = 0.0f;
+        float s[K] = {};
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            s += a[i][j];
-            q = fmaf(a[i][j], b[i][j], q);
-        }
+        for (int j = 0; j < V; ++j) terms(i, j, s);
         if (c.shared()) {
-            s = q = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[k] = 0.0f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                s = c.counts(j) ? s + a[i][j] : s;
-                q = c.counts(j) ? fmaf(a[i][j], b[i][j], q) : q;
+                float more[K];
+#pragma unroll
+                for (int k = 0; k < K; ++k) more[k] = s[k];
+                terms(i, j, more);
+#pragma unroll
+                for (int k = 0; k < K; ++k) s[k] = c.counts(j) ? more[k] : s[k];
             }
         }
-        sums[0] += c.live() ? s : 0.0f;
-        sums[1] += c.live() ? q : 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) sums[k] += c.live() ? s[k] : 0.0f;
     }
     row(sums);
 }
 
-// What centres a row: e = k (h - mean), rho = 1 / sqrt(mean e^2 + k^2 eps).  k is a power of two, 1 but where
-// squares would leave fp32's range: of h, before the mean is taken, or of h - mean, where they would vanish.
+// What centres a row: e - shift = k (h - mean h), rho = 1 / sqrt(mean of its square + k^2 eps).  k is a power of two, 1 but
+// where squares would leave fp32's range.
 struct Spread {
     float rho, k;
-    float mean, left;   // e = (k h - mean) - left, or k (h - mean) - left where k > 1
+    float mean, left;   // k (h - mean h) = (k h - mean) - left, or k (h - mean) - left where k > 1
 };
-template <int LANES, int V, int N>
-__device__ __forceinline__ Spread centre(LayerSums<LANES> &row, float (&e)[N][V], int me, int TPR, int cols, float eps)
+// With a gradient g: mean g, and the mean of g times k (h - mean h) rho.
+struct Along {
+    float mean_g, along;
+};
+
+// In two turns, for any row; e: h on the way in, centred on the way out.
+template <int LANES, int V, int N, bool kGrad>
+__device__ __forceinline__ Spread centre(LayerSums<LANES> &row, float (&e)[N][V], const float (&g)[kGrad ? N : 1][V], float sum_g,
+                                         int me, int TPR, int cols, float eps, Along *along)
 {
     const float over_cols = 1.0f / (float)cols;
-    float sums[2], k = 1.0f, mean;
+    constexpr int K = kGrad ? 3 : 2;
+    float sums[K], k = 1.0f, mean, left = 0.0f;
     auto times = [&](float by) {
         k *= by;
 #pragma unroll
@@ -97,30 +132,36 @@ __device__ __forceinline__ Spread centre(LayerSums<LANES> &row, float (&e)[N][V]
 #pragma unroll
             for (int j = 0; j < V; ++j) e[i][j] -= by;
     };
-    row_sums<LANES, V, N>(row, e, e, me, TPR, cols, sums);
+    auto squares = [&] {
+        row_sums<LANES, V, N>(row, me, TPR, cols, sums, [&](int i, int j, float (&s)[K]) {
+            s[0] += e[i][j];
+            s[1] = fmaf(e[i][j], e[i][j], s[1]);
+            if constexpr (kGrad) s[2] = fmaf(g[i][j], e[i][j], s[2]);
+        });
+    };
+    squares();
     if (!(sums[1] < __builtin_inff())) {
         times(0x1p-80f);
-        row_sums<LANES, V, N>(row, e, e, me, TPR, cols, sums);
+        squares();
     }
     mean = sums[0] * over_cols;
     less(mean);
-    row_sums<LANES, V, N>(row, e, e, me, TPR, cols, sums);
-    float left = 0.0f;
+    squares();
     // Values within some 2^-10 of their mean: their differences from it are exact, and so are those from the first
     // one's, which are zeros where the values are equal (differences from a rounded mean would be noise).
     auto from_first = [&] {
-        float first[2] = {me == 0 ? e[0][0] : 0.0f, 0.0f};
+        float first[1] = {me == 0 ? e[0][0] : 0.0f};
         row(first);
         less(first[0]);
         left += first[0];
-        row_sums<LANES, V, N>(row, e, e, me, TPR, cols, sums);
+        squares();
     };
     if (sums[1] < 0x1p-20f * (mean * mean) * (float)cols) from_first();
     if (k < 1.0f && sums[1] < 0x1p-40f) {   // large, but nearly alike
         times(0x1p80f);
         mean *= 0x1p80f;
         left *= 0x1p80f;
-        row_sums<LANES, V, N>(row, e, e, me, TPR, cols, sums);
+        squares();
     }
     if (k == 1.0f && sums[1] < kSmallSum && eps < kSmallSum) {
         times(0x1p94f);
@@ -131,7 +172,39 @@ __device__ __forceinline__ Spread centre(LayerSums<LANES> &row, float (&e)[N][V]
     less(rest);
     float var = fmaf(sums[1], over_cols, -rest * rest);
     var = var < 0.0f ? 0.0f : var;
-    return {__builtin_amdgcn_rsqf(var + eps * k * k), k, mean, left + rest};
+    const float rho = __builtin_amdgcn_rsqf(var + eps * k * k);
+    if constexpr (kGrad) *along = {sum_g * over_cols, fmaf(-rest, sum_g, sums[K - 1]) * rho * over_cols};
+    return {rho, k, mean, left + rest};
+}
+
+// In one turn where that is precise.  e: h - h0 on the way in (and out, `shift` above zero mean), or centred on the way out;
+// `again` forms h once more.
+template <int LANES, int V, int N, bool kGrad, typename Again>
+__device__ __forceinline__ Spread spread(LayerSums<LANES> &row, float (&e)[N][V], const float (&g)[kGrad ? N : 1][V], float h0,
+                                         int me, int TPR, int cols, float eps, float &shift, Along *along, Again again)
+{
+    const float over_cols = 1.0f / (float)cols;
+    constexpr int K = kGrad ? 4 : 2;
+    float sums[K];
+    row_sums<LANES, V, N>(row, me, TPR, cols, sums, [&](int i, int j, float (&s)[K]) {
+        s[0] += e[i][j];
+        s[1] = fmaf(e[i][j], e[i][j], s[1]);
+        if constexpr (kGrad) {
+            s[2] += g[i][j];
+            s[3] = fmaf(g[i][j], e[i][j], s[3]);
+        }
+    });
+    const float sum_g = kGrad ? sums[K - 2] : 0.0f;
+    shift = sums[0] * over_cols;
+    const float var = fmaf(sums[1], over_cols, -shift * shift);
+    if (sums[1] < __builtin_inff() && 16.0f * var >= shift * shift && (sums[1] >= kSmallSum || eps >= kSmallSum)) {
+        const float rho = __builtin_amdgcn_rsqf(var + eps);
+        if constexpr (kGrad) *along = {sum_g * over_cols, fmaf(-shift, sum_g, sums[K - 1]) * rho * over_cols};
+        return {rho, 1.0f, h0, shift};
+    }
+    shift = 0.0f;
+    again();
+    return centre<LANES, V, N, kGrad>(row, e, g, sum_g, me, TPR, cols, eps, along);
 }
 
 // N vectors of V columns per thread.  MORE: a thread keeps its weights over its rows and reads a row ahead.
@@ -158,7 +231,10 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_layer(umap_rows x,
         for (int i = 0; i < N; ++i) read_weight(i, w[i], b[i]);
     }
     Raw<TX, V> a[N], r[N];
+    Elem<TX> a0, r0;   // the row's first value
     auto read = [&](int64_t t) {
+        a0 = row_ptr<TX>(x, t)[0];
+        if (residual.data) r0 = row_ptr<TX>(residual, t)[0];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = Cols<V>(V * (me + i * TPR), cols).at;
@@ -172,6 +248,8 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_layer(umap_rows x,
     for (; t < y.rows; t += step) {
         if (!MORE) read(t);
         float e[N][V];
+        const float h0 = residual.data ? elem_float<TX>(a0) + elem_float<TX>(r0) : elem_float<TX>(a0);
+        Raw<TX, V> keep[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             floats_of<TX, V>(a[i], e[i]);
@@ -181,20 +259,34 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_layer(umap_rows x,
 #pragma unroll
                 for (int j = 0; j < V; ++j) e[i][j] += more[j];
             }
+            if (h.data) keep[i] = raw_of<TX, V>(e[i]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) e[i][j] -= h0;
         }
         if (MORE && t + step < y.rows) read(t + step);
-        Raw<TX, V> keep[N];
-        if (h.data) {
+        const float none[1][V] = {};
+        float shift;
+        const Spread s = spread<LANES, V, N, false>(row, e, none, h0, me, TPR, cols, eps, shift, nullptr, [&] {
 #pragma unroll
-            for (int i = 0; i < N; ++i) keep[i] = raw_of<TX, V>(e[i]);
-        }
-        const Spread s = centre<LANES, V, N>(row, e, me, TPR, cols, eps);
+            for (int i = 0; i < N; ++i) {
+                const int at = Cols<V>(V * (me + i * TPR), cols).at;
+                floats_of<TX, V>(load_raw<TX, V>(row_ptr<TX>(x, t) + at), e[i]);
+                if (residual.data) {
+                    float more[V];
+                    floats_of<TX, V>(load_raw<TX, V>(row_ptr<TX>(residual, t) + at), more);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) e[i][j] += more[j];
+                }
+            }
+        });
+        const float less = -shift * s.rho;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const Cols<V> c(V * (me + i * TPR), cols);
             if constexpr (!MORE) read_weight(i, w[0], b[0]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) e[i][j] = fmaf(e[i][j] * s.rho, w[MORE ? i : 0][j], b[MORE ? i : 0][j]);
+            for (int j = 0; j < V; ++j)
+                e[i][j] = fmaf(fmaf(e[i][j], s.rho, less), w[MORE ? i : 0][j], b[MORE ? i : 0][j]);
             if (!c.live()) continue;
             // behind the sums' barriers: h may lie where other waves read
             if (h.data) store_once<TX, V>(row_out<TX>(h, t) + c.at, keep[i]);
@@ -232,7 +324,9 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_layer_grad(umap_ro
             else dw[i][j] = db[i][j] = 0.0f;
         }
     Raw<TX, V> a[N], b[N], u[N];
+    Elem<TX> a0;   // the row's first value
     auto read = [&](int64_t t) {
+        a0 = row_ptr<TX>(h, t)[0];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = Cols<V>(V * (me + i * TPR), cols).at;
@@ -247,43 +341,58 @@ __global__ __launch_bounds__(kMostThreads<LANES>) void k_rows_layer_grad(umap_ro
     for (; t < dy.rows; t += step) {
         if (!MORE) read(t);
         Raw<TX, V> db_raw[N], ua[N];
-        float e[N][V];
+        float e[N][V], g[N][V];
+        const float h0 = elem_float<TX>(a0);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             floats_of<TX, V>(a[i], e[i]);
+            floats_of<TX, V>(b[i], g[i]);
             db_raw[i] = b[i];
             if (dh.data) ua[i] = u[i];
-        }
-        if (MORE && t + step < dy.rows) read(t + step);
-        const Spread s = centre<LANES, V, N>(row, e, me, TPR, cols, eps);
-        float g[N][V], sums[2];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const Cols<V> c(V * (me + i * TPR), cols);
-            floats_of<TX, V>(db_raw[i], g[i]);
-            if constexpr (!MORE) load_weight<V>(weight, c.at, w[0]);
+            if constexpr (!MORE) load_weight<V>(weight, Cols<V>(V * (me + i * TPR), cols).at, w[0]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                e[i][j] *= s.rho;   // u
-                if constexpr (kInLds) {
-                    lds_at(0, i, j) = fmaf(g[i][j], e[i][j], lds_at(0, i, j));
-                    lds_at(1, i, j) += g[i][j];
-                } else if constexpr (DW) {
-                    dw[i][j] = fmaf(g[i][j], e[i][j], dw[i][j]);
-                    db[i][j] += g[i][j];
-                }
+                e[i][j] -= h0;
                 g[i][j] *= w[MORE ? i : 0][j];
             }
         }
-        row_sums<LANES, V, N>(row, g, e, me, TPR, cols, sums);
-        const float mean_g = sums[0] * over_cols, along = sums[1] * over_cols;
+        if (MORE && t + step < dy.rows) read(t + step);
+        Along means;
+        float shift;
+        const Spread s = spread<LANES, V, N, true>(row, e, g, h0, me, TPR, cols, eps, shift, &means, [&] {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                floats_of<TX, V>(load_raw<TX, V>(row_ptr<TX>(h, t) + Cols<V>(V * (me + i * TPR), cols).at), e[i]);
+        });
+        const float less = -shift * s.rho;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float y[V];   // dy
+            if constexpr (DW) floats_of<TX, V>(db_raw[i], y);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                e[i][j] = fmaf(e[i][j], s.rho, less);   // u
+                if constexpr (kInLds) {
+                    lds_at(0, i, j) = fmaf(y[j], e[i][j], lds_at(0, i, j));
+                    lds_at(1, i, j) += y[j];
+                } else if constexpr (DW) {
+                    dw[i][j] = fmaf(y[j], e[i][j], dw[i][j]);
+                    db[i][j] += y[j];
+                }
+            }
+        }
         if (stats && me == 0) stats[t] = s;
+        const float off = -means.mean_g * s.rho, along = -means.along * s.rho;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const Cols<V> c(V * (me + i * TPR), cols);
-            // in this order: k rho may be beyond fp32's range where dx is not
+            if (s.k == 1.0f) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) g[i][j] = s.k * (s.rho * ((g[i][j] - mean_g) - e[i][j] * along));
+                for (int j = 0; j < V; ++j) g[i][j] = fmaf(e[i][j], along, fmaf(g[i][j], s.rho, off));
+            } else {   // in this order: k rho may be beyond fp32's range where dx is not
+#pragma unroll
+                for (int j = 0; j < V; ++j) g[i][j] = s.k * (s.rho * ((g[i][j] - means.mean_g) - e[i][j] * means.along));
+            }
             if (dh.data) {
                 float more[V];
                 floats_of<TX, V>(ua[i], more);
