@@ -532,13 +532,18 @@ struct Layer {
     };
 };
 
-// Workgroups of the gradient, each of which hands over sums of its rows.
+// Workgroups of the gradient, each of which hands over sums of its rows: as many as make this number of waves on a CU.
+// us per call at 8 / 12 / 16 / 24, three sets of inputs in turn: 131,072 x 300 bf16 79 / 68 / 61 / 73, 512 74 / 72 / 73 / 91, 768
+// 112 / 106 / 128 / 116, 1,024 139 / 146 / 156 / 151, 65,536 x 2,048 169 / 141 / 149 / 174, 32,768 x 4,096 with upstream
+// gradient 227 / 227 / 177 / 221 (one workgroup, one, two, two uneven ones), 131,072 x 200 fp16 44 / 45 / 42 / 51, 50,000 x
+// 1,024 fp32 121 / 128 / 128 / 134, 16,384 x 4,096 fp32 154 / 154 / 158 / 168.
+constexpr int layer_waves(int lanes, int vec, int threads) { return lanes == 64 && vec == 2 ? 8 : lanes == kBlock && threads <= 256 ? 12 : 16; }
 template <int LANES, int VEC>
 struct LayerBlocks {
     static int64_t go(RowShape of, int64_t n)
     {
         const RowShape shape = LayerShape<LANES, VEC, UMAP_BF16, UMAP_BF16>::shape(of);
-        return even_grid((n + shape.rows - 1) / shape.rows, shape.threads, 16);
+        return even_grid((n + shape.rows - 1) / shape.rows, shape.threads, layer_waves(LANES, VEC, shape.threads));
     }
 };
 constexpr int kLayerLdsCols = 16384;   // beyond these the sums have a launch of their own
