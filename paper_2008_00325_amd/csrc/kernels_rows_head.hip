@@ -235,7 +235,7 @@ template <int T, int WAVES>
 __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Elem<T> *h, const ProductSide &w,
                                            const OwnToken<WAVES> &own, int k, float scale)
 {
-    constexpr int kAtOnce = 4;
+    constexpr int kAtOnce = WAVES == 1 ? 4 : 8;
     const int cols = (int)w.cols, lane = team.me & 63;
     float z = 0.0f;
     if (k == 1 && own.alone) {
@@ -249,36 +249,43 @@ __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Ele
         }
         return team.sum(z) * scale;
     }
-    for (int e0 = kAtOnce * team.wave; e0 < k; e0 += kAtOnce * WAVES) {
+    // `lanes` lanes to a token, as many tokens side by side as a wave then has, kAtOnce of them one after the other
+    const int lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64, side = 64 / lanes, sub = lane / lanes;
+    for (int e0 = kAtOnce * side * team.wave; e0 < k; e0 += kAtOnce * side * WAVES) {
         const Elem<T> *row[kAtOnce];
         float sum[kAtOnce] = {};
-        int id[kAtOnce];
-        bool some = false;
+        bool there[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < kAtOnce; ++e) {
-            id[e] = e0 + e < k ? team.of(own.id, team.lds->id, e0 + e) : -1;
-            some |= id[e] >= 0;
-            row[e] = static_cast<const Elem<T> *>(w.data) + (int64_t)max(id[e], 0) * w.stride;
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int e = e0 + q * side + sub;
+            const int id = WAVES == 1 ? __shfl(own.id, min(e, 63)) : team.lds->id[min(e, kMostTokens - 1)];
+            there[q] = e < k && id >= 0;
+            row[q] = static_cast<const Elem<T> *>(w.data) + (int64_t)(there[q] ? id : 0) * w.stride;
         }
-        if (some) {
-            for (int c = lane * 8; c < cols; c += 512) {
-                float a[8];
-                fetch8<T>(h, c, cols, a);
+        for (int c = (lane % lanes) * 8; c < cols; c += 8 * lanes) {
+            float a[8];
+            fetch8<T>(h, c, cols, a);
 #pragma unroll
-                for (int e = 0; e < kAtOnce; ++e) {
-                    if (id[e] < 0) continue;
-                    float b[8];
-                    fetch8<T>(row[e], c, cols, b);
+            for (int q = 0; q < kAtOnce; ++q) {
+                if (!there[q]) continue;
+                float b[8];
+                fetch8<T>(row[q], c, cols, b);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum[e] = fmaf(a[j], b[j], sum[e]);
-                }
+                for (int j = 0; j < 8; ++j) sum[q] = fmaf(a[j], b[j], sum[q]);
             }
         }
 #pragma unroll
-        for (int e = 0; e < kAtOnce; ++e) {
-            const float all = wave_sum(sum[e]) * scale;
-            if constexpr (WAVES == 1) z = lane == e0 + e ? all : z;
-            else if (lane == 0) team.lds->z[e0 + e] = all;
+        for (int q = 0; q < kAtOnce; ++q) {
+            for (int o = 1; o < lanes; o <<= 1) sum[q] += __shfl_xor(sum[q], o);
+            const int e = e0 + q * side + sub;
+            if constexpr (WAVES == 1) {
+                for (int s = 0; s < side; ++s) {
+                    const float other = __shfl(sum[q], s * lanes);
+                    z = lane == e0 + q * side + s ? other * scale : z;
+                }
+            } else if (lane % lanes == 0 && e < kMostTokens) {
+                team.lds->z[e] = sum[q] * scale;
+            }
         }
     }
     if constexpr (WAVES > 1) {
@@ -422,18 +429,37 @@ __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h,
     }
 }
 
-// An entry of D as it is stored: rounded, and with two parts what the rounding left below it, `below` elements on.
-template <int T>
-__device__ __forceinline__ void store_entries(Elem<T> *at, int64_t below, float (&v)[4])
+// Rounds to type T, and leaves in v what the rounding took away.
+template <int T, int V>
+__device__ __forceinline__ Raw<T, V> rounded(float (&v)[V])
 {
-    const Raw<T, 4> r = raw_of<T, 4>(v);
-    store_raw<T, 4>(at, r);
-    if (!below) return;
-    float back[4];
-    floats_of<T, 4>(r, back);
+    const Raw<T, V> r = raw_of<T, V>(v);
+    float back[V];
+    floats_of<T, V>(r, back);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] -= back[i];
-    store_raw<T, 4>(at + below, raw_of<T, 4>(v));
+    for (int i = 0; i < V; ++i) v[i] -= back[i];
+    return r;
+}
+
+// Two fragments' rows of A, one above the other, as 8 next to each other.  A lane has 4 of each; the hardware swaps the
+// odd groups of 16 lanes of the first with the even groups of the second, so that a lane has 8 of one of them and a store
+// instruction 64 bytes of every row: rows first + pair_row() on.
+template <int T>
+__device__ __forceinline__ Raw<T, 8> pair_of(const Raw<T, 4> &a, const Raw<T, 4> &b)
+{
+    Raw<T, 8> r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto s = __builtin_amdgcn_permlane16_swap(a.w[i], b.w[i], false, false);
+        r.w[i] = s[0];
+        r.w[2 + i] = s[1];
+    }
+    return r;
+}
+__device__ __forceinline__ int pair_row()
+{
+    const int g = threadIdx.x >> 4 & 3;
+    return (g & 1) * 16 + (g >> 1) * 8;
 }
 
 // D of a piece of the table: d[t][v], `pitch` columns, zeros past the piece's rows.  token and value: null, or each
@@ -456,24 +482,50 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
         const int64_t t = n0 + P::n_of(j);
         if (t >= h.rows) continue;
         const float number = weights.number[t], less = Logit<T>::of_natural(lse[t]);
-        const int64_t own = token ? token[t] - first - m0 : -1;
-        const int own_m = token && token[t] >= 0 && own >= 0 && own < live ? (int)own : -1;
-        const float own_value = own_m >= 0 ? value[t] : 0.0f;
+        Elem<T> *const to = d + t * pitch + m0;
+        float v[FM][4];
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int m = P::m_of(i);
-            float v[4];
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = number * logit.exp_less(acc[i][j][r], less);
-                v[r] = number != 0.0f ? p : 0.0f;
-                v[r] = m + r == own_m ? own_value : v[r];
+            for (int r = 0; r < 4; ++r) v[i][r] = number * logit.exp_less(acc[i][j][r], less);
+        if (live < P::M || number == 0.0f) {   // past the table, or a row without part
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[i][r] = number != 0.0f && P::m_of(i) + r < live ? v[i][r] : 0.0f;
+        }
+        auto store = [&](Elem<T> *at, auto round) {
+            if constexpr (sizeof(Elem<T>) == 2 && FM % 2 == 0) {
+#pragma unroll
+                for (int i = 0; i < FM; i += 2) {
+                    const Raw<T, 4> a = round(v[i]), b = round(v[i + 1]);
+                    store_raw<T, 8>(at + P::m_first(i) + pair_row(), pair_of<T>(a, b));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < FM; ++i) store_raw<T, 4>(at + P::m_of(i), round(v[i]));
             }
-            if (live < P::M) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = m + r < live ? v[r] : 0.0f;
-            }
-            store_entries<T>(d + t * pitch + m0 + m, below, v);
+        };
+        if (!below) {
+            store(to, [](float(&x)[4]) { return raw_of<T, 4>(x); });
+        } else {
+            store(to, [](float(&x)[4]) { return rounded<T, 4>(x); });
+            store(to + below, [](float(&x)[4]) { return raw_of<T, 4>(x); });
+        }
+    }
+    if (!token) return;
+    // the entries of the rows' own tokens, over those just stored: by other lanes, so behind their stores
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (int n = threadIdx.x; n < P::N; n += P::kThreads) {
+        const int64_t t = n0 + n;
+        if (t >= h.rows || token[t] < 0) continue;
+        const int64_t own = token[t] - first - m0;
+        if (own < 0 || own >= live) continue;
+        float v[1] = {value[t]};
+        for (int64_t part = 0;; part = below) {
+            store_raw<T, 1>(d + t * pitch + m0 + own + part, rounded<T, 1>(v));
+            if (part == below) break;
         }
     }
 }
@@ -588,33 +640,53 @@ __device__ __forceinline__ void table_tile(const TableRows &x, int block, Piece 
     for (int j = 0; j < FN; ++j) {
         const int64_t v = n0 + P::n_of(j);
         if (v >= dw.rows) continue;
+        Elem<T> *const to = static_cast<Elem<T> *>(dw.data) + v * dw.stride + m0;
+        auto four = [&](int i, int64_t c, float (&g)[4]) {   // columns c .. c + 3 of acc[i][j]
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int64_t c = m0 + P::m_of(i);
-            if (c >= dw.cols) continue;
-            Elem<T> *const to = static_cast<Elem<T> *>(dw.data) + v * dw.stride + c;
-            float g[4], old[4] = {};
-            const bool whole = c + 4 <= dw.cols;
-            if (add) {
-                if (whole) {
-                    floats_of<T, 4>(load_raw<T, 4>(to), old);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (c + r < dw.cols) old[r] = elem_float<T>(to[r]);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                g[r] = ldexpf(acc[i][j][r], e);
-                if (add) g[r] += old[r];
-            }
-            if (whole) {
-                store_raw<T, 4>(to, raw_of<T, 4>(g));
+            for (int r = 0; r < 4; ++r) g[r] = ldexpf(acc[i][j][r], e);
+            if (!add) return;
+            float old[4] = {};
+            if (c + 4 <= dw.cols) {
+                floats_of<T, 4>(load_raw<T, 4>(to + (c - m0)), old);
             } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (c + r < dw.cols) to[r] = float_elem<T>(g[r]);
+                    if (c + r < dw.cols) old[r] = elem_float<T>(to[c - m0 + r]);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) g[r] += old[r];
+        };
+        if constexpr (sizeof(Elem<T>) == 2 && FM % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < FM; i += 2) {
+                float a[4], b[4];
+                const int64_t c = m0 + P::m_first(i) + pair_row();
+                four(i, m0 + P::m_of(i), a);
+                four(i + 1, m0 + P::m_of(i + 1), b);
+                const Raw<T, 8> r = pair_of<T>(raw_of<T, 4>(a), raw_of<T, 4>(b));
+                if (c + 8 <= dw.cols) {
+                    store_raw<T, 8>(to + (c - m0), r);
+                } else {
+                    float g[8];
+                    floats_of<T, 8>(r, g);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (c + q < dw.cols) to[c - m0 + q] = float_elem<T>(g[q]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                float g[4];
+                const int64_t c = m0 + P::m_of(i);
+                four(i, c, g);
+                if (c + 4 <= dw.cols) {
+                    store_raw<T, 4>(to + (c - m0), raw_of<T, 4>(g));
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (c + r < dw.cols) to[c - m0 + r] = float_elem<T>(g[r]);
+                }
             }
         }
     }
@@ -649,20 +721,20 @@ constexpr int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
 
-// Tiles of 256 x 256; of 128 x 128, two workgroups to a CU or, where there is but one, with more steps on their way;
-// of 64 x 64; and of 64 x 32 for few rows of h.
+// Tiles of 256 x 256; of 128 x 128 and 64 x 64, several workgroups to a CU or, where there are few, with more steps on
+// their way; and for few rows of h of 64 x 32 and 64 x 64, or 128 of dh's columns.
 template <int T, bool AA, bool AB, bool DA, bool DB>
 using Large = Product<T, AA, AB, 2, 4, 8, 4, DA, DB, 2>;
 template <int T, bool AA, bool AB, bool DA, bool DB, int DEPTH>
 using Small = Product<T, AA, AB, 2, 2, 4, 4, DA, DB, DEPTH>;
-template <int T, bool AA, bool AB, bool DA, bool DB>
-using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DA, DB, DA && DB ? 4 : 2>;
-template <int T, bool DA, bool DB>
-using Few = Product<T, false, false, 4, 1, 1, 2, DA, DB, DA && DB ? 4 : 2>;
-constexpr int64_t kFewRows = 32;
+template <int T, bool AA, bool AB, bool DA, bool DB, int DEPTH>
+using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DA, DB, DEPTH>;
+template <int T, bool AA, bool DA, bool DB, int FN, int DEPTH>
+using Few = Product<T, AA, false, 4, 1, AA ? 2 : 1, FN, DA, DB, DEPTH>;
+constexpr int64_t kFewRows = 64;
 
-enum class Shape { large, pairs, deep, tiny };
-constexpr int64_t side_of(Shape s) { return s == Shape::large ? 256 : s == Shape::tiny ? 64 : 128; }
+enum class Shape { large, small, small_deep, tiny, tiny_deep };
+constexpr int64_t side_of(Shape s) { return s == Shape::large ? 256 : s == Shape::small || s == Shape::small_deep ? 128 : 64; }
 
 // Parts of a product's depth, `most` of them at the utmost, so that `tiles` tiles fill `places`.
 constexpr int64_t parts_for(int64_t tiles, int64_t places, int64_t most) { return std::max<int64_t>(1, std::min(places / tiles, most)); }
@@ -674,25 +746,31 @@ double rounds_of(int64_t tiles, int64_t places, int64_t most)
 }
 
 // The shape for a product of m x n (n of h's side) whose depth may be split into `most` parts.  A round of 256 large
-// tiles takes as long as two of 512 small ones would, if these were not 1.2 times as slow (fp32's are not: there the
-// matrix cores are).
+// tiles takes 4 units of time, of 512 small ones 2.4, of 1,024 tiny ones 1.6 (fp32's, whose bound are the matrix cores, 2
+// and 1).
 Shape shape_for(int64_t m, int64_t n, int64_t most, int64_t elem)
 {
     n = std::max<int64_t>(n, 1);
-    const int64_t large = over(m, 256) * over(n, 256), small = over(m, 128) * over(n, 128);
-    if (small * most < 128) return Shape::tiny;
-    if (large * most >= 192 && 4.0 * rounds_of(large, 256, most) <= (elem == 2 ? 2.4 : 2.0) * rounds_of(small, 512, most)) return Shape::large;
-    return small > 256 || most > 1 ? Shape::pairs : Shape::deep;
+    const int64_t large = over(m, 256) * over(n, 256), small = over(m, 128) * over(n, 128), tiny = over(m, 64) * over(n, 64);
+    const double by_large = 4.0 * rounds_of(large, 256, most), by_small = (elem == 2 ? 2.4 : 2.0) * rounds_of(small, 512, most);
+    const double by_tiny = (elem == 2 ? 1.6 : 1.0) * rounds_of(tiny, 1024, most);
+    if (large * most >= 192 && by_large <= by_small && by_large <= by_tiny) return Shape::large;
+    if (small * most >= 128 && by_small <= by_tiny) return small <= 256 && most == 1 ? Shape::small_deep : Shape::small;
+    return tiny * most <= 512 ? Shape::tiny_deep : Shape::tiny;
 }
 
-// Rows of h from which on a table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at
-// most at a time: unaligned loads go at half the rate, and the products read a piece once for every 256 rows of h.
+// When a table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at most at a time:
+// unaligned loads go at half the rate, and the products read a piece once for every 256 rows of h; and a copy that takes a
+// few us lets more steps be on their way.
 constexpr int64_t kPackLossRows = 768, kPackGradRows = 384;
+constexpr int64_t kPackSmall = (int64_t)8 << 20;
+bool packs(int64_t n, int64_t rows, int64_t pitch, int64_t elem, int64_t from) { return n >= from || rows * pitch * elem <= kPackSmall; }
 constexpr int64_t kPackBytes = (int64_t)128 << 20;
 int64_t pack_rows(int64_t pitch, int64_t elem) { return std::max<int64_t>(256, kPackBytes / (pitch * elem) / 256 * 256); }
 
 // Forward: rows of h at a time, so that the partial sums stay within 128 MB (a quarter of that with the large tiles).
 struct LossSizes {
+    bool packing;   // of a table that needs it
     int64_t tiles, rows, pitch, piece;
     int64_t partial, copy, table, total;   // offsets into the workspace
     LossSizes(int64_t n, int64_t vocab, int32_t cols, int32_t type)
@@ -705,8 +783,9 @@ struct LossSizes {
         piece = std::min(pack_rows(pitch, elem), up(vocab, 256));
         partial = 0;
         copy = up(rows * tiles * (int64_t)sizeof(MaxSum), 256);
-        table = copy + up(n > kFewRows ? rows * pitch * elem : 0, 256);
-        total = std::max<int64_t>(16, table + (n >= kPackLossRows ? piece * pitch * elem : 0));
+        table = copy + up(rows * pitch * elem, 256);
+        packing = packs(n, vocab, pitch, elem, kPackLossRows);
+        total = std::max<int64_t>(16, table + (packing ? piece * pitch * elem : 0));
     }
 };
 
@@ -719,6 +798,7 @@ struct GradSizes {
     int64_t n, vocab, cols, k, elem;
     int64_t parts;     // of D
     Shape dh_shape;
+    bool dh_few;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
     int64_t largest, number, exponent, token, value, copy, scaled, d, sums, packed, total;
@@ -736,9 +816,11 @@ struct GradSizes {
         sum_pitch = up(cols, 4);
         // the product for dh: parts of the piece at a time where its tiles alone do not fill the card
         const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / (elem == 4 ? 2 : 4));
+        dh_few = n * parts <= kFewRows && vocab * cols * elem >= kPackSmall;   // less, and one launch does both products
         dh_shape = shape_for(cols, n * parts, most_splits, elem);
-        const int64_t side = side_of(dh_shape), tiles = over(cols, side) * over(std::max<int64_t>(n * parts, 1), side);
-        splits = parts_for(tiles, dh_shape == Shape::large ? 256 : 512, most_splits);
+        const int64_t side = side_of(dh_shape);
+        if (dh_few) splits = parts_for(over(cols, 128), 512, most_splits);
+        else splits = parts_for(over(cols, side) * over(std::max<int64_t>(n * parts, 1), side), side == 256 ? 256 : side == 128 ? 512 : 1024, most_splits);
         depth = over(steps, splits) * step;
         splits = over(piece, depth);
         int64_t at = 0;
@@ -768,15 +850,22 @@ hipError_t by_shape(Shape shape, F f)
 {
     if constexpr (DA) {
         if (shape == Shape::large) return f(Large<T, AA, AB, DA, true>{});
-        if (shape == Shape::deep) return f(Small<T, AA, AB, DA, true, 4>{});
+        if (shape == Shape::small_deep) return f(Small<T, AA, AB, DA, true, 4>{});
+        if (shape == Shape::tiny_deep) return f(Tiny<T, AA, AB, DA, true, 4>{});
     }
-    return shape != Shape::tiny ? f(Small<T, AA, AB, DA, true, 2>{}) : f(Tiny<T, AA, AB, DA, true>{});
+    return side_of(shape) >= 128 ? f(Small<T, AA, AB, DA, true, 2>{}) : f(Tiny<T, AA, AB, DA, true, 2>{});
 }
-// `rows` of a table, which goes straight or not, against rows of h.
+template <int T, bool AA, typename F>
+hipError_t by_few(bool direct, int64_t n, F f)
+{
+    if (n <= 32) return direct ? f(Few<T, AA, true, true, 2, 4>{}) : f(Few<T, AA, false, true, 2, 2>{});
+    return direct ? f(Few<T, AA, true, true, 4, 4>{}) : f(Few<T, AA, false, true, 4, 2>{});
+}
+// `rows` of a table, which goes straight or not, against rows of h, which do.
 template <int T, typename F>
 hipError_t by_logits(int64_t rows, bool direct, const ProductSide &h, F f)
 {
-    if (h.rows <= kFewRows) return direct && direct_side<T>(h) ? f(Few<T, true, true>{}) : f(Few<T, false, false>{});
+    if (h.rows <= kFewRows) return by_few<T, false>(direct, h.rows, f);
     const Shape shape = shape_for(rows, h.rows, 1, sizeof(Elem<T>));
     return direct ? by_shape<T, false, false, true>(shape, f) : by_shape<T, false, false, false>(shape, f);
 }
@@ -823,12 +912,12 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
     char *const base = static_cast<char *>(workspace);
     auto *const partial = reinterpret_cast<MaxSum *>(base + z.partial);
     const ProductSide all = side_of<T>(table, 0, table.rows);
-    const bool whole = direct_side<T>(all), packing = !whole && h.rows >= kPackLossRows;
+    const bool whole = direct_side<T>(all), packing = !whole && z.packing;
     const int64_t piece = packing ? z.piece : table.rows;
     for (int64_t first = 0; first < h.rows; first += z.rows) {
         const ProductSide given = side_of<T>(h, first, std::min(z.rows, h.rows - first));
         ProductSide rows = given;
-        if (h.rows > kFewRows && !direct_side<T>(given)) {
+        if (!direct_side<T>(given)) {
             UL_LAUNCHED(pack<T>(given, reinterpret_cast<Elem<T> *>(base + z.copy), z.pitch, s));
             rows = {base + z.copy, z.pitch, given.rows, z.pitch};
         }
@@ -866,7 +955,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                 const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable, bool add, void *workspace,
                 hipStream_t s)
 {
-    const bool whole = direct_side<T>(side_of<T>(table, 0, table.rows)), packing = !whole && h.rows >= kPackGradRows;
+    const bool whole = direct_side<T>(side_of<T>(table, 0, table.rows)), packing = !whole && packs(h.rows, table.rows, up(table.cols, 64), sizeof(Elem<T>), kPackGradRows);
     const GradSizes z(h.rows, table.rows, table.cols, taught.k, h.type, packing);
     char *const base = static_cast<char *>(workspace);
     auto *const token = reinterpret_cast<int *>(base + z.token);
@@ -918,7 +1007,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
             }
         }
         umap_rows part = {};
-        Shape dw_shape = Shape::tiny;
+        Shape dw_shape = Shape::tiny_deep;
         if (dtable) {
             part = *dtable;
             part.data = static_cast<Elem<T> *>(dtable->data) + first * dtable->stride;
@@ -928,9 +1017,9 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         const bool sums_due = dh && z.n > 0;
         auto row_sums = [&](Tiles g) { return RowSums{w, d_side, g, z.depth, first > 0, sums, z.sum_pitch}; };
         auto table_rows = [&](Tiles g) { return TableRows{weighted, d_side, g, weights, add, part}; };
-        if (sums_due && dtable && (whole || packing) && z.dh_shape == Shape::tiny && dw_shape == Shape::tiny) {
-            using P = Tiny<T, true, false, true, true>;
-            using Q = Tiny<T, true, true, true, true>;
+        if (sums_due && dtable && (whole || packing) && !z.dh_few && z.dh_shape == Shape::tiny_deep && dw_shape == Shape::tiny_deep) {
+            using P = Tiny<T, true, false, true, true, 4>;
+            using Q = Tiny<T, true, true, true, true, 4>;
             const Tiles g = tiles_of<P>(z.cols, d_rows), o = tiles_of<Q>(z.cols, here);
             const int64_t rows_count = (int64_t)g.m * g.n * z.splits;
             hipLaunchKernelGGL((k_head_dh_dw<T, P, Q>), dim3((unsigned)(rows_count + (int64_t)o.m * o.n)), dim3(P::kThreads), 0, s,
@@ -946,8 +1035,9 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                                    row_sums(g));
                 return hipGetLastError();
             };
-            UL_LAUNCHED(whole || packing ? (by_shape<T, true, false, true>(z.dh_shape, launch))
-                                         : (by_shape<T, true, false, false>(z.dh_shape, launch)));
+            UL_LAUNCHED(z.dh_few           ? (by_few<T, true>(whole || packing, d_rows, launch))
+                        : whole || packing ? (by_shape<T, true, false, true>(z.dh_shape, launch))
+                                           : (by_shape<T, true, false, false>(z.dh_shape, launch)));
         }
         if (dtable) {
             UL_LAUNCHED((by_shape<T, true, true, true>(dw_shape, [&](auto shape) {
@@ -996,7 +1086,8 @@ hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds i
 int64_t rows_head_grad_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t k, int32_t type)
 {
     const int64_t plain = GradSizes(n, vocab, cols, k, type, false).total;   // how the table lies is not known here
-    return n < kPackGradRows ? plain : std::max(plain, GradSizes(n, vocab, cols, k, type, true).total);
+    const bool packing = packs(n, vocab, up(cols, 64), elem_size(type), kPackGradRows);
+    return packing ? std::max(plain, GradSizes(n, vocab, cols, k, type, true).total) : plain;
 }
 
 hipError_t launch_rows_head_grad(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,

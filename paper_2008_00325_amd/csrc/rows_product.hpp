@@ -336,12 +336,9 @@ struct Product {
         landed<0>();
     }
 
-    // Where a lane's values lie: acc[i][j][r] is row m_of(i) + r of A and row n_of(j) of B.
-    static __device__ __forceinline__ int m_of(int i)
-    {
-        const int wave = threadIdx.x >> 6;
-        return ((wave / WN) * FM + i) * 16 + (threadIdx.x >> 4 & 3) * 4;
-    }
+    // Where a lane's values lie: acc[i][j][r] is row m_of(i) + r of A, one of 16 from m_first(i) on, and row n_of(j) of B.
+    static __device__ __forceinline__ int m_first(int i) { return ((int)(threadIdx.x >> 6) / WN * FM + i) * 16; }
+    static __device__ __forceinline__ int m_of(int i) { return m_first(i) + (threadIdx.x >> 4 & 3) * 4; }
     static __device__ __forceinline__ int n_of(int j)
     {
         const int wave = threadIdx.x >> 6;
