@@ -143,12 +143,12 @@ __device__ __forceinline__ float teacher_at(const Taught &x, int64_t t, int e)
     }
 }
 
-// A row has a wave (up to 64 tokens) or a workgroup of four; each thread one of its tokens.
+// A row has a wave (up to 64 tokens) or a workgroup of 4 or 16; each thread one of its tokens.
 template <int WAVES>
 struct RowTeam {
-    static constexpr int kThreads = 64 * WAVES, kRows = 4 / WAVES;   // rows of a workgroup
+    static constexpr int kThreads = 64 * WAVES, kRows = WAVES == 1 ? 4 : 1, kBlock = kThreads * kRows;   // of a workgroup
     struct Lds {
-        float part[4];
+        float part[WAVES];
         int id[kMostTokens];
         float share[kMostTokens], z[kMostTokens];
     };
@@ -166,7 +166,9 @@ struct RowTeam {
             __syncthreads();
             if ((me & 63) == 0) lds->part[wave] = v;
             __syncthreads();
-            v = op(op(lds->part[0], lds->part[1]), op(lds->part[2], lds->part[3]));
+            v = lds->part[0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) v = op(v, lds->part[i]);
         }
         return v;
     }
@@ -205,7 +207,7 @@ struct OwnToken {
             log_share = teacher_at(x, t, team.me) * x.scale;
             if (log_share == minus_inf()) id = -1;
         }
-        if constexpr (WAVES > 1) team.lds->id[team.me] = id;   // read behind the reductions' barriers
+        if (WAVES > 1 && team.me < kMostTokens) team.lds->id[team.me] = id;   // read behind the reductions' barriers
         const float most = MaxSum::base(team.max(log_share));
         share = id >= 0 ? exp_of(log_share - most) : 0.0f;
         any = team.max(id >= 0 ? 1.0f : 0.0f) > 0.0f;
@@ -213,7 +215,7 @@ struct OwnToken {
         share = id >= 0 ? share / sum : 0.0f;
         log_share = log_share - most - logf(sum);
         if constexpr (WAVES > 1) {
-            team.lds->share[team.me] = share;
+            if (team.me < kMostTokens) team.lds->share[team.me] = share;
             __syncthreads();
         }
     }
@@ -235,7 +237,7 @@ template <int T, int WAVES>
 __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Elem<T> *h, const ProductSide &w,
                                            const OwnToken<WAVES> &own, int k, float scale)
 {
-    constexpr int kAtOnce = WAVES == 1 ? 4 : 8;
+    constexpr int kAtOnce = 4;
     const int cols = (int)w.cols, lane = team.me & 63;
     float z = 0.0f;
     if (k == 1 && own.alone) {
@@ -249,9 +251,38 @@ __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Ele
         }
         return team.sum(z) * scale;
     }
-    // `lanes` lanes to a token, as many tokens side by side as a wave then has, kAtOnce of them one after the other
-    const int lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64, side = 64 / lanes, sub = lane / lanes;
-    for (int e0 = kAtOnce * side * team.wave; e0 < k; e0 += kAtOnce * side * WAVES) {
+    // a wave to a token, whose number and row all its lanes know
+    for (int e0 = kAtOnce * team.wave; cols > 256 && e0 < k; e0 += kAtOnce * WAVES) {
+        const Elem<T> *row[kAtOnce];
+        float sum[kAtOnce] = {};
+        int id[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            id[q] = e0 + q < k ? team.of(own.id, team.lds->id, e0 + q) : -1;
+            row[q] = static_cast<const Elem<T> *>(w.data) + (int64_t)max(id[q], 0) * w.stride;
+        }
+        for (int c = lane * 8; c < cols; c += 512) {
+            float a[8];
+            fetch8<T>(h, c, cols, a);
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) {
+                if (id[q] < 0) continue;
+                float b[8];
+                fetch8<T>(row[q], c, cols, b);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[q] = fmaf(a[j], b[j], sum[q]);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const float all = wave_sum(sum[q]) * scale;
+            if constexpr (WAVES == 1) z = lane == e0 + q ? all : z;
+            else if (lane == 0) team.lds->z[e0 + q] = all;
+        }
+    }
+    // few columns: `lanes` lanes to a token, as many tokens side by side as a wave then has, kAtOnce times
+    const int lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : 32, side = 64 / lanes, sub = lane / lanes;
+    for (int e0 = kAtOnce * side * team.wave; cols <= 256 && e0 < k; e0 += kAtOnce * side * WAVES) {
         const Elem<T> *row[kAtOnce];
         float sum[kAtOnce] = {};
         bool there[kAtOnce];
@@ -311,7 +342,7 @@ __global__ __launch_bounds__(256) void k_head_pack(ProductSide from, Elem<T> *to
 
 // Joins a row's tiles, and sums its loss.
 template <int T, int WAVES>
-__global__ __launch_bounds__(256) void k_head_loss(ProductSide w, ProductSide h, float scale, Taught taught, int64_t first,
+__global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_loss(ProductSide w, ProductSide h, float scale, Taught taught, int64_t first,
                                                    int64_t tiles, const MaxSum *partial, float *loss, float *lse)
 {
     __shared__ typename RowTeam<WAVES>::Lds lds;
@@ -379,7 +410,7 @@ __global__ __launch_bounds__(1024) void k_head_largest(const float *dloss, int64
 // A row's weight, its tokens with the entries of D, and the copies of h that the products take, without gaps
 // (`pitch` columns, zeros past the last) and zeros in rows without part.
 template <int T, int WAVES>
-__global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
+__global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
                                                    const float *dloss, float factor, RowWeights weights, int *token,
                                                    float *value, Elem<T> *copy, Elem<T> *scaled, int pitch, int parts)
 {
@@ -401,6 +432,7 @@ __global__ __launch_bounds__(256) void k_head_rows(ProductSide w, ProductSide h,
     float share = 0.0f;
     bool again = false;
     if (own.alone) share = 1.0f;
+#pragma unroll 8
     for (int o = 0; o < (own.alone ? 0 : taught.k); ++o) {
         const int other = team.of(own.id, lds.id, o);
         const float more = team.of(own.share, lds.share, o);
@@ -723,14 +755,14 @@ int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
 
 // Tiles of 256 x 256; of 128 x 128 and 64 x 64, several workgroups to a CU or, where there are few, with more steps on
 // their way; and for few rows of h of 64 x 32 and 64 x 64, or 128 of dh's columns.
-template <int T, bool AA, bool AB, bool DA, bool DB>
-using Large = Product<T, AA, AB, 2, 4, 8, 4, DA, DB, 2>;
-template <int T, bool AA, bool AB, bool DA, bool DB, int DEPTH>
-using Small = Product<T, AA, AB, 2, 2, 4, 4, DA, DB, DEPTH>;
-template <int T, bool AA, bool AB, bool DA, bool DB, int DEPTH>
-using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DA, DB, DEPTH>;
-template <int T, bool AA, bool DA, bool DB, int FN, int DEPTH>
-using Few = Product<T, AA, false, 4, 1, AA ? 2 : 1, FN, DA, DB, DEPTH>;
+template <int T, bool AA, bool AB>
+using Large = Product<T, AA, AB, 2, 4, 8, 4, 2>;
+template <int T, bool AA, bool AB, int DEPTH>
+using Small = Product<T, AA, AB, 2, 2, 4, 4, DEPTH>;
+template <int T, bool AA, bool AB, int DEPTH>
+using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DEPTH>;
+template <int T, bool AA, int FN>
+using Few = Product<T, AA, false, 4, 1, AA ? 2 : 1, FN, 4>;
 constexpr int64_t kFewRows = 64;
 
 enum class Shape { large, small, small_deep, tiny, tiny_deep };
@@ -759,18 +791,14 @@ Shape shape_for(int64_t m, int64_t n, int64_t most, int64_t elem)
     return tiny * most <= 512 ? Shape::tiny_deep : Shape::tiny;
 }
 
-// When a table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at most at a time:
-// unaligned loads go at half the rate, and the products read a piece once for every 256 rows of h; and a copy that takes a
-// few us lets more steps be on their way.
-constexpr int64_t kPackLossRows = 768, kPackGradRows = 384;
-constexpr int64_t kPackSmall = (int64_t)8 << 20;
-bool packs(int64_t n, int64_t rows, int64_t pitch, int64_t elem, int64_t from) { return n >= from || rows * pitch * elem <= kPackSmall; }
+// A table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at most at a time.  (Taken by
+// way of registers instead, with unaligned loads, 1,023 rows of fp16 against 32,003 x 1,001 took 118 us, of which the copy
+// saved 16; 17 rows of bf16 against 15,824 x 3,999 took 60 us, with the copy 75, but their gradient 250, with it 200.)
 constexpr int64_t kPackBytes = (int64_t)128 << 20;
 int64_t pack_rows(int64_t pitch, int64_t elem) { return std::max<int64_t>(256, kPackBytes / (pitch * elem) / 256 * 256); }
 
 // Forward: rows of h at a time, so that the partial sums stay within 128 MB (a quarter of that with the large tiles).
 struct LossSizes {
-    bool packing;   // of a table that needs it
     int64_t tiles, rows, pitch, piece;
     int64_t partial, copy, table, total;   // offsets into the workspace
     LossSizes(int64_t n, int64_t vocab, int32_t cols, int32_t type)
@@ -784,8 +812,7 @@ struct LossSizes {
         partial = 0;
         copy = up(rows * tiles * (int64_t)sizeof(MaxSum), 256);
         table = copy + up(rows * pitch * elem, 256);
-        packing = packs(n, vocab, pitch, elem, kPackLossRows);
-        total = std::max<int64_t>(16, table + (packing ? piece * pitch * elem : 0));
+        total = table + piece * pitch * elem;
     }
 };
 
@@ -816,7 +843,7 @@ struct GradSizes {
         sum_pitch = up(cols, 4);
         // the product for dh: parts of the piece at a time where its tiles alone do not fill the card
         const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / (elem == 4 ? 2 : 4));
-        dh_few = n * parts <= kFewRows && vocab * cols * elem >= kPackSmall;   // less, and one launch does both products
+        dh_few = n * parts <= kFewRows && vocab * cols * elem >= ((int64_t)8 << 20);   // less, and one launch does both products
         dh_shape = shape_for(cols, n * parts, most_splits, elem);
         const int64_t side = side_of(dh_shape);
         if (dh_few) splits = parts_for(over(cols, 128), 512, most_splits);
@@ -843,37 +870,35 @@ struct GradSizes {
     }
 };
 
-// Calls f with a product's tiles.  A table that does not go straight to LDS is only met with few rows of h (with more of
-// them it is copied), for which the large tiles are none.
-template <int T, bool AA, bool AB, bool DA, typename F>
+// Calls f with a product's tiles.
+template <int T, bool AA, bool AB, typename F>
 hipError_t by_shape(Shape shape, F f)
 {
-    if constexpr (DA) {
-        if (shape == Shape::large) return f(Large<T, AA, AB, DA, true>{});
-        if (shape == Shape::small_deep) return f(Small<T, AA, AB, DA, true, 4>{});
-        if (shape == Shape::tiny_deep) return f(Tiny<T, AA, AB, DA, true, 4>{});
+    switch (shape) {
+    case Shape::large: return f(Large<T, AA, AB>{});
+    case Shape::small: return f(Small<T, AA, AB, 2>{});
+    case Shape::small_deep: return f(Small<T, AA, AB, 4>{});
+    case Shape::tiny: return f(Tiny<T, AA, AB, 2>{});
+    default: return f(Tiny<T, AA, AB, 4>{});
     }
-    return side_of(shape) >= 128 ? f(Small<T, AA, AB, DA, true, 2>{}) : f(Tiny<T, AA, AB, DA, true, 2>{});
 }
 template <int T, bool AA, typename F>
-hipError_t by_few(bool direct, int64_t n, F f)
+hipError_t by_few(int64_t n, F f)
 {
-    if (n <= 32) return direct ? f(Few<T, AA, true, true, 2, 4>{}) : f(Few<T, AA, false, true, 2, 2>{});
-    return direct ? f(Few<T, AA, true, true, 4, 4>{}) : f(Few<T, AA, false, true, 4, 2>{});
+    return n <= 32 ? f(Few<T, AA, 2>{}) : f(Few<T, AA, 4>{});
 }
-// `rows` of a table, which goes straight or not, against rows of h, which do.
+// `rows` of a table against n rows of h.
 template <int T, typename F>
-hipError_t by_logits(int64_t rows, bool direct, const ProductSide &h, F f)
+hipError_t by_logits(int64_t rows, int64_t n, F f)
 {
-    if (h.rows <= kFewRows) return by_few<T, false>(direct, h.rows, f);
-    const Shape shape = shape_for(rows, h.rows, 1, sizeof(Elem<T>));
-    return direct ? by_shape<T, false, false, true>(shape, f) : by_shape<T, false, false, false>(shape, f);
+    return n <= kFewRows ? by_few<T, false>(n, f) : by_shape<T, false, false>(shape_for(rows, n, 1, sizeof(Elem<T>)), f);
 }
 
-// Calls f with the waves of a row: one, or four where rows are few or have many tokens.
+// Calls f with the waves of a row: one; four where rows are few or have many tokens, and 16 where both holds.
 template <typename F>
 hipError_t by_team(int64_t rows, int64_t k, F f)
 {
+    if (rows <= 256 && k >= 8) return f(std::integral_constant<int, 16>{});
     if (rows < 2048 || k >= 8) return f(std::integral_constant<int, 4>{});
     return f(std::integral_constant<int, 1>{});
 }
@@ -912,7 +937,7 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
     char *const base = static_cast<char *>(workspace);
     auto *const partial = reinterpret_cast<MaxSum *>(base + z.partial);
     const ProductSide all = side_of<T>(table, 0, table.rows);
-    const bool whole = direct_side<T>(all), packing = !whole && z.packing;
+    const bool packing = !direct_side<T>(all);
     const int64_t piece = packing ? z.piece : table.rows;
     for (int64_t first = 0; first < h.rows; first += z.rows) {
         const ProductSide given = side_of<T>(h, first, std::min(z.rows, h.rows - first));
@@ -922,7 +947,7 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
             rows = {base + z.copy, z.pitch, given.rows, z.pitch};
         }
         int64_t tiles = 0;   // of all pieces, whose tiles are of one size: that of the whole table
-        (void)by_logits<T>(table.rows, whole || packing, rows, [&](auto shape) {
+        (void)by_logits<T>(table.rows, rows.rows, [&](auto shape) {
             tiles = over(table.rows, decltype(shape)::M);
             return hipSuccess;
         });
@@ -932,7 +957,7 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
                 UL_LAUNCHED(pack<T>(w, reinterpret_cast<Elem<T> *>(base + z.table), z.pitch, s));
                 w = {base + z.table, z.pitch, w.rows, z.pitch};
             }
-            UL_LAUNCHED(by_logits<T>(table.rows, whole || packing, rows, [&](auto shape) {
+            UL_LAUNCHED(by_logits<T>(table.rows, rows.rows, [&](auto shape) {
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(w.rows, rows.rows);
                 hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
@@ -942,7 +967,7 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
         }
         UL_LAUNCHED(by_team(rows.rows, taught.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
-            hipLaunchKernelGGL((k_head_loss<T, W>), dim3((unsigned)over(rows.rows, RowTeam<W>::kRows)), dim3(256), 0, s, all, given, scale,
+            hipLaunchKernelGGL((k_head_loss<T, W>), dim3((unsigned)over(rows.rows, RowTeam<W>::kRows)), dim3(RowTeam<W>::kBlock), 0, s, all, given, scale,
                                taught, first, tiles, partial, out, lse);
             return hipGetLastError();
         }));
@@ -955,7 +980,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                 const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable, bool add, void *workspace,
                 hipStream_t s)
 {
-    const bool whole = direct_side<T>(side_of<T>(table, 0, table.rows)), packing = !whole && packs(h.rows, table.rows, up(table.cols, 64), sizeof(Elem<T>), kPackGradRows);
+    const bool packing = !direct_side<T>(side_of<T>(table, 0, table.rows));
     const GradSizes z(h.rows, table.rows, table.cols, taught.k, h.type, packing);
     char *const base = static_cast<char *>(workspace);
     auto *const token = reinterpret_cast<int *>(base + z.token);
@@ -974,7 +999,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         }
         UL_LAUNCHED(by_team(z.n, z.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
-            hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(256), 0, s,
+            hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(RowTeam<W>::kBlock), 0, s,
                                side_of<T>(table, 0, table.rows), side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
                                token, value, copy, scaled, (int)z.h_pitch, (int)z.parts);
             return hipGetLastError();
@@ -993,7 +1018,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         const ProductSide d_side{d, z.d_pitch, d_rows, z.d_pitch};
         if (z.n > 0) {
             const bool one = z.k == 1;
-            UL_LAUNCHED((by_logits<T>(here, whole || packing, rows, [&](auto shape) {
+            UL_LAUNCHED((by_logits<T>(here, z.n, [&](auto shape) {
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(z.d_pitch, z.n);
                 hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
@@ -1017,9 +1042,9 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         const bool sums_due = dh && z.n > 0;
         auto row_sums = [&](Tiles g) { return RowSums{w, d_side, g, z.depth, first > 0, sums, z.sum_pitch}; };
         auto table_rows = [&](Tiles g) { return TableRows{weighted, d_side, g, weights, add, part}; };
-        if (sums_due && dtable && (whole || packing) && !z.dh_few && z.dh_shape == Shape::tiny_deep && dw_shape == Shape::tiny_deep) {
-            using P = Tiny<T, true, false, true, true, 4>;
-            using Q = Tiny<T, true, true, true, true, 4>;
+        if (sums_due && dtable && !z.dh_few && z.dh_shape == Shape::tiny_deep && dw_shape == Shape::tiny_deep) {
+            using P = Tiny<T, true, false, 4>;
+            using Q = Tiny<T, true, true, 4>;
             const Tiles g = tiles_of<P>(z.cols, d_rows), o = tiles_of<Q>(z.cols, here);
             const int64_t rows_count = (int64_t)g.m * g.n * z.splits;
             hipLaunchKernelGGL((k_head_dh_dw<T, P, Q>), dim3((unsigned)(rows_count + (int64_t)o.m * o.n)), dim3(P::kThreads), 0, s,
@@ -1035,12 +1060,10 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                                    row_sums(g));
                 return hipGetLastError();
             };
-            UL_LAUNCHED(z.dh_few           ? (by_few<T, true>(whole || packing, d_rows, launch))
-                        : whole || packing ? (by_shape<T, true, false, true>(z.dh_shape, launch))
-                                           : (by_shape<T, true, false, false>(z.dh_shape, launch)));
+            UL_LAUNCHED(z.dh_few ? (by_few<T, true>(d_rows, launch)) : (by_shape<T, true, false>(z.dh_shape, launch)));
         }
         if (dtable) {
-            UL_LAUNCHED((by_shape<T, true, true, true>(dw_shape, [&](auto shape) {
+            UL_LAUNCHED((by_shape<T, true, true>(dw_shape, [&](auto shape) {
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(z.cols, here);
                 hipLaunchKernelGGL((k_head_dw<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, table_rows(g));
@@ -1086,8 +1109,7 @@ hipError_t launch_rows_head(const umap_rows &h, const umap_rows &table, RowIds i
 int64_t rows_head_grad_bytes(int64_t n, int64_t vocab, int32_t cols, int32_t k, int32_t type)
 {
     const int64_t plain = GradSizes(n, vocab, cols, k, type, false).total;   // how the table lies is not known here
-    const bool packing = packs(n, vocab, up(cols, 64), elem_size(type), kPackGradRows);
-    return packing ? std::max(plain, GradSizes(n, vocab, cols, k, type, true).total) : plain;
+    return std::max(plain, GradSizes(n, vocab, cols, k, type, true).total);
 }
 
 hipError_t launch_rows_head_grad(const umap_rows &h, const umap_rows &table, RowIds ids, const umap_rows *teacher, float scale,

@@ -46,23 +46,6 @@ __device__ __forceinline__ Acc4 multiply(const Piece &a, const Piece &b, Acc4 c)
     }
 }
 
-// 16 bytes of a row from column c on; columns past the row and rows past the last are zeros.
-template <int T>
-__device__ __forceinline__ Piece fetch_piece(const ProductSide &side, int64_t r, int64_t c)
-{
-    constexpr int kPer = 16 / sizeof(Elem<T>);
-    Piece p = {};
-    if (r >= side.rows || c >= side.cols) return p;
-    const Elem<T> *at = static_cast<const Elem<T> *>(side.data) + r * side.stride + c;
-    if (c + kPer <= side.cols) return __builtin_bit_cast(Piece, load_raw<T, kPer>(at));
-    Elem<T> e[kPer] = {};
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-        if (c + j < side.cols) e[j] = at[j];
-    __builtin_memcpy(&p, e, 16);
-    return p;
-}
-
 // One side's step of a tile of I rows.
 template <int T, bool kAcross, int I>
 struct Step {
@@ -132,16 +115,13 @@ __device__ __forceinline__ void landed()
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// How a side's steps get into LDS, where piece p of a tile's step is thread p % THREADS's.
-
-// Straight: 64 lanes, 64 pieces next to each other.  Lanes whose piece lies outside the matrix are given an offset
-// beyond the buffer, which loads zeros.
+// How a side's steps get into LDS: straight, 64 lanes, 64 pieces next to each other; piece p of a step is thread
+// p % THREADS's.  Lanes whose piece lies outside the matrix are given an offset beyond the buffer, which loads zeros.
 template <int T, bool kAcross, int I, int THREADS>
 struct DirectSide {
     using S = Step<T, kAcross, I>;
     typedef uint32_t Words __attribute__((ext_vector_type(4)));
     static constexpr int kElem = S::kElem, kCount = S::kPieces / THREADS, kRows = THREADS / S::kRow;
-    static constexpr int kInFlight = kCount;   // of a step, behind whose loads a wave waits
     const ProductSide &side;
     const int64_t i0;
     int row, col;
@@ -176,61 +156,6 @@ struct DirectSide {
                      "v"(x.at + q * x.step), "s"(x.buffer)
                      : "memory");
     }
-    __device__ __forceinline__ void start(int64_t) {}
-};
-
-// By way of registers, which hold a step until its place in LDS is free: any alignment and any length of rows.
-template <int T, bool kAcross, int I, int THREADS>
-struct AnySide {
-    using S = Step<T, kAcross, I>;
-    static constexpr int kElem = S::kElem, kCount = S::kPieces / THREADS, kRows = THREADS / S::kRow;
-    static constexpr int kInFlight = 0;
-    const ProductSide &side;
-    const int64_t i0;
-    int64_t offset;
-    Piece held[kCount];
-    static_assert(kRows % (kAcross && kElem == 2 ? 16 : 8) == 0, "a piece's row is turned alike kRows rows on");
-    __device__ __forceinline__ AnySide(const ProductSide &of, int64_t first) : side(of), i0(first)
-    {
-        int row, col;
-        S::place(threadIdx.x, row, col);
-        offset = row * side.stride + col;
-    }
-    __device__ __forceinline__ void take(int64_t k, bool there, int q)
-    {
-        const int64_t r0 = kAcross ? k : i0, c0 = kAcross ? i0 : k;
-        constexpr int R = kAcross ? S::kDepth : I, C = kAcross ? I : S::kDepth;
-        if (r0 + R <= side.rows && c0 + C <= side.cols) {   // the same for all
-            const Elem<T> *const base = static_cast<const Elem<T> *>(side.data) + (r0 + q * kRows) * side.stride + c0;
-            held[q] = __builtin_bit_cast(Piece, load_raw<T, S::kPer>(base + offset));
-        } else if (there) {
-            int row, col;
-            S::place(threadIdx.x + q * THREADS, row, col);
-            held[q] = fetch_piece<T>(side, r0 + row, c0 + col);
-        }
-    }
-    struct Loads {   // puts the step that is held, takes the one behind it
-        int64_t next;
-        bool there;
-        Piece *lds;
-    };
-    __device__ __forceinline__ Loads loads(int64_t k, bool there, Piece *to) const
-    {
-        return {k + S::kDepth, there, to + threadIdx.x};
-    }
-    __device__ __forceinline__ void one(const Loads &x, int q)
-    {
-        x.lds[q * THREADS] = held[q];
-        take(x.next, x.there, q);
-    }
-    __device__ __forceinline__ void start(int64_t k)
-    {
-#pragma unroll
-        for (int q = 0; q < kCount; ++q) {
-            held[q] = Piece{};
-            take(k, true, q);
-        }
-    }
 };
 
 // Tiles of a grid of m x n of them, one per workgroup.  Workgroups go round the 8 XCDs in turn; each XCD takes a
@@ -251,23 +176,22 @@ __device__ __forceinline__ TileAt tile_at(const Tiles &tiles, int block)
     return {first + in % rows, in / rows};
 }
 
-// A tile of WM x WN waves of FM x FN fragments each; sides that go straight to LDS (direct_side) or any; DEPTH steps
-// in LDS, all but one of them on their way.
+// A tile of WM x WN waves of FM x FN fragments each, of sides in whole pieces (direct_side); DEPTH steps in LDS, all but
+// one of them on their way.
 //
 // A step is two halves.  The fragments of a half are fetched while the half before is multiplied, and a step's loads
 // are issued, when its place has become free, between the products too: evenly, since eight waves that issue
 // theirs at once wait for each other.
-template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN, bool kDirectA, bool kDirectB, int DEPTH>
+template <int T, bool kAcrossA, bool kAcrossB, int WM, int WN, int FM, int FN, int DEPTH>
 struct Product {
     static constexpr int kWM = WM, kWN = WN, kFM = FM, kFN = FN;
     static constexpr int kThreads = 64 * WM * WN, M = 16 * WM * FM, N = 16 * WN * FN;
     using A = Step<T, kAcrossA, M>;
     using B = Step<T, kAcrossB, N>;
-    using SideA = std::conditional_t<kDirectA, DirectSide<T, kAcrossA, M, kThreads>, AnySide<T, kAcrossA, M, kThreads>>;
-    using SideB = std::conditional_t<kDirectB, DirectSide<T, kAcrossB, N, kThreads>, AnySide<T, kAcrossB, N, kThreads>>;
+    using SideA = DirectSide<T, kAcrossA, M, kThreads>;
+    using SideB = DirectSide<T, kAcrossB, N, kThreads>;
     static constexpr int kDepth = A::kDepth, kStage = A::kPieces + B::kPieces;
     static constexpr int kLds = kStage * 16 * DEPTH;
-    static_assert(DEPTH == 2 || (kDirectA && kDirectB), "what goes by way of registers is a step ahead there already");
 
     // acc of rows m0 .. of A and n0 .. of B, over k0 <= k < k1 (k0 a multiple of kDepth).
     static __device__ __forceinline__ void run(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
@@ -279,11 +203,10 @@ struct Product {
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
         if (k0 >= k1) return;
-        SideA da(a, m0);
-        SideB db(b, n0);
+        const SideA da(a, m0);
+        const SideB db(b, n0);
         const int steps = (int)((k1 - k0 + kDepth - 1) / kDepth);
         constexpr int kA = SideA::kCount, kLoads = kA + SideB::kCount;
-        constexpr int kInFlight = kDirectA && kDirectB ? SideA::kInFlight + SideB::kInFlight : 0;
         Piece fa[FM], fb[2][FN];
         // A half step's products with fb[set], row by row, and between the rows the fetches of the next half's fragments
         // (step s, half `half`; a row's of A once its own are multiplied) and, if `loading`, the loads of step l.
@@ -315,8 +238,6 @@ struct Product {
         };
         constexpr auto yes = std::true_type{};
         constexpr auto no = std::false_type{};
-        da.start(k0);
-        db.start(k0);
         for (int s = 0; s < DEPTH; ++s) {
             Piece *const to = lds + s * kStage;
             const auto la = da.loads(k0 + (int64_t)s * kDepth, s < steps, to);
@@ -326,11 +247,11 @@ struct Product {
 #pragma unroll
             for (int q = 0; q < SideB::kCount; ++q) db.one(lb, q);
         }
-        landed<(DEPTH - 1) * kInFlight>();
+        landed<(DEPTH - 1) * kLoads>();
         half_step(no, 1, 0, 0, no, 0);
         for (int s = 0; s < steps; ++s) {
             half_step(yes, 0, s, 1, no, 0);
-            landed<(DEPTH - 2) * kInFlight>();   // step s + 1 is there, and everybody has fetched all of step s
+            landed<(DEPTH - 2) * kLoads>();   // step s + 1 is there, and everybody has fetched all of step s
             half_step(yes, 1, s + 1, 0, yes, s + DEPTH);   // behind the last step: nobody takes them
         }
         landed<0>();
