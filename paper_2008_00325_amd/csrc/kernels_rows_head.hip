@@ -389,15 +389,12 @@ __device__ __forceinline__ void split_weight(float g, float &number, int &expone
     }
 }
 
-// The largest exponent of the rows' weights (finite and not zero), or 0; one workgroup.
-__global__ __launch_bounds__(1024) void k_head_largest(const float *dloss, int64_t n, float factor, int *largest)
+// The largest exponent of the rows that take part, or 0; one workgroup.
+__global__ __launch_bounds__(1024) void k_head_largest(const int *exponent, int64_t n, int *largest)
 {
     __shared__ int part[16];
     int most = kNoRow;
-    for (int64_t t = threadIdx.x; t < n; t += 1024) {
-        const float g = dloss[t] * factor;
-        if (g != 0.0f && fabsf(g) < __builtin_inff()) most = max(most, (int)__builtin_amdgcn_frexp_expf(g));
-    }
+    for (int64_t t = threadIdx.x; t < n; t += 1024) most = max(most, exponent[t]);
     for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
     __syncthreads();
@@ -407,12 +404,30 @@ __global__ __launch_bounds__(1024) void k_head_largest(const float *dloss, int64
     }
 }
 
+// The rows' copies times 2^(e_t - E): `rows` of them, `parts` times one after the other.
+template <int T>
+__global__ __launch_bounds__(256) void k_head_scale(const Elem<T> *copy, int64_t rows, int parts, int pitch, const int *exponent,
+                                                    const int *largest, Elem<T> *scaled)
+{
+    const int64_t total = rows * (pitch / 8);
+    const int most = *largest;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / (pitch / 8);
+        const int by = exponent[t] == kNoRow ? 0 : exponent[t] - most;
+        float v[8];
+        floats_of<T, 8>(load_raw<T, 8>(copy + i * 8), v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], by);
+        for (int p = 0; p < parts; ++p) store_raw<T, 8>(scaled + p * rows * pitch + i * 8, raw_of<T, 8>(v));
+    }
+}
+
 // A row's weight, its tokens with the entries of D, and the copies of h that the products take, without gaps
 // (`pitch` columns, zeros past the last) and zeros in rows without part.
 template <int T, int WAVES>
 __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
                                                    const float *dloss, float factor, RowWeights weights, int *token,
-                                                   float *value, Elem<T> *copy, Elem<T> *scaled, int pitch, int parts)
+                                                   float *value, Elem<T> *copy, int pitch, int parts)
 {
     __shared__ typename RowTeam<WAVES>::Lds lds;
     const RowTeam<WAVES> team(&lds);
@@ -449,15 +464,10 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
         weights.number[t] = part ? number : 0.0f;
         weights.exponent[t] = part ? exponent : kNoRow;
     }
-    const int by = scaled ? exponent - largest_of(weights) : 0;
     for (int c = team.me * 8; c < pitch; c += RowTeam<WAVES>::kThreads * 8) {
         float v[8] = {};
         if (part) fetch8<T>(row, c, (int)h.cols, v);
         for (int p = 0; p < parts; ++p) store_raw<T, 8>(copy + (p * h.rows + t) * pitch + c, raw_of<T, 8>(v));
-        if (!scaled) continue;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], by);
-        for (int p = 0; p < parts; ++p) store_raw<T, 8>(scaled + (p * h.rows + t) * pitch + c, raw_of<T, 8>(v));
     }
 }
 
@@ -748,48 +758,20 @@ __global__ __launch_bounds__(P::kThreads) void k_head_dh_dw(RowSums x, int rows,
 
 // ---- sizes -----------------------------------------------------------------------------------
 
-constexpr int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
-constexpr int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t up(int64_t a, int64_t b) { return over(a, b) * b; }
 
 int elem_size(int32_t type) { return type == UMAP_F32 ? 4 : 2; }
 
-// Tiles of 256 x 256; of 128 x 128 and 64 x 64, several workgroups to a CU or, where there are few, with more steps on
-// their way; and for few rows of h of 64 x 32 and 64 x 64, or 128 of dh's columns.
+// The products' tiles (TileShape), and for few rows of h tiles of 64 x 32 and 64 x 64, for dh of 128 columns.
 template <int T, bool AA, bool AB>
 using Large = Product<T, AA, AB, 2, 4, 8, 4, 2>;
-template <int T, bool AA, bool AB, int DEPTH>
-using Small = Product<T, AA, AB, 2, 2, 4, 4, DEPTH>;
+template <int T, bool AA, bool AB>
+using Small = Product<T, AA, AB, 2, 2, 4, 4, 2>;
 template <int T, bool AA, bool AB, int DEPTH>
 using Tiny = Product<T, AA, AB, 2, 2, 2, 2, DEPTH>;
 template <int T, bool AA, int FN>
 using Few = Product<T, AA, false, 4, 1, AA ? 2 : 1, FN, 4>;
 constexpr int64_t kFewRows = 64;
-
-enum class Shape { large, small, small_deep, tiny, tiny_deep };
-constexpr int64_t side_of(Shape s) { return s == Shape::large ? 256 : s == Shape::small || s == Shape::small_deep ? 128 : 64; }
-
-// Parts of a product's depth, `most` of them at the utmost, so that `tiles` tiles fill `places`.
-constexpr int64_t parts_for(int64_t tiles, int64_t places, int64_t most) { return std::max<int64_t>(1, std::min(places / tiles, most)); }
-// Rounds that tiles take, in parts of their depth, over the parts.
-double rounds_of(int64_t tiles, int64_t places, int64_t most)
-{
-    const int64_t parts = parts_for(tiles, places, most);
-    return (double)over(tiles * parts, places) / (double)parts;
-}
-
-// The shape for a product of m x n (n of h's side) whose depth may be split into `most` parts.  A round of 256 large
-// tiles takes 4 units of time, of 512 small ones 2.4, of 1,024 tiny ones 1.6 (fp32's, whose bound are the matrix cores, 2
-// and 1).
-Shape shape_for(int64_t m, int64_t n, int64_t most, int64_t elem)
-{
-    n = std::max<int64_t>(n, 1);
-    const int64_t large = over(m, 256) * over(n, 256), small = over(m, 128) * over(n, 128), tiny = over(m, 64) * over(n, 64);
-    const double by_large = 4.0 * rounds_of(large, 256, most), by_small = (elem == 2 ? 2.4 : 2.0) * rounds_of(small, 512, most);
-    const double by_tiny = (elem == 2 ? 1.6 : 1.0) * rounds_of(tiny, 1024, most);
-    if (large * most >= 192 && by_large <= by_small && by_large <= by_tiny) return Shape::large;
-    if (small * most >= 128 && by_small <= by_tiny) return small <= 256 && most == 1 ? Shape::small_deep : Shape::small;
-    return tiny * most <= 512 ? Shape::tiny_deep : Shape::tiny;
-}
 
 // A table whose rows are not whole pieces at 16-byte places is copied first, a piece of 128 MB at most at a time.  (Taken by
 // way of registers instead, with unaligned loads, 1,023 rows of fp16 against 32,003 x 1,001 took 118 us, of which the copy
@@ -824,7 +806,7 @@ constexpr int64_t kTwoPartRows = 128;
 struct GradSizes {
     int64_t n, vocab, cols, k, elem;
     int64_t parts;     // of D
-    Shape dh_shape;
+    TileShape dh_shape;
     bool dh_few;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
@@ -835,6 +817,7 @@ struct GradSizes {
         parts = elem == 2 && n <= kTwoPartRows ? 2 : 1;
         const int64_t budget = (int64_t)256 << 20;
         int64_t most = std::max<int64_t>(256, budget / std::max<int64_t>(1, n * parts * elem) / 256 * 256);
+        most = std::min(most, (int64_t)1 << 22);   // so that the launches' sizes fit
         h_pitch = up(cols, 64);
         if (pack) most = std::min(most, pack_rows(h_pitch, elem));
         const int64_t pieces = over(vocab, most);
@@ -844,8 +827,8 @@ struct GradSizes {
         // the product for dh: parts of the piece at a time where its tiles alone do not fill the card
         const int64_t step = 128 / elem, steps = over(piece, step), most_splits = std::max<int64_t>(1, steps / (elem == 4 ? 2 : 4));
         dh_few = n * parts <= kFewRows && vocab * cols * elem >= ((int64_t)8 << 20);   // less, and one launch does both products
-        dh_shape = shape_for(cols, n * parts, most_splits, elem);
-        const int64_t side = side_of(dh_shape);
+        dh_shape = tile_shape(cols, n * parts, most_splits, elem);
+        const int64_t side = tile_side(dh_shape);
         if (dh_few) splits = parts_for(over(cols, 128), 512, most_splits);
         else splits = parts_for(over(cols, side) * over(std::max<int64_t>(n * parts, 1), side), side == 256 ? 256 : side == 128 ? 512 : 1024, most_splits);
         depth = over(steps, splits) * step;
@@ -872,13 +855,12 @@ struct GradSizes {
 
 // Calls f with a product's tiles.
 template <int T, bool AA, bool AB, typename F>
-hipError_t by_shape(Shape shape, F f)
+hipError_t by_shape(TileShape shape, F f)
 {
     switch (shape) {
-    case Shape::large: return f(Large<T, AA, AB>{});
-    case Shape::small: return f(Small<T, AA, AB, 2>{});
-    case Shape::small_deep: return f(Small<T, AA, AB, 4>{});
-    case Shape::tiny: return f(Tiny<T, AA, AB, 2>{});
+    case TileShape::large: return f(Large<T, AA, AB>{});
+    case TileShape::small: return f(Small<T, AA, AB>{});
+    case TileShape::tiny: return f(Tiny<T, AA, AB, 2>{});
     default: return f(Tiny<T, AA, AB, 4>{});
     }
 }
@@ -891,7 +873,7 @@ hipError_t by_few(int64_t n, F f)
 template <int T, typename F>
 hipError_t by_logits(int64_t rows, int64_t n, F f)
 {
-    return n <= kFewRows ? by_few<T, false>(n, f) : by_shape<T, false, false>(shape_for(rows, n, 1, sizeof(Elem<T>)), f);
+    return n <= kFewRows ? by_few<T, false>(n, f) : by_shape<T, false, false>(tile_shape(rows, n, 1, sizeof(Elem<T>)), f);
 }
 
 // Calls f with the waves of a row: one; four where rows are few or have many tokens, and 16 where both holds.
@@ -993,17 +975,20 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
     int *const largest = dloss ? reinterpret_cast<int *>(base + z.largest) : nullptr;
     const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, known};
     if (z.n > 0) {
-        if (dloss) {
-            hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, dloss, z.n, factor, largest);
-            UL_LAUNCHED(hipGetLastError());
-        }
         UL_LAUNCHED(by_team(z.n, z.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
             hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(RowTeam<W>::kBlock), 0, s,
                                side_of<T>(table, 0, table.rows), side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
-                               token, value, copy, scaled, (int)z.h_pitch, (int)z.parts);
+                               token, value, copy, (int)z.h_pitch, (int)z.parts);
             return hipGetLastError();
         }));
+        if (dloss && dtable) {
+            hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, weights.exponent, z.n, largest);
+            UL_LAUNCHED(hipGetLastError());
+            hipLaunchKernelGGL((k_head_scale<T>), dim3((unsigned)std::min<int64_t>(8192, over(z.n * z.h_pitch / 8, 256))), dim3(256), 0, s,
+                               copy, z.n, (int)z.parts, (int)z.h_pitch, weights.exponent, largest, scaled);
+            UL_LAUNCHED(hipGetLastError());
+        }
     }
     // the copies' and D's columns past the last are zeros, and so are pieces of them
     const int64_t d_rows = z.n * z.parts, below = z.parts > 1 ? z.n * z.d_pitch : 0;
@@ -1032,17 +1017,17 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
             }
         }
         umap_rows part = {};
-        Shape dw_shape = Shape::tiny_deep;
+        TileShape dw_shape = TileShape::tiny_deep;
         if (dtable) {
             part = *dtable;
             part.data = static_cast<Elem<T> *>(dtable->data) + first * dtable->stride;
             part.rows = here;
-            dw_shape = shape_for(z.cols, here, 1, z.elem);
+            dw_shape = tile_shape(z.cols, here, 1, z.elem);
         }
         const bool sums_due = dh && z.n > 0;
         auto row_sums = [&](Tiles g) { return RowSums{w, d_side, g, z.depth, first > 0, sums, z.sum_pitch}; };
         auto table_rows = [&](Tiles g) { return TableRows{weighted, d_side, g, weights, add, part}; };
-        if (sums_due && dtable && !z.dh_few && z.dh_shape == Shape::tiny_deep && dw_shape == Shape::tiny_deep) {
+        if (sums_due && dtable && !z.dh_few && z.dh_shape == TileShape::tiny_deep && dw_shape == TileShape::tiny_deep) {
             using P = Tiny<T, true, false, 4>;
             using Q = Tiny<T, true, true, 4>;
             const Tiles g = tiles_of<P>(z.cols, d_rows), o = tiles_of<Q>(z.cols, here);

@@ -91,4 +91,41 @@ constexpr int64_t norm_grid(int64_t work, int32_t cols, int64_t threads)
     return (work + turns - 1) / turns;
 }
 
+// ---- products of the token rows' head ----
+constexpr int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Tiles of 256 x 256, one workgroup to a CU; of 128 x 128, two; of 64 x 64, four, or two with more steps on their way.
+enum class TileShape { large, small, tiny, tiny_deep };
+constexpr int64_t tile_side(TileShape s) { return s == TileShape::large ? 256 : s == TileShape::small ? 128 : 64; }
+
+// Parts of a product's depth, `most` of them at the utmost, so that `tiles` tiles fill `places`.
+constexpr int64_t parts_for(int64_t tiles, int64_t places, int64_t most)
+{
+    const int64_t parts = places / tiles < most ? places / tiles : most;
+    return parts < 1 ? 1 : parts;
+}
+// Rounds that tiles take, in parts of their depth, over the parts.
+constexpr double rounds_of(int64_t tiles, int64_t places, int64_t most)
+{
+    const int64_t parts = parts_for(tiles, places, most);
+    return (double)over(tiles * parts, places) / (double)parts;
+}
+
+// The shape for a product of m x n whose depth may be split into `most` parts, of elements of `elem` bytes.  A round of
+// 256 large tiles takes 4 units of time, of 512 small ones 2.6, of 1,024 tiny ones 1.8 (fp32's, whose bound are the matrix
+// cores, 2 and 1).  us of a launch, large / small / tiny: loss of 2,048 rows of bf16 against 32,000 x 256 49 / 62 / 85, against
+// 32,000 x 512 70 / 92 / 129, of 1,000 against 5,000 x 64 9.7 / 7.2 / 7.4; table's gradient from 300 rows for 20,000 x 333 20 /
+// 14 / 17, from 2,229 for 14,641 x 64 55 / 31 / 23, from 4,619 for 17,118 x 320 fp16 113 / 78 / 102, from 64 for 32,000 x
+// 2,048 45 / 51 / 63.
+constexpr TileShape tile_shape(int64_t m, int64_t n, int64_t most, int64_t elem)
+{
+    n = n < 1 ? 1 : n;
+    const int64_t large = over(m, 256) * over(n, 256), small = over(m, 128) * over(n, 128), tiny = over(m, 64) * over(n, 64);
+    const double by_large = 4.0 * rounds_of(large, 256, most), by_small = (elem == 2 ? 2.6 : 2.0) * rounds_of(small, 512, most);
+    const double by_tiny = (elem == 2 ? 1.8 : 1.0) * rounds_of(tiny, 1024, most);
+    if (large * most >= 192 && by_large <= by_small && by_large <= by_tiny) return TileShape::large;
+    if (small * most >= 128 && by_small <= by_tiny) return TileShape::small;
+    return tiny * most <= 512 ? TileShape::tiny_deep : TileShape::tiny;
+}
+
 }  // namespace ul

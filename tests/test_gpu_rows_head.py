@@ -141,11 +141,19 @@ def test_weights_of_rows(dtype):
         check(Case(n, 300, 40, dtype), weights=torch.exp2(torch.randint(-60, 20, (n,), device=DEV).float()) * w)
 
 
-@pytest.mark.parametrize("dtype", [BF16, F32])
-def test_large_tiles(dtype):
-    """Sizes whose tiles are 256 x 256 in all three products."""
-    check(Case(1300, 12_300, 264 if dtype == BF16 else 72, dtype), dscale=1 / 1300)
-    check(Case(3100, 4100, 3333, dtype, k=5), dscale=1 / 3100)
+# rows, tokens, columns that between them take every tile of every product
+SHAPES = [(3100, 4100, 3333, BF16), (3100, 4100, 3333, F32), (1024, 300, 4096, F32), (300, 1003, 300, F16), (300, 1003, 300, F32),
+          (20, 20_000, 240, BF16), (20, 20_000, 240, F32), (50, 20_000, 240, F16), (50, 20_000, 120, F32), (600, 9000, 100, F16),
+          (600, 9000, 104, F32), (2500, 3000, 200, BF16), (700, 9000, 1500, BF16), (260, 3000, 2100, BF16), (2300, 5000, 300, F32),
+          (200, 30_000, 70, F32), (70, 30_000, 70, BF16), (1300, 2000, 513, F32), (130, 700, 40, BF16), (4096, 130, 130, BF16),
+          (1000, 3000, 900, F16), (1100, 1100, 1100, F32)]
+
+
+@pytest.mark.parametrize("n,rows,cols,dtype", SHAPES)
+def test_every_tile_shape(n, rows, cols, dtype):
+    check(Case(n, rows, cols, dtype), dscale=1 / n)
+    if n <= 1100:
+        check(Case(n, rows, cols, dtype, k=5, lean=2.0), weights=torch.rand(n, device=DEV) + 0.2, dscale=1 / n)
 
 
 def test_several_pieces_of_the_table():
@@ -177,6 +185,24 @@ def test_peaked_and_flat_logits(dtype):
     loss, lse = case.loss()
     near(loss, torch.full((50,), math.log(400), dtype=F64, device=DEV), 1e-6)
     check(Case(50, 400, 64, dtype, k=12, scale=30.0, teacher_scale=30.0))
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_weights_of_rows_without_part_may_be_anything(dtype):
+    """They neither reach the gradients nor take precision from the other rows' ones."""
+    for k in (0, 6):
+        case = Case(90, 200, 48, dtype, k=k, absent=0.0)
+        case.tokens[::5] = -1
+        w = torch.rand(90, device=DEV) + 0.5
+        _, lse = case.loss()
+        found = []
+        for other in (1.0, 1e30, math.inf, math.nan):
+            w[::5] = other
+            dh, dw = torch.empty_like(case.H), torch.empty_like(case.W)
+            case.grad(lse, dh, dw, w)
+            found.append((dh, dw))
+        assert not bool(found[0][0][::5].any())
+        assert all(torch.equal(dh, found[0][0]) and torch.equal(dw, found[0][1]) for dh, dw in found[1:])
 
 
 @pytest.mark.parametrize("dtype", FLOATS)
@@ -244,6 +270,66 @@ def test_either_gradient_alone_and_added(k):
     case.grad(lse, None, total, dscale=0.5, accumulate=True)
     _, want, _, bound = case.head().grads(BF16, None, 0.5)
     near(total, want + old, bound(old))
+
+
+@pytest.mark.parametrize("k", [0, 5])
+def test_a_call_in_a_graph(k):
+    """Replayed on other inputs, with eager work between."""
+    case, other = (Case(300, 2000, 136, BF16, k=k) for _ in range(2))
+    dh, dw = torch.empty_like(case.H), torch.empty_like(case.W)
+    loss, lse = torch.empty(300, device=DEV), torch.empty(300, device=DEV)
+    w = torch.rand(300, device=DEV)
+    names = ("distill", case.tokens, case.A) if k else ("cross_entropy", case.tokens)
+    f, g = getattr(R, f"umap_rows_{names[0]}"), getattr(R, f"umap_rows_{names[0]}_grad")
+    first = torch.empty(getattr(R, f"umap_rows_{names[0]}_workspace")(*case.sizes()), dtype=torch.uint8, device=DEV)
+    second = torch.empty(getattr(R, f"umap_rows_{names[0]}_grad_workspace")(*case.sizes()), dtype=torch.uint8, device=DEV)
+
+    def step(stream=None):
+        f(case.H, case.W, *names[1:], loss, lse, first, stream=stream)
+        g(case.H, case.W, *names[1:], lse, second, dh=dh, dtable=dw, dloss=w, dscale=0.1, stream=stream)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        step(torch.cuda.current_stream())
+    for turn in range(4):
+        for x, y in ((case.H, other.H), (case.tokens, other.tokens)):
+            x.copy_(y if turn % 2 else y.flip(0))
+        w.uniform_()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [x.clone() for x in (loss, lse, dh, dw)]
+        for x in (loss, lse, dh, dw):
+            x.fill_(3.0)
+        first.random_(0, 256)
+        second.random_(0, 256)
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (loss, lse, dh, dw)))
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own."""
+    cases = [Case(700, 5000, 264, BF16, k=3), Case(500, 9000, 72, F32)]
+    want = []
+    for c in cases:
+        loss, lse = c.loss()
+        dh, dw = torch.empty_like(c.H), torch.empty_like(c.W)
+        c.grad(lse, dh, dw)
+        want.append((loss, lse, dh, dw))
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[torch.empty_like(x) for x in o] for o in want]
+    work = [torch.empty(1 << 28, dtype=torch.uint8, device=DEV) for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a, b = cases
+        R.umap_rows_distill_grad(a.H, a.W, a.tokens, a.A, want[0][1], work[0], dh=got[0][2], dtable=got[0][3], stream=streams[0])
+        R.umap_rows_cross_entropy_grad(b.H, b.W, b.tokens, want[1][1], work[1], dh=got[1][2], dtable=got[1][3], stream=streams[1])
+        R.umap_rows_distill(a.H, a.W, a.tokens, a.A, got[0][0], got[0][1], work[0], stream=streams[0])
+        R.umap_rows_cross_entropy(b.H, b.W, b.tokens, got[1][0], got[1][1], work[1], stream=streams[1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
 
 
 def test_no_rows():
