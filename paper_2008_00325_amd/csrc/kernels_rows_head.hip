@@ -12,11 +12,11 @@
 // in the last place of every entry, which sums of many entries average out), its entries at the rows' own tokens
 // from those tokens' unrounded p and q, which may nearly cancel; then come the two products.
 //
-// g_t is a number in [1/2, 1) times 2^e_t.  D holds the number, times 2^14 in fp16, whose smallest
-// values would swallow the probabilities of rare tokens; dh gets 2^e_t on the way out, exactly.  dW takes
-// h_t times 2^(e_t - E), E the largest, instead: also exact.
+// Where all g_t are alike they are left to the very end: D is then p - q, whose largest entries, those of the rows' tokens,
+// lie just below 1 and so are rounded least.  Else g_t is a number in [1/2, 1) times 2^e_t.  D holds the number; dh gets
+// 2^e_t on the way out, exactly, and dW takes h_t times 2^(e_t - E), E the largest, instead: also exact.  In fp16, whose smallest
+// values would swallow the probabilities of rare tokens, D is 2^14 times as large.
 #include <algorithm>
-#include <cmath>
 
 #include "launch_sizes.hpp"
 #include "rows_product.hpp"
@@ -374,10 +374,10 @@ constexpr int kShift = T == UMAP_F16 ? 14 : 0;
 struct RowWeights {
     float *number;
     int *exponent;   // kNoRow: the row takes no part
-    const int *largest;   // null: largest_known
-    int largest_known;
+    const int *largest;   // null, and the numbers 1, the exponents 0: all rows have the weight `all`
+    float all;            // times it, what the products give
 };
-__device__ __forceinline__ int largest_of(const RowWeights &x) { return x.largest ? *x.largest : x.largest_known; }
+__device__ __forceinline__ int largest_of(const RowWeights &x) { return x.largest ? *x.largest : 0; }
 
 __device__ __forceinline__ void split_weight(float g, float &number, int &exponent)
 {
@@ -422,12 +422,19 @@ __global__ __launch_bounds__(256) void k_head_scale(const Elem<T> *copy, int64_t
     }
 }
 
-// A row's weight, its tokens with the entries of D, and the copies of h that the products take, without gaps
-// (`pitch` columns, zeros past the last) and zeros in rows without part.
+// What rounding takes from a row's largest entry at its own tokens, where D has one 16-bit part: dh's rows get it back in
+// fp32 at the end, since it alone would be off as a whole (a row's token often has most of its gradient).
+struct RowRests {
+    int *token;    // null: none; -1: none for the row
+    float *rest;
+};
+
+// A row's weight, its tokens with the entries of D, and its copy for the products, without gaps (`pitch` columns, zeros
+// past the last), zeros in rows without part, and once for each part of D.
 template <int T, int WAVES>
 __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
                                                    const float *dloss, float factor, RowWeights weights, int *token,
-                                                   float *value, Elem<T> *copy, int pitch, int parts)
+                                                   float *value, RowRests rests, Elem<T> *copy, int pitch, int parts)
 {
     __shared__ typename RowTeam<WAVES>::Lds lds;
     const RowTeam<WAVES> team(&lds);
@@ -436,9 +443,9 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
     const Elem<T> *const row = static_cast<const Elem<T> *>(h.data) + t * h.stride;
     const OwnToken<WAVES> own(team, taught, t, w.rows);
     const float g = dloss ? dloss[t] * factor : factor;
-    float number;
-    int exponent;
-    split_weight(g, number, exponent);
+    float number = 1.0f;
+    int exponent = 0;
+    if (dloss) split_weight(g, number, exponent);
     number = ldexpf(number, kShift<T>);
     const bool part = own.any && g != 0.0f;
     const float z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
@@ -456,9 +463,20 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
         again |= o < team.me;
     }
     if (again) id = -1;
+    if (team.me >= taught.k) id = -1;
+    const float entry = id < 0 ? 0.0f : number * ((T == UMAP_F32 ? expf(z - lse[t]) : exp_of(z - lse[t])) - share);
     if (team.me < taught.k) {
         token[t * taught.k + team.me] = id;
-        value[t * taught.k + team.me] = id < 0 ? 0.0f : number * ((T == UMAP_F32 ? expf(z - lse[t]) : exp_of(z - lse[t])) - share);
+        value[t * taught.k + team.me] = entry;
+    }
+    if (rests.token) {
+        int place = 0;   // of the largest entry, the first of several
+        if (!own.alone) {
+            const float most = team.max(fabsf(entry));
+            place = (int)-team.max(id >= 0 && fabsf(entry) == most ? -(float)team.me : -(float)kMostTokens);
+        }
+        if (team.me == place) rests.rest[t] = entry - elem_float<T>(float_elem<T>(entry));
+        if (team.me == (place < kMostTokens ? place : 0)) rests.token[t] = place < kMostTokens ? id : -1;
     }
     if (team.me == 0) {
         weights.number[t] = part ? number : 0.0f;
@@ -623,7 +641,8 @@ __device__ __forceinline__ void rows_tile(const RowSums &x, int block, Piece *ld
 // dh from the sums' parts: four columns per thread, or per 16 threads where there are many parts, each of which adds
 // every 16th.
 template <int T, int SLICES>
-__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int parts, int64_t pitch, const int *exponent, umap_rows dh)
+__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int parts, int64_t pitch, RowWeights weights, RowRests rests,
+                                                      ProductSide w, umap_rows dh)
 {
     constexpr int kGroups = 256 / SLICES;
     __shared__ Acc4 part[SLICES > 1 ? SLICES : 1][kGroups];
@@ -645,10 +664,17 @@ __global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int par
             for (int s = 1; s < SLICES; ++s) sum += part[s][in];
         }
         if (i >= total) continue;
-        const int e = exponent[t];
+        const int e = weights.exponent[t], own = rests.token ? rests.token[t] : -1;
+        if (own >= 0) {
+            const Elem<T> *const row = static_cast<const Elem<T> *>(w.data) + own * w.stride;
+            const float rest = rests.rest[t];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < dh.cols) sum[j] = fmaf(rest, elem_float<T>(row[c + j]), sum[j]);
+        }
         float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = e == kNoRow ? 0.0f : ldexpf(sum[j], e - kShift<T>);
+        for (int j = 0; j < 4; ++j) v[j] = e == kNoRow ? 0.0f : ldexpf(sum[j], e - kShift<T>) * weights.all;
         Elem<T> *const to = static_cast<Elem<T> *>(dh.data) + t * dh.stride + c;
         if (c + 4 <= dh.cols) {
             store_raw<T, 4>(to, raw_of<T, 4>(v));
@@ -685,7 +711,7 @@ __device__ __forceinline__ void table_tile(const TableRows &x, int block, Piece 
         Elem<T> *const to = static_cast<Elem<T> *>(dw.data) + v * dw.stride + m0;
         auto four = [&](int i, int64_t c, float (&g)[4]) {   // columns c .. c + 3 of acc[i][j]
 #pragma unroll
-            for (int r = 0; r < 4; ++r) g[r] = ldexpf(acc[i][j][r], e);
+            for (int r = 0; r < 4; ++r) g[r] = ldexpf(acc[i][j][r], e) * weights.all;
             if (!add) return;
             float old[4] = {};
             if (c + 4 <= dw.cols) {
@@ -801,7 +827,7 @@ struct LossSizes {
 // Rows up to which a 16-bit D has two parts, a value and what its rounding left: few rows do not average the rounding out (a
 // row's token often has most of its gradient, in one entry), and what the products of so few take is the time of the
 // table's bytes.
-constexpr int64_t kTwoPartRows = 128;
+constexpr int64_t kTwoPartRows = 256;
 
 struct GradSizes {
     int64_t n, vocab, cols, k, elem;
@@ -810,7 +836,7 @@ struct GradSizes {
     bool dh_few;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
-    int64_t largest, number, exponent, token, value, copy, scaled, d, sums, packed, total;
+    int64_t largest, number, exponent, token, value, rest_token, rest, copy, scaled, d, sums, packed, total;
     GradSizes(int64_t n_, int64_t vocab_, int32_t cols_, int64_t k_, int32_t type, bool pack)
         : n(n_), vocab(vocab_), cols(cols_), k(k_), elem(elem_size(type))
     {
@@ -844,6 +870,8 @@ struct GradSizes {
         exponent = take(n * 4);
         token = take(n * k * 4);
         value = take(n * k * 4);
+        rest_token = take(n * 4);
+        rest = take(n * 4);
         copy = take(n * parts * h_pitch * elem);
         scaled = take(n * parts * h_pitch * elem);
         d = take(n * parts * d_pitch * elem);
@@ -962,7 +990,8 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                 const float *dloss, float dscale, const umap_rows *dh, const umap_rows *dtable, bool add, void *workspace,
                 hipStream_t s)
 {
-    const bool packing = !direct_side<T>(side_of<T>(table, 0, table.rows));
+    const ProductSide all = side_of<T>(table, 0, table.rows);
+    const bool packing = !direct_side<T>(all);
     const GradSizes z(h.rows, table.rows, table.cols, taught.k, h.type, packing);
     char *const base = static_cast<char *>(workspace);
     auto *const token = reinterpret_cast<int *>(base + z.token);
@@ -970,16 +999,16 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
     auto *const copy = reinterpret_cast<Elem<T> *>(base + z.copy), *const d = reinterpret_cast<Elem<T> *>(base + z.d);
     auto *const scaled = dloss ? reinterpret_cast<Elem<T> *>(base + z.scaled) : nullptr;
     const float factor = dscale * scale;
-    int known = 0;
-    if (factor != 0.0f && std::isfinite(factor)) std::frexp(factor, &known);
     int *const largest = dloss ? reinterpret_cast<int *>(base + z.largest) : nullptr;
-    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, known};
+    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, dloss ? 1.0f : factor};
+    const bool fixing = dh && z.parts == 1 && sizeof(Elem<T>) == 2;
+    const RowRests rests{fixing ? reinterpret_cast<int *>(base + z.rest_token) : nullptr, reinterpret_cast<float *>(base + z.rest)};
     if (z.n > 0) {
         UL_LAUNCHED(by_team(z.n, z.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
             hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(RowTeam<W>::kBlock), 0, s,
                                side_of<T>(table, 0, table.rows), side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
-                               token, value, copy, (int)z.h_pitch, (int)z.parts);
+                               token, value, rests, copy, (int)z.h_pitch, (int)z.parts);
             return hipGetLastError();
         }));
         if (dloss && dtable) {
@@ -1061,10 +1090,10 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         const int parts = (int)(z.splits * z.parts);
         if (parts >= 8)
             hipLaunchKernelGGL((k_head_dh_join<T, 16>), dim3((unsigned)std::min<int64_t>(4096, over(total, 16))), dim3(256), 0, s, sums,
-                               parts, z.sum_pitch, weights.exponent, *dh);
+                               parts, z.sum_pitch, weights, rests, all, *dh);
         else
             hipLaunchKernelGGL((k_head_dh_join<T, 1>), dim3((unsigned)std::min<int64_t>(4096, over(total, 256))), dim3(256), 0, s, sums,
-                               parts, z.sum_pitch, weights.exponent, *dh);
+                               parts, z.sum_pitch, weights, rests, all, *dh);
         UL_LAUNCHED(hipGetLastError());
     }
     return hipSuccess;

@@ -47,7 +47,7 @@ def test_gpu_tests_reach_every_shape(shapes):
     asked, seen = [], {}
     for n, rows, cols, dtype in SHAPES:
         elem = dtype.itemsize
-        parts = 2 if elem == 2 and n <= 128 else 1
+        parts = 2 if elem == 2 and n <= 256 else 1
         steps = -(-(-(-rows // 256) * 256) // (128 // elem))
         if n > 64:
             asked.append(("logits", elem, (rows, n, 1, elem)))
