@@ -290,9 +290,10 @@ int64_t umap_rows_cross_entropy_grad_workspace(int64_t n, int64_t rows, int32_t 
 /*
  * umap_rows_distill -- the divergence of the softmax over a table from a teacher
  * of which each row's largest logits are known.  With z and lse as for
- * umap_rows_cross_entropy, k = teacher->cols and e, f < k:
- *   q[t][e] = exp(teacher_scale teacher[t][e]) / sum_f exp(teacher_scale teacher[t][f])
- *   loss[t] = sum_e q[t][e] (log q[t][e] - (z[t][ids[t][e]] - lse[t]))
+ * umap_rows_cross_entropy, k = teacher->cols, places e, f < k and tokens v:
+ *   s[t][e] = exp(teacher_scale teacher[t][e]) / sum_f exp(teacher_scale teacher[t][f])
+ *   q[t][v] = sum of s[t][e] over ids[t][e] = v
+ *   loss[t] = sum_v q[t][v] (log q[t][v] - (z[t][v] - lse[t])),  0 log 0 = 0
  * scale and teacher_scale are one over the temperature, times what else scales the
  * logits; the factor temperature^2 that usually goes with it is dscale's.
  *
@@ -301,7 +302,7 @@ int64_t umap_rows_cross_entropy_grad_workspace(int64_t n, int64_t rows, int32_t 
  *             Places whose id lies outside [0, table->rows), and places with a
  *             logit of -infinity, are empty: they take no part in the sums.  A row
  *             with empty places only takes no part: its loss is 0.  A token may come
- *             twice in a row; its shares add up.
+ *             in several places of a row.
  *   teacher   UMAP_F32, UMAP_F16 or UMAP_BF16, h->rows rows of 1 <= k <= 256 logits.
  *
  * Errors: UMAP_E_INVAL, UMAP_E_DEVICE.
@@ -316,7 +317,7 @@ int64_t umap_rows_distill_workspace(int64_t n, int64_t rows, int32_t cols, int32
 /*
  * umap_rows_distill_grad -- its gradient for h and table (the teacher's logits are
  * constants): umap_rows_cross_entropy_grad with
- *   D[t][v] = dscale dloss[t] (exp(z[t][v] - lse[t]) - sum of q[t][e] over ids[t][e] = v)
+ *   D[t][v] = dscale dloss[t] (exp(z[t][v] - lse[t]) - q[t][v])
  * and the arguments of both.
  */
 int umap_rows_distill_grad(const umap_rows *h, const umap_rows *table, const void *ids, int32_t id_type,

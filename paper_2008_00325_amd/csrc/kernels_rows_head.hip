@@ -1,9 +1,9 @@
 // kernels_rows_head.hip -- the head over a table of tokens (umap_rows.h): softmax cross entropy
 // and the divergence from a teacher's largest logits, and their gradient.
 //
-//   z_tv = scale h_t . W_v,  lse_t = log sum_v exp z_tv,  shares q_te of the row's tokens id_te
-//   loss_t = sum_e q_te (log q_te + lse_t - z_{t, id_te})          (cross entropy: one token, q = 1)
-//   D_tv = g_t (exp(z_tv - lse_t) - sum_{e: id_te = v} q_te),  dh = D W,  dW = D^T h,  g_t = dscale scale dloss_t
+//   z_tv = scale h_t . W_v,  lse_t = log sum_v exp z_tv,  shares q_tv of the row's own tokens v
+//   loss_t = sum_v q_tv (log q_tv + lse_t - z_tv)          (cross entropy: one token, q = 1)
+//   D_tv = g_t (exp(z_tv - lse_t) - q_tv),  dh = D W,  dW = D^T h,  g_t = dscale scale dloss_t
 //
 // The logits are never kept.  Forward: a tile of them (rows of the table times rows of h) leaves
 // a maximum and a sum of exponentials for each row of h, which a second launch joins; that launch
@@ -221,6 +221,24 @@ struct OwnToken {
     }
 };
 
+// All shares of a thread's token in its row: of a token that comes twice the first place has them, the others none.
+template <int WAVES>
+__device__ __forceinline__ float all_shares(const RowTeam<WAVES> &team, const OwnToken<WAVES> &own, int k)
+{
+    if (own.alone) return own.share;
+    float share = 0.0f;
+    bool again = false;
+#pragma unroll 8
+    for (int o = 0; o < k; ++o) {
+        const int other = team.of(own.id, team.lds->id, o);
+        const float more = team.of(own.share, team.lds->share, o);
+        if (other != own.id) continue;
+        share += more;
+        again |= o < team.me;
+    }
+    return again ? -1.0f : share;
+}
+
 template <int T>
 __device__ __forceinline__ void fetch8(const Elem<T> *row, int c, int cols, float v[8])
 {
@@ -355,7 +373,9 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_loss(ProductSid
     const float z = own_logit<T, WAVES>(team, static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, scale);
     const float most = team.max(mine.m);
     const float sum = Logit<T>::natural(most + Logit<T>::log(team.sum(mine.s * Logit<T>::exp(mine.m - MaxSum::base(most)))));
-    float all = own.id >= 0 && own.share != 0.0f ? own.share * (own.log_share + (sum - z)) : 0.0f;
+    const float share = all_shares(team, own, taught.k);   // > 0, or NaN, where there is one
+    const float log_share = share == own.share ? own.log_share : logf(share);
+    float all = own.id >= 0 && !(share <= 0.0f) ? share * (log_share + (sum - z)) : 0.0f;
     if (!own.alone) all = team.sum(all);
     if (team.me == 0) {
         lse[first + t] = sum;
@@ -450,19 +470,8 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
     const bool part = own.any && g != 0.0f;
     const float z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
     int id = part ? own.id : -1;
-    // a token that comes twice: the first place has all its shares
-    float share = 0.0f;
-    bool again = false;
-    if (own.alone) share = 1.0f;
-#pragma unroll 8
-    for (int o = 0; o < (own.alone ? 0 : taught.k); ++o) {
-        const int other = team.of(own.id, lds.id, o);
-        const float more = team.of(own.share, lds.share, o);
-        if (other != own.id) continue;
-        share += more;
-        again |= o < team.me;
-    }
-    if (again) id = -1;
+    const float share = all_shares(team, own, taught.k);
+    if (share < 0.0f) id = -1;
     if (team.me >= taught.k) id = -1;
     const float entry = id < 0 ? 0.0f : number * ((T == UMAP_F32 ? expf(z - lse[t]) : exp_of(z - lse[t])) - share);
     if (team.me < taught.k) {
@@ -1007,7 +1016,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         UL_LAUNCHED(by_team(z.n, z.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
             hipLaunchKernelGGL((k_head_rows<T, W>), dim3((unsigned)over(z.n, RowTeam<W>::kRows)), dim3(RowTeam<W>::kBlock), 0, s,
-                               side_of<T>(table, 0, table.rows), side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
+                               all, side_of<T>(h, 0, h.rows), scale, taught, lse, dloss, factor, weights,
                                token, value, rests, copy, (int)z.h_pitch, (int)z.parts);
             return hipGetLastError();
         }));

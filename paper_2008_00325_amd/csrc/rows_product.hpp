@@ -99,12 +99,13 @@ struct Step {
     }
 };
 
-// Whether a side is made of whole pieces at 16-byte places, close enough together for 32-bit offsets.
+// Whether a side is made of whole pieces at 16-byte places, its rows apart, but close enough for 32-bit offsets.
 template <int T>
 bool direct_side(const ProductSide &s)
 {
     constexpr int kElem = sizeof(Elem<T>), kPer = 16 / kElem;
-    return (uintptr_t)s.data % 16 == 0 && s.stride % kPer == 0 && s.cols % kPer == 0 && s.stride < ((int64_t)1 << 30) / 256 / kElem;
+    return (uintptr_t)s.data % 16 == 0 && s.stride % kPer == 0 && s.cols % kPer == 0 && s.stride >= s.cols &&
+           s.stride < ((int64_t)1 << 30) / 256 / kElem;
 }
 
 // All of this wave's loads into LDS but the newest `left` have landed, then all waves'.

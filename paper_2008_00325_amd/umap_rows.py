@@ -353,8 +353,9 @@ def umap_rows_distill_workspace(n: int, rows: int, cols: int, k: int, dtype) -> 
 
 def umap_rows_distill(h, table, ids, teacher, loss, lse, workspace, scale: float = 1.0, teacher_scale: float = 1.0,
                       stream=None) -> None:
-    """loss[t] = sum over e of q[t, e] * (log q[t, e] - log p[t, ids[t, e]]), q = softmax(teacher_scale * teacher) over the
-    row's tokens, p = softmax(scale * h @ table.T) over the table; lse as for umap_rows_cross_entropy.
+    """loss[t] = sum over v of q[t, v] * (log q[t, v] - log p[t, v]), q = softmax(teacher_scale * teacher) over the row's
+    tokens ids[t] (of a token that comes twice the sum), p = softmax(scale * h @ table.T); lse as for
+    umap_rows_cross_entropy.
 
     Places whose id lies outside the table are empty; a row with empty places only has loss 0."""
     H, n, _ = _rows(h, "h", _FLOAT)

@@ -30,7 +30,7 @@ def shares(ids, rows, teacher64=None, teacher_scale=1.0):
         q = e / torch.where(there.any(1, keepdim=True), e.sum(1, keepdim=True), 1.0)
     full = torch.zeros((n, rows), dtype=F64, device=ids.device)
     full.scatter_add_(1, torch.where(there, ids, 0), torch.where(there, q, 0.0))
-    inner = torch.where(q > 0, q * torch.log(torch.where(q > 0, q, 1.0)), torch.where(q.isnan(), q, 0.0)).sum(1)
+    inner = torch.where(full > 0, full * torch.log(torch.where(full > 0, full, 1.0)), torch.where(full.isnan(), full, 0.0)).sum(1)
     return full, inner, there.any(1)
 
 

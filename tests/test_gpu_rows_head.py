@@ -130,6 +130,40 @@ def test_strides_and_alignment(dtype, pad, table_pad):
 
 
 @pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("n,rows", [(40, 300), (300, 40), (1, 90), (90, 1)])
+def test_rows_that_are_one_row(n, rows, dtype):
+    """A matrix that is only read may have the stride 0, and a single row any."""
+    for k in (0, 2):
+        for of_h, of_table in ((True, False), (False, True), (True, True)):
+            case = Case(n, rows, 64, dtype, k=k, lean=2.0)
+            if of_h:
+                case.H = case.H[:1].expand(n, 64)
+                assert case.H.stride(0) == 0 or n == 1
+            if of_table:
+                case.W = case.W[:1].expand(rows, 64)
+            check(case)
+            if n == 1:
+                case.H = torch.as_strided(case.H, (1, 64), (24, 1))
+                check(case)
+            if rows == 1:
+                case.W = torch.as_strided(case.W, (1, 64), (8, 1))
+                check(case)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_far_apart(dtype):
+    """Rows a megabyte apart: beyond what a product's 32-bit offsets reach."""
+    whole = torch.zeros(40, 1 << 20, dtype=dtype, device=DEV)
+    for shift in (0, 3):
+        case = Case(40, 40, 72, dtype)
+        case.H = whole[:, shift:shift + 72].copy_(case.H)
+        check(case)
+        case = Case(30, 40, 72, dtype, k=3)
+        case.W = whole[:, shift:shift + 72].copy_(case.W)
+        check(case)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
 def test_weights_of_rows(dtype):
     n = 200
     w = torch.rand(n, device=DEV) + 0.1
