@@ -210,8 +210,8 @@ struct OwnToken {
         if (WAVES > 1 && team.me < kMostTokens) team.lds->id[team.me] = id;   // read behind the reductions' barriers
         const float most = MaxSum::base(team.max(log_share));
         share = id >= 0 ? exp_of(log_share - most) : 0.0f;
-        any = team.max(id >= 0 ? 1.0f : 0.0f) > 0.0f;
         const float sum = team.sum(share);
+        any = !(sum == 0.0f);   // the largest counts 1
         share = id >= 0 ? share / sum : 0.0f;
         log_share = log_share - most - logf(sum);
         if constexpr (WAVES > 1) {
@@ -424,13 +424,27 @@ __global__ __launch_bounds__(1024) void k_head_largest(const int *exponent, int6
     }
 }
 
-// The rows' copies times 2^(e_t - E): `rows` of them, `parts` times one after the other.
+// The rows' copies times 2^(e_t - E): `rows` of them, `parts` times one after the other.  With few rows every workgroup
+// finds the largest exponent for itself, and the first leaves it to the launches that follow.
+constexpr int64_t kFindRows = 8192;
 template <int T>
 __global__ __launch_bounds__(256) void k_head_scale(const Elem<T> *copy, int64_t rows, int parts, int pitch, const int *exponent,
-                                                    const int *largest, Elem<T> *scaled)
+                                                    int *largest, Elem<T> *scaled)
 {
     const int64_t total = rows * (pitch / 8);
-    const int most = *largest;
+    int most = kNoRow;
+    if (rows <= kFindRows) {
+        __shared__ int part[4];
+        for (int t = threadIdx.x; t < (int)rows; t += 256) most = max(most, exponent[t]);
+        for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+        __syncthreads();
+        most = max(max(part[0], part[1]), max(part[2], part[3]));
+        most = most == kNoRow ? 0 : most;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *largest = most;
+    } else {
+        most = *largest;
+    }
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t t = i / (pitch / 8);
         const int by = exponent[t] == kNoRow ? 0 : exponent[t] - most;
@@ -479,10 +493,11 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
         value[t * taught.k + team.me] = entry;
     }
     if (rests.token) {
-        int place = 0;   // of the largest entry, the first of several
+        int place = 0;   // of the largest entry (to 2^-15): its magnitude and its place as one number
         if (!own.alone) {
-            const float most = team.max(fabsf(entry));
-            place = (int)-team.max(id >= 0 && fabsf(entry) == most ? -(float)team.me : -(float)kMostTokens);
+            const uint32_t key = (__float_as_uint(fabsf(entry)) & ~255u) | (255u - team.me);
+            const float most = team.max(id >= 0 ? __uint_as_float(key) : -1.0f);
+            place = most < 0.0f ? kMostTokens : 255 - (int)(__float_as_uint(most) & 255u);
         }
         if (team.me == place) rests.rest[t] = entry - elem_float<T>(float_elem<T>(entry));
         if (team.me == (place < kMostTokens ? place : 0)) rests.token[t] = place < kMostTokens ? id : -1;
@@ -1021,8 +1036,10 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
             return hipGetLastError();
         }));
         if (dloss && dtable) {
-            hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, weights.exponent, z.n, largest);
-            UL_LAUNCHED(hipGetLastError());
+            if (z.n > kFindRows) {
+                hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, weights.exponent, z.n, largest);
+                UL_LAUNCHED(hipGetLastError());
+            }
             hipLaunchKernelGGL((k_head_scale<T>), dim3((unsigned)std::min<int64_t>(8192, over(z.n * z.h_pitch / 8, 256))), dim3(256), 0, s,
                                copy, z.n, (int)z.parts, (int)z.h_pitch, weights.exponent, largest, scaled);
             UL_LAUNCHED(hipGetLastError());

@@ -171,6 +171,7 @@ def test_weights_of_rows(dtype):
     w[3] = -2.5
     check(Case(n, 700, 72, dtype), weights=w, dscale=1 / n)
     check(Case(n, 700, 72, dtype, k=9), weights=w, dscale=3.0)
+    check(Case(9000, 300, 16, dtype, lean=3.0), weights=torch.rand(9000, device=DEV) + 0.1, dscale=1 / n)
     if dtype != F16:   # weights that no 16-bit exponent holds side by side
         check(Case(n, 300, 40, dtype), weights=torch.exp2(torch.randint(-60, 20, (n,), device=DEV).float()) * w)
 
