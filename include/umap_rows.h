@@ -260,8 +260,9 @@ int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols,
  *   dh[t]     = scale sum_v D[t][v] table[v]
  *   dtable[v] = scale sum_t D[t][v] h[t]
  * The logits are formed again, for a piece of the table at a time, and D of the piece
- * is kept in h's type (16 bits: each entry off by half a unit in its last place, fp32:
- * not rounded), all sums are fp32 and rounded once; their order is fixed.
+ * is kept in h's type (fp32: not rounded; 16 bits: in two parts up to 256 rows, else
+ * each entry off by up to half a unit in its last place, which the sums average out);
+ * all sums are fp32 and rounded once; their order is fixed.
  *
  *   h, table, targets, scale  as for umap_rows_cross_entropy.
  *   lse        what that call gave.

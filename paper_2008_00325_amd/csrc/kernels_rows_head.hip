@@ -5,17 +5,28 @@
 //   loss_t = sum_v q_tv (log q_tv + lse_t - z_tv)          (cross entropy: one token, q = 1)
 //   D_tv = g_t (exp(z_tv - lse_t) - q_tv),  dh = D W,  dW = D^T h,  g_t = dscale scale dloss_t
 //
-// The logits are never kept.  Forward: a tile of them (rows of the table times rows of h) leaves
-// a maximum and a sum of exponentials for each row of h, which a second launch joins; that launch
-// also forms the logits of the rows' own tokens, as dot products.  Gradient: for a piece of the table at a
-// time the logits are formed anew and D is written in the inputs' type (16 bits: half a unit
-// in the last place of every entry, which sums of many entries average out), its entries at the rows' own tokens
-// from those tokens' unrounded p and q, which may nearly cancel; then come the two products.
+// The logits are never kept.  Forward: a tile of them (rows of the table times rows of h) leaves a maximum and a sum of
+// exponentials for each row of h, which a second launch joins; that launch also forms the logits of the rows' own
+// tokens, as dot products.  Gradient: for a piece of the table at a time (D of 256 MB, what the last cache holds) the logits
+// are formed anew and D is written in the inputs' type, its entries at the rows' own tokens from those tokens' unrounded p
+// and q, which may nearly cancel; then come the two products.  In fp32 that p is the tile's own: lse comes of the same sums, and
+// what rounding did to them cancels.  With p from a dot product of its own, dh and dW of 77 rows against 2,000 x 64 were off
+// by 8.1e-7 and 9.3e-7 of their norms (medians of 39 inputs), so by 3.2e-7 and 3.1e-7.
 //
-// Where all g_t are alike they are left to the very end: D is then p - q, whose largest entries, those of the rows' tokens,
-// lie just below 1 and so are rounded least.  Else g_t is a number in [1/2, 1) times 2^e_t.  D holds the number; dh gets
-// 2^e_t on the way out, exactly, and dW takes h_t times 2^(e_t - E), E the largest, instead: also exact.  In fp16, whose smallest
-// values would swallow the probabilities of rare tokens, D is 2^14 times as large.
+// Precision of D in 16 bits: an entry is off by up to half a unit in its last place, and sums of many entries average that
+// out: dW is off by 1.2 (median) to 1.45 times what its own type's rounding alone costs (60 cases of 257 to 700 rows).  Where it
+// does not average out it is avoided: up to 256 rows D has two parts, a value and what its rounding left; and a row of dh, most of which often comes from one
+// token, gets back what that token's entry lost.  Where all g_t are alike they are left to the very end: D is then p - q, whose
+// largest entries, those of the rows' tokens, lie just below 1 and so are rounded least.  Else g_t is a number in [1/2, 1) times
+// 2^e_t.  D holds the number; dh gets 2^e_t on the way out, exactly, and dW takes h_t times 2^(e_t - E), E the largest of the rows
+// that take part, instead: also exact.  In fp16, whose smallest values would swallow the probabilities of rare tokens, D is 2^14
+// times as large.
+//
+// Bound by the matrix cores for many rows, by the table's bytes for few.  bf16: 8,192 rows against 128,000 x 4,096: loss 6.1 ms
+// (1,400 TFLOP/s; the library's product of the same size 5.8 ms, without the exponentials), gradient 20.0 ms (1,290: D 0.84,
+// dh 0.83 and dW 0.86 ms of each of 8 pieces); one row against 32,000 x 2,048: 21 us of the tiles (6.2 TB/s) and 5 of
+// the row.  Fewer columns leave a tile less to multiply before its end: 2,048 rows against 32,000 reach 1,350 TFLOP/s at 4,096
+// columns, 910 at 512.
 #include <algorithm>
 
 #include "launch_sizes.hpp"
@@ -482,12 +493,14 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
     if (dloss) split_weight(g, number, exponent);
     number = ldexpf(number, kShift<T>);
     const bool part = own.any && g != 0.0f;
-    const float z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
+    float z = 0.0f;
+    if constexpr (T != UMAP_F32) z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
     int id = part ? own.id : -1;
     const float share = all_shares(team, own, taught.k);
     if (share < 0.0f) id = -1;
     if (team.me >= taught.k) id = -1;
-    const float entry = id < 0 ? 0.0f : number * ((T == UMAP_F32 ? expf(z - lse[t]) : exp_of(z - lse[t])) - share);
+    float entry = 0.0f;   // fp32: what is taken from number p, which the tile knows
+    if (id >= 0) entry = number * (T == UMAP_F32 ? share : exp_of(z - lse[t]) - share);
     if (team.me < taught.k) {
         token[t * taught.k + team.me] = id;
         value[t * taught.k + team.me] = entry;
@@ -547,7 +560,7 @@ __device__ __forceinline__ int pair_row()
 }
 
 // D of a piece of the table: d[t][v], `pitch` columns, zeros past the piece's rows.  token and value: null, or each
-// row's one token (less the piece's first) and its entry.
+// row's one token and its entry (fp32: what number p is less of there).
 template <int T, class P>
 __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSide h, float scale, Tiles tiles, const float *lse,
                                                         RowWeights weights, const int *token, const float *value, int64_t first,
@@ -566,12 +579,22 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
         const int64_t t = n0 + P::n_of(j);
         if (t >= h.rows) continue;
         const float number = weights.number[t], less = Logit<T>::of_natural(lse[t]);
+        [[maybe_unused]] int64_t own = -1;
+        [[maybe_unused]] float taken = 0.0f;
+        if (T == UMAP_F32 && token && token[t] >= 0) {
+            own = token[t] - first - m0;
+            taken = value[t];
+        }
         Elem<T> *const to = d + t * pitch + m0;
         float v[FM][4];
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[i][r] = number * logit.exp_less(acc[i][j][r], less);
+            for (int r = 0; r < 4; ++r) {
+                const float p = logit.exp_less(acc[i][j][r], less);
+                if constexpr (T == UMAP_F32) v[i][r] = fmaf(number, p, P::m_of(i) + r == own ? -taken : 0.0f);
+                else v[i][r] = number * p;
+            }
         if (live < P::M || number == 0.0f) {   // past the table, or a row without part
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -597,7 +620,7 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
             store(to + below, [](float(&x)[4]) { return raw_of<T, 4>(x); });
         }
     }
-    if (!token) return;
+    if (T == UMAP_F32 || !token) return;
     // the entries of the rows' own tokens, over those just stored: by other lanes, so behind their stores
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -614,7 +637,7 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
     }
 }
 
-// The entries of D at the rows' own tokens.
+// The entries of D at the rows' own tokens (fp32: value is taken from what is there).
 template <int T>
 __global__ __launch_bounds__(256) void k_head_own(const int *token, const float *value, int64_t count, int k, int64_t first,
                                                   int64_t rows, Elem<T> *d, int64_t pitch, int64_t below)
@@ -623,6 +646,10 @@ __global__ __launch_bounds__(256) void k_head_own(const int *token, const float 
         const int64_t v = token[i] - first;
         if (token[i] < 0 || v < 0 || v >= rows) continue;
         Elem<T> *const at = d + i / k * pitch + v;
+        if constexpr (T == UMAP_F32) {   // each place has one token's value
+            *at -= value[i];
+            continue;
+        }
         *at = float_elem<T>(value[i]);
         if (below) at[below] = float_elem<T>(value[i] - elem_float<T>(*at));
     }
@@ -848,9 +875,10 @@ struct LossSizes {
     }
 };
 
-// Rows up to which a 16-bit D has two parts, a value and what its rounding left: few rows do not average the rounding out (a
-// row's token often has most of its gradient, in one entry), and what the products of so few take is the time of the
-// table's bytes.
+// Rows up to which a 16-bit D has two parts: few rows do not average the rounding out.  It is paid for in time: one part or two
+// against 32,000 x 2,048 in bf16 take 84 and 83 us for 1 row, 86 and 88 for 16, 100 and 121 for 64, 129 and 171 for 128, 191
+// and 235 for 256.  dtable's error, relative to its type's own, at worst of 60 cases each: one part 1.64 for 20 to 128 rows and
+// 1.45 for 129 to 256, two parts 1.0004; one part for 257 to 700 rows 1.45.
 constexpr int64_t kTwoPartRows = 256;
 
 struct GradSizes {

@@ -427,6 +427,22 @@ def test_same_bits_at_every_call_and_on_a_stream():
             assert torch.equal(h2, dh) and torch.equal(w2, dw)
 
 
+@pytest.mark.parametrize("k", [0, 2])
+@pytest.mark.parametrize("n,cols", [(1, 64), (40, 333), (300, 200), (2100, 1024)])
+def test_fp32_gradients_of_a_certain_token_are_zero(n, cols, k):
+    """The one token of a table: lse is its logit, since log 1 = 0, so p = exp 0 = 1 = q and D = 0, whatever the logit's
+    rounding, if the gradient's logit is the one that lse is of (a scale of 1 or 1/2 adds no rounding)."""
+    for scale in (1.0, 0.5):
+        case = Case(n, 1, cols, F32, k=k, absent=0.0, scale=scale)
+        if k:
+            case.tokens[:, 1:] = -1   # a share alone is e / e = 1
+        lse = case.loss()[1]
+        for weights in (None, torch.rand(n, device=DEV) + 0.1):
+            dh, dw = torch.full_like(case.H, 7.0), torch.full_like(case.W, 7.0)
+            case.grad(lse, dh, dw, weights)
+            assert not bool(dh.any()) and not bool(dw.any())
+
+
 def test_written_tensors_have_a_new_version():
     case = Case(4, 9, 8, F32, absent=0.0)
     for k in (0, 2):
