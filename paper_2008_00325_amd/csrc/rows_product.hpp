@@ -11,9 +11,10 @@
 // from (lane / 16) * 16 bytes on.  How the matrix instruction numbers k does not matter as long as
 // both sides agree.
 //
-// The large tile, 256 x 256 by eight waves of 128 x 64, keeps 128 KB of LDS, two steps, and the matrix cores busy 60 % of the
-// time at the clock that their power leaves (2.05 of 2.4 GHz): 1,400 TFLOP/s of bf16 with random values, 1,750 with a table of
-// zeros (the library's product 1,490 and 2,000).  Four waves of 128 x 128 (one to a SIMD, 512 registers) took 9.0 ms where these
+// The large tile, 256 x 256 by eight waves of 128 x 64, takes 128 KB of LDS, two steps.  The matrix cores are busy 61 to 65 %
+// of the cycles in the gradient's three products at 2.0 GHz, 73 % in the loss's single long launch, whose clock their power
+// holds at 1.5 while counted: 1,400 TFLOP/s of bf16 with random values, 1,750 with a table of zeros (the library's product 1,490
+// and 2,000).  Four waves of 128 x 128 (one to a SIMD, 512 registers) took 9.0 ms where these
 // took 7.1; loads not spread between the products cost 2 to 3 %.  No read meets another's bank (counted).
 #pragma once
 
@@ -157,9 +158,10 @@ struct DirectSide {
     // The q-th of the step's loads.
     __device__ __forceinline__ void one(const Loads &x, int q) const
     {
-        // the whole offset in the lane's register: it is what the hardware compares with the buffer's length
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(x.lds + q * THREADS * 16),
-                     "v"(x.at + q * x.step), "s"(x.buffer)
+        // the whole offset in the lane's register: it is what the hardware compares with the buffer's length.  The others are
+        // alike in all lanes, which a build without optimization has to be told.
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)__builtin_amdgcn_readfirstlane(x.lds + q * THREADS * 16)),
+                     "v"(x.at + q * x.step), "s"(Words{(uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.x), (uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.y), (uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.z), (uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.w)})
                      : "memory");
     }
 };
