@@ -443,6 +443,21 @@ def test_fp32_gradients_of_a_certain_token_are_zero(n, cols, k):
             assert not bool(dh.any()) and not bool(dw.any())
 
 
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_one_teacher_and_one_row_for_all(dtype):
+    """Inputs of stride 0 give the bits that their copies give."""
+    case = Case(90, 500, 72, dtype, k=12)
+    case.H, case.A = case.H[3:4].expand(90, 72), case.A[5:6].expand(90, 12)
+    outs = []
+    for _ in range(2):
+        loss, lse = case.loss()
+        dh, dw = torch.empty(90, 72, dtype=dtype, device=DEV), torch.empty_like(case.W)
+        case.grad(lse, dh, dw)
+        outs.append((loss, lse, dh, dw))
+        case.H, case.A = case.H.contiguous(), case.A.contiguous()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
 def test_written_tensors_have_a_new_version():
     case = Case(4, 9, 8, F32, absent=0.0)
     for k in (0, 2):

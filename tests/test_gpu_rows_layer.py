@@ -291,3 +291,52 @@ def test_same_bits_at_every_call_on_a_stream_and_new_versions():
             assert all(x._version > v for x, v in zip((y, dx, dw, db), before))
             outs.append((y, dx, dw, db))
         assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(outs[0], o))
+
+
+@pytest.mark.parametrize("cols", [100, 3000, 20_000])
+def test_one_row_for_all(cols):
+    """Inputs of stride 0 give the bits that their copies give."""
+    n = 70
+    one, other, more = (rand(1, cols, BF16).expand(n, cols) for _ in range(3))
+    assert one.stride(0) == 0
+    outs = []
+    for x, dy, r in ((one, other, more), (one.contiguous(), other.contiguous(), more.contiguous())):
+        y, h, dx = (torch.empty(n, cols, dtype=BF16, device=DEV) for _ in range(3))
+        dw, db = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+        work = Workspace(R.umap_rows_layer_norm_grad_workspace(n, cols))
+        R.umap_rows_layer_norm(x, y, residual=r, h=h)
+        R.umap_rows_layer_norm_grad(dy, x, dx, dh=r, dweight=dw, dbias=db, workspace=work.inside)
+        assert work.framed()
+        outs.append((y, h, dx, dw, db))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("cols", [300, 5000, 20_000])
+def test_a_call_in_a_graph(cols):
+    """Replayed on other inputs, with eager work between."""
+    x, r, dy = (rand(200, cols, F16) for _ in range(3))
+    W, B = vector(cols, F32, 1.0), vector(cols, F32, 0.0)
+    y, h, dx = (torch.empty(200, cols, dtype=F16, device=DEV) for _ in range(3))
+    dw, db = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    work = torch.empty(R.umap_rows_layer_norm_grad_workspace(200, cols), dtype=torch.uint8, device=DEV)
+
+    def step(stream=None):
+        R.umap_rows_layer_norm(x, y, weight=W, bias=B, residual=r, h=h, stream=stream)
+        R.umap_rows_layer_norm_grad(dy, h, dx, weight=W, dweight=dw, dbias=db, workspace=work, stream=stream)
+
+    step()
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        step(torch.cuda.current_stream())
+    for turn in range(4):
+        for t in (x, r, dy, W):
+            t.normal_(0.2 * turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in (y, h, dx, dw, db)]
+        for t in (y, h, dx, dw, db):
+            t.fill_(3.0)
+        work.random_(0, 256)
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (y, h, dx, dw, db)))
