@@ -938,7 +938,9 @@ template <int T, bool AA, bool AB, typename F>
 hipError_t by_shape(TileShape shape, F f)
 {
     switch (shape) {
-    case TileShape::large: return f(Large<T, AA, AB>{});
+    case TileShape::large:
+        if constexpr (!Small<T, AA, AB>::kBlocks) return f(Large<T, AA, AB>{});   // else the registers are short
+        [[fallthrough]];
     case TileShape::small: return f(Small<T, AA, AB>{});
     case TileShape::tiny: return f(Tiny<T, AA, AB, 2>{});
     default: return f(Tiny<T, AA, AB, 4>{});

@@ -443,6 +443,18 @@ def test_fp32_gradients_of_a_certain_token_are_zero(n, cols, k):
             assert not bool(dh.any()) and not bool(dw.any())
 
 
+@pytest.mark.parametrize("n", [1, 40, 300, 2100])
+def test_fp32_logits_of_long_rows(n):
+    """One token's lse is its logit.  A sum in blocks of 256 terms of one sign, whatever their order, is off by at most 255
+    roundings in a block and one for each block, each 2^-24 of the sum; one more is for the scale and one for lse."""
+    cols = 8192
+    case = Case(n, 1, cols, F32, absent=0.0)
+    case.H.copy_(torch.rand(n, cols, device=DEV) + 0.5)
+    case.W.copy_((torch.rand(1, cols, device=DEV) + 0.5) / 64)
+    exact = (case.H.to(F64) * case.W.to(F64)).sum(1)
+    near(case.loss()[1], exact, (255 + cols // 256 + 2) * 2.0**-24 * exact, "lse")
+
+
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_one_teacher_and_one_row_for_all(dtype):
     """Inputs of stride 0 give the bits that their copies give."""
