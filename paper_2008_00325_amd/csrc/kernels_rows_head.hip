@@ -214,17 +214,21 @@ struct OwnToken {
             return;
         }
         if (team.me < x.k) id = (int)row_of(x.ids, t * x.k + team.me, rows);
+        float logit = minus_inf();   // the largest of these counts 1
         if (id >= 0) {
-            log_share = teacher_at(x, t, team.me) * x.scale;
-            if (log_share == minus_inf()) id = -1;
+            const float a = teacher_at(x, t, team.me);
+            if (a == minus_inf()) id = -1;
+            else logit = x.scale < 0.0f ? -a : a;
         }
         if (WAVES > 1 && team.me < kMostTokens) team.lds->id[team.me] = id;   // read behind the reductions' barriers
-        const float most = MaxSum::base(team.max(log_share));
-        share = id >= 0 ? exp_of(log_share - most) : 0.0f;
+        // the difference first: it is in fp32's range, or far below, where a product with the scale may not be
+        const float less = logit - MaxSum::base(team.max(logit));
+        log_share = (less == minus_inf() ? -__FLT_MAX__ : less) * fabsf(x.scale);   // the scale may be 0
+        share = id >= 0 ? exp_of(log_share) : 0.0f;
         const float sum = team.sum(share);
         any = !(sum == 0.0f);   // the largest counts 1
         share = id >= 0 ? share / sum : 0.0f;
-        log_share = log_share - most - logf(sum);
+        log_share -= logf(sum);
         if constexpr (WAVES > 1) {
             if (team.me < kMostTokens) team.lds->share[team.me] = share;
             __syncthreads();
