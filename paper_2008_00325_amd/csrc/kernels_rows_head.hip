@@ -224,7 +224,7 @@ struct OwnToken {
         // the difference first: it is in fp32's range, or far below, where a product with the scale may not be
         const float less = logit - MaxSum::base(team.max(logit));
         log_share = (less == minus_inf() ? -__FLT_MAX__ : less) * fabsf(x.scale);   // the scale may be 0
-        share = id >= 0 ? exp_of(log_share) : 0.0f;
+        share = id >= 0 ? expf(log_share) : 0.0f;   // not rounded any further in fp32, nor in the loss
         const float sum = team.sum(share);
         any = !(sum == 0.0f);   // the largest counts 1
         share = id >= 0 ? share / sum : 0.0f;

@@ -1,10 +1,12 @@
-"""A teacher's shares: empty places at every scale, and products beyond fp32's range."""
+"""A teacher's shares: empty places at every scale, products beyond fp32's range, and the precision of small shares."""
 
 import math
 
 import pytest
 import torch
 
+from paper_2008_00325_amd import umap_rows as R
+from rows_reference import E32
 from test_gpu_rows import DEV, F32, FLOATS
 from test_gpu_rows_head import F64, Case, near
 
@@ -69,3 +71,24 @@ def test_products_beyond_the_range(scale):
     assert torch.equal(lse, want[1])
     for got, ref in ((dh, want[2]), (dw, want[3])):
         near(got, ref.to(F64), 1e-5 + 0 * ref.to(F64), "gradient")
+
+
+def test_small_shares_are_as_exact_as_fp32():
+    """A table of unit vectors and rows whose probability of the teacher's tokens is 0 (a logit of -200): dh is -q.  A share is off
+    by 2 E32 of its exponential, 2 of the others' and 6 of their sum in a tree of 64, 1 of the quotient, and 2 where D and dh
+    are formed: 13 E32.  (Its argument is exact: the largest logit is 0 and the scale 1.)"""
+    k, cols = 16, 64
+    table = torch.eye(cols, device=DEV)
+    h = torch.full((50, cols), -200.0, device=DEV)
+    h[:, 63] = 0.0
+    ids = torch.arange(k, device=DEV).expand(50, k).contiguous()
+    logits = -40 - 45 * torch.rand(50, k, device=DEV)
+    logits[:, 0] = 0.0
+    loss, lse = torch.empty(50, device=DEV), torch.empty(50, device=DEV)
+    sizes = (50, cols, cols, k, F32)
+    work = torch.empty(max(R.umap_rows_distill_workspace(*sizes), R.umap_rows_distill_grad_workspace(*sizes)), dtype=torch.uint8, device=DEV)
+    dh = torch.empty_like(h)
+    R.umap_rows_distill(h, table, ids, logits, loss, lse, work)
+    R.umap_rows_distill_grad(h, table, ids, logits, lse, work, dh=dh)
+    q = torch.softmax(logits.to(F64), 1)
+    near(dh[:, :k], -q, 13 * E32 * q, "q")
