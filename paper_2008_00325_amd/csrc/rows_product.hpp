@@ -162,7 +162,7 @@ struct DirectSide {
         // alike in all lanes, which a build without optimization has to be told.
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)__builtin_amdgcn_readfirstlane(x.lds + q * THREADS * 16)),
                      "v"(x.at + q * x.step), "s"(Words{(uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.x), (uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.y), (uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.z), (uint32_t)__builtin_amdgcn_readfirstlane(x.buffer.w)})
-                     : "memory");
+                     : "m0", "memory");
     }
 };
 
