@@ -27,6 +27,8 @@
 // dh 0.83 and dW 0.86 ms of each of 8 pieces); one row against 32,000 x 2,048: 21 us of the tiles (6.2 TB/s) and 5 of
 // the row.  Fewer columns leave a tile less to multiply before its end: 2,048 rows against 32,000 reach 1,350 TFLOP/s at 4,096
 // columns, 910 at 512.
+#include <math.h>
+
 #include <algorithm>
 
 #include "launch_sizes.hpp"
@@ -410,7 +412,13 @@ struct RowWeights {
     float *number;
     int *exponent;   // kNoRow: the row takes no part
     const int *largest;   // null, and the numbers 1, the exponents 0: all rows have the weight `all`
-    float all;            // times it, what the products give
+    float all;            // times it and 2^power, what the products give
+    int power;
+};
+// x times 2^power, x in [1/2, 1) or 0.
+struct Factor {
+    float x;
+    int power;
 };
 __device__ __forceinline__ int largest_of(const RowWeights &x) { return x.largest ? *x.largest : 0; }
 
@@ -482,7 +490,7 @@ struct RowRests {
 // past the last), zeros in rows without part, and once for each part of D.
 template <int T, int WAVES>
 __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSide w, ProductSide h, float scale, Taught taught, const float *lse,
-                                                   const float *dloss, float factor, RowWeights weights, int *token,
+                                                   const float *dloss, Factor factor, RowWeights weights, int *token,
                                                    float *value, RowRests rests, Elem<T> *copy, int pitch, int parts)
 {
     __shared__ typename RowTeam<WAVES>::Lds lds;
@@ -491,12 +499,16 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
     if (t >= h.rows) return;
     const Elem<T> *const row = static_cast<const Elem<T> *>(h.data) + t * h.stride;
     const OwnToken<WAVES> own(team, taught, t, w.rows);
-    const float g = dloss ? dloss[t] * factor : factor;
     float number = 1.0f;
     int exponent = 0;
-    if (dloss) split_weight(g, number, exponent);
+    if (dloss) {   // both factors in parts, since their product may be in fp32's range where one of them is not
+        int more;
+        split_weight(dloss[t], number, exponent);
+        split_weight(number * factor.x, number, more);
+        exponent += more + factor.power;
+    }
+    const bool part = own.any && number != 0.0f && factor.x != 0.0f;
     number = ldexpf(number, kShift<T>);
-    const bool part = own.any && g != 0.0f;
     float z = 0.0f;
     if constexpr (T != UMAP_F32) z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
     int id = part ? own.id : -1;
@@ -729,7 +741,7 @@ __global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int par
         }
         float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = e == kNoRow ? 0.0f : ldexpf(sum[j], e - kShift<T>) * weights.all;
+        for (int j = 0; j < 4; ++j) v[j] = e == kNoRow ? 0.0f : ldexpf(sum[j] * weights.all, e - kShift<T> + weights.power);
         Elem<T> *const to = static_cast<Elem<T> *>(dh.data) + t * dh.stride + c;
         if (c + 4 <= dh.cols) {
             store_raw<T, 4>(to, raw_of<T, 4>(v));
@@ -758,7 +770,7 @@ __device__ __forceinline__ void table_tile(const TableRows &x, int block, Piece 
     const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
     P::run(h, d, m0, n0, 0, h.rows, lds, acc);
-    const int e = h.rows > 0 ? largest_of(weights) - kShift<T> : 0;
+    const int e = h.rows > 0 ? largest_of(weights) - kShift<T> + weights.power : 0;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int64_t v = n0 + P::n_of(j);
@@ -766,7 +778,7 @@ __device__ __forceinline__ void table_tile(const TableRows &x, int block, Piece 
         Elem<T> *const to = static_cast<Elem<T> *>(dw.data) + v * dw.stride + m0;
         auto four = [&](int i, int64_t c, float (&g)[4]) {   // columns c .. c + 3 of acc[i][j]
 #pragma unroll
-            for (int r = 0; r < 4; ++r) g[r] = ldexpf(acc[i][j][r], e) * weights.all;
+            for (int r = 0; r < 4; ++r) g[r] = ldexpf(acc[i][j][r] * weights.all, e);
             if (!add) return;
             float old[4] = {};
             if (c + 4 <= dw.cols) {
@@ -1056,9 +1068,12 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
     auto *const value = reinterpret_cast<float *>(base + z.value), *const sums = reinterpret_cast<float *>(base + z.sums);
     auto *const copy = reinterpret_cast<Elem<T> *>(base + z.copy), *const d = reinterpret_cast<Elem<T> *>(base + z.d);
     auto *const scaled = dloss ? reinterpret_cast<Elem<T> *>(base + z.scaled) : nullptr;
-    const float factor = dscale * scale;
+    // a product that fp32 may not hold; of two fp32 numbers, so a double does
+    Factor factor;
+    factor.x = (float)frexp((double)dscale * scale, &factor.power);
     int *const largest = dloss ? reinterpret_cast<int *>(base + z.largest) : nullptr;
-    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, dloss ? 1.0f : factor};
+    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, dloss ? 1.0f : factor.x,
+                             dloss ? 0 : factor.power};
     const bool fixing = dh && z.parts == 1 && sizeof(Elem<T>) == 2;
     const RowRests rests{fixing ? reinterpret_cast<int *>(base + z.rest_token) : nullptr, reinterpret_cast<float *>(base + z.rest)};
     if (z.n > 0) {
