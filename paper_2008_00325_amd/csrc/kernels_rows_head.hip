@@ -6,12 +6,14 @@
 //   D_tv = g_t (exp(z_tv - lse_t) - q_tv),  dh = D W,  dW = D^T h,  g_t = dscale scale dloss_t
 //
 // The logits are never kept.  Forward: a tile of them (rows of the table times rows of h) leaves a maximum and a sum of
-// exponentials for each row of h, which a second launch joins; that launch also forms the logits of the rows' own
+// exponentials for each row of h, and its one token's logit; a second launch joins the tiles, and forms the logits of rows of more
 // tokens, as dot products.  Gradient: for a piece of the table at a time (D of 256 MB, what the last cache holds) the logits
 // are formed anew and D is written in the inputs' type, its entries at the rows' own tokens from those tokens' unrounded p
-// and q, which may nearly cancel; then come the two products.  In fp32 that p is the tile's own: lse comes of the same sums, and
-// what rounding did to them cancels.  With p from a dot product of its own, dh and dW of 77 rows against 2,000 x 64 were off
-// by 8.1e-7 and 9.3e-7 of their norms (medians of 39 inputs), so by 3.2e-7 and 3.1e-7.
+// and q, which may nearly cancel; then come the two products.  That p is the tile's own or, in 16 bits with more tokens than
+// one, comes of the same instructions in the same order: lse comes of the same sums, and what rounding did to them cancels.  With
+// p from a dot product in another order, rows whose partial sums reach 2,000 had entries off by 2e-4 to 5e-4 where p = q, 600 to
+// 700 times what lse's own rounding makes (now less than once); dh and dW of 77 rows against 2,000 x 64 in fp32 were off by 8.1e-7
+// and 9.3e-7 of their norms, so, with the lse of the forward call, by 3.2e-7 and 3.1e-7 (medians of 39 inputs).
 //
 // Precision of D in 16 bits: an entry is off by up to half a unit in its last place, and sums of many entries average that
 // out: dW is off by 1.2 (median) to 1.45 times what its own type's rounding alone costs (60 cases of 257 to 700 rows).  Where it
@@ -25,7 +27,7 @@
 // Bound by the matrix cores for many rows, by the table's bytes for few.  bf16: 8,192 rows against 128,000 x 4,096: loss 6.1 ms
 // (1,400 TFLOP/s; the library's product of the same size 5.8 ms, without the exponentials), gradient 20.0 ms (1,290: D 0.84,
 // dh 0.83 and dW 0.86 ms of each of 8 pieces); one row against 32,000 x 2,048: 21 us of the tiles (6.2 TB/s) and 5 of
-// the row.  Fewer columns leave a tile less to multiply before its end: 2,048 rows against 32,000 reach 1,350 TFLOP/s at 4,096
+// their join.  Fewer columns leave a tile less to multiply before its end: 2,048 rows against 32,000 reach 1,350 TFLOP/s at 4,096
 // columns, 910 at 512.
 #include <math.h>
 
@@ -39,8 +41,6 @@ namespace ul {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// exp(x): hardware's 2^x, off by a unit in the last place and |x| 2^-24; 0 below 2^-126
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ __forceinline__ float minus_inf() { return -__builtin_inff(); }
 
 // What the tiles' exponentials are of, and to what base: 16-bit types' logits are in units of log 2, so that a product
@@ -83,9 +83,31 @@ __device__ __forceinline__ float wave_sum(float v)
 
 // ---- the logits' tiles: forward -------------------------------------------------------------
 
+// A row's one token in a tile: f(i, r) for the place of acc[i][j] that is `own` rows of A from the tile's first.  Few waves have one
+// among theirs, and the others see it at once.
+template <class P, typename F>
+__device__ __forceinline__ void own_place(int64_t own, F f)
+{
+    const int first = P::m_first(0);
+    if (!__any(own >= first && own < first + 16 * P::kFM)) return;
+#pragma unroll
+    for (int i = 0; i < P::kFM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (P::m_of(i) + r == own) f(i, r);
+}
+
+// Rows of one token each: its logit, as it is among the exponentials, in their units.
+struct OwnLogits {
+    RowIds ids;
+    int64_t first;   // row of h's first
+    int64_t vocab, piece;   // rows of the table, and which of them w's first is
+    float *z;        // null: rows of more tokens
+};
+
 template <int T, class P>
 __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, ProductSide h, float scale, Tiles tiles, int64_t first_tile,
-                                                          int64_t all_tiles, MaxSum *partial)
+                                                          int64_t all_tiles, MaxSum *partial, OwnLogits one)
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
@@ -107,6 +129,10 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
     }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
+        if (one.z) {
+            const int64_t t = n0 + P::n_of(j), id = t < h.rows ? row_of(one.ids, one.first + t, one.vocab) : -1;
+            own_place<P>(id - one.piece - m0, [&](int i, int r) { one.z[t] = acc[i][j][r] * logit.unit; });
+        }
         float most = minus_inf();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -267,7 +293,7 @@ __device__ __forceinline__ void fetch8(const Elem<T> *row, int c, int cols, floa
     }
 }
 
-// Dot products of a row of h with the table's rows of its k tokens: each thread's token's (the one token's, for all).
+// Logits of a row's k tokens, as dot products with the table's rows: each thread's token's.
 template <int T, int WAVES>
 __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Elem<T> *h, const ProductSide &w,
                                            const OwnToken<WAVES> &own, int k, float scale)
@@ -275,17 +301,6 @@ __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Ele
     constexpr int kAtOnce = 4;
     const int cols = (int)w.cols, lane = team.me & 63;
     float z = 0.0f;
-    if (k == 1 && own.alone) {
-        const Elem<T> *const row = static_cast<const Elem<T> *>(w.data) + (int64_t)max(own.id, 0) * w.stride;
-        for (int c = team.me * 8; own.id >= 0 && c < cols; c += 8 * RowTeam<WAVES>::kThreads) {
-            float a[8], b[8];
-            fetch8<T>(h, c, cols, a);
-            fetch8<T>(row, c, cols, b);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z = fmaf(a[j], b[j], z);
-        }
-        return team.sum(z) * scale;
-    }
     // a wave to a token, whose number and row all its lanes know
     for (int e0 = kAtOnce * team.wave; cols > 256 && e0 < k; e0 += kAtOnce * WAVES) {
         const Elem<T> *row[kAtOnce];
@@ -361,6 +376,72 @@ __device__ __forceinline__ float own_logit(const RowTeam<WAVES> &team, const Ele
     return z;
 }
 
+template <int T>
+__device__ __forceinline__ Piece piece_at(const Elem<T> *p)
+{
+    return __builtin_bit_cast(Piece, load_raw<T, 16 / (int)sizeof(Elem<T>)>(p));
+}
+
+// The same in 16 bits, without the scale, by the tiles' instructions in the tiles' order, 16 tokens by a wave: they round as the
+// tiles' do.  (fp32's instruction takes 16 times the cycles of the products that are wanted: a loss of 1,000 rows with 33 tokens
+// each against 3,000 x 3,000 would take 230 us instead of 187.)
+template <int T, int WAVES>
+__device__ __forceinline__ float own_dot(const RowTeam<WAVES> &team, const Elem<T> *h, const ProductSide &w, const OwnToken<WAVES> &own, int k)
+{
+    constexpr int kPer = 8, kHalf = 4 * kPer;   // columns of a piece, and of a half step
+    const int cols = (int)w.cols, lane = team.me & 63, g = lane >> 4;
+    const Elem<T> *const mine = h + g * kPer;
+    float z = 0.0f;
+    for (int e0 = 16 * team.wave; e0 < k; e0 += 16 * WAVES) {
+        const int e = e0 + (lane & 15), id = WAVES == 1 ? __shfl(own.id, min(e, 63)) : team.lds->id[min(e, kMostTokens - 1)];
+        const Elem<T> *const row = static_cast<const Elem<T> *>(w.data) + (int64_t)(e < k ? max(id, 0) : 0) * w.stride + g * kPer;
+        Acc4 dot = {0.0f, 0.0f, 0.0f, 0.0f};
+        int c = 0;
+        auto pieces = [&](auto count) {
+            constexpr int N = decltype(count)::value;
+            for (; c + N * kHalf <= cols; c += N * kHalf) {
+                Piece a[N], b[N] = {};
+#pragma unroll
+                for (int q = 0; q < N; ++q) a[q] = piece_at<T>(row + c + q * kHalf);
+                if ((lane & 15) == 0) {   // of the product's 16 columns one is looked at
+#pragma unroll
+                    for (int q = 0; q < N; ++q) b[q] = piece_at<T>(mine + c + q * kHalf);
+                }
+#pragma unroll
+                for (int q = 0; q < N; ++q) dot = multiply<T>(a[q], b[q], dot);
+            }
+        };
+        pieces(std::integral_constant<int, 4>{});
+        pieces(std::integral_constant<int, 1>{});
+        if (c < cols) {   // past the last column: zeros
+            float a[kPer], b[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const bool there = c + g * kPer + j < cols;
+                a[j] = there ? elem_float<T>(row[c + j]) : 0.0f;
+                b[j] = there ? elem_float<T>(mine[c + j]) : 0.0f;
+            }
+            dot = multiply<T>(__builtin_bit_cast(Piece, raw_of<T, kPer>(a)), __builtin_bit_cast(Piece, raw_of<T, kPer>(b)), dot);
+        }
+        // lanes 16 g have tokens e0 + 4 g .. + 3
+        if constexpr (WAVES == 1) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float other = __shfl(dot[r], (lane & 12) * 4);
+                z = lane >> 4 == e0 >> 4 && (lane & 3) == r ? other : z;
+            }
+        } else if ((lane & 15) == 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) team.lds->z[e0 + 4 * g + r] = dot[r];
+        }
+    }
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        z = team.me < k ? team.lds->z[team.me] : 0.0f;
+    }
+    return z;
+}
+
 // A copy of rows for the products, in whole pieces of 16 bytes: `pitch` columns, zeros past the last.
 template <int T>
 __global__ __launch_bounds__(256) void k_head_pack(ProductSide from, Elem<T> *to, int pitch)
@@ -378,7 +459,7 @@ __global__ __launch_bounds__(256) void k_head_pack(ProductSide from, Elem<T> *to
 // Joins a row's tiles, and sums its loss.
 template <int T, int WAVES>
 __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_loss(ProductSide w, ProductSide h, float scale, Taught taught, int64_t first,
-                                                   int64_t tiles, const MaxSum *partial, float *loss, float *lse)
+                                                   int64_t tiles, const MaxSum *partial, const float *one, float *loss, float *lse)
 {
     __shared__ typename RowTeam<WAVES>::Lds lds;
     const RowTeam<WAVES> team(&lds);
@@ -387,7 +468,9 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_loss(ProductSid
     MaxSum mine{minus_inf(), 0.0f};
     for (int64_t i = team.me; i < tiles; i += RowTeam<WAVES>::kThreads) mine.template join<T>(partial[t * tiles + i]);
     const OwnToken<WAVES> own(team, taught, first + t, w.rows);
-    const float z = own_logit<T, WAVES>(team, static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, scale);
+    float z;
+    if (one) z = Logit<T>::natural(one[t]);
+    else z = own_logit<T, WAVES>(team, static_cast<const Elem<T> *>(h.data) + t * h.stride, w, own, taught.k, scale);
     const float most = team.max(mine.m);
     const float sum = Logit<T>::natural(most + Logit<T>::log(team.sum(mine.s * Logit<T>::exp(mine.m - MaxSum::base(most)))));
     const float share = all_shares(team, own, taught.k);   // > 0, or NaN, where there is one
@@ -509,25 +592,28 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_rows(ProductSid
     }
     const bool part = own.any && number != 0.0f && factor.x != 0.0f;
     number = ldexpf(number, kShift<T>);
-    float z = 0.0f;
-    if constexpr (T != UMAP_F32) z = own_logit<T, WAVES>(team, row, w, own, part ? taught.k : 0, scale);
+    const bool in_tile = T == UMAP_F32 || taught.k == 1;   // p is then taken from the tile, value from number p
+    float p = 0.0f;
+    if constexpr (T != UMAP_F32) {
+        if (!in_tile) p = Logit<T>(scale).exp_less(own_dot<T, WAVES>(team, row, w, own, part ? taught.k : 0), Logit<T>::of_natural(lse[t]));
+    }
     int id = part ? own.id : -1;
     const float share = all_shares(team, own, taught.k);
     if (share < 0.0f) id = -1;
     if (team.me >= taught.k) id = -1;
-    float entry = 0.0f;   // fp32: what is taken from number p, which the tile knows
-    if (id >= 0) entry = number * (T == UMAP_F32 ? share : exp_of(z - lse[t]) - share);
+    float entry = 0.0f;
+    if (id >= 0) entry = number * (in_tile ? share : p - share);
     if (team.me < taught.k) {
         token[t * taught.k + team.me] = id;
         value[t * taught.k + team.me] = entry;
     }
-    if (rests.token) {
-        int place = 0;   // of the largest entry (to 2^-15): its magnitude and its place as one number
-        if (!own.alone) {
-            const uint32_t key = (__float_as_uint(fabsf(entry)) & ~255u) | (255u - team.me);
-            const float most = team.max(id >= 0 ? __uint_as_float(key) : -1.0f);
-            place = most < 0.0f ? kMostTokens : 255 - (int)(__float_as_uint(most) & 255u);
-        }
+    if (rests.token && in_tile) {
+        if (team.me == 0) rests.token[t] = id;   // the rest is the tile's too
+    } else if (rests.token) {
+        // of the largest entry (to 2^-15): its magnitude and its place as one number
+        const uint32_t key = (__float_as_uint(fabsf(entry)) & ~255u) | (255u - team.me);
+        const float most = team.max(id >= 0 ? __uint_as_float(key) : -1.0f);
+        const int place = most < 0.0f ? kMostTokens : 255 - (int)(__float_as_uint(most) & 255u);
         if (team.me == place) rests.rest[t] = entry - elem_float<T>(float_elem<T>(entry));
         if (team.me == (place < kMostTokens ? place : 0)) rests.token[t] = place < kMostTokens ? id : -1;
     }
@@ -576,11 +662,11 @@ __device__ __forceinline__ int pair_row()
 }
 
 // D of a piece of the table: d[t][v], `pitch` columns, zeros past the piece's rows.  token and value: null, or each
-// row's one token and its entry (fp32: what number p is less of there).
+// row's one token and what number p is less of there; rest: null, or receives what rounding takes from that entry.
 template <int T, class P>
 __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSide h, float scale, Tiles tiles, const float *lse,
-                                                        RowWeights weights, const int *token, const float *value, int64_t first,
-                                                        Elem<T> *d, int64_t pitch, int64_t below)
+                                                        RowWeights weights, const int *token, const float *value, float *rest,
+                                                        int64_t first, Elem<T> *d, int64_t pitch, int64_t below)
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
@@ -595,9 +681,9 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
         const int64_t t = n0 + P::n_of(j);
         if (t >= h.rows) continue;
         const float number = weights.number[t], less = Logit<T>::of_natural(lse[t]);
-        [[maybe_unused]] int64_t own = -1;
-        [[maybe_unused]] float taken = 0.0f;
-        if (T == UMAP_F32 && token && token[t] >= 0) {
+        int64_t own = -1;
+        float taken = 0.0f;
+        if (token && token[t] >= 0) {
             own = token[t] - first - m0;
             taken = value[t];
         }
@@ -617,6 +703,12 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[i][r] = number != 0.0f && P::m_of(i) + r < live ? v[i][r] : 0.0f;
         }
+        if constexpr (T != UMAP_F32) {
+            own_place<P>(own, [&](int i, int r) {
+                v[i][r] -= taken;
+                if (rest) rest[t] = v[i][r] - elem_float<T>(float_elem<T>(v[i][r]));
+            });
+        }
         auto store = [&](Elem<T> *at, auto round) {
             if constexpr (sizeof(Elem<T>) == 2 && FM % 2 == 0) {
 #pragma unroll
@@ -634,21 +726,6 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
         } else {
             store(to, [](float(&x)[4]) { return rounded<T, 4>(x); });
             store(to + below, [](float(&x)[4]) { return raw_of<T, 4>(x); });
-        }
-    }
-    if (T == UMAP_F32 || !token) return;
-    // the entries of the rows' own tokens, over those just stored: by other lanes, so behind their stores
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    for (int n = threadIdx.x; n < P::N; n += P::kThreads) {
-        const int64_t t = n0 + n;
-        if (t >= h.rows || token[t] < 0) continue;
-        const int64_t own = token[t] - first - m0;
-        if (own < 0 || own >= live) continue;
-        float v[1] = {value[t]};
-        for (int64_t part = 0;; part = below) {
-            store_raw<T, 1>(d + t * pitch + m0 + own + part, rounded<T, 1>(v));
-            if (part == below) break;
         }
     }
 }
@@ -875,7 +952,7 @@ int64_t pack_rows(int64_t pitch, int64_t elem) { return std::max<int64_t>(256, k
 // Forward: rows of h at a time, so that the partial sums stay within 128 MB (a quarter of that with the large tiles).
 struct LossSizes {
     int64_t tiles, rows, pitch, piece;
-    int64_t partial, copy, table, total;   // offsets into the workspace
+    int64_t partial, own, copy, table, total;   // offsets into the workspace
     LossSizes(int64_t n, int64_t vocab, int32_t cols, int32_t type)
     {
         const int64_t elem = elem_size(type);
@@ -885,7 +962,8 @@ struct LossSizes {
         pitch = up(cols, 64);
         piece = std::min(pack_rows(pitch, elem), up(vocab, 256));
         partial = 0;
-        copy = up(rows * tiles * (int64_t)sizeof(MaxSum), 256);
+        own = up(rows * tiles * (int64_t)sizeof(MaxSum), 256);
+        copy = own + up(rows * 4, 256);
         table = copy + up(rows * pitch * elem, 256);
         total = table + piece * pitch * elem;
     }
@@ -1016,6 +1094,7 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
     const LossSizes z(h.rows, table.rows, h.cols, h.type);
     char *const base = static_cast<char *>(workspace);
     auto *const partial = reinterpret_cast<MaxSum *>(base + z.partial);
+    float *const own = taught.k == 1 ? reinterpret_cast<float *>(base + z.own) : nullptr;
     const ProductSide all = side_of<T>(table, 0, table.rows);
     const bool packing = !direct_side<T>(all);
     const int64_t piece = packing ? z.piece : table.rows;
@@ -1041,14 +1120,14 @@ hipError_t loss(const umap_rows &h, const umap_rows &table, const Taught &taught
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(w.rows, rows.rows);
                 hipLaunchKernelGGL((k_head_lse<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
-                                   v / P::M, tiles, partial);
+                                   v / P::M, tiles, partial, OwnLogits{taught.ids, first, table.rows, v, own});
                 return hipGetLastError();
             }));
         }
         UL_LAUNCHED(by_team(rows.rows, taught.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
             hipLaunchKernelGGL((k_head_loss<T, W>), dim3((unsigned)over(rows.rows, RowTeam<W>::kRows)), dim3(RowTeam<W>::kBlock), 0, s, all, given, scale,
-                               taught, first, tiles, partial, out, lse);
+                               taught, first, tiles, partial, own, out, lse);
             return hipGetLastError();
         }));
     }
@@ -1111,7 +1190,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(z.d_pitch, z.n);
                 hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
-                                   lse, weights, one ? token : nullptr, one ? value : nullptr, first, d, z.d_pitch, below);
+                                   lse, weights, one ? token : nullptr, one ? value : nullptr, one && fixing ? rests.rest : nullptr, first, d, z.d_pitch, below);
                 return hipGetLastError();
             })));
             if (!one) {
