@@ -11,9 +11,9 @@
 // are formed anew and D is written in the inputs' type, its entries at the rows' own tokens from those tokens' unrounded p
 // and q, which may nearly cancel; then come the two products.  That p is the tile's own or, in 16 bits with more tokens than
 // one, comes of the same instructions in the same order: lse comes of the same sums, and what rounding did to them cancels.  With
-// p from a dot product in another order, rows whose partial sums reach 2,000 had entries off by 2e-4 to 5e-4 where p = q, 600 to
-// 700 times what lse's own rounding makes (now less than once); dh and dW of 77 rows against 2,000 x 64 in fp32 were off by 8.1e-7
-// and 9.3e-7 of their norms, so, with the lse of the forward call, by 3.2e-7 and 3.1e-7 (medians of 39 inputs).
+// p from a dot product in another order, 16-bit entries of 300 rows with partial sums up to 2,300, where p = q, were off by 1.7e-4 to
+// 3.7e-4 (medians), so not at all; dh and dW of 77 rows against 2,000 x 64 in fp32 by 8.1e-7 and 9.3e-7 of their norms, so, with the
+// lse of the forward call, by 3.2e-7 and 3.1e-7 (medians of 39 inputs).
 //
 // Precision of D in 16 bits: an entry is off by up to half a unit in its last place, and sums of many entries average that
 // out: dW is off by 1.2 (median) to 1.45 times what its own type's rounding alone costs (60 cases of 257 to 700 rows).  Where it
