@@ -269,6 +269,9 @@ int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols,
  *   dloss      NULL (ones), or a weight for each row, fp32.  Rows of weight 0 and
  *              rows whose target lies outside the table take no part: their dh is
  *              zeros, and nothing of them reaches dtable (they may hold NaN).
+ *              Weights may lie far apart: in fp16 dtable takes rows within 2^6 of the
+ *              largest weight together, then those within 2^12, and so on down to
+ *              2^96, beyond which they do not reach it.
  *   dscale     finite (one over the rows for a mean, times a loss scale for fp16).
  *   dh         NULL, or receives the gradient of h: its type and shape.
  *   dtable     NULL, or receives the gradient of table: its type and shape.  Not

@@ -21,8 +21,13 @@
 // token, gets back what that token's entry lost.  Where all g_t are alike they are left to the very end: D is then p - q, whose
 // largest entries, those of the rows' tokens, lie just below 1 and so are rounded least.  Else g_t is a number in [1/2, 1) times
 // 2^e_t.  D holds the number; dh gets 2^e_t on the way out, exactly, and dW takes h_t times 2^(e_t - E), E the largest of the rows
-// that take part, instead: also exact.  In fp16, whose smallest values would swallow the probabilities of rare tokens, D is 2^14
-// times as large.
+// that take part, instead: exact too, down to the smallest exponent of fp32 and bf16.  fp16, which has few exponents, leaves h_t
+// as it is: D, 2^15 times as large so that the probabilities of rare tokens are not among its smallest values, holds the number
+// times 2^-((E - e_t) mod 6), and the rows of D and of h's copy are put in order of (E - e_t) / 6, their bands, whose sums dW takes one
+// after the other from the smallest weights on, times 2^-6 from band to band.  (With h_t times 2^(e_t - E) in fp16, dW of tokens
+// that only rows with 2^-20 of the largest weight know was off by 1.7e-2 of its norm, so by 2.8e-4, of which 2.2e-4 is its own
+// rounding.)  Weights within 2^6 are one band, in their order, and cost nothing; weights over 2^40, seven bands, took 1,358 -> 1,507 us
+// for 2,048 rows against 32,000 x 4,096, 49 -> 65 for 300 against 10,007 x 300.
 //
 // Bound by the matrix cores for many rows, by the table's bytes for few.  bf16: 8,192 rows against 128,000 x 4,096: loss 6.1 ms
 // (1,400 TFLOP/s; the library's product of the same size 5.8 ms, without the exponentials), gradient 20.0 ms (1,290: D 0.84,
@@ -488,7 +493,7 @@ __global__ __launch_bounds__(RowTeam<WAVES>::kBlock) void k_head_loss(ProductSid
 
 constexpr int kNoRow = INT32_MIN;
 template <int T>
-constexpr int kShift = T == UMAP_F16 ? 14 : 0;
+constexpr int kShift = T == UMAP_F16 ? 15 : 0;
 
 // What the gradient's launches share of a row: its number in [1/2, 1), with kShift, and its exponent.
 struct RowWeights {
@@ -505,6 +510,27 @@ struct Factor {
 };
 __device__ __forceinline__ int largest_of(const RowWeights &x) { return x.largest ? *x.largest : 0; }
 
+// fp16's rows of different weights: where a row lies in D and in h's copy, what its entries are times, and where the bands
+// begin (and the last ends), and the last one that has rows.  Null: each in its own place, times 1, one band.
+struct RowPlaces {
+    const int *slot;
+    const float *shrink;
+    const int *start;   // kBands + 2
+};
+constexpr int kBandBits = 6, kBands = 16;
+// Of a row's exponent.  Rows beyond the last band, 2^-96 of the largest weight, are not seen by dW.
+struct Band {
+    int band, less;
+    bool lost;
+    __device__ __forceinline__ Band(int exponent, int largest)
+    {
+        const int off = exponent == kNoRow ? 0 : largest - exponent;
+        lost = off >= kBandBits * kBands;
+        band = lost ? kBands - 1 : off / kBandBits;
+        less = lost ? 0 : off % kBandBits;
+    }
+};
+
 __device__ __forceinline__ void split_weight(float g, float &number, int &exponent)
 {
     exponent = 0;
@@ -515,19 +541,34 @@ __device__ __forceinline__ void split_weight(float g, float &number, int &expone
     }
 }
 
-// The largest exponent of the rows that take part, or 0; one workgroup.
-__global__ __launch_bounds__(1024) void k_head_largest(const int *exponent, int64_t n, int *largest)
+// The largest and the smallest exponent of the rows that take part, found by one of WAVES waves' threads; 0 where there is none.
+struct Exponents {
+    int most, least;
+};
+template <int WAVES>
+__device__ __forceinline__ Exponents exponents_of(const int *exponent, int64_t n)
 {
-    __shared__ int part[16];
-    int most = kNoRow;
-    for (int64_t t = threadIdx.x; t < n; t += 1024) most = max(most, exponent[t]);
-    for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) most = max(most, part[i]);
-        *largest = most == kNoRow ? 0 : most;
+    __shared__ Exponents part[WAVES];
+    Exponents x{kNoRow, INT32_MAX};
+    for (int64_t t = threadIdx.x; t < n; t += 64 * WAVES) {
+        const int e = exponent[t];
+        x.most = max(x.most, e);
+        if (e != kNoRow) x.least = min(x.least, e);
     }
+    for (int o = 1; o < 64; o <<= 1) {
+        x.most = max(x.most, __shfl_xor(x.most, o));
+        x.least = min(x.least, __shfl_xor(x.least, o));
+    }
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) x = {max(x.most, part[i].most), min(x.least, part[i].least)};
+    return x.most == kNoRow ? Exponents{0, 0} : x;
+}
+__global__ __launch_bounds__(1024) void k_head_largest(const int *exponent, int64_t n, Exponents *found)
+{
+    const Exponents x = exponents_of<16>(exponent, n);
+    if (threadIdx.x == 0) *found = x;
 }
 
 // The rows' copies times 2^(e_t - E): `rows` of them, `parts` times one after the other.  With few rows every workgroup
@@ -535,21 +576,16 @@ __global__ __launch_bounds__(1024) void k_head_largest(const int *exponent, int6
 constexpr int64_t kFindRows = 8192;
 template <int T>
 __global__ __launch_bounds__(256) void k_head_scale(const Elem<T> *copy, int64_t rows, int parts, int pitch, const int *exponent,
-                                                    int *largest, Elem<T> *scaled)
+                                                    Exponents *found, Elem<T> *scaled)
 {
     const int64_t total = rows * (pitch / 8);
-    int most = kNoRow;
+    int most;
     if (rows <= kFindRows) {
-        __shared__ int part[4];
-        for (int t = threadIdx.x; t < (int)rows; t += 256) most = max(most, exponent[t]);
-        for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-        __syncthreads();
-        most = max(max(part[0], part[1]), max(part[2], part[3]));
-        most = most == kNoRow ? 0 : most;
-        if (blockIdx.x == 0 && threadIdx.x == 0) *largest = most;
+        const Exponents x = exponents_of<4>(exponent, rows);
+        most = x.most;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *found = x;
     } else {
-        most = *largest;
+        most = found->most;
     }
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t t = i / (pitch / 8);
@@ -559,6 +595,120 @@ __global__ __launch_bounds__(256) void k_head_scale(const Elem<T> *copy, int64_t
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], by);
         for (int p = 0; p < parts; ++p) store_raw<T, 8>(scaled + p * rows * pitch + i * 8, raw_of<T, 8>(v));
+    }
+}
+
+// fp16's order of many rows: their places by band, in a band by number, unless there is one band only.  Each thread takes a
+// stretch of the rows.
+__global__ __launch_bounds__(1024) void k_head_order(const int *exponent, int64_t n, Exponents *found, int *slot, float *shrink, int *start)
+{
+    static_assert(kBands == 16, "a wave to a band");
+    __shared__ int count[kBands][1024], base[kBands + 1];
+    const Exponents x = exponents_of<16>(exponent, n);
+    const int me = threadIdx.x, wave = me >> 6, lane = me & 63;
+    const int64_t each = (n + 1023) / 1024, first = me * each, last = min(first + each, n);
+    if (me == 0) *found = x;
+    if (x.most - x.least < kBandBits) {
+        if (me <= kBands + 1) start[me] = me == 0 || me > kBands ? 0 : (int)n;
+        return;
+    }
+    for (int b = 0; b < kBands; ++b) count[b][me] = 0;
+    for (int64_t t = first; t < last; ++t) ++count[Band(exponent[t], x.most).band][me];
+    __syncthreads();
+    int sum = 0;
+    for (int i = 0; i < 16; ++i) sum += count[wave][lane * 16 + i];
+    int before = sum;   // and those of the lanes below
+    for (int o = 1; o < 64; o <<= 1) {
+        const int other = __shfl_up(before, o);
+        if (lane >= o) before += other;
+    }
+    if (lane == 63) base[wave + 1] = before;
+    before -= sum;
+    for (int i = 0; i < 16; ++i) {
+        const int here = count[wave][lane * 16 + i];
+        count[wave][lane * 16 + i] = before;
+        before += here;
+    }
+    __syncthreads();
+    if (me == 0) {
+        int top = 0;
+        base[0] = 0;
+        for (int b = 1; b <= kBands; ++b) {
+            if (base[b]) top = b - 1;
+            base[b] += base[b - 1];
+        }
+        start[kBands + 1] = top;
+    }
+    __syncthreads();
+    if (me <= kBands) start[me] = base[me];
+    for (int64_t t = first; t < last; ++t) {
+        const Band band(exponent[t], x.most);
+        slot[t] = base[band.band] + count[band.band][me]++;
+        shrink[t] = ldexpf(1.0f, -band.less);
+    }
+}
+
+// fp16's copies of the rows, unscaled, in that order.  With few rows every workgroup finds the exponents and, where there is more
+// than one band, counts its rows' places among all; the first leaves the bands to the launches that follow.
+__global__ __launch_bounds__(256) void k_head_place(const Elem<UMAP_F16> *copy, int64_t rows, int parts, int pitch, const int *exponent,
+                                                    Exponents *found, Elem<UMAP_F16> *placed, int *slot, float *shrink, int *start)
+{
+    constexpr int T = UMAP_F16;
+    __shared__ int part[4], count[kBands];
+    const bool finds = rows <= kFindRows;
+    const int64_t per = pitch / 8, total = rows * per;
+    const Exponents x = finds ? exponents_of<4>(exponent, rows) : *found;
+    const bool many = x.most - x.least >= kBandBits, counts = finds && many;
+    if (finds && blockIdx.x == 0) {
+        if (threadIdx.x == 0) *found = x;
+        if (many) {
+            if (threadIdx.x < kBands) count[threadIdx.x] = 0;
+            __syncthreads();
+            for (int t = threadIdx.x; t < (int)rows; t += 256) atomicAdd(&count[Band(exponent[t], x.most).band], 1);
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                int before = 0, top = 0;
+                for (int b = 0; b < kBands; ++b) {
+                    start[b] = before;
+                    before += count[b];
+                    if (count[b]) top = b;
+                }
+                start[kBands] = before;
+                start[kBands + 1] = top;
+            }
+        } else if (threadIdx.x <= kBands + 1) {
+            start[threadIdx.x] = threadIdx.x == 0 || threadIdx.x > kBands ? 0 : (int)rows;
+        }
+    }
+    for (int64_t i0 = (int64_t)blockIdx.x * 256; i0 < total; i0 += (int64_t)gridDim.x * 256) {
+        const int64_t i = i0 + threadIdx.x, t = i / per;
+        const int c = (int)(i - t * per);
+        int64_t to = t;
+        if (!finds && many && i < total) to = slot[t];
+        if (counts) {
+            for (int row = (int)(i0 / per), last = (int)((min(i0 + 256, total) - 1) / per); row <= last; ++row) {
+                const int band = Band(exponent[row], x.most).band;
+                int before = 0;
+                for (int u = threadIdx.x; u < (int)rows; u += 256) {
+                    const int other = Band(exponent[u], x.most).band;
+                    before += other < band || (other == band && u < row);
+                }
+                for (int o = 1; o < 64; o <<= 1) before += __shfl_xor(before, o);
+                __syncthreads();
+                if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = before;
+                __syncthreads();
+                if (t == row) to = part[0] + part[1] + part[2] + part[3];
+            }
+        }
+        if (i >= total) continue;
+        const Band band(exponent[t], x.most);
+        if ((finds || !many) && c == 0) {
+            slot[t] = (int)to;
+            shrink[t] = ldexpf(1.0f, -band.less);
+        }
+        Raw<T, 8> v = {};
+        if (!band.lost) v = load_raw<T, 8>(copy + i * 8);
+        for (int p = 0; p < parts; ++p) store_raw<T, 8>(placed + (p * rows + to) * pitch + c * 8, v);
     }
 }
 
@@ -665,8 +815,8 @@ __device__ __forceinline__ int pair_row()
 // row's one token and what number p is less of there; rest: null, or receives what rounding takes from that entry.
 template <int T, class P>
 __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSide h, float scale, Tiles tiles, const float *lse,
-                                                        RowWeights weights, const int *token, const float *value, float *rest,
-                                                        int64_t first, Elem<T> *d, int64_t pitch, int64_t below)
+                                                        RowWeights weights, RowPlaces places, const int *token, const float *value,
+                                                        float *rest, int64_t first, Elem<T> *d, int64_t pitch, int64_t below)
 {
     __shared__ __align__(16) Piece lds[P::kLds / 16];
     constexpr int FM = P::kFM, FN = P::kFN;
@@ -680,14 +830,15 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
     for (int j = 0; j < FN; ++j) {
         const int64_t t = n0 + P::n_of(j);
         if (t >= h.rows) continue;
-        const float number = weights.number[t], less = Logit<T>::of_natural(lse[t]);
+        const float shrink = T == UMAP_F16 && places.slot ? places.shrink[t] : 1.0f;
+        const float number = weights.number[t] * shrink, less = Logit<T>::of_natural(lse[t]);
         int64_t own = -1;
         float taken = 0.0f;
         if (token && token[t] >= 0) {
             own = token[t] - first - m0;
-            taken = value[t];
+            taken = value[t] * shrink;
         }
-        Elem<T> *const to = d + t * pitch + m0;
+        Elem<T> *const to = d + (T == UMAP_F16 && places.slot ? places.slot[t] : t) * pitch + m0;
         float v[FM][4];
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -706,7 +857,7 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
         if constexpr (T != UMAP_F32) {
             own_place<P>(own, [&](int i, int r) {
                 v[i][r] -= taken;
-                if (rest) rest[t] = v[i][r] - elem_float<T>(float_elem<T>(v[i][r]));
+                if (rest) rest[t] = (v[i][r] - elem_float<T>(float_elem<T>(v[i][r]))) * (1.0f / shrink);
             });
         }
         auto store = [&](Elem<T> *at, auto round) {
@@ -733,18 +884,20 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
 // The entries of D at the rows' own tokens (fp32: value is taken from what is there).
 template <int T>
 __global__ __launch_bounds__(256) void k_head_own(const int *token, const float *value, int64_t count, int k, int64_t first,
-                                                  int64_t rows, Elem<T> *d, int64_t pitch, int64_t below)
+                                                  int64_t rows, RowPlaces places, Elem<T> *d, int64_t pitch, int64_t below)
 {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
         const int64_t v = token[i] - first;
         if (token[i] < 0 || v < 0 || v >= rows) continue;
-        Elem<T> *const at = d + i / k * pitch + v;
+        const int64_t t = i / k;
+        Elem<T> *const at = d + (T == UMAP_F16 && places.slot ? places.slot[t] : t) * pitch + v;
         if constexpr (T == UMAP_F32) {   // each place has one token's value
             *at -= value[i];
             continue;
         }
-        *at = float_elem<T>(value[i]);
-        if (below) at[below] = float_elem<T>(value[i] - elem_float<T>(*at));
+        const float entry = T == UMAP_F16 && places.slot ? value[i] * places.shrink[t] : value[i];
+        *at = float_elem<T>(entry);
+        if (below) at[below] = float_elem<T>(entry - elem_float<T>(*at));
     }
 }
 
@@ -785,8 +938,8 @@ __device__ __forceinline__ void rows_tile(const RowSums &x, int block, Piece *ld
 // dh from the sums' parts: four columns per thread, or per 16 threads where there are many parts, each of which adds
 // every 16th.
 template <int T, int SLICES>
-__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int parts, int64_t pitch, RowWeights weights, RowRests rests,
-                                                      ProductSide w, umap_rows dh)
+__global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int parts, int64_t pitch, RowWeights weights, RowPlaces places,
+                                                      RowRests rests, ProductSide w, umap_rows dh)
 {
     constexpr int kGroups = 256 / SLICES;
     __shared__ Acc4 part[SLICES > 1 ? SLICES : 1][kGroups];
@@ -796,8 +949,9 @@ __global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int par
         const int64_t i = i0 + in, t = i / groups, c = i % groups * 4;
         Acc4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         if (i < total) {
+            const int64_t at = T == UMAP_F16 && places.slot ? places.slot[t] : t;
 #pragma unroll 4
-            for (int s = slice; s < parts; s += SLICES) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + t) * pitch + c);
+            for (int s = slice; s < parts; s += SLICES) sum += *reinterpret_cast<const Acc4 *>(sums + (s * dh.rows + at) * pitch + c);
         }
         if constexpr (SLICES > 1) {
             __syncthreads();
@@ -808,6 +962,7 @@ __global__ __launch_bounds__(256) void k_head_dh_join(const float *sums, int par
             for (int s = 1; s < SLICES; ++s) sum += part[s][in];
         }
         if (i >= total) continue;
+        if (T == UMAP_F16 && places.slot) sum *= 1.0f / places.shrink[t];
         const int e = weights.exponent[t], own = rests.token ? rests.token[t] : -1;
         if (own >= 0) {
             const Elem<T> *const row = static_cast<const Elem<T> *>(w.data) + own * w.stride;
@@ -835,6 +990,8 @@ struct TableRows {
     ProductSide h, d;
     Tiles tiles;
     RowWeights weights;
+    RowPlaces places;
+    int parts;   // of D, one after the other
     bool add;
     umap_rows dw;
 };
@@ -842,11 +999,37 @@ template <int T, class P>
 __device__ __forceinline__ void table_tile(const TableRows &x, int block, Piece *lds)
 {
     constexpr int FM = P::kFM, FN = P::kFN;
-    const auto &[h, d, tiles, weights, add, dw] = x;
-    const TileAt at = tile_at(tiles, block);
+    const ProductSide &h = x.h, &d = x.d;
+    const RowWeights &weights = x.weights;
+    const umap_rows &dw = x.dw;
+    const bool add = x.add;
+    const TileAt at = tile_at(x.tiles, block);
     const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
-    P::run(h, d, m0, n0, 0, h.rows, lds, acc);
+    if constexpr (T != UMAP_F16) {
+        P::run(h, d, m0, n0, 0, h.rows, lds, acc);
+    } else {   // the bands, from the smallest weights on
+        const int *const start = x.places.start;
+        const int64_t each = start ? h.rows / x.parts : h.rows;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
+        const int top = start ? __builtin_amdgcn_readfirstlane(start[kBands + 1]) : 0;
+        for (int b = top; b >= 0; --b) {
+            const int64_t k0 = start ? __builtin_amdgcn_readfirstlane(start[b]) : 0, k1 = start ? __builtin_amdgcn_readfirstlane(start[b + 1]) : each;
+            if (b < top) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] *= 1.0f / (1 << kBandBits);
+            }
+            for (int64_t of = 0; k0 < k1 && of < h.rows; of += each) {   // a part of D
+                const ProductSide some{h.data, h.stride, of + k1, h.cols}, entries{d.data, d.stride, of + k1, d.cols};
+                P::template run<true>(some, entries, m0, n0, of + k0, of + k1, lds, acc);
+            }
+        }
+    }
     const int e = h.rows > 0 ? largest_of(weights) - kShift<T> + weights.power : 0;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
@@ -982,7 +1165,7 @@ struct GradSizes {
     bool dh_few;
     int64_t piece, d_pitch, h_pitch, sum_pitch, splits, depth;
     // offsets into the workspace
-    int64_t largest, number, exponent, token, value, rest_token, rest, copy, scaled, d, sums, packed, total;
+    int64_t largest, start, number, exponent, slot, shrink, token, value, rest_token, rest, copy, scaled, d, sums, packed, total;
     GradSizes(int64_t n_, int64_t vocab_, int32_t cols_, int64_t k_, int32_t type, bool pack)
         : n(n_), vocab(vocab_), cols(cols_), k(k_), elem(elem_size(type))
     {
@@ -1011,9 +1194,12 @@ struct GradSizes {
             at += up(bytes, 256);
             return was;
         };
-        largest = take(16);
+        largest = take(sizeof(Exponents));
+        start = take((kBands + 2) * 4);
         number = take(n * 4);
         exponent = take(n * 4);
+        slot = take(n * 4);
+        shrink = take(n * 4);
         token = take(n * k * 4);
         value = take(n * k * 4);
         rest_token = take(n * 4);
@@ -1150,11 +1336,12 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
     // a product that fp32 may not hold; of two fp32 numbers, so a double does
     Factor factor;
     factor.x = (float)frexp((double)dscale * scale, &factor.power);
-    int *const largest = dloss ? reinterpret_cast<int *>(base + z.largest) : nullptr;
-    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), largest, dloss ? 1.0f : factor.x,
+    auto *const found = reinterpret_cast<Exponents *>(base + z.largest);
+    const RowWeights weights{reinterpret_cast<float *>(base + z.number), reinterpret_cast<int *>(base + z.exponent), dloss ? &found->most : nullptr, dloss ? 1.0f : factor.x,
                              dloss ? 0 : factor.power};
     const bool fixing = dh && z.parts == 1 && sizeof(Elem<T>) == 2;
     const RowRests rests{fixing ? reinterpret_cast<int *>(base + z.rest_token) : nullptr, reinterpret_cast<float *>(base + z.rest)};
+    RowPlaces places{};
     if (z.n > 0) {
         UL_LAUNCHED(by_team(z.n, z.k, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
@@ -1164,12 +1351,24 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
             return hipGetLastError();
         }));
         if (dloss && dtable) {
+            auto *const slot = reinterpret_cast<int *>(base + z.slot), *const start = reinterpret_cast<int *>(base + z.start);
+            auto *const shrink = reinterpret_cast<float *>(base + z.shrink);
             if (z.n > kFindRows) {
-                hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, weights.exponent, z.n, largest);
+                if constexpr (T == UMAP_F16)
+                    hipLaunchKernelGGL(k_head_order, dim3(1), dim3(1024), 0, s, weights.exponent, z.n, found, slot, shrink, start);
+                else
+                    hipLaunchKernelGGL(k_head_largest, dim3(1), dim3(1024), 0, s, weights.exponent, z.n, found);
                 UL_LAUNCHED(hipGetLastError());
             }
-            hipLaunchKernelGGL((k_head_scale<T>), dim3((unsigned)std::min<int64_t>(8192, over(z.n * z.h_pitch / 8, 256))), dim3(256), 0, s,
-                               copy, z.n, (int)z.parts, (int)z.h_pitch, weights.exponent, largest, scaled);
+            const dim3 blocks((unsigned)std::min<int64_t>(8192, over(z.n * z.h_pitch / 8, 256)));
+            if constexpr (T == UMAP_F16) {
+                places = {slot, shrink, start};
+                hipLaunchKernelGGL(k_head_place, blocks, dim3(256), 0, s, copy, z.n, (int)z.parts, (int)z.h_pitch, weights.exponent, found,
+                                   scaled, slot, shrink, start);
+            } else {
+                hipLaunchKernelGGL((k_head_scale<T>), blocks, dim3(256), 0, s, copy, z.n, (int)z.parts, (int)z.h_pitch, weights.exponent,
+                                   found, scaled);
+            }
             UL_LAUNCHED(hipGetLastError());
         }
     }
@@ -1190,12 +1389,12 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
                 using P = decltype(shape);
                 const Tiles g = tiles_of<P>(z.d_pitch, z.n);
                 hipLaunchKernelGGL((k_head_d<T, P>), dim3((unsigned)((int64_t)g.m * g.n)), dim3(P::kThreads), 0, s, w, rows, scale, g,
-                                   lse, weights, one ? token : nullptr, one ? value : nullptr, one && fixing ? rests.rest : nullptr, first, d, z.d_pitch, below);
+                                   lse, weights, places, one ? token : nullptr, one ? value : nullptr, one && fixing ? rests.rest : nullptr, first, d, z.d_pitch, below);
                 return hipGetLastError();
             })));
             if (!one) {
                 hipLaunchKernelGGL((k_head_own<T>), dim3((unsigned)std::min<int64_t>(1024, over(z.n * z.k, 256))), dim3(256), 0, s,
-                                   token, value, z.n * z.k, (int)z.k, first, here, d, z.d_pitch, below);
+                                   token, value, z.n * z.k, (int)z.k, first, here, places, d, z.d_pitch, below);
                 UL_LAUNCHED(hipGetLastError());
             }
         }
@@ -1209,7 +1408,7 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         }
         const bool sums_due = dh && z.n > 0;
         auto row_sums = [&](Tiles g) { return RowSums{w, d_side, g, z.depth, first > 0, sums, z.sum_pitch}; };
-        auto table_rows = [&](Tiles g) { return TableRows{weighted, d_side, g, weights, add, part}; };
+        auto table_rows = [&](Tiles g) { return TableRows{weighted, d_side, g, weights, places, (int)z.parts, add, part}; };
         if (sums_due && dtable && !z.dh_few && z.dh_shape == TileShape::tiny_deep && dw_shape == TileShape::tiny_deep) {
             using P = Tiny<T, true, false, 4>;
             using Q = Tiny<T, true, true, 4>;
@@ -1244,10 +1443,10 @@ hipError_t grad(const umap_rows &h, const umap_rows &table, const Taught &taught
         const int parts = (int)(z.splits * z.parts);
         if (parts >= 8)
             hipLaunchKernelGGL((k_head_dh_join<T, 16>), dim3((unsigned)std::min<int64_t>(4096, over(total, 16))), dim3(256), 0, s, sums,
-                               parts, z.sum_pitch, weights, rests, all, *dh);
+                               parts, z.sum_pitch, weights, places, rests, all, *dh);
         else
             hipLaunchKernelGGL((k_head_dh_join<T, 1>), dim3((unsigned)std::min<int64_t>(4096, over(total, 256))), dim3(256), 0, s, sums,
-                               parts, z.sum_pitch, weights, rests, all, *dh);
+                               parts, z.sum_pitch, weights, places, rests, all, *dh);
         UL_LAUNCHED(hipGetLastError());
     }
     return hipSuccess;

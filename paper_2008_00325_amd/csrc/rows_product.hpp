@@ -206,7 +206,9 @@ struct Product {
     static constexpr bool kBlocks = T == UMAP_F32 && !kAcrossA && !kAcrossB;
     static constexpr int kBlockSteps = 8;
 
-    // acc of rows m0 .. of A and n0 .. of B, over k0 <= k < k1 (k0 a multiple of kDepth).
+    // acc of rows m0 .. of A and n0 .. of B, over k0 <= k < k1: along k a multiple of kDepth to the sides' columns or another one,
+    // across it any to the sides' rows or a multiple of kDepth further.  kMore: added to what acc holds.
+    template <bool kMore = false>
     static __device__ __forceinline__ void run(const ProductSide &a, const ProductSide &b, int64_t m0, int64_t n0,
                                                int64_t k0, int64_t k1, Piece *lds, Acc4 acc[FM][FN])
     {
@@ -214,7 +216,7 @@ struct Product {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = Acc4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < FN; ++j) acc[i][j] = kMore ? acc[i][j] : Acc4{0.0f, 0.0f, 0.0f, 0.0f};
         if (k0 >= k1) return;
         const SideA da(a, m0);
         const SideB db(b, n0);
