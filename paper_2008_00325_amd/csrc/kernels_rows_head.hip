@@ -1219,8 +1219,8 @@ hipError_t by_shape(TileShape shape, F f)
 {
     switch (shape) {
     case TileShape::large:
-        if constexpr (!Small<T, AA, AB>::kBlocks) return f(Large<T, AA, AB>{});   // else the registers are short
-        [[fallthrough]];
+        if constexpr (!Small<T, AA, AB>::kBlocks) return f(Large<T, AA, AB>{});
+        [[fallthrough]];   // logits_shape() does not ask for it
     case TileShape::small: return f(Small<T, AA, AB>{});
     case TileShape::tiny: return f(Tiny<T, AA, AB, 2>{});
     default: return f(Tiny<T, AA, AB, 4>{});
@@ -1235,7 +1235,7 @@ hipError_t by_few(int64_t n, F f)
 template <int T, typename F>
 hipError_t by_logits(int64_t rows, int64_t n, F f)
 {
-    return n <= kFewRows ? by_few<T, false>(n, f) : by_shape<T, false, false>(tile_shape(rows, n, 1, sizeof(Elem<T>)), f);
+    return n <= kFewRows ? by_few<T, false>(n, f) : by_shape<T, false, false>(logits_shape(rows, n, sizeof(Elem<T>)), f);
 }
 
 // Calls f with the waves of a row: one; four where rows are few or have many tokens, and 16 where both holds.

@@ -128,4 +128,12 @@ constexpr TileShape tile_shape(int64_t m, int64_t n, int64_t most, int64_t elem)
     return tiny * most <= 512 ? TileShape::tiny_deep : TileShape::tiny;
 }
 
+// For the logits of n rows against `rows` tokens, whose depth is not split.  fp32's, summed in blocks, have no large tile (its
+// registers are short for two sums): small ones take its place.
+constexpr TileShape logits_shape(int64_t rows, int64_t n, int64_t elem)
+{
+    const TileShape s = tile_shape(rows, n, 1, elem);
+    return elem == 4 && s == TileShape::large ? TileShape::small : s;
+}
+
 }  // namespace ul
