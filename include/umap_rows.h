@@ -251,7 +251,11 @@ int umap_rows_cross_entropy(const umap_rows *h, const umap_rows *table, const vo
                             float scale, float *loss, float *lse, void *workspace, int64_t workspace_bytes,
                             void *stream);
 
-/* Bytes of umap_rows_cross_entropy's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+/* Bytes of umap_rows_cross_entropy's workspace (> 0), or UMAP_E_INVAL.  Host only.
+ * They do for any stride and alignment: room for a copy of h (its columns a
+ * multiple of 64), for one of 128 MB of the table (or of 256 of its rows, if that is
+ * more), used where they are not whole pieces of 16 bytes, and for the tiles' sums,
+ * 128 MB at most, or 32 bytes for each of the table's rows if that is more. */
 int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type);
 
 /*
@@ -288,7 +292,15 @@ int umap_rows_cross_entropy_grad(const umap_rows *h, const umap_rows *table, con
                                  const umap_rows *dtable, int32_t accumulate, void *workspace,
                                  int64_t workspace_bytes, void *stream);
 
-/* Bytes of umap_rows_cross_entropy_grad's workspace (> 0), or UMAP_E_INVAL.  Host only. */
+/* Bytes of umap_rows_cross_entropy_grad's workspace (> 0), or UMAP_E_INVAL.  Host only.
+ * Room for two copies of h (of up to 256 rows of 16 bits, four), for 128 MB of the
+ * table as above, for D, 256 MB at most, or 256 entries for each row of h if that is
+ * more, for dh in fp32 (once; up to 72 MB of it if that is more), and 100 + 8 k bytes
+ * for each row.  The more rows, the fewer tokens a piece has, and every piece reads
+ * and writes all sums of dh: of a very large batch, calls of some 16,384 rows each that
+ * add to dtable take less time than one (131,072 rows of bf16 against 32,000 x 2,048:
+ * 43 ms and 92), at the price of dtable's rounding in each.
+ */
 int64_t umap_rows_cross_entropy_grad_workspace(int64_t n, int64_t rows, int32_t cols, int32_t type);
 
 /*

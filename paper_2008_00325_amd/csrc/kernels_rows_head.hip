@@ -1132,7 +1132,8 @@ constexpr int64_t kFewRows = 64;
 constexpr int64_t kPackBytes = (int64_t)128 << 20;
 int64_t pack_rows(int64_t pitch, int64_t elem) { return std::max<int64_t>(256, kPackBytes / (pitch * elem) / 256 * 256); }
 
-// Forward: rows of h at a time, so that the partial sums stay within 128 MB (a quarter of that with the large tiles).
+// Forward: rows of h at a time, so that the partial sums stay within 128 MB (a quarter of that with the large tiles), but 256 rows
+// at least, since each turn reads the whole table: from 4.2 million tokens on they take 32 bytes a token.
 struct LossSizes {
     int64_t tiles, rows, pitch, piece;
     int64_t partial, own, copy, table, total;   // offsets into the workspace
@@ -1170,7 +1171,7 @@ struct GradSizes {
         : n(n_), vocab(vocab_), cols(cols_), k(k_), elem(elem_size(type))
     {
         parts = elem == 2 && n <= kTwoPartRows ? 2 : 1;
-        const int64_t budget = (int64_t)256 << 20;
+        const int64_t budget = (int64_t)256 << 20;   // of D, but 256 tokens at least: 512 bytes a row of 16 bits
         int64_t most = std::max<int64_t>(256, budget / std::max<int64_t>(1, n * parts * elem) / 256 * 256);
         most = std::min(most, (int64_t)1 << 22);   // so that the launches' sizes fit
         h_pitch = up(cols, 64);
