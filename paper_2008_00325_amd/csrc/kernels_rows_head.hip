@@ -88,19 +88,42 @@ __device__ __forceinline__ float wave_sum(float v)
 
 // ---- the logits' tiles: forward -------------------------------------------------------------
 
-// A row's one token in a tile: f(i, r) for the place of acc[i][j] that is `own` rows of A from the tile's first.  Few waves have one
-// among theirs, and the others see it at once.
-template <class P, typename F>
-__device__ __forceinline__ void own_place(int64_t own, F f)
-{
-    const int first = P::m_first(0);
-    if (!__any(own >= first && own < first + 16 * P::kFM)) return;
+// The one tokens of a wave's 16 FN rows of B, a row to a lane, in the wave's part of a tile.  Few waves have one there, and the
+// others see it at once.
+template <class P>
+struct OwnPlaces {
+    static_assert(P::kFN <= 4, "a lane to a row");
+    int at = -1;   // rows of A from the wave's first
+    uint64_t rows;
+    // This lane's row, from the tile's first; behind the wave's rows: no row.
+    static __device__ __forceinline__ int row(int none)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        return lane < 16 * P::kFN ? wave % P::kWN * 16 * P::kFN + lane : none;
+    }
+    // own: rows of A from the tile's first, negative: none
+    __device__ __forceinline__ explicit OwnPlaces(int64_t own)
+    {
+        const int64_t in = own - P::m_first(0);
+        if (own >= 0 && in >= 0 && in < 16 * P::kFM) at = (int)in;
+        rows = __ballot(at >= 0);
+    }
+    __device__ __forceinline__ bool any(int j) const { return (rows >> (16 * j) & 0xffff) != 0; }
+    // acc[i][j][r] is a row's own token's where this is 16 i + r.
+    __device__ __forceinline__ int place(int j) const { return __shfl(at, 16 * j + (threadIdx.x & 15)) - (int)(threadIdx.x >> 4 & 3) * 4; }
+    // Its acc, or 0.
+    static __device__ __forceinline__ float pick(int place, const Acc4 (&acc)[P::kFM][P::kFN], int j)
+    {
+        float x = 0.0f;
 #pragma unroll
-    for (int i = 0; i < P::kFM; ++i)
+        for (int i = 0; i < P::kFM; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (P::m_of(i) + r == own) f(i, r);
-}
+            for (int r = 0; r < 4; ++r) x = place == 16 * i + r ? acc[i][j][r] : x;
+        return x;
+    }
+    // Whether this lane has it.
+    static __device__ __forceinline__ bool here(int place) { return place >= 0 && (place & 15) < 4; }
+};
 
 // Rows of one token each: its logit, as it is among the exponentials, in their units.
 struct OwnLogits {
@@ -108,6 +131,20 @@ struct OwnLogits {
     int64_t first;   // row of h's first
     int64_t vocab, piece;   // rows of the table, and which of them w's first is
     float *z;        // null: rows of more tokens
+    // An id as it lies in memory, for a load that nobody waits for before id().
+    struct Words {
+        int32_t low, high;
+    };
+    __device__ __forceinline__ Words fetch(int64_t t) const
+    {
+        const auto *const at = reinterpret_cast<const int32_t *>(static_cast<const char *>(ids.data) + (first + t) * ids.bytes);
+        return {at[0], at[ids.bytes / 4 - 1]};
+    }
+    __device__ __forceinline__ int64_t id(const Words &w) const
+    {
+        const int64_t v = ids.bytes == 4 ? (int64_t)w.low : (int64_t)w.high << 32 | (uint32_t)w.low;
+        return v >= 0 && v < vocab ? v : -1;
+    }
 };
 
 template <int T, class P>
@@ -120,6 +157,8 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
     const int64_t m0 = (int64_t)at.m * P::M, n0 = (int64_t)at.n * P::N;
     Acc4 acc[FM][FN];
     P::run(w, h, m0, n0, 0, w.cols, lds, acc);
+    OwnLogits::Words own = {};   // on its way while the exponentials are formed
+    if (one.z) own = one.fetch(min(n0 + OwnPlaces<P>::row(0), h.rows - 1));
     MaxSum(*const part)[P::N] = reinterpret_cast<MaxSum(*)[P::N]>(lds);   // behind the product's last barrier
     const int live = (int)min((int64_t)P::M, w.rows - m0);
     Logit<T> logit(scale);
@@ -134,10 +173,6 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
     }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-        if (one.z) {
-            const int64_t t = n0 + P::n_of(j), id = t < h.rows ? row_of(one.ids, one.first + t, one.vocab) : -1;
-            own_place<P>(id - one.piece - m0, [&](int i, int r) { one.z[t] = acc[i][j][r] * logit.unit; });
-        }
         float most = minus_inf();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -154,6 +189,19 @@ __global__ __launch_bounds__(P::kThreads) void k_head_lse(ProductSide w, Product
 #pragma unroll
         for (int o = 16; o < 64; o <<= 1) all.template join<T>({__shfl_xor(all.m, o), __shfl_xor(all.s, o)});
         if ((threadIdx.x & 63) < 16) part[(threadIdx.x >> 6) / P::kWN][P::n_of(j)] = all;
+    }
+    if (one.z) {
+        const int row = OwnPlaces<P>::row(-1);
+        const OwnPlaces<P> places(row >= 0 && n0 + row < h.rows ? one.id(own) - one.piece - m0 : -1);
+        if (places.rows) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                if (!places.any(j)) continue;
+                const int place = places.place(j);
+                const float z = OwnPlaces<P>::pick(place, acc, j) * logit.unit;
+                if (OwnPlaces<P>::here(place)) one.z[n0 + P::n_of(j)] = z;
+            }
+        }
     }
     __syncthreads();
     for (int n = threadIdx.x; n < P::N; n += P::kThreads) {
@@ -826,39 +874,34 @@ __global__ __launch_bounds__(P::kThreads) void k_head_d(ProductSide w, ProductSi
     P::run(w, h, m0, n0, 0, w.cols, lds, acc);
     const int live = (int)min((int64_t)P::M, w.rows - m0);
     const Logit<T> logit(scale);
+    const int row = OwnPlaces<P>::row(-1), own = token && row >= 0 && n0 + row < h.rows ? token[n0 + row] : -1;
+    const OwnPlaces<P> tokens(own >= 0 ? own - first - m0 : -1);
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int64_t t = n0 + P::n_of(j);
+        const int place = tokens.any(j) ? tokens.place(j) : -1;   // of all lanes
         if (t >= h.rows) continue;
         const float shrink = T == UMAP_F16 && places.slot ? places.shrink[t] : 1.0f;
         const float number = weights.number[t] * shrink, less = Logit<T>::of_natural(lse[t]);
-        int64_t own = -1;
-        float taken = 0.0f;
-        if (token && token[t] >= 0) {
-            own = token[t] - first - m0;
-            taken = value[t] * shrink;
-        }
         Elem<T> *const to = d + (T == UMAP_F16 && places.slot ? places.slot[t] : t) * pitch + m0;
         float v[FM][4];
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = logit.exp_less(acc[i][j][r], less);
-                if constexpr (T == UMAP_F32) v[i][r] = fmaf(number, p, P::m_of(i) + r == own ? -taken : 0.0f);
-                else v[i][r] = number * p;
-            }
+            for (int r = 0; r < 4; ++r) v[i][r] = number * logit.exp_less(acc[i][j][r], less);
+        if (tokens.any(j)) {
+            const float taken = value[t] * shrink, entry = fmaf(number, logit.exp_less(OwnPlaces<P>::pick(place, acc, j), less), -taken);
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[i][r] = place == 16 * i + r ? entry : v[i][r];
+            if (rest && OwnPlaces<P>::here(place)) rest[t] = (entry - elem_float<T>(float_elem<T>(entry))) * (1.0f / shrink);
+        }
         if (live < P::M || number == 0.0f) {   // past the table, or a row without part
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[i][r] = number != 0.0f && P::m_of(i) + r < live ? v[i][r] : 0.0f;
-        }
-        if constexpr (T != UMAP_F32) {
-            own_place<P>(own, [&](int i, int r) {
-                v[i][r] -= taken;
-                if (rest) rest[t] = (v[i][r] - elem_float<T>(float_elem<T>(v[i][r]))) * (1.0f / shrink);
-            });
         }
         auto store = [&](Elem<T> *at, auto round) {
             if constexpr (sizeof(Elem<T>) == 2 && FM % 2 == 0) {
