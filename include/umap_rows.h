@@ -275,7 +275,8 @@ int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols,
  *              zeros, and nothing of them reaches dtable (they may hold NaN).
  *              Weights may lie far apart: in fp16 dtable takes rows within 2^6 of the
  *              largest weight together, then those within 2^12, and so on down to
- *              2^96, beyond which they do not reach it.
+ *              2^96, beyond which they do not reach it; in bf16 and fp32 a row counts
+ *              as far as h times its weight over the largest is in its type's range.
  *   dscale     finite (one over the rows for a mean, times a loss scale for fp16).
  *   dh         NULL, or receives the gradient of h: its type and shape.
  *   dtable     NULL, or receives the gradient of table: its type and shape.  Not

@@ -16,7 +16,7 @@
 // lse of the forward call, by 3.2e-7 and 3.1e-7 (medians of 39 inputs).
 //
 // Precision of D in 16 bits: an entry is off by up to half a unit in its last place, and sums of many entries average that
-// out: dW is off by 1.2 (median) to 1.45 times what its own type's rounding alone costs (60 cases of 257 to 700 rows).  Where it
+// out: dW is off by 1.22 (median) to 1.44 times what its own type's rounding alone costs (60 cases of 257 to 700 rows).  Where it
 // does not average out it is avoided: up to 256 rows D has two parts, a value and what its rounding left; and a row of dh, most of which often comes from one
 // token, gets back what that token's entry lost.  Where all g_t are alike they are left to the very end: D is then p - q, whose
 // largest entries, those of the rows' tokens, lie just below 1 and so are rounded least.  Else g_t is a number in [1/2, 1) times
@@ -26,12 +26,13 @@
 // times 2^-((E - e_t) mod 6), and the rows of D and of h's copy are put in order of (E - e_t) / 6, their bands, whose sums dW takes one
 // after the other from the smallest weights on, times 2^-6 from band to band.  (With h_t times 2^(e_t - E) in fp16, dW of tokens
 // that only rows with 2^-20 of the largest weight know was off by 1.7e-2 of its norm, so by 2.8e-4, of which 2.2e-4 is its own
-// rounding.)  Weights within 2^6 are one band, in their order, and cost nothing; weights over 2^40, seven bands, took 1,358 -> 1,507 us
-// for 2,048 rows against 32,000 x 4,096, 49 -> 65 for 300 against 10,007 x 300.
+// rounding.)  Weights within 2^6 are one band, in their order, and take no longer (2,048 rows against 32,000 x 4,096 1,413 and 1,423 us,
+// 8,000 against 3,000 x 256 171 and 159); weights over 2^40, seven bands, 1,394 -> 1,548 us for the former, 49 -> 65 for 300 rows against
+// 10,007 x 300.
 //
 // Bound by the matrix cores for many rows, by the table's bytes for few.  bf16: 8,192 rows against 128,000 x 4,096: loss 6.1 ms
-// (1,400 TFLOP/s; the library's product of the same size 5.8 ms, without the exponentials), gradient 20.0 ms (1,290: D 0.84,
-// dh 0.83 and dW 0.86 ms of each of 8 pieces); one row against 32,000 x 2,048: 21 us of the tiles (6.2 TB/s) and 5 of
+// (1,400 TFLOP/s; the library's product of the same size 5.8 ms, without the exponentials), gradient 20.2 ms (1,280: D 0.84,
+// dh 0.82 and dW 0.84 ms of each of 8 pieces); one row against 32,000 x 2,048: 22 us of the tiles (6.0 TB/s) and 4 of
 // their join.  Fewer columns leave a tile less to multiply before its end: 2,048 rows against 32,000 reach 1,350 TFLOP/s at 4,096
 // columns, 910 at 512.
 #include <math.h>
@@ -1197,9 +1198,9 @@ struct LossSizes {
 };
 
 // Rows up to which a 16-bit D has two parts: few rows do not average the rounding out.  It is paid for in time: one part or two
-// against 32,000 x 2,048 in bf16 take 84 and 83 us for 1 row, 86 and 88 for 16, 100 and 121 for 64, 129 and 171 for 128, 191
+// against 32,000 x 2,048 in bf16 take 81 and 81 us for 1 row, 84 and 86 for 16, 98 and 118 for 64, 128 and 170 for 128, 190
 // and 235 for 256.  dtable's error, relative to its type's own, at worst of 60 cases each: one part 1.64 for 20 to 128 rows and
-// 1.45 for 129 to 256, two parts 1.0004; one part for 257 to 700 rows 1.45.
+// 1.49 for 129 to 256, two parts 1.0006; one part for 257 to 700 rows 1.44.
 constexpr int64_t kTwoPartRows = 256;
 
 struct GradSizes {
