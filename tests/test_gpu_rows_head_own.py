@@ -92,3 +92,45 @@ def test_a_nearly_certain_token(dtype, n, k):
     near(dh, want.expand_as(dh), bound.expand_as(dh), "dh")
     if k < 2:
         near(loss, torch.full((n,), -math.log1p(-rest), dtype=F64, device=DEV), torch.tensor(rest * moved, device=DEV), "loss")
+
+
+@pytest.mark.parametrize("ids", [torch.int32, torch.int64])
+@pytest.mark.parametrize("k", [0, 1])
+@pytest.mark.parametrize("n,rows,cols", [(70, 1_100_003, 7), (1300, 1_100_003, 7), (300, 2_100_000, 64)])
+def test_tokens_in_every_piece_and_turn(n, rows, cols, k, ids):
+    """Tables of several copied pieces (odd rows, over 128 MB of copies) and rows in several turns: the loss of whole numbers' exact
+    logits, from each row's own token wherever it lies."""
+    case = Case(n, rows, cols, BF16, k=k, ids=ids, absent=0.2)
+    case.H.copy_(torch.randint(-1, 2, case.H.shape, device=DEV))
+    case.W.copy_(torch.randint(-1, 2, case.W.shape, device=DEV))
+    ends = torch.tensor([0, 63, 64, 255, rows // 2, 1 << 20, (1 << 20) - 1, rows - 1, rows - 2], device=DEV)
+    case.tokens.view(-1)[:9] = ends.to(ids)
+    loss, lse = case.loss()
+    tokens = case.tokens.view(-1).long()
+    for first in range(0, n, 100):
+        part = slice(first, min(n, first + 100))
+        z = case.H[part].float() @ case.W.float().T   # whole numbers
+        want = torch.logsumexp(z.to(F64), 1)
+        # 300 additions, and exponentials and logits of at most 64, in fp32
+        off = (300 + 8 * 64) * E32 + 4e-7
+        near(lse[part], want, torch.full_like(want, off), "lse")
+        there = (tokens[part] >= 0) & (tokens[part] < rows)
+        own = z.gather(1, torch.where(there, tokens[part], 0)[:, None])[:, 0].to(F64)
+        near(loss[part], torch.where(there, want - own, 0.0), torch.full_like(want, 2 * off), "loss")
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("n", [20, 300])
+def test_rows_that_are_not_finite(n, dtype):
+    case = Case(n, 400, 40, dtype, absent=0.0)
+    clean = case.loss()
+    case.H[3, 5] = math.nan
+    case.H[11, 0] = math.inf
+    loss, lse = case.loss()
+    ok = torch.ones(n, dtype=torch.bool, device=DEV)
+    ok[[3, 11]] = False
+    assert torch.equal(loss[ok], clean[0][ok]) and torch.equal(lse[ok], clean[1][ok])
+    assert math.isnan(float(loss[3])) and math.isnan(float(lse[3])) and not math.isfinite(float(lse[11]))
+    dh = torch.empty_like(case.H)
+    case.grad(lse, dh, None)
+    assert bool(torch.isfinite(dh[ok]).all()) and bool(dh[3].isnan().all())

@@ -138,3 +138,25 @@ def test_ordinary_weights_of_wider_types(dtype):
     want_h, want_w, bound_h, bound_w = case.head().grads(dtype, w.to(F64))
     near(dh, want_h, bound_h, "dh")
     near(dw, want_w, bound_w(), "dtable")
+
+
+@pytest.mark.parametrize("spread", [0, 5, 6, 7, 95, 96, 110])
+@pytest.mark.parametrize("n", [250, 8191, 8192, 8193])
+def test_places_at_the_bounds_of_bands_and_launches(n, spread):
+    """Two kinds of weights, 2^-spread apart: the smaller ones' rows count up to 2^-95 of the largest, beyond which they are not in
+    dtable (nor are they in what fp16 holds, unless the largest weight's rows have no gradient there)."""
+    case, kind = apart(n, 2, 24)
+    w = torch.where(kind == 0, 2.0**60, 2.0 ** (60 - spread)) * torch.ones(n, device=DEV)
+    dscale = 2.0 ** (spread - 60)   # the smaller weights are 1
+    lse = case.loss()[1]
+    dh, dw = torch.empty_like(case.H), torch.empty_like(case.W)
+    case.grad(lse, dh, dw, w, dscale)
+    ones = torch.ones(n, device=DEV)
+    want_h, want_w = torch.empty_like(case.H), torch.empty_like(case.W)
+    # the smaller weights' rows alone: the others' probability of their tokens is some 2^-57
+    case.tokens[kind == 0] = -1
+    case.grad(lse, want_h, want_w, ones)
+    assert torch.equal(dh[1::2], want_h[1::2])
+    if spread <= 40:
+        near(dw[20:], want_w[20:].to(F64), 2.0**-9 * want_w[20:].to(F64).abs() + 2.0**-24 + 2.0 ** (spread - 54) * n, "dtable")
+    assert bool(torch.isfinite(dw[20:]).all()) or spread > 60
