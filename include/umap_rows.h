@@ -265,11 +265,12 @@ int64_t umap_rows_cross_entropy_workspace(int64_t n, int64_t rows, int32_t cols,
  *   dtable[v] = scale sum_t D[t][v] h[t]
  * The logits are formed again, for a piece of the table at a time, and D of the piece
  * is kept in h's type (fp32: not rounded; 16 bits: in two parts up to 256 rows, else
- * each entry off by up to half a unit in its last place, which the sums average out);
+ * each entry rounded, by up to half a unit in its last place, which the sums average out);
  * all sums are fp32 and rounded once; their order is fixed.
  *
  *   h, table, targets, scale  as for umap_rows_cross_entropy.
- *   lse        what that call gave.
+ *   lse        what that call gave: the rounding of its logits then cancels against
+ *              that of the same logits here, which one formed otherwise brings along.
  *   dloss      NULL (ones), or a weight for each row, fp32.  Rows of weight 0 and
  *              rows whose target lies outside the table take no part: their dh is
  *              zeros, and nothing of them reaches dtable (they may hold NaN).
